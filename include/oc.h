@@ -565,6 +565,95 @@ oc_status oc_softmax_ce(int32_t batch, int32_t nc, const float* z, const int32_t
 oc_status oc_sgd(int64_t n, float* w, const float* g, float* v, float lr, float momentum,
                  float decay, hipStream_t stream);
 
+/* ---- Dense layers over rows: pointwise layers on the octants of a depth (rows
+ * = N_l) or on whole shapes, on the matrix cores.  Rows are independent of each
+ * other and contiguous, as feature maps are.
+ *
+ * y = act(x w + bias) + res
+ *   dt      OC_F32: every operand and y fp32; OC_BF16: x, w, res and y bf16.
+ *           bias is fp32.  Sums are fp32; an OC_BF16 result is rounded once.
+ *   act     OC_ACT_NONE, OC_ACT_RELU, OC_ACT_SILU (z / (1 + e^-z)) or
+ *           OC_ACT_GELU (z Phi(z), Phi the normal distribution function).
+ *   x       dev [rows][cin].  w dev [cin][cout].  rows 0 .. 2^31 - 1 (0: nothing
+ *           is done), cin, cout 1 .. 65536.
+ *   bias    dev f32 [cout] or NULL.  res dev [rows][cout] or NULL; may be y.
+ *   y       dev [rows][cout].
+ *   pre     dev [rows][cout] or NULL: receives x w + bias for the backward, in
+ *           fp32; for OC_ACT_RELU in the type dt.
+ *   ws      dev workspace of at least oc_dense_fwd_workspace() bytes (may be NULL
+ *           when that is 0).
+ * Buffers need the alignment of their elements only.  Deterministic: no
+ * floating-point atomics. */
+#define OC_ACT_NONE 0
+#define OC_ACT_RELU 1
+#define OC_ACT_SILU 2
+#define OC_ACT_GELU 3
+size_t oc_dense_fwd_workspace(oc_dtype dt, int64_t rows, int32_t cin, int32_t cout);
+oc_status oc_dense_fwd(oc_dtype dt, int32_t act, int64_t rows, int32_t cin, int32_t cout,
+                       const void* x, const void* w, const float* bias, const void* res, void* y,
+                       void* pre, void* ws, size_t ws_bytes, hipStream_t stream);
+
+/* Gradients of oc_dense_fwd: with dz = dy act'(x w + bias),
+ *   dx = dz w^T, dw = x^T dz, dbias = the sum of dz over the rows
+ * (the residual's gradient is dy itself).
+ *   pre     what oc_dense_fwd left there; may be NULL for OC_ACT_NONE.  A ReLU's
+ *           slope is [pre > 0], so the output y of a forward without a residual
+ *           does as well.
+ *   dy      dev [rows][cout] and dx dev [rows][cin] or NULL, of type dt.
+ *   dw      dev [cin][cout] or NULL, of type dw_dt: OC_F32 or dt.
+ *   dbias   dev f32 [cout] or NULL.
+ * OC_BF16: dz is rounded to bf16 (the operand of dx and dw), as oc_conv_bwd's dy
+ * is; dbias is summed from the values before that.  With rows 0, dw and dbias
+ * are 0. */
+size_t oc_dense_bwd_workspace(oc_dtype dt, int32_t act, int64_t rows, int32_t cin, int32_t cout);
+oc_status oc_dense_bwd(oc_dtype dt, int32_t act, int64_t rows, int32_t cin, int32_t cout,
+                       const void* x, const void* w, const void* pre, const void* dy, void* dx,
+                       oc_dtype dw_dt, void* dw, float* dbias, void* ws, size_t ws_bytes,
+                       hipStream_t stream);
+
+/* Gated layer: both projections, the activation and the product in one kernel,
+ *   y = act(g) u,  g = (x w + bias)[:, :cout],  u = (x w + bias)[:, cout:]
+ *   w       dev [cin][2 cout]: the gate's columns, then the other projection's.
+ *           cout 1 .. 32768.  bias dev f32 [2 cout] or NULL.
+ *   y       dev [rows][cout].
+ *   pre     dev f32 [rows][2 cout] or NULL: receives x w + bias for the backward.
+ * Types, sizes and the workspace otherwise as oc_dense_fwd. */
+size_t oc_glu_fwd_workspace(oc_dtype dt, int64_t rows, int32_t cin, int32_t cout);
+oc_status oc_glu_fwd(oc_dtype dt, int32_t act, int64_t rows, int32_t cin, int32_t cout,
+                     const void* x, const void* w, const float* bias, void* y, float* pre,
+                     void* ws, size_t ws_bytes, hipStream_t stream);
+
+/* Gradients of oc_glu_fwd: dz = [dy u act'(g) | dy act(g)] [rows][2 cout], then
+ * dx, dw [cin][2 cout] and dbias [2 cout] as oc_dense_bwd. */
+size_t oc_glu_bwd_workspace(oc_dtype dt, int64_t rows, int32_t cin, int32_t cout);
+oc_status oc_glu_bwd(oc_dtype dt, int32_t act, int64_t rows, int32_t cin, int32_t cout,
+                     const void* x, const void* w, const float* pre, const void* dy, void* dx,
+                     oc_dtype dw_dt, void* dw, float* dbias, void* ws, size_t ws_bytes,
+                     hipStream_t stream);
+
+/* norm (dev f32 scalar) = the square root of the sum of the squares of every
+ * value of n tensors, squares and sums in double.  Host arrays: grads (device
+ * pointers), dts (OC_F32 or OC_BF16 each), counts (values each, 0 allowed); they
+ * are read during the call.  ws: dev, at least oc_grad_workspace(n, counts)
+ * bytes.  n 0: norm = 0. */
+size_t oc_grad_workspace(int32_t n, const int64_t* counts);
+oc_status oc_grad_norm(int32_t n, const void* const* grads, const oc_dtype* dts,
+                       const int64_t* counts, float* norm, void* ws, size_t ws_bytes,
+                       hipStream_t stream);
+
+/* Clipping by the global norm, ahead of oc_sgd: outs[i] = c grads[i], c = 1 where
+ * norm <= max_norm, else max_norm / norm (max_norm >= 0; infinity only copies).
+ *   outs    host array of device pointers, of types out_dts: OC_F32 or the
+ *           gradient's own.  outs[i] may be grads[i] (same type); otherwise no
+ *           output overlaps a gradient or another output.
+ *   norm    dev f32 scalar, the norm before clipping, or NULL.
+ * A NaN gradient makes every output NaN; an infinite one (and no NaN) makes
+ * itself NaN and every finite one 0. */
+oc_status oc_grad_clip(int32_t n, const void* const* grads, const oc_dtype* dts,
+                       const int64_t* counts, double max_norm, void* const* outs,
+                       const oc_dtype* out_dts, float* norm, void* ws, size_t ws_bytes,
+                       hipStream_t stream);
+
 /* Profiling: the next launch, on the calling thread, of the kernel that does
  * the main work of an entry point (the kernel oc_conv_kernel names for a
  * convolution pass; the pooling, routing or unpooling kernel of oc_pool_* /

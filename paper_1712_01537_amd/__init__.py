@@ -55,6 +55,16 @@ __all__ = [
     "oc_dropout",
     "oc_softmax_ce",
     "oc_sgd",
+    "oc_dense_fwd",
+    "oc_dense_bwd",
+    "oc_glu_fwd",
+    "oc_glu_bwd",
+    "oc_grad_norm",
+    "oc_grad_clip",
+    "OC_ACT_NONE",
+    "OC_ACT_RELU",
+    "OC_ACT_SILU",
+    "OC_ACT_GELU",
     "EXPORTS",
 ]
 
@@ -62,6 +72,7 @@ _HERE = os.path.dirname(os.path.abspath(__file__))
 OC_FUSE_RELU = 1
 OC_DEFER_DW = 2
 OC_POOL_MAX, OC_POOL_AVG = 0, 1
+OC_ACT_NONE, OC_ACT_RELU, OC_ACT_SILU, OC_ACT_GELU = 0, 1, 2, 3
 OC_F32, OC_BF16 = 0, 1
 STATUS = {0: "OC_OK", 1: "OC_ERR_ARG", 2: "OC_ERR_RANGE", 3: "OC_ERR_NOMEM", 4: "OC_ERR_DEVICE",
           5: "OC_ERR_UNSUPPORTED"}
@@ -78,6 +89,9 @@ EXPORTS = (
     "oc_softmax_ce_workspace", "oc_softmax_ce", "oc_sgd", "oc_conv_pool_fwd",
     "oc_conv_pool_fwd_workspace", "oc_bn_pool_fwd", "oc_conv_bwd_pool_workspace",
     "oc_conv_bwd_pool", "oc_conv_dw_partials", "oc_sum_partials", "oc_round_bf16",
+    "oc_dense_fwd", "oc_dense_fwd_workspace", "oc_dense_bwd", "oc_dense_bwd_workspace",
+    "oc_glu_fwd", "oc_glu_fwd_workspace", "oc_glu_bwd", "oc_glu_bwd_workspace",
+    "oc_grad_workspace", "oc_grad_norm", "oc_grad_clip",
 )
 
 
@@ -206,6 +220,19 @@ def load():
         "oc_softmax_ce_workspace": ([i32], sz),
         "oc_softmax_ce": ([i32, i32, p, p, p, p, p, sz, p], C.c_int),
         "oc_sgd": ([i64, p, p, p, C.c_float, C.c_float, C.c_float, p], C.c_int),
+        "oc_dense_fwd_workspace": ([C.c_int, i64, i32, i32], sz),
+        "oc_dense_fwd": ([C.c_int, i32, i64, i32, i32, p, p, p, p, p, p, p, sz, p], C.c_int),
+        "oc_dense_bwd_workspace": ([C.c_int, i32, i64, i32, i32], sz),
+        "oc_dense_bwd": ([C.c_int, i32, i64, i32, i32, p, p, p, p, p, C.c_int, p, p, p, sz, p],
+                         C.c_int),
+        "oc_glu_fwd_workspace": ([C.c_int, i64, i32, i32], sz),
+        "oc_glu_fwd": ([C.c_int, i32, i64, i32, i32, p, p, p, p, p, p, sz, p], C.c_int),
+        "oc_glu_bwd_workspace": ([C.c_int, i64, i32, i32], sz),
+        "oc_glu_bwd": ([C.c_int, i32, i64, i32, i32, p, p, p, p, p, C.c_int, p, p, p, sz, p],
+                       C.c_int),
+        "oc_grad_workspace": ([i32, p], sz),
+        "oc_grad_norm": ([i32, p, p, p, p, p, sz, p], C.c_int),
+        "oc_grad_clip": ([i32, p, p, p, C.c_double, p, p, p, p, sz, p], C.c_int),
     }
     for name, (args, res) in sigs.items():
         f = getattr(L, name)
@@ -856,3 +883,154 @@ def oc_sgd(w, g, v, lr, momentum, decay):
                          _dev(g, "g", torch.float32, tuple(w.shape)),
                          _dev(v, "v", torch.float32, tuple(w.shape)), lr, momentum, decay,
                          _stream()))
+
+
+# --- dense layers and gradient clipping ------------------------------------
+
+
+def _here(**tensors):
+    """Every given tensor is on the current device, whose stream and kernels the
+    call uses."""
+    given = {name: t for name, t in tensors.items() if t is not None}
+    for name, t in given.items():
+        if not isinstance(t, torch.Tensor) or not t.is_cuda:
+            raise OcError(1, f"{name} must be a CUDA (HIP) tensor")
+    d = torch.cuda.current_device()
+    for name, t in given.items():
+        if t.device.index != d:
+            raise OcError(1, f"{name} is on {t.device}, the current device is cuda:{d}")
+
+
+def _ws(nbytes: int, device):
+    return torch.empty(max(int(nbytes), 1), dtype=torch.uint8, device=device)
+
+
+def _dense_dims(x, w, halves):
+    if x.dim() != 2 or w.dim() != 2 or w.shape[0] != x.shape[1] or w.shape[1] % halves:
+        raise OcError(1, f"x {tuple(x.shape)} and w {tuple(w.shape)} do not go together")
+    if w.dtype != x.dtype:
+        raise OcError(1, "x and w must share a dtype")
+    return x.shape[0], x.shape[1], w.shape[1] // halves
+
+
+def _layer_fwd(glu, x, w, b, res, act, need_pre):
+    _here(x=x, w=w, b=b, res=res)
+    L, dt = load(), _dtype_code(x)
+    rows, cin, cout = _dense_dims(x, w, 2 if glu else 1)
+    nz = w.shape[1]
+    y = torch.empty((rows, cout), dtype=x.dtype, device=x.device)
+    pre = None
+    if need_pre:
+        pre = torch.empty((rows, nz), device=x.device,
+                          dtype=x.dtype if act == OC_ACT_RELU and not glu else torch.float32)
+    need = (L.oc_glu_fwd_workspace if glu else L.oc_dense_fwd_workspace)(dt, rows, cin, cout)
+    ws = _ws(need, x.device)
+    bias = _opt(b, "b", dtype=torch.float32, shape=(nz,))
+    if glu:
+        _check(L.oc_glu_fwd(dt, act, rows, cin, cout, _dev(x, "x"), _dev(w, "w"), bias,
+                            _dev(y, "y"), _opt(pre, "pre"), _dev(ws, "ws"), ws.numel(), _stream()))
+    else:
+        _check(L.oc_dense_fwd(dt, act, rows, cin, cout, _dev(x, "x"), _dev(w, "w"), bias,
+                              _opt(res, "res", dtype=x.dtype, shape=(rows, cout)), _dev(y, "y"),
+                              _opt(pre, "pre"), _dev(ws, "ws"), ws.numel(), _stream()))
+    return y, pre
+
+
+def _layer_bwd(glu, x, w, dy, pre, act, need_dx, need_dw, need_db, dw, db, dw_dtype):
+    _here(x=x, w=w, dy=dy, pre=pre, dw=dw, db=db)
+    L, dt = load(), _dtype_code(x)
+    rows, cin, cout = _dense_dims(x, w, 2 if glu else 1)
+    nz = w.shape[1]
+    dx = torch.empty_like(x) if need_dx else None
+    if dw is None and need_dw:
+        dw = torch.empty((cin, nz), dtype=dw_dtype or torch.float32, device=x.device)
+    if db is None and need_db:
+        db = torch.empty(nz, dtype=torch.float32, device=x.device)
+    dw_dt = OC_F32 if dw is None else _dtype_code(dw)
+    need = (L.oc_glu_bwd_workspace(dt, rows, cin, cout) if glu
+            else L.oc_dense_bwd_workspace(dt, act, rows, cin, cout))
+    ws = _ws(need, x.device)
+    pre_dt = x.dtype if act == OC_ACT_RELU and not glu else torch.float32
+    f = L.oc_glu_bwd if glu else L.oc_dense_bwd
+    _check(f(dt, act, rows, cin, cout, _dev(x, "x"), _dev(w, "w"),
+             _opt(pre, "pre", dtype=pre_dt, shape=(rows, nz)),
+             _dev(dy, "dy", x.dtype, (rows, cout)), _opt(dx, "dx"), dw_dt,
+             _opt(dw, "dw", shape=(cin, nz)), _opt(db, "db", dtype=torch.float32, shape=(nz,)),
+             _dev(ws, "ws"), ws.numel(), _stream()))
+    return dx, dw, db
+
+
+def oc_dense_fwd(x, w, b=None, res=None, act=OC_ACT_NONE, need_pre=False):
+    """y = act(x w + b) + res over the rows of x: (y, pre), pre the values ahead of
+    the activation for the backward (fp32; of x's dtype for OC_ACT_RELU) or None.
+    x, w, res and y share a dtype (float32 or bfloat16); b is float32."""
+    return _layer_fwd(False, x, w, b, res, act, need_pre)
+
+
+def oc_dense_bwd(x, w, dy, act=OC_ACT_NONE, pre=None, need_dx=True, need_dw=True, need_db=True,
+                 dw=None, db=None, dw_dtype=None):
+    """(dx, dw, db) of oc_dense_fwd (None where not needed).  pre: as the forward
+    returned it; for OC_ACT_RELU without a residual y does as well.  dw, db:
+    optional caller tensors to write into; a new dw is of dw_dtype (float32 if
+    not given, or x's dtype)."""
+    return _layer_bwd(False, x, w, dy, pre, act, need_dx, need_dw, need_db, dw, db, dw_dtype)
+
+
+def oc_glu_fwd(x, w, b=None, act=OC_ACT_SILU, need_pre=False):
+    """y = act(g) u, [g | u] = x w + b, w [cin][2 cout]: (y, pre), pre [rows][2 cout]
+    float32 for the backward or None."""
+    return _layer_fwd(True, x, w, b, None, act, need_pre)
+
+
+def oc_glu_bwd(x, w, dy, pre, act=OC_ACT_SILU, need_dx=True, need_dw=True, need_db=True, dw=None,
+               db=None, dw_dtype=None):
+    """(dx, dw, db) of oc_glu_fwd; arguments as oc_dense_bwd."""
+    return _layer_bwd(True, x, w, dy, pre, act, need_dx, need_dw, need_db, dw, db, dw_dtype)
+
+
+def _grad_list(tensors, name, dtypes):
+    """Host arrays of the tensors' addresses, dtype codes and counts."""
+    d = torch.cuda.current_device() if torch.cuda.is_available() else -1
+    ptrs, dts, counts = [], [], []
+    for i, t in enumerate(tensors):
+        if not t.is_cuda or t.device.index != d or not t.is_contiguous() or t.dtype not in dtypes:
+            raise OcError(1, f"{name}[{i}] must be a contiguous float32 or bfloat16 tensor on "
+                             f"cuda:{d}")
+        ptrs.append(t.data_ptr())
+        dts.append(OC_BF16 if t.dtype is torch.bfloat16 else OC_F32)
+        counts.append(t.numel())
+    n = len(ptrs)
+    return n, (C.c_void_p * n)(*ptrs), (C.c_int * n)(*dts), (C.c_int64 * n)(*counts)
+
+
+_GRAD_TYPES = (torch.float32, torch.bfloat16)
+
+
+def oc_grad_norm(grads):
+    """The global 2-norm of a list of tensors, as a 0-d device tensor."""
+    n, ptrs, dts, counts = _grad_list(grads, "grads", _GRAD_TYPES)
+    L, dev = load(), torch.device("cuda", torch.cuda.current_device())
+    norm = torch.empty((), dtype=torch.float32, device=dev)
+    ws = _ws(L.oc_grad_workspace(n, counts), dev)
+    _check(L.oc_grad_norm(n, ptrs, dts, counts, _dev(norm, "norm"), _dev(ws, "ws"), ws.numel(),
+                          _stream()))
+    return norm
+
+
+def oc_grad_clip(grads, max_norm, outs=None):
+    """Scale the gradients to a global norm of at most max_norm, in place or into
+    outs (tensors of float32 or the gradients' own dtype); the norm before that,
+    as a 0-d device tensor."""
+    n, ptrs, dts, counts = _grad_list(grads, "grads", _GRAD_TYPES)
+    if outs is None:
+        optrs, odts = ptrs, dts
+    else:
+        m, optrs, odts, ocounts = _grad_list(outs, "outs", _GRAD_TYPES)
+        if m != n or list(ocounts) != list(counts):
+            raise OcError(1, "outs and grads differ in number or size")
+    L, dev = load(), torch.device("cuda", torch.cuda.current_device())
+    norm = torch.empty((), dtype=torch.float32, device=dev)
+    ws = _ws(L.oc_grad_workspace(n, counts), dev)
+    _check(L.oc_grad_clip(n, ptrs, dts, counts, max_norm, optrs, odts, _dev(norm, "norm"),
+                          _dev(ws, "ws"), ws.numel(), _stream()))
+    return norm

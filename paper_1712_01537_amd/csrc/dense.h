@@ -1,0 +1,183 @@
+// Dense layers over rows: the matrix products of oc_dense_* and oc_glu_* and
+// what their epilogues do.
+#pragma once
+
+#include "common.h"
+
+namespace oc {
+
+typedef float d_v4f __attribute__((ext_vector_type(4)));
+typedef uint32_t d_v4u __attribute__((ext_vector_type(4)));
+typedef uint32_t d_v2u __attribute__((ext_vector_type(2)));
+// Vectors at any element's address: global memory takes them at any alignment.
+typedef d_v4f d_v4f_any __attribute__((aligned(4)));
+typedef d_v4u d_v4u_any __attribute__((aligned(2)));
+
+// What becomes of the product z [M][nz] (nz = n, or 2 n when glu):
+//   glu 0: y[m][c] = act(z[m][c] + bias[c]) + res[m][c]
+//   glu 1: y[m][c] = act(z[m][c] + bias[c]) (z[m][n + c] + bias[n + c])
+// pre (if any) receives z + bias.  y and res are bf16 when y_bf16, pre when
+// pre_bf16, else fp32.  A residual may be y itself: a lane reads its elements
+// before it writes them.
+struct Epi {
+  int32_t act, glu, n;
+  int32_t y_bf16, pre_bf16;
+  const float* bias;
+  const void* res;
+  void* y;
+  void* pre;
+};
+
+// out [P][Q] = sum over r < R of A(p, r) B(r, q), then `epi` (M = P, nz = Q).
+//   a_rs 0: A is stored [P][R], 1: [R][P].  b_rs 1: B is stored [R][Q], 0: [Q][R].
+// Leading dimensions are those row lengths.  dt: type of A and B.
+struct Gemm {
+  oc_dtype dt;
+  int64_t P, R;
+  int32_t Q;
+  const void *a, *b;
+  bool a_rs, b_rs;
+  Epi epi;
+};
+
+// Bytes of workspace the product needs (partial sums of a split reduction);
+// a function of the type, the sizes and the layout alone.
+size_t gemm_ws(oc_dtype dt, int64_t P, int64_t Q, int64_t R, bool a_rs, bool b_rs, bool glu);
+// Enqueue it.  main: its kernel does the call's main arithmetic (profiling).
+void gemm(const Gemm& g, void* ws, bool main, hipStream_t s);
+
+// --- device side ---------------------------------------------------------
+
+__device__ __forceinline__ float bf_up(uint32_t h) {
+  return __builtin_bit_cast(float, h << 16);
+}
+// Two values rounded to bf16 (nearest, ties to even), the first in the low half.
+__device__ __forceinline__ uint32_t bf_pair(float a, float b) {
+  typedef float v2f __attribute__((ext_vector_type(2)));
+  typedef __bf16 v2bf __attribute__((ext_vector_type(2)));
+  return __builtin_bit_cast(uint32_t, __builtin_convertvector((v2f){a, b}, v2bf));
+}
+
+// Activations and their slopes in fp32.  SiLU is z s, s = 1 / (1 + e^-z), of
+// slope s (1 + z (1 - s)); GELU is z Phi(z), of slope Phi(z) + z phi(z), Phi
+// and phi the normal distribution and its density.
+__device__ __forceinline__ float act_value(int act, float z) {
+  if (act == OC_ACT_RELU) return z > 0.f || z != z ? z : 0.f;
+  if (act == OC_ACT_SILU) return z / (1.f + expf(-z));
+  if (act == OC_ACT_GELU) return 0.5f * z * (1.f + erff(z * 0.70710678118654752f));
+  return z;
+}
+__device__ __forceinline__ float act_slope(int act, float z) {
+  if (act == OC_ACT_RELU) return z > 0.f ? 1.f : 0.f;
+  if (act == OC_ACT_SILU) {
+    const float s = 1.f / (1.f + expf(-z));
+    return s * (1.f + z * (1.f - s));
+  }
+  if (act == OC_ACT_GELU)
+    return 0.5f * (1.f + erff(z * 0.70710678118654752f)) +
+           z * expf(-0.5f * z * z) * 0.39894228040143268f;
+  return 1.f;
+}
+
+// Eight consecutive elements i .. i + 7 of an fp32 or bf16 array.
+__device__ __forceinline__ void load8(const void* p, bool bf16, int64_t i, float (&v)[8]) {
+  if (bf16) {
+    const d_v4u u = *(const d_v4u_any*)((const uint16_t*)p + i);
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+      v[2 * k] = bf_up(u[k] & 0xffffu);
+      v[2 * k + 1] = __builtin_bit_cast(float, u[k] & 0xffff0000u);
+    }
+  } else {
+    const d_v4f a = *(const d_v4f_any*)((const float*)p + i);
+    const d_v4f b = *(const d_v4f_any*)((const float*)p + i + 4);
+#pragma unroll
+    for (int k = 0; k < 4; ++k) v[k] = a[k], v[4 + k] = b[k];
+  }
+}
+__device__ __forceinline__ void store8(void* p, bool bf16, int64_t i, const float (&v)[8]) {
+  if (bf16) {
+    *(d_v4u_any*)((uint16_t*)p + i) = d_v4u{bf_pair(v[0], v[1]), bf_pair(v[2], v[3]),
+                                            bf_pair(v[4], v[5]), bf_pair(v[6], v[7])};
+  } else {
+    *(d_v4f_any*)((float*)p + i) = d_v4f{v[0], v[1], v[2], v[3]};
+    *(d_v4f_any*)((float*)p + i + 4) = d_v4f{v[4], v[5], v[6], v[7]};
+  }
+}
+__device__ __forceinline__ float load1(const void* p, bool bf16, int64_t i) {
+  return bf16 ? bf_up(((const uint16_t*)p)[i]) : ((const float*)p)[i];
+}
+__device__ __forceinline__ void store1(void* p, bool bf16, int64_t i, float v) {
+  if (bf16)
+    ((uint16_t*)p)[i] = (uint16_t)bf_pair(v, v);
+  else
+    ((float*)p)[i] = v;
+}
+// The first cnt (1..8) of them; the others read as zero and are not written.
+__device__ __forceinline__ void load8n(const void* p, bool bf16, int64_t i, int cnt, float (&v)[8]) {
+  if (cnt >= 8) {
+    load8(p, bf16, i, v);
+  } else {
+#pragma unroll
+    for (int k = 0; k < 8; ++k) v[k] = k < cnt ? load1(p, bf16, i + k) : 0.f;
+  }
+}
+__device__ __forceinline__ void store8n(void* p, bool bf16, int64_t i, int cnt,
+                                        const float (&v)[8]) {
+  if (cnt >= 8) {
+    store8(p, bf16, i, v);
+  } else {
+#pragma unroll
+    for (int k = 0; k < 8; ++k)
+      if (k < cnt) store1(p, bf16, i + k, v[k]);
+  }
+}
+
+// Eight columns c .. c + 7 of row m (those below e.n) without glu; z is used up.
+__device__ __forceinline__ void epi8(const Epi& e, int64_t m, int c, float (&z)[8]) {
+  const int cnt = e.n - c;
+  if (cnt <= 0) return;
+  if (e.bias) {
+    float b[8];
+    load8n(e.bias, false, c, cnt, b);
+#pragma unroll
+    for (int k = 0; k < 8; ++k) z[k] += b[k];
+  }
+  if (e.pre) store8n(e.pre, e.pre_bf16, m * e.n + c, cnt, z);
+  if (e.act != OC_ACT_NONE) {
+#pragma unroll
+    for (int k = 0; k < 8; ++k) z[k] = act_value(e.act, z[k]);
+  }
+  if (e.res) {
+    float r[8];
+    load8n(e.res, e.y_bf16, m * e.n + c, cnt, r);
+#pragma unroll
+    for (int k = 0; k < 8; ++k) z[k] += r[k];
+  }
+  store8n(e.y, e.y_bf16, m * e.n + c, cnt, z);
+}
+
+// The same with glu: g the gate's columns c .. c + 7, u the other half's.
+__device__ __forceinline__ void epi8_glu(const Epi& e, int64_t m, int c, float (&g)[8],
+                                         float (&u)[8]) {
+  const int cnt = e.n - c;
+  if (cnt <= 0) return;
+  if (e.bias) {
+    float b[8];
+    load8n(e.bias, false, c, cnt, b);
+#pragma unroll
+    for (int k = 0; k < 8; ++k) g[k] += b[k];
+    load8n(e.bias, false, e.n + c, cnt, b);
+#pragma unroll
+    for (int k = 0; k < 8; ++k) u[k] += b[k];
+  }
+  if (e.pre) {
+    store8n(e.pre, e.pre_bf16, m * 2 * e.n + c, cnt, g);
+    store8n(e.pre, e.pre_bf16, m * 2 * e.n + e.n + c, cnt, u);
+  }
+#pragma unroll
+  for (int k = 0; k < 8; ++k) g[k] = act_value(e.act, g[k]) * u[k];
+  store8n(e.y, e.y_bf16, m * e.n + c, cnt, g);
+}
+
+}  // namespace oc

@@ -1,0 +1,303 @@
+// Dense layers over rows (oc_dense_*, oc_glu_*): argument checks, the
+// elementwise part of the backward and the order of the launches.  The
+// products are in dense_gemm.hip.
+//
+// Backward: dz = dy act'(z) (gated: dg = dy u act'(g), du = dy act(g), dz = [dg
+// | du]) is written once, in the type of the products' operands, and read by
+// both of them: dx = dz w^T and dw = x^T dz.  Forming dz inside the products
+// instead would read z (fp32) and dy once per tile column of each.  In bf16
+// that rounds dz once (half a step, 2^-9), as the matrix cores' operand has to
+// be; z itself is kept in fp32, since a rounded z would move the slope and so
+// round the gradients a second time.  dbias is summed from the unrounded dz in
+// the same pass.
+#include <algorithm>
+
+#include "dense.h"
+
+namespace {
+
+using oc::cdiv;
+
+constexpr int TB = 256;
+
+// --- dz and its column sums -------------------------------------------------
+//
+// A thread has eight columns and every rl-th row of the block's range; block
+// (b, k) has rows M b / nb .. and columns 8 ct k ..  Column sums: per thread
+// fp32 over its rows (about 30), then the row lanes in order through LDS into
+// part[b][column], then k_colsum in double over the blocks: a fixed order.
+// Bound by memory: dy and z read, dz written.
+struct DzShape {
+  int ct, rl, kb, nb;  // column threads, row lanes, column blocks, row blocks
+};
+DzShape dz_shape(int64_t M, int n) {
+  DzShape d;
+  const int chunks = (int)cdiv(n, 8);
+  d.ct = 1;
+  while (d.ct < chunks && d.ct < 32) d.ct *= 2;
+  d.rl = TB / d.ct;
+  d.kb = (int)cdiv(chunks, d.ct);
+  const int64_t most = std::max<int64_t>(64, 2048 / d.kb);
+  d.nb = (int)std::max<int64_t>(1, std::min<int64_t>(most, cdiv(M, 8 * d.rl)));
+  return d;
+}
+
+// glu 0: z, dz [M][n]; 1: z, dz [M][2 n].  dz NULL: column sums only (dz = dy).
+template <bool GLU>
+__global__ __launch_bounds__(TB) void k_dz(const void* dy, const void* z, bool bf16, bool z_bf16,
+                                           int act, int64_t M, int n, int ct, void* dz,
+                                           float* part) {
+  __shared__ float red[GLU ? 2 : 1][8][TB];
+  const int tid = threadIdx.x, tc = tid % ct, tr = tid / ct, rl = TB / ct;
+  const int nb = gridDim.x, b = blockIdx.x;
+  const int64_t r0 = M * b / nb, r1 = M * (b + 1) / nb;
+  const int c = (blockIdx.y * ct + tc) * 8, cnt = n - c;
+  float s0[8] = {}, s1[8] = {};
+  if (cnt > 0)
+    for (int64_t m = r0 + tr; m < r1; m += rl) {
+      float g[8], v[8], u[8];
+      oc::load8n(dy, bf16, m * n + c, cnt, g);
+      if (GLU) {
+        oc::load8n(z, false, m * 2 * n + c, cnt, v);
+        oc::load8n(z, false, m * 2 * n + n + c, cnt, u);
+#pragma unroll
+        for (int k = 0; k < 8; ++k) {
+          const float d = g[k];
+          g[k] = d * u[k] * oc::act_slope(act, v[k]);
+          u[k] = d * oc::act_value(act, v[k]);
+          s0[k] += g[k];
+          s1[k] += u[k];
+        }
+        oc::store8n(dz, bf16, m * 2 * n + c, cnt, g);
+        oc::store8n(dz, bf16, m * 2 * n + n + c, cnt, u);
+      } else {
+        if (act != OC_ACT_NONE) {
+          oc::load8n(z, z_bf16, m * n + c, cnt, v);
+#pragma unroll
+          for (int k = 0; k < 8; ++k) g[k] *= oc::act_slope(act, v[k]);
+        }
+#pragma unroll
+        for (int k = 0; k < 8; ++k) s0[k] += g[k];
+        if (dz) oc::store8n(dz, bf16, m * n + c, cnt, g);
+      }
+    }
+  if (!part) return;
+#pragma unroll
+  for (int k = 0; k < 8; ++k) {
+    red[0][k][tid] = s0[k];
+    if (GLU) red[GLU][k][tid] = s1[k];
+  }
+  __syncthreads();
+  const int nz = GLU ? 2 * n : n;
+  for (int i = tid; i < ct * 8; i += TB) {  // column i of the block
+    const int cc = blockIdx.y * ct * 8 + i;
+    if (cc >= n) continue;
+    for (int h = 0; h < (GLU ? 2 : 1); ++h) {
+      float a = 0.f;
+      for (int r = 0; r < rl; ++r) a += red[h][i & 7][r * ct + (i >> 3)];
+      part[(int64_t)b * nz + h * n + cc] = a;
+    }
+  }
+}
+
+// out[c] = sum of part[b][c] over the nb blocks: 16 lanes per column take
+// every 16th block in double, then their sums are added in lane order.
+__global__ __launch_bounds__(TB) void k_colsum(const float* part, int nb, int nz, float* out) {
+  __shared__ double red[16][17];
+  const int cl = threadIdx.x & 15, l = threadIdx.x >> 4, c = blockIdx.x * 16 + cl;
+  double a = 0.0;
+  if (c < nz)
+    for (int b = l; b < nb; b += 16) a += (double)part[(int64_t)b * nz + c];
+  red[l][cl] = a;
+  __syncthreads();
+  if (l == 0 && c < nz) {
+    double t = 0.0;
+    for (int j = 0; j < 16; ++j) t += red[j][cl];
+    out[c] = (float)t;
+  }
+}
+
+// --- arguments ---------------------------------------------------------------
+
+constexpr int64_t MOST_ROWS = (int64_t)1 << 31;
+constexpr int32_t MOST_COLS = 1 << 16;
+
+oc_status check(const char* who, oc_dtype dt, int32_t act, bool glu, int64_t rows, int32_t cin,
+                int32_t cout) {
+  if (dt != OC_F32 && dt != OC_BF16) return oc::fail(OC_ERR_ARG, "%s: dtype %d", who, (int)dt);
+  if (act < OC_ACT_NONE || act > OC_ACT_GELU)
+    return oc::fail(OC_ERR_ARG, "%s: activation %d", who, act);
+  const int32_t most = glu ? MOST_COLS / 2 : MOST_COLS;
+  if (rows < 0 || rows >= MOST_ROWS || cin < 1 || cin > MOST_COLS || cout < 1 || cout > most)
+    return oc::fail(OC_ERR_ARG, "%s: %lld rows, %d -> %d channels", who, (long long)rows, cin,
+                    cout);
+  return OC_OK;
+}
+
+bool sizes_ok(oc_dtype dt, int64_t rows, int32_t cin, int32_t cout, bool glu) {
+  return (dt == OC_F32 || dt == OC_BF16) && rows > 0 && rows < MOST_ROWS && cin >= 1 &&
+         cin <= MOST_COLS && cout >= 1 && cout <= (glu ? MOST_COLS / 2 : MOST_COLS);
+}
+
+oc_status check_ws(const char* who, const void* ws, size_t have, size_t need) {
+  if (need && (!ws || have < need))
+    return oc::fail(OC_ERR_ARG, "%s: workspace %zu bytes < %zu", who, ws ? have : 0, need);
+  return OC_OK;
+}
+
+// n values of the type set to zero (two bytes a thread: bf16 buffers are not
+// aligned to four).
+__global__ __launch_bounds__(TB) void k_zero16(uint16_t* p, int64_t n) {
+  const int64_t i = (int64_t)blockIdx.x * TB + threadIdx.x;
+  if (i < n) p[i] = 0;
+}
+void zero(void* p, oc_dtype dt, int64_t n, hipStream_t s) {
+  const int64_t halves = dt == OC_F32 ? 2 * n : n;
+  oc::launch(k_zero16, dim3((unsigned)cdiv(halves, TB)), dim3(TB), 0, s, (uint16_t*)p, halves);
+}
+
+// --- the two layers -----------------------------------------------------------
+
+size_t fwd_ws(oc_dtype dt, int64_t rows, int32_t cin, int32_t cout, bool glu) {
+  return oc::gemm_ws(dt, rows, glu ? 2 * cout : cout, cin, false, true, glu);
+}
+
+oc_status fwd(const char* who, bool glu, oc_dtype dt, int32_t act, int64_t rows, int32_t cin,
+              int32_t cout, const void* x, const void* w, const float* bias, const void* res,
+              void* y, void* pre, void* ws, size_t ws_bytes, hipStream_t s) {
+  oc_status st = check(who, dt, act, glu, rows, cin, cout);
+  if (st != OC_OK) return st;
+  if (rows == 0) return OC_OK;
+  if (!x || !w || !y) return oc::fail(OC_ERR_ARG, "%s: NULL buffer", who);
+  st = check_ws(who, ws, ws_bytes, fwd_ws(dt, rows, cin, cout, glu));
+  if (st != OC_OK) return st;
+  const int32_t bf16 = dt == OC_BF16;
+  oc::Gemm g{dt,    rows, cin,  glu ? 2 * cout : cout, x, w, false, true,
+             {act, glu, cout, bf16, bf16 && act == OC_ACT_RELU && !glu, bias, res, y, pre}};
+  oc::gemm(g, ws, true, s);
+  OC_LAUNCH_CHECK();
+  return OC_OK;
+}
+
+struct BwdWs {
+  size_t dz, part, gemm, total;  // offsets, bytes in all
+};
+BwdWs bwd_ws(oc_dtype dt, int32_t act, int64_t rows, int32_t cin, int32_t cout, bool glu) {
+  const int64_t nz = glu ? 2 * cout : cout;
+  const DzShape d = dz_shape(rows, cout);
+  BwdWs b;
+  b.dz = 0;
+  b.part = glu || act != OC_ACT_NONE
+               ? oc::align256((size_t)rows * nz * (dt == OC_BF16 ? 2 : 4)) : 0;
+  b.gemm = b.part + oc::align256((size_t)d.nb * nz * 4);
+  b.total = b.gemm + oc::align256(std::max(oc::gemm_ws(dt, rows, cin, nz, false, false, false),
+                                           oc::gemm_ws(dt, cin, nz, rows, true, true, false)));
+  return b;
+}
+
+oc_status bwd(const char* who, bool glu, oc_dtype dt, int32_t act, int64_t rows, int32_t cin,
+              int32_t cout, const void* x, const void* w, const void* pre, const void* dy,
+              void* dx, oc_dtype dw_dt, void* dw, float* dbias, void* ws, size_t ws_bytes,
+              hipStream_t s) {
+  oc_status st = check(who, dt, act, glu, rows, cin, cout);
+  if (st != OC_OK) return st;
+  if (dw && dw_dt != OC_F32 && dw_dt != dt)
+    return oc::fail(OC_ERR_ARG, "%s: dw of dtype %d", who, (int)dw_dt);
+  const int32_t nz = glu ? 2 * cout : cout;
+  if (rows == 0) {  // sums over no rows
+    if (dw) zero(dw, dw_dt, (int64_t)cin * nz, s);
+    if (dbias) zero(dbias, OC_F32, nz, s);
+    OC_LAUNCH_CHECK();
+    return OC_OK;
+  }
+  const bool slope = glu || act != OC_ACT_NONE;
+  if (!dy || (slope && !pre) || (dx && !w) || (dw && !x))
+    return oc::fail(OC_ERR_ARG, "%s: NULL buffer", who);
+  if (!dx && !dw && !dbias) return OC_OK;
+  const BwdWs o = bwd_ws(dt, act, rows, cin, cout, glu);
+  st = check_ws(who, ws, ws_bytes, o.total);
+  if (st != OC_OK) return st;
+  char* base = (char*)ws;
+  const bool bf16 = dt == OC_BF16;
+  const void* dz = slope ? base + o.dz : dy;
+  if (slope || dbias) {
+    const DzShape d = dz_shape(rows, cout);
+    float* part = dbias ? (float*)(base + o.part) : nullptr;
+    void* out = slope && (dx || dw) ? base + o.dz : nullptr;
+    const dim3 grid(d.nb, d.kb);
+    if (glu)
+      oc::launch(k_dz<true>, grid, dim3(TB), 0, s, dy, pre, bf16, false, act, rows, cout, d.ct,
+                 (void*)(base + o.dz), part);
+    else
+      oc::launch(k_dz<false>, grid, dim3(TB), 0, s, dy, pre, bf16, bf16 && act == OC_ACT_RELU, act,
+                 rows, cout, d.ct, out, part);
+    if (dbias)
+      oc::launch(k_colsum, dim3((unsigned)cdiv(nz, 16)), dim3(TB), 0, s, (const float*)part, d.nb,
+                 nz, dbias);
+  }
+  if (dx) {
+    oc::Gemm g{dt,    rows, nz, cin, dz, w, false, false,
+               {OC_ACT_NONE, 0, cin, bf16, 0, nullptr, nullptr, dx, nullptr}};
+    oc::gemm(g, base + o.gemm, true, s);
+  }
+  if (dw) {
+    oc::Gemm g{dt,    cin, rows, nz, x, dz, true, true,
+               {OC_ACT_NONE, 0, nz, dw_dt == OC_BF16, 0, nullptr, nullptr, dw, nullptr}};
+    oc::gemm(g, base + o.gemm, !dx, s);
+  }
+  OC_LAUNCH_CHECK();
+  return OC_OK;
+}
+
+}  // namespace
+
+extern "C" {
+
+size_t oc_dense_fwd_workspace(oc_dtype dt, int64_t rows, int32_t cin, int32_t cout) {
+  return sizes_ok(dt, rows, cin, cout, false) ? fwd_ws(dt, rows, cin, cout, false) : 0;
+}
+
+oc_status oc_dense_fwd(oc_dtype dt, int32_t act, int64_t rows, int32_t cin, int32_t cout,
+                       const void* x, const void* w, const float* bias, const void* res, void* y,
+                       void* pre, void* ws, size_t ws_bytes, hipStream_t s) {
+  return fwd("oc_dense_fwd", false, dt, act, rows, cin, cout, x, w, bias, res, y, pre, ws,
+             ws_bytes, s);
+}
+
+size_t oc_dense_bwd_workspace(oc_dtype dt, int32_t act, int64_t rows, int32_t cin, int32_t cout) {
+  return sizes_ok(dt, rows, cin, cout, false) ? bwd_ws(dt, act, rows, cin, cout, false).total : 0;
+}
+
+oc_status oc_dense_bwd(oc_dtype dt, int32_t act, int64_t rows, int32_t cin, int32_t cout,
+                       const void* x, const void* w, const void* pre, const void* dy, void* dx,
+                       oc_dtype dw_dt, void* dw, float* dbias, void* ws, size_t ws_bytes,
+                       hipStream_t s) {
+  return bwd("oc_dense_bwd", false, dt, act, rows, cin, cout, x, w, pre, dy, dx, dw_dt, dw, dbias,
+             ws, ws_bytes, s);
+}
+
+size_t oc_glu_fwd_workspace(oc_dtype dt, int64_t rows, int32_t cin, int32_t cout) {
+  return sizes_ok(dt, rows, cin, cout, true) ? fwd_ws(dt, rows, cin, cout, true) : 0;
+}
+
+oc_status oc_glu_fwd(oc_dtype dt, int32_t act, int64_t rows, int32_t cin, int32_t cout,
+                     const void* x, const void* w, const float* bias, void* y, float* pre,
+                     void* ws, size_t ws_bytes, hipStream_t s) {
+  return fwd("oc_glu_fwd", true, dt, act, rows, cin, cout, x, w, bias, nullptr, y, pre, ws,
+             ws_bytes, s);
+}
+
+size_t oc_glu_bwd_workspace(oc_dtype dt, int64_t rows, int32_t cin, int32_t cout) {
+  return sizes_ok(dt, rows, cin, cout, true)
+             ? bwd_ws(dt, OC_ACT_NONE, rows, cin, cout, true).total : 0;
+}
+
+oc_status oc_glu_bwd(oc_dtype dt, int32_t act, int64_t rows, int32_t cin, int32_t cout,
+                     const void* x, const void* w, const float* pre, const void* dy, void* dx,
+                     oc_dtype dw_dt, void* dw, float* dbias, void* ws, size_t ws_bytes,
+                     hipStream_t s) {
+  return bwd("oc_glu_bwd", true, dt, act, rows, cin, cout, x, w, pre, dy, dx, dw_dt, dw, dbias, ws,
+             ws_bytes, s);
+}
+
+}  // extern "C"
