@@ -1,0 +1,40 @@
+// The dense layers' tile kernel for bf16 operands.
+#include "dense_tile.h"
+
+namespace {
+
+template <int SHAPE, bool ARS, bool BRS, bool GLU, bool DIRECT>
+void go(bool main, const oc::TileArgs& t, hipStream_t s) {
+  constexpr oc::TileInfo i = oc::tile_info<uint16_t>(SHAPE);
+  constexpr int WGM = i.threads / 64 / (i.bn / 64);
+  const auto k = oc::k_dense_tile<uint16_t, i.bm, i.bn, WGM, i.bk, ARS, BRS, GLU, DIRECT>;
+  const dim3 grid((unsigned)((int64_t)t.ntm * t.ntn * t.splits));
+  if (main) oc::launch_main(k, grid, dim3(i.threads), s, t);
+  else oc::launch(k, grid, dim3(i.threads), 0, s, t);
+}
+
+template <int SHAPE, bool DIRECT>
+void pick(bool a_rs, bool b_rs, bool main, const oc::TileArgs& t, hipStream_t s) {
+  if (a_rs) go<SHAPE, true, true, false, DIRECT>(main, t, s);
+  else if (!b_rs) go<SHAPE, false, false, false, DIRECT>(main, t, s);
+  else if (t.epi.glu) go<SHAPE, false, true, true, DIRECT>(main, t, s);
+  else go<SHAPE, false, true, false, DIRECT>(main, t, s);
+}
+
+}  // namespace
+
+namespace oc {
+
+void tile_bf16(int shape, bool a_rs, bool b_rs, bool direct, bool main, const TileArgs& t,
+               hipStream_t s) {
+  switch (shape * 2 + direct) {
+    case 0: return pick<TILE_LARGE, false>(a_rs, b_rs, main, t, s);
+    case 1: return pick<TILE_LARGE, true>(a_rs, b_rs, main, t, s);
+    case 2: return pick<TILE_MEDIUM, false>(a_rs, b_rs, main, t, s);
+    case 3: return pick<TILE_MEDIUM, true>(a_rs, b_rs, main, t, s);
+    case 4: return pick<TILE_SMALL, false>(a_rs, b_rs, main, t, s);
+    default: return pick<TILE_SMALL, true>(a_rs, b_rs, main, t, s);
+  }
+}
+
+}  // namespace oc

@@ -1,0 +1,36 @@
+// The dense layers' tile kernel for fp32 operands.
+#include "dense_tile.h"
+
+namespace {
+
+template <int SHAPE, bool ARS, bool BRS, bool GLU>
+void go(bool main, const oc::TileArgs& t, hipStream_t s) {
+  constexpr oc::TileInfo i = oc::tile_info<float>(SHAPE);
+  constexpr int WGM = i.threads / 64 / (i.bn / 64);
+  const auto k = oc::k_dense_tile<float, i.bm, i.bn, WGM, i.bk, ARS, BRS, GLU, false>;
+  const dim3 grid((unsigned)((int64_t)t.ntm * t.ntn * t.splits));
+  if (main) oc::launch_main(k, grid, dim3(i.threads), s, t);
+  else oc::launch(k, grid, dim3(i.threads), 0, s, t);
+}
+
+template <int SHAPE>
+void pick(bool a_rs, bool b_rs, bool main, const oc::TileArgs& t, hipStream_t s) {
+  if (a_rs) go<SHAPE, true, true, false>(main, t, s);
+  else if (!b_rs) go<SHAPE, false, false, false>(main, t, s);
+  else if (t.epi.glu) go<SHAPE, false, true, true>(main, t, s);
+  else go<SHAPE, false, true, false>(main, t, s);
+}
+
+}  // namespace
+
+namespace oc {
+
+void tile_f32(int shape, bool a_rs, bool b_rs, bool main, const TileArgs& t, hipStream_t s) {
+  switch (shape) {
+    case TILE_LARGE: return pick<TILE_LARGE>(a_rs, b_rs, main, t, s);
+    case TILE_MEDIUM: return pick<TILE_MEDIUM>(a_rs, b_rs, main, t, s);
+    default: return pick<TILE_SMALL>(a_rs, b_rs, main, t, s);
+  }
+}
+
+}  // namespace oc

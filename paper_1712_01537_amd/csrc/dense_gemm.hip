@@ -1,108 +1,115 @@
-// The matrix products of the dense layers, in plain fp32 FMAs: a 64 x 64 tile
-// per workgroup, 16 terms of the reduction at a time through LDS.  Each thread
-// forms 2 rows of eight columns (with glu: eight gate columns and the eight of
-// the other half).  Every 1024 terms the running sum is added to the total and
-// starts again, so that a sum of 10^6 terms rounds like one of 10^3.
-#include "dense.h"
+// Which tiles a dense layer's product runs on, and the sum of a split reduction.
+#include <algorithm>
+
+#include "dense_tile.h"
 
 namespace {
 
 using oc::Epi;
+using oc::cdiv;
 
-constexpr int TB = 256, BM = 64, BN = 64, BK = 16;
+constexpr int TB = 256;
 
-__device__ __forceinline__ float at(const void* p, bool bf16, int64_t i) {
-  return oc::load1(p, bf16, i);
+// out = the epilogue of the sum of the splits' partial sums, in index order: a
+// thread per row and eight columns.
+template <bool GLU>
+__global__ __launch_bounds__(TB) void k_split_sum(const float* part, int splits, int64_t P, int Q,
+                                                  Epi e) {
+  const int nc = (e.n + 7) / 8;
+  const int64_t i = (int64_t)blockIdx.x * TB + threadIdx.x;
+  if (i >= P * nc) return;
+  const int64_t p = i / nc;
+  const int c = (int)(i - p * nc) * 8;
+  const int64_t step = P * Q;
+  const float* src = part + p * Q + c;
+  float v[8] = {}, u[8] = {};
+  for (int s = 0; s < splits; ++s, src += step) {
+    float w[8];
+    oc::load8n(src, false, 0, e.n - c, w);
+#pragma unroll
+    for (int k = 0; k < 8; ++k) v[k] += w[k];
+    if (GLU) {
+      oc::load8n(src, false, e.n, e.n - c, w);
+#pragma unroll
+      for (int k = 0; k < 8; ++k) u[k] += w[k];
+    }
+  }
+  if (GLU) oc::epi8_glu(e, p, c, v, u);
+  else oc::epi8(e, p, c, v);
 }
 
-__global__ __launch_bounds__(TB) void k_gemm(const void* a, const void* b, bool bf16, bool a_rs,
-                                             bool b_rs, int64_t P, int Q, int64_t R, Epi e) {
-  __shared__ float A[BK][BM + 1], B[BK][BN + 1];
-  const int tid = threadIdx.x;
-  const int64_t p0 = (int64_t)blockIdx.x * BM;
-  const int half = BN / 2;
-  // column of tile position j: glu tiles hold 32 gate columns, then the other half's 32
-  const int q0 = blockIdx.y * (e.glu ? half : BN);
-  auto col = [&](int j) {
-    if (!e.glu) return q0 + j < Q ? q0 + j : -1;
-    const int c = q0 + (j & (half - 1));
-    return c < e.n ? c + (j >= half ? e.n : 0) : -1;
+struct Plan {
+  int shape;
+  int ntm, ntn, splits;
+  int64_t per;
+};
+
+// Expected time of each shape and number of splits; the least is taken.  A step
+// of BK terms takes a workgroup `step` microseconds with `fit` of them on a CU,
+// a workgroup 3 more to start and finish; splits write and read their partial
+// sums at 4 TB/s and take another launch of 3.
+Plan plan(oc_dtype dt, int64_t P, int64_t Q, int64_t R, bool glu) {
+  struct Cost {
+    double step;
+    int fit;
   };
-  const int tm = tid >> 3, tn = tid & 7;
-  float acc[2][8] = {}, sum[2][8] = {};
-  for (int64_t r0 = 0; r0 < R; r0 += BK) {
-    for (int i = tid; i < BK * BM; i += TB) {
-      const int r = a_rs ? i / BM : i % BK, p = a_rs ? i % BM : i / BK;
-      const bool ok = p0 + p < P && r0 + r < R;
-      A[r][p] = ok ? at(a, bf16, a_rs ? (r0 + r) * P + p0 + p : (p0 + p) * R + r0 + r) : 0.f;
+  static const Cost cost[2][oc::TILE_SHAPES] = {{{2.4, 1}, {1.5, 1}, {1.4, 3}},
+                                                {{1.6, 1}, {0.9, 2}, {0.7, 4}}};
+  const int cus = oc::cu_count();
+  const int64_t n = glu ? Q / 2 : Q;
+  Plan best{};
+  double least = 1e300;
+  for (int k = 0; k < oc::TILE_SHAPES; ++k) {
+    const oc::TileInfo i = dt == OC_BF16 ? oc::tile_info<uint16_t>(k) : oc::tile_info<float>(k);
+    const Cost& c = cost[dt == OC_BF16][k];
+    const int64_t ntm = cdiv(P, i.bm), ntn = cdiv(n, glu ? i.bn / 2 : i.bn);
+    const int64_t steps = cdiv(R, i.bk), slots = (int64_t)cus * c.fit;
+    int64_t last = 0;
+    for (int64_t want = 1; want <= 256 && want <= steps; want = want < 8 ? want + 1 : want * 5 / 4) {
+      const int64_t each = cdiv(steps, want), splits = cdiv(steps, each);
+      if (splits == last || (splits > 1 && ntm * ntn * splits > 4 * slots)) continue;
+      last = splits;
+      const double rounds = (double)cdiv(ntm * ntn * splits, slots);
+      double us = rounds * (each * c.step + 3.0);
+      if (splits > 1) us += 3.0 + (double)splits * P * Q * 8 / 4e6;
+      if (us < least) {
+        least = us;
+        best = Plan{k, (int)ntm, (int)ntn, (int)splits, each * i.bk};
+      }
     }
-    for (int i = tid; i < BK * BN; i += TB) {
-      const int r = b_rs ? i / BN : i % BK, j = b_rs ? i % BN : i / BK;
-      const int q = col(j);
-      const bool ok = q >= 0 && r0 + r < R;
-      B[r][j] = ok ? at(b, bf16, b_rs ? (r0 + r) * Q + q : q * R + r0 + r) : 0.f;
-    }
-    __syncthreads();
-    for (int r = 0; r < BK; ++r)
-#pragma unroll
-      for (int i = 0; i < 2; ++i)
-#pragma unroll
-        for (int j = 0; j < 8; ++j)
-          acc[i][j] = fmaf(A[r][tm + 32 * i], B[r][tn * 8 + j], acc[i][j]);
-    __syncthreads();
-    if (r0 + BK >= R || (r0 / BK + 1) % 64 == 0)
-#pragma unroll
-      for (int i = 0; i < 2; ++i)
-#pragma unroll
-        for (int j = 0; j < 8; ++j) {
-          sum[i][j] += acc[i][j];
-          acc[i][j] = 0.f;
-        }
   }
-#pragma unroll
-  for (int i = 0; i < 2; ++i)
-#pragma unroll
-    for (int j = 0; j < 8; ++j) acc[i][j] = sum[i][j];
-  if (!e.glu) {
-#pragma unroll
-    for (int i = 0; i < 2; ++i) {
-      const int64_t m = p0 + tm + 32 * i;
-      if (m < P) oc::epi8(e, m, q0 + tn * 8, acc[i]);
-    }
-    return;
-  }
-  __shared__ float U[BM][half + 1];
-#pragma unroll
-  for (int i = 0; i < 2; ++i)
-#pragma unroll
-    for (int j = 0; j < 8; ++j)
-      if (tn >= 4) U[tm + 32 * i][(tn - 4) * 8 + j] = acc[i][j];
-  __syncthreads();
-  if (tn < 4)
-#pragma unroll
-    for (int i = 0; i < 2; ++i) {
-      const int64_t m = p0 + tm + 32 * i;
-      float u[8];
-#pragma unroll
-      for (int j = 0; j < 8; ++j) u[j] = U[tm + 32 * i][tn * 8 + j];
-      if (m < P) oc::epi8_glu(e, m, q0 + tn * 8, acc[i], u);
-    }
+  return best;
 }
+
+// Rows that are whole 16-byte vectors at 16-byte addresses.
+bool vectors(const void* p, int64_t ld) { return (uintptr_t)p % 16 == 0 && ld % 8 == 0; }
 
 }  // namespace
 
 namespace oc {
 
-size_t gemm_ws(oc_dtype, int64_t, int64_t, int64_t, bool, bool, bool) { return 0; }
+size_t gemm_ws(oc_dtype dt, int64_t P, int64_t Q, int64_t R, bool, bool, bool glu) {
+  const Plan p = plan(dt, P, Q, R, glu);
+  return p.splits > 1 ? align256((size_t)p.splits * P * Q * 4) : 0;
+}
 
-void gemm(const Gemm& g, void*, bool main, hipStream_t s) {
-  const dim3 grid((unsigned)cdiv(g.P, BM), (unsigned)cdiv(g.epi.n, g.epi.glu ? BN / 2 : BN));
-  if (main)
-    launch_main(k_gemm, grid, dim3(TB), s, g.a, g.b, g.dt == OC_BF16, g.a_rs, g.b_rs, g.P, g.Q,
-                g.R, g.epi);
+void gemm(const Gemm& g, void* ws, bool main, hipStream_t s) {
+  const Plan p = plan(g.dt, g.P, g.Q, g.R, g.epi.glu);
+  const TileArgs t{g.a, g.b, g.P, g.R, g.Q, p.ntm, p.ntn, p.splits, p.per,
+                   p.splits > 1 ? (float*)ws : nullptr, g.epi};
+  if (g.dt == OC_F32) {
+    tile_f32(p.shape, g.a_rs, g.b_rs, main, t, s);
+  } else {
+    const bool direct = vectors(g.a, g.a_rs ? g.P : g.R) && vectors(g.b, g.b_rs ? g.Q : g.R) &&
+                        (!g.epi.glu || g.epi.n % 8 == 0);
+    tile_bf16(p.shape, g.a_rs, g.b_rs, direct, main, t, s);
+  }
+  if (p.splits == 1) return;
+  const dim3 grid((unsigned)cdiv(g.P * cdiv(g.epi.n, 8), TB));
+  if (g.epi.glu)
+    launch(k_split_sum<true>, grid, dim3(TB), 0, s, (const float*)ws, p.splits, g.P, g.Q, g.epi);
   else
-    launch(k_gemm, grid, dim3(TB), 0, s, g.a, g.b, g.dt == OC_BF16, g.a_rs, g.b_rs, g.P, g.Q, g.R,
-           g.epi);
+    launch(k_split_sum<false>, grid, dim3(TB), 0, s, (const float*)ws, p.splits, g.P, g.Q, g.epi);
 }
 
 }  // namespace oc

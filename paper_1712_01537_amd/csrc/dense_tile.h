@@ -1,0 +1,413 @@
+// The tile kernel of the dense layers' products on the matrix cores:
+//   out[p][q] = sum over r of A(p, r) B(r, q)
+// with either operand stored along the reduction ("row" operands: [P][R], [Q][R])
+// or across it ("column" operands: [R][P], [R][Q]), so that one kernel serves the
+// forward (x, w), the input gradient (dz, w along its columns) and the weight
+// gradient (x and dz across their rows) without transposing anything in memory.
+//
+// A workgroup owns a BM x BN tile, its waves TM x 64 pieces of it, and walks the
+// reduction BK at a time through two LDS buffers: while one is multiplied the
+// next lands in the other, one barrier a step.  The product is formed transposed
+// (the MFMA's first operand is B), so that a lane ends up with consecutive
+// columns of one row: with the columns of a 64-wide piece dealt out as q = 16 t
+// + 4 j + i (lane group t, MFMA j, accumulator register i), sixteen of them, and
+// the epilogue reads and writes whole vectors straight from the accumulators.
+//
+// bf16 operands whose rows are whole 16-byte vectors go from memory to LDS
+// directly (buffer_load ... lds; what is out of range reads as zero); others, and
+// fp32 ones, pass through registers, where fp32 values are split in three bf16
+// parts (split3.h), so that each is split once per tile.  fp32: six MFMAs a
+// product.
+//
+// LDS layouts, in 16-byte vectors: a row operand keeps its rows (BK values) with
+// the vectors of a row rotated by XOR, a column operand keeps [BK][BM or BN] the
+// same way and is read by the transposing load (ds_read_b64_tr_b16: lane i of a
+// 16-lane group receives element i % 4 of the 8-byte rows read by lanes 4 r + i /
+// 4, r = 0..3).  The XORs put the vectors that one pass of a read serves on
+// distinct banks (in permuted columns, on at most two to a bank).
+#pragma once
+
+#include "dense.h"
+#include "split3.h"
+
+namespace oc {
+
+struct TileArgs {
+  const void *a, *b;
+  int64_t P, R;
+  int32_t Q;                // B's columns in memory (2 n with glu)
+  int32_t ntm, ntn;         // tiles
+  int32_t splits;           // ranges of the reduction, `per` terms each
+  int64_t per;
+  float* part;              // [splits][P][Q] partial sums, where splits > 1
+  Epi epi;
+};
+
+// Tile shapes, by type; see gemm() for which is taken.
+enum TileShape { TILE_LARGE, TILE_MEDIUM, TILE_SMALL, TILE_SHAPES };
+struct TileInfo {
+  int bm, bn, threads, bk;
+};
+template <typename T>
+constexpr TileInfo tile_info(int shape) {
+  constexpr bool f32 = sizeof(T) == 4;
+  return shape == TILE_LARGE    ? TileInfo{256, f32 ? 128 : 256, 512, f32 ? 32 : 64}
+         : shape == TILE_MEDIUM ? TileInfo{128, 128, f32 ? 512 : 256, f32 ? 32 : 64}
+                                : TileInfo{64, 64, 256, f32 ? 32 : 64};
+}
+
+// Enqueue the tile kernel for fp32 or bf16 operands (dense_f32.hip, dense_bf16.hip).
+void tile_f32(int shape, bool a_rs, bool b_rs, bool main, const TileArgs& t, hipStream_t s);
+void tile_bf16(int shape, bool a_rs, bool b_rs, bool direct, bool main, const TileArgs& t,
+               hipStream_t s);
+
+// --- device side ---------------------------------------------------------
+
+typedef __attribute__((address_space(3))) void* dt_lptr;
+typedef short dt_v4s __attribute__((ext_vector_type(4)));
+typedef __attribute__((address_space(3))) dt_v4s dt_lds_v4s;
+typedef int32_t dt_sv4 __attribute__((ext_vector_type(4)));
+
+// The rotation of row `row`'s vectors in a row operand (CK vectors a row).
+// perm: columns dealt out over groups of 16 NT as the file's head says.
+template <int CK, bool PERM, int NT>
+__device__ __forceinline__ int row_xor(int row) {
+  const int rr = PERM ? ((row / (4 * NT)) & 3) * 4 + (row & 3) : row & 15;
+  return CK == 8 ? (rr >> 1) & 7 : (4 - (rr >> 2)) & 3;
+}
+// The rotation of line k's vectors in a column operand (CR vectors a line).
+template <int CR, bool PERM, int NT>
+__device__ __forceinline__ int col_xor(int k) {
+  if (!PERM)
+    return CR >= 16 ? 2 * ((k & 3) | ((k >> 3) & 1) << 2)
+                    : 2 * (((k >> 1) & 1) | ((k >> 3) & 1) << 1);
+  if (NT == 4) return CR >= 16 ? (k & 1) | ((k >> 1) & 1) << 3 : (k >> 1) & 1;
+  return CR >= 16 ? 4 * (k & 3) : 4 * ((k >> 1) & 1);
+}
+
+// Workgroup barrier that orders LDS accesses only.
+__device__ __forceinline__ void dt_barrier() {
+  asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
+}
+// All of this wave's vector memory operations are done.
+__device__ __forceinline__ void dt_wait_vm() { __builtin_amdgcn_s_waitcnt(0x0F70); }
+
+// Memory to LDS: lane i's 16 bytes at byte `off` of the resource land at lds +
+// 16 i; an offset past the resource's end stores zeros.
+__device__ __forceinline__ void dt_lds_load16(dt_sv4 rsrc, uint32_t off, uint32_t lds) {
+  asm volatile("s_mov_b32 m0, %0\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds" ::"s"(lds), "v"(off),
+               "s"(rsrc)
+               : "memory", "m0");
+}
+constexpr uint32_t kPastEnd = 0x80000000u;  // of any resource
+__device__ __forceinline__ dt_sv4 dt_rsrc(const char* p, int64_t bytes) {
+  const uint64_t a = (uint64_t)(uintptr_t)p;
+  const int64_t most = 0x7ffffff0;
+  return dt_sv4{(int32_t)(uint32_t)a, (int32_t)((a >> 32) & 0xffffu),
+                (int32_t)(bytes < most ? bytes : most), 0x00020000};
+}
+
+// Tile of block `bid`: each XCD (blocks are dealt out to the eight in turn) takes
+// a contiguous range, splits outermost, in groups of eight rows of tiles, so that
+// the tiles an XCD works on at a time share operands in its L2.
+struct TilePos {
+  int m, n, split;
+};
+__device__ __forceinline__ TilePos tile_pos(const TileArgs& t, uint32_t bid) {
+  const uint32_t total = gridDim.x, x = bid & 7, per = total >> 3, rem = total & 7;
+  const uint32_t idx = x * per + (x < rem ? x : rem) + (bid >> 3);
+  const uint32_t tiles = (uint32_t)t.ntm * t.ntn, split = idx / tiles, i = idx - split * tiles;
+  const uint32_t group = i / (8 * t.ntn), j = i - group * 8 * t.ntn;
+  const uint32_t left = t.ntm - group * 8, rows = left < 8 ? left : 8;
+  const uint32_t n = j / rows;
+  return TilePos{(int)(group * 8 + (j - n * rows)), (int)n, (int)split};
+}
+
+template <typename T, int BM, int BN, int WGM, int BK, bool ARS, bool BRS, bool GLU, bool DIRECT>
+__global__ __launch_bounds__(64 * WGM * (BN / 64)) void k_dense_tile(TileArgs t) {
+  constexpr bool F32 = sizeof(T) == 4;
+  static_assert(!(F32 && DIRECT), "fp32 operands are split in registers");
+  constexpr int PARTS = F32 ? 3 : 1;
+  constexpr int WGN = BN / 64, NTHR = 64 * WGM * WGN;
+  constexpr int TM = BM / WGM, TN = 64, MI = TM / 16, NI = 4;
+  constexpr int NT = GLU ? 2 : 4;  // MFMAs a lane's consecutive columns span
+  constexpr int CK = BK / 8, CA = BM * CK, CB = BN * CK;
+  constexpr int ITA = CA / NTHR, ITB = CB / NTHR, IT = ITA + ITB;
+  static_assert(CA % NTHR == 0 && CB % NTHR == 0 && TM % 16 == 0, "whole vectors per thread");
+  static_assert(!GLU || (!ARS && BRS), "the gated layer is a forward product");
+  constexpr int STAGE = PARTS * (CA + CB);
+  __shared__ __attribute__((aligned(16))) s3_v4u lds[2 * STAGE];
+
+  const int tid = threadIdx.x, lane = tid & 63, li = lane & 15, q = lane >> 4;
+  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int wm = wave / WGN, wn = wave % WGN;
+  const TilePos pos = tile_pos(t, blockIdx.x);
+  const int64_t p0 = (int64_t)pos.m * BM;
+  const int n = t.epi.n;
+  const int q0 = pos.n * (GLU ? BN / 2 : BN);  // first output column
+  const int64_t r0 = pos.split * t.per;
+  const int64_t r1 = r0 + t.per < t.R ? r0 + t.per : t.R;
+  const int nk = (int)((r1 - r0 + BK - 1) / BK);
+
+  // This thread's vectors: element offset from the operand's tile corner, how
+  // many of the eight values exist (rows past the end repeat the last one, whose
+  // results are dropped), and the vector's place along the reduction.
+  uint32_t off[IT];
+  int cnt[IT], kof[IT];
+#pragma unroll
+  for (int i = 0; i < IT; ++i) {
+    const bool isa = i < ITA;
+    const int c = (isa ? i : i - ITA) * NTHR + tid;
+    if (isa ? !ARS : !BRS) {
+      const int row = c / CK;
+      const int x = isa ? row_xor<CK, false, NT>(row) : row_xor<CK, true, NT>(row);
+      kof[i] = ((c % CK) ^ x) * 8;
+      const int64_t lim = isa ? t.P - p0 : (int64_t)t.Q - q0;
+      const int rr = row < lim ? row : (int)lim - 1;
+      off[i] = (uint32_t)rr * (uint32_t)t.R + kof[i];
+      cnt[i] = 8;
+    } else {
+      constexpr int CRA = BM / 8, CRB = BN / 8;
+      const int cr = isa ? CRA : CRB;
+      kof[i] = c / cr;
+      const int x = isa ? col_xor<CRA, false, NT>(kof[i]) : col_xor<CRB, true, NT>(kof[i]);
+      const int col = ((c % cr) ^ x) * 8;
+      int lim, e, add = 0;  // of the columns' range, the column, what is added to it
+      if (isa) {
+        lim = (int)(t.P - p0 < BM ? t.P - p0 : BM), e = col;
+      } else if (GLU) {
+        lim = n - q0;
+        e = col / TN * (TN / 2) + col % (TN / 2);
+        add = col % TN >= TN / 2 ? n : 0;
+      } else {
+        lim = t.Q - q0, e = col;
+      }
+      cnt[i] = lim - e < 0 ? 0 : lim - e < 8 ? lim - e : 8;
+      const uint32_t ld = isa ? (uint32_t)t.P : (uint32_t)t.Q;
+      off[i] = (uint32_t)kof[i] * ld + (cnt[i] > 0 ? e + add : 0);
+    }
+  }
+  const char* const abase = (const char*)t.a + (ARS ? r0 * t.P + p0 : p0 * t.R + r0) * sizeof(T);
+  const char* const bbase =
+      (const char*)t.b + (BRS ? r0 * t.Q + q0 : (int64_t)q0 * t.R + r0) * sizeof(T);
+  const int64_t astep = (ARS ? BK * t.P : BK) * sizeof(T);
+  const int64_t bstep = (BRS ? (int64_t)BK * t.Q : BK) * sizeof(T);
+
+  // Direct: start the loads of step ks into buffer s.
+  const uint32_t lds0 = __builtin_amdgcn_readfirstlane((uint32_t)(uintptr_t)(dt_lptr)lds);
+  auto issue = [&](int ks, int s) __attribute__((always_inline)) {
+    const char* pa = abase + ks * astep;
+    const char* pb = bbase + ks * bstep;
+    const dt_sv4 ra = dt_rsrc(pa, (const char*)t.a + t.P * t.R * (int64_t)sizeof(T) - pa);
+    const dt_sv4 rb = dt_rsrc(pb, (const char*)t.b + t.R * t.Q * (int64_t)sizeof(T) - pb);
+    const int64_t left = r1 - r0 - (int64_t)ks * BK;
+#pragma unroll
+    for (int i = 0; i < IT; ++i) {
+      const bool isa = i < ITA;
+      const uint32_t o = cnt[i] > 0 && kof[i] < left ? off[i] * 2 : kPastEnd;
+      const uint32_t at = (isa ? i : i - ITA) * NTHR + wave * 64 + (isa ? 0 : CA);
+      dt_lds_load16(isa ? ra : rb, o, lds0 + (s * STAGE + at) * 16);
+    }
+  };
+
+  // Through registers: load step ks, then split and store it to buffer s.
+  s3_v4u reg[IT][F32 ? 2 : 1];
+  bool whole = true;  // every vector of the tile exists, ends of the reduction aside
+  if constexpr (!DIRECT) {
+#pragma unroll
+    for (int i = 0; i < IT; ++i) whole = whole && (cnt[i] == 8 || cnt[i] == 0);
+    whole = __syncthreads_and(whole);
+  }
+  auto fetch = [&](int ks) __attribute__((always_inline)) {
+    const char* pa = abase + ks * astep;
+    const char* pb = bbase + ks * bstep;
+    const int64_t left = r1 - r0 - (int64_t)ks * BK;
+    if (whole && left >= BK) {
+#pragma unroll
+      for (int i = 0; i < IT; ++i) {
+        const char* p = (i < ITA ? pa : pb) + (uint64_t)off[i] * sizeof(T);
+        if (F32) {
+          reg[i][0] = __builtin_bit_cast(s3_v4u, *(const d_v4f_any*)p);
+          reg[i][F32] = __builtin_bit_cast(s3_v4u, *(const d_v4f_any*)(p + 16));
+        } else {
+          reg[i][0] = *(const d_v4u_any*)p;
+        }
+      }
+    } else {
+#pragma unroll
+      for (int i = 0; i < IT; ++i) {
+        const bool isa = i < ITA;
+        const char* p = (isa ? pa : pb) + (uint64_t)off[i] * sizeof(T);
+        const int64_t l = left - kof[i];
+        int m = l <= 0 ? 0 : cnt[i];
+        if ((isa ? !ARS : !BRS) && l < m) m = l < 0 ? 0 : (int)l;
+        float v[8] = {};
+        if (m > 0) load8n(p, !F32, 0, m, v);
+        if (F32) {
+#pragma unroll
+          for (int k = 0; k < 4; ++k) {
+            reg[i][0][k] = __builtin_bit_cast(uint32_t, v[k]);
+            reg[i][F32][k] = __builtin_bit_cast(uint32_t, v[4 + k]);
+          }
+        } else {
+          reg[i][0] = s3_v4u{bf_pair(v[0], v[1]), bf_pair(v[2], v[3]), bf_pair(v[4], v[5]),
+                             bf_pair(v[6], v[7])};
+        }
+      }
+    }
+  };
+  const SplitK sk = s3_consts();
+  auto stash = [&](int s) __attribute__((always_inline)) {
+#pragma unroll
+    for (int i = 0; i < IT; ++i) {
+      const bool isa = i < ITA;
+      const int c = s * STAGE + (isa ? i : i - ITA) * NTHR + tid + (isa ? 0 : PARTS * CA);
+      if constexpr (F32) {
+        const Split8 p = s3_split8(sk, __builtin_bit_cast(s3_v4f, reg[i][0]),
+                                   __builtin_bit_cast(s3_v4f, reg[i][F32]));
+#pragma unroll
+        for (int k = 0; k < 3; ++k) lds[c + k * (isa ? CA : CB)] = p.p[k];
+      } else {
+        lds[c] = reg[i][0];
+      }
+    }
+  };
+
+  s3_v4f acc[MI][NI];
+#pragma unroll
+  for (int i = 0; i < MI; ++i)
+#pragma unroll
+    for (int j = 0; j < NI; ++j) acc[i][j] = s3_v4f{0.f, 0.f, 0.f, 0.f};
+
+  // Operands of one MFMA: eight consecutive terms of the reduction for row (A) or
+  // column (B) li of the fragment, terms 8 q .. of the 32 of sub-step kk.
+  auto tr = [&](const char* p, int line) __attribute__((always_inline)) {
+    const auto* a = (const __attribute__((address_space(3))) char*)p;
+    const s3_v2u lo = __builtin_bit_cast(s3_v2u, __builtin_amdgcn_ds_read_tr16_b64_v4i16((dt_lds_v4s*)a));
+    const s3_v2u hi = __builtin_bit_cast(
+        s3_v2u, __builtin_amdgcn_ds_read_tr16_b64_v4i16((dt_lds_v4s*)(a + 4 * line)));
+    return s3_v4u{lo[0], lo[1], hi[0], hi[1]};
+  };
+  auto frag_a = [&](int s, int part, int kk, int mi) __attribute__((always_inline)) {
+    const s3_v4u* base = lds + s * STAGE + part * CA;
+    if constexpr (!ARS) {
+      const int row = wm * TM + mi * 16 + li;
+      return base[row * CK + ((kk * 4 + q) ^ row_xor<CK, false, NT>(li))];
+    } else {
+      constexpr int CR = BM / 8;
+      const int k = kk * 32 + q * 8 + (li >> 2);
+      const int c = wm * (TM / 8) + mi * 2 + ((li & 3) >> 1);
+      return tr((const char*)(base + k * CR + (c ^ col_xor<CR, false, NT>(k))) + (li & 1) * 8,
+                CR * 16);
+    }
+  };
+  auto frag_b = [&](int s, int part, int kk, int ni) __attribute__((always_inline)) {
+    const s3_v4u* base = lds + s * STAGE + PARTS * CA + part * CB;
+    const int g = ni / NT, j = ni % NT;
+    if constexpr (!BRS) {
+      const int row = wn * TN + g * 16 * NT + (li >> 2) * 4 * NT + j * 4 + (li & 3);
+      return base[row * CK + ((kk * 4 + q) ^ row_xor<CK, true, NT>(row))];
+    } else {
+      constexpr int CR = BN / 8;
+      const int k = kk * 32 + q * 8 + (li >> 2);
+      const int col = wn * TN + g * 16 * NT + (li & 3) * 4 * NT + j * 4;
+      return tr((const char*)(base + k * CR + ((col >> 3) ^ col_xor<CR, true, NT>(k))) +
+                    (j & 1) * 8,
+                CR * 16);
+    }
+  };
+  auto compute = [&](int s) __attribute__((always_inline)) {
+#pragma unroll
+    for (int kk = 0; kk < BK / 32; ++kk) {
+      s3_v4u b[NI][PARTS];
+#pragma unroll
+      for (int j = 0; j < NI; ++j)
+#pragma unroll
+        for (int k = 0; k < PARTS; ++k) b[j][k] = frag_b(s, k, kk, j);
+#pragma unroll
+      for (int i = 0; i < MI; ++i) {
+        s3_v4u a[PARTS];
+#pragma unroll
+        for (int k = 0; k < PARTS; ++k) a[k] = frag_a(s, k, kk, i);
+#pragma unroll
+        for (int j = 0; j < NI; ++j) {
+          if constexpr (F32) {
+#pragma unroll
+            for (int x = 0; x < 6; ++x) acc[i][j] = s3_product(x, b[j], a, acc[i][j]);
+          } else {
+            acc[i][j] = s3_mfma(b[j][0], a[0], acc[i][j]);
+          }
+        }
+      }
+    }
+  };
+
+  if constexpr (DIRECT) {
+    issue(0, 0);
+    for (int ks = 0; ks < nk; ++ks) {
+      dt_wait_vm();  // this wave's loads of step ks have landed
+      dt_barrier();  // everyone's have, and step ks - 1 is no longer read
+      if (ks + 1 < nk) issue(ks + 1, (ks + 1) & 1);
+      compute(ks & 1);
+    }
+  } else {
+    fetch(0);
+    stash(0);
+    dt_barrier();
+    for (int ks = 0; ks < nk; ++ks) {
+      if (ks + 1 < nk) fetch(ks + 1);
+      compute(ks & 1);
+      if (ks + 1 < nk) stash((ks + 1) & 1);
+      dt_barrier();
+    }
+  }
+
+  // fp32: what the three parts cannot represent is formed again in plain fp32
+  // (operands of 2^103 and more, sums of 2^80 and more, infinities, NaN).
+  auto plain = [&](int64_t p, int c) {
+    float z = 0.f;
+    for (int64_t r = r0; r < r1; ++r) {
+      const float x = ((const float*)t.a)[ARS ? r * t.P + p : p * t.R + r];
+      const float y = ((const float*)t.b)[BRS ? r * t.Q + c : c * t.R + r];
+      z = fmaf(x, y, z);
+    }
+    return z;
+  };
+  auto take = [&](int i, int j, int64_t p, int c, float* v) __attribute__((always_inline)) {
+    const bool bad = F32 && s3_bad(acc[i][j]);
+#pragma unroll
+    for (int k = 0; k < 4; ++k) v[k] = F32 ? acc[i][j][k] * kSplitDown : acc[i][j][k];
+    if (F32 && bad)
+#pragma unroll
+      for (int k = 0; k < 4; ++k)
+        if (c + k < t.Q && !(fabsf(v[k]) < INFINITY)) v[k] = plain(p, c + k);
+  };
+#pragma unroll
+  for (int i = 0; i < MI; ++i) {
+    const int64_t p = p0 + wm * TM + i * 16 + li;
+    if (p >= t.P) continue;
+#pragma unroll
+    for (int h = 0; h < (GLU ? 1 : 2); ++h) {
+      float v[8], u[8];
+      const int c = q0 + (GLU ? wn * (TN / 2) + q * 8 : wn * TN + q * 16 + h * 8);
+      if (c >= n) continue;
+      take(i, 2 * h, p, c, v);
+      take(i, 2 * h + 1, p, c + 4, v + 4);
+      if (GLU) {
+        take(i, 2, p, n + c, u);
+        take(i, 3, p, n + c + 4, u + 4);
+      }
+      if (t.part) {
+        float* o = t.part + ((int64_t)pos.split * t.P + p) * t.Q;
+        store8n(o, false, c, n - c, v);
+        if (GLU) store8n(o, false, n + c, n - c, u);
+      } else if (GLU) {
+        epi8_glu(t.epi, p, c, v, u);
+      } else {
+        epi8(t.epi, p, c, v);
+      }
+    }
+  }
+}
+
+}  // namespace oc
