@@ -133,51 +133,66 @@ __device__ __forceinline__ void store8n(void* p, bool bf16, int64_t i, int cnt,
   }
 }
 
-// Eight columns c .. c + 7 of row m (those below e.n) without glu; z is used up.
-__device__ __forceinline__ void epi8(const Epi& e, int64_t m, int c, float (&z)[8]) {
+// The epilogue of U rows m[] (those below M), columns c .. c + 7 (those below e.n):
+// z the sums and b0 the bias there; with GLU z and b0 are the gate's, u and b1 the
+// other half's.  z and u are used up.
+template <int U, bool GLU>
+__device__ __forceinline__ void epilogue(const Epi& e, const int64_t (&m)[U], int64_t M, int c,
+                                         const float (&b0)[8], const float (&b1)[8],
+                                         float (&z)[U][8], float (&u)[U][8]) {
   const int cnt = e.n - c;
-  if (cnt <= 0) return;
-  if (e.bias) {
-    float b[8];
-    load8n(e.bias, false, c, cnt, b);
+  float r[U][8];
+  if (!GLU && e.res) {
 #pragma unroll
-    for (int k = 0; k < 8; ++k) z[k] += b[k];
+    for (int i = 0; i < U; ++i)
+      if (m[i] < M) load8n(e.res, e.y_bf16, m[i] * e.n + c, cnt, r[i]);
   }
-  if (e.pre) store8n(e.pre, e.pre_bf16, m * e.n + c, cnt, z);
-  if (e.act != OC_ACT_NONE) {
 #pragma unroll
-    for (int k = 0; k < 8; ++k) z[k] = act_value(e.act, z[k]);
-  }
-  if (e.res) {
-    float r[8];
-    load8n(e.res, e.y_bf16, m * e.n + c, cnt, r);
+  for (int i = 0; i < U; ++i)
 #pragma unroll
-    for (int k = 0; k < 8; ++k) z[k] += r[k];
-  }
-  store8n(e.y, e.y_bf16, m * e.n + c, cnt, z);
-}
-
-// The same with glu: g the gate's columns c .. c + 7, u the other half's.
-__device__ __forceinline__ void epi8_glu(const Epi& e, int64_t m, int c, float (&g)[8],
-                                         float (&u)[8]) {
-  const int cnt = e.n - c;
-  if (cnt <= 0) return;
-  if (e.bias) {
-    float b[8];
-    load8n(e.bias, false, c, cnt, b);
-#pragma unroll
-    for (int k = 0; k < 8; ++k) g[k] += b[k];
-    load8n(e.bias, false, e.n + c, cnt, b);
-#pragma unroll
-    for (int k = 0; k < 8; ++k) u[k] += b[k];
-  }
+    for (int k = 0; k < 8; ++k) {
+      z[i][k] += b0[k];
+      if (GLU) u[i][k] += b1[k];
+    }
   if (e.pre) {
-    store8n(e.pre, e.pre_bf16, m * 2 * e.n + c, cnt, g);
-    store8n(e.pre, e.pre_bf16, m * 2 * e.n + e.n + c, cnt, u);
+#pragma unroll
+    for (int i = 0; i < U; ++i)
+      if (m[i] < M) {
+        const int64_t at = m[i] * (GLU ? 2 : 1) * e.n + c;
+        store8n(e.pre, e.pre_bf16, at, cnt, z[i]);
+        if (GLU) store8n(e.pre, e.pre_bf16, at + e.n, cnt, u[i]);
+      }
+  }
+  if (e.act == OC_ACT_RELU) {
+#pragma unroll
+    for (int i = 0; i < U; ++i)
+#pragma unroll
+      for (int k = 0; k < 8; ++k) z[i][k] = act_value(OC_ACT_RELU, z[i][k]);
+  } else if (e.act == OC_ACT_SILU) {
+#pragma unroll
+    for (int i = 0; i < U; ++i)
+#pragma unroll
+      for (int k = 0; k < 8; ++k) z[i][k] = act_value(OC_ACT_SILU, z[i][k]);
+  } else if (e.act == OC_ACT_GELU) {
+#pragma unroll
+    for (int i = 0; i < U; ++i)
+#pragma unroll
+      for (int k = 0; k < 8; ++k) z[i][k] = act_value(OC_ACT_GELU, z[i][k]);
+  }
+  if (GLU) {
+#pragma unroll
+    for (int i = 0; i < U; ++i)
+#pragma unroll
+      for (int k = 0; k < 8; ++k) z[i][k] *= u[i][k];
+  } else if (e.res) {
+#pragma unroll
+    for (int i = 0; i < U; ++i)
+#pragma unroll
+      for (int k = 0; k < 8; ++k) z[i][k] += r[i][k];
   }
 #pragma unroll
-  for (int k = 0; k < 8; ++k) g[k] = act_value(e.act, g[k]) * u[k];
-  store8n(e.y, e.y_bf16, m * e.n + c, cnt, g);
+  for (int i = 0; i < U; ++i)
+    if (m[i] < M) store8n(e.y, e.y_bf16, m[i] * e.n + c, cnt, z[i]);
 }
 
 }  // namespace oc

@@ -38,7 +38,7 @@ DzShape dz_shape(int64_t M, int n) {
   d.rl = TB / d.ct;
   d.kb = (int)cdiv(chunks, d.ct);
   const int64_t most = std::max<int64_t>(64, 2048 / d.kb);
-  d.nb = (int)std::max<int64_t>(1, std::min<int64_t>(most, cdiv(M, 8 * d.rl)));
+  d.nb = (int)std::max<int64_t>(1, std::min<int64_t>(most, cdiv(M, 4 * d.rl)));
   return d;
 }
 
@@ -100,21 +100,23 @@ __global__ __launch_bounds__(TB) void k_dz(const void* dy, const void* z, bool b
   }
 }
 
-// out[c] = sum of part[b][c] over the nb blocks: 16 lanes per column take
-// every 16th block in double, then their sums are added in lane order.
+// out[c] = sum of part[b][c] over the nb blocks, in double: 64 lanes per column
+// take every 64th block, then a fixed tree through LDS.
 __global__ __launch_bounds__(TB) void k_colsum(const float* part, int nb, int nz, float* out) {
-  __shared__ double red[16][17];
-  const int cl = threadIdx.x & 15, l = threadIdx.x >> 4, c = blockIdx.x * 16 + cl;
+  __shared__ double red[TB];
+  const int cl = threadIdx.x & 3, l = threadIdx.x >> 2, c = blockIdx.x * 4 + cl;
   double a = 0.0;
-  if (c < nz)
-    for (int b = l; b < nb; b += 16) a += (double)part[(int64_t)b * nz + c];
-  red[l][cl] = a;
-  __syncthreads();
-  if (l == 0 && c < nz) {
-    double t = 0.0;
-    for (int j = 0; j < 16; ++j) t += red[j][cl];
-    out[c] = (float)t;
+  if (c < nz) {
+#pragma unroll 8
+    for (int b = l; b < nb; b += 64) a += (double)part[(int64_t)b * nz + c];
   }
+  red[threadIdx.x] = a;
+  __syncthreads();
+  for (int h = TB / 2; h >= 4; h >>= 1) {
+    if ((int)threadIdx.x < h) red[threadIdx.x] += red[threadIdx.x + h];
+    __syncthreads();
+  }
+  if (l == 0 && c < nz) out[c] = (float)red[cl];
 }
 
 // --- arguments ---------------------------------------------------------------
@@ -232,7 +234,7 @@ oc_status bwd(const char* who, bool glu, oc_dtype dt, int32_t act, int64_t rows,
       oc::launch(k_dz<false>, grid, dim3(TB), 0, s, dy, pre, bf16, bf16 && act == OC_ACT_RELU, act,
                  rows, cout, d.ct, out, part);
     if (dbias)
-      oc::launch(k_colsum, dim3((unsigned)cdiv(nz, 16)), dim3(TB), 0, s, (const float*)part, d.nb,
+      oc::launch(k_colsum, dim3((unsigned)cdiv(nz, 4)), dim3(TB), 0, s, (const float*)part, d.nb,
                  nz, dbias);
   }
   if (dx) {

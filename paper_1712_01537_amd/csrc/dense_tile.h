@@ -24,7 +24,7 @@
 // same way and is read by the transposing load (ds_read_b64_tr_b16: lane i of a
 // 16-lane group receives element i % 4 of the 8-byte rows read by lanes 4 r + i /
 // 4, r = 0..3).  The XORs put the vectors that one pass of a read serves on
-// distinct banks (in permuted columns, on at most two to a bank).
+// distinct banks.
 #pragma once
 
 #include "dense.h"
@@ -69,20 +69,15 @@ typedef __attribute__((address_space(3))) dt_v4s dt_lds_v4s;
 typedef int32_t dt_sv4 __attribute__((ext_vector_type(4)));
 
 // The rotation of row `row`'s vectors in a row operand (CK vectors a row).
-// perm: columns dealt out over groups of 16 NT as the file's head says.
-template <int CK, bool PERM, int NT>
+template <int CK>
 __device__ __forceinline__ int row_xor(int row) {
-  const int rr = PERM ? ((row / (4 * NT)) & 3) * 4 + (row & 3) : row & 15;
-  return CK == 8 ? (rr >> 1) & 7 : (4 - (rr >> 2)) & 3;
+  return CK == 8 ? (row >> 1) & 7 : (4 - (row >> 2)) & 3;
 }
 // The rotation of line k's vectors in a column operand (CR vectors a line).
-template <int CR, bool PERM, int NT>
+template <int CR>
 __device__ __forceinline__ int col_xor(int k) {
-  if (!PERM)
-    return CR >= 16 ? 2 * ((k & 3) | ((k >> 3) & 1) << 2)
-                    : 2 * (((k >> 1) & 1) | ((k >> 3) & 1) << 1);
-  if (NT == 4) return CR >= 16 ? (k & 1) | ((k >> 1) & 1) << 3 : (k >> 1) & 1;
-  return CR >= 16 ? 4 * (k & 3) : 4 * ((k >> 1) & 1);
+  return CR >= 16 ? 2 * ((k & 3) | ((k >> 3) & 1) << 2)
+                  : 2 * (((k >> 1) & 1) | ((k >> 3) & 1) << 1);
 }
 
 // Workgroup barrier that orders LDS accesses only.
@@ -97,7 +92,7 @@ __device__ __forceinline__ void dt_wait_vm() { __builtin_amdgcn_s_waitcnt(0x0F70
 __device__ __forceinline__ void dt_lds_load16(dt_sv4 rsrc, uint32_t off, uint32_t lds) {
   asm volatile("s_mov_b32 m0, %0\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds" ::"s"(lds), "v"(off),
                "s"(rsrc)
-               : "memory", "m0");
+               : "memory");
 }
 constexpr uint32_t kPastEnd = 0x80000000u;  // of any resource
 __device__ __forceinline__ dt_sv4 dt_rsrc(const char* p, int64_t bytes) {
@@ -130,13 +125,14 @@ __global__ __launch_bounds__(64 * WGM * (BN / 64)) void k_dense_tile(TileArgs t)
   constexpr int PARTS = F32 ? 3 : 1;
   constexpr int WGN = BN / 64, NTHR = 64 * WGM * WGN;
   constexpr int TM = BM / WGM, TN = 64, MI = TM / 16, NI = 4;
-  constexpr int NT = GLU ? 2 : 4;  // MFMAs a lane's consecutive columns span
   constexpr int CK = BK / 8, CA = BM * CK, CB = BN * CK;
   constexpr int ITA = CA / NTHR, ITB = CB / NTHR, IT = ITA + ITB;
   static_assert(CA % NTHR == 0 && CB % NTHR == 0 && TM % 16 == 0, "whole vectors per thread");
   static_assert(!GLU || (!ARS && BRS), "the gated layer is a forward product");
   constexpr int STAGE = PARTS * (CA + CB);
-  __shared__ __attribute__((aligned(16))) s3_v4u lds[2 * STAGE];
+  // the epilogue's pieces: ROWS rows of 64 sums per wave at a time
+  constexpr int ROWS = TM < 64 ? TM : 64, EPI = WGM * WGN * ROWS * 16;
+  __shared__ __attribute__((aligned(16))) s3_v4u lds[2 * STAGE > EPI ? 2 * STAGE : EPI];
 
   const int tid = threadIdx.x, lane = tid & 63, li = lane & 15, q = lane >> 4;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
@@ -160,8 +156,7 @@ __global__ __launch_bounds__(64 * WGM * (BN / 64)) void k_dense_tile(TileArgs t)
     const int c = (isa ? i : i - ITA) * NTHR + tid;
     if (isa ? !ARS : !BRS) {
       const int row = c / CK;
-      const int x = isa ? row_xor<CK, false, NT>(row) : row_xor<CK, true, NT>(row);
-      kof[i] = ((c % CK) ^ x) * 8;
+      kof[i] = ((c % CK) ^ row_xor<CK>(row)) * 8;
       const int64_t lim = isa ? t.P - p0 : (int64_t)t.Q - q0;
       const int rr = row < lim ? row : (int)lim - 1;
       off[i] = (uint32_t)rr * (uint32_t)t.R + kof[i];
@@ -170,7 +165,7 @@ __global__ __launch_bounds__(64 * WGM * (BN / 64)) void k_dense_tile(TileArgs t)
       constexpr int CRA = BM / 8, CRB = BN / 8;
       const int cr = isa ? CRA : CRB;
       kof[i] = c / cr;
-      const int x = isa ? col_xor<CRA, false, NT>(kof[i]) : col_xor<CRB, true, NT>(kof[i]);
+      const int x = isa ? col_xor<CRA>(kof[i]) : col_xor<CRB>(kof[i]);
       const int col = ((c % cr) ^ x) * 8;
       int lim, e, add = 0;  // of the columns' range, the column, what is added to it
       if (isa) {
@@ -292,28 +287,25 @@ __global__ __launch_bounds__(64 * WGM * (BN / 64)) void k_dense_tile(TileArgs t)
     const s3_v4u* base = lds + s * STAGE + part * CA;
     if constexpr (!ARS) {
       const int row = wm * TM + mi * 16 + li;
-      return base[row * CK + ((kk * 4 + q) ^ row_xor<CK, false, NT>(li))];
+      return base[row * CK + ((kk * 4 + q) ^ row_xor<CK>(li))];
     } else {
       constexpr int CR = BM / 8;
       const int k = kk * 32 + q * 8 + (li >> 2);
       const int c = wm * (TM / 8) + mi * 2 + ((li & 3) >> 1);
-      return tr((const char*)(base + k * CR + (c ^ col_xor<CR, false, NT>(k))) + (li & 1) * 8,
+      return tr((const char*)(base + k * CR + (c ^ col_xor<CR>(k))) + (li & 1) * 8,
                 CR * 16);
     }
   };
   auto frag_b = [&](int s, int part, int kk, int ni) __attribute__((always_inline)) {
     const s3_v4u* base = lds + s * STAGE + PARTS * CA + part * CB;
-    const int g = ni / NT, j = ni % NT;
     if constexpr (!BRS) {
-      const int row = wn * TN + g * 16 * NT + (li >> 2) * 4 * NT + j * 4 + (li & 3);
-      return base[row * CK + ((kk * 4 + q) ^ row_xor<CK, true, NT>(row))];
+      const int row = wn * TN + ni * 16 + li;
+      return base[row * CK + ((kk * 4 + q) ^ row_xor<CK>(li))];
     } else {
       constexpr int CR = BN / 8;
       const int k = kk * 32 + q * 8 + (li >> 2);
-      const int col = wn * TN + g * 16 * NT + (li & 3) * 4 * NT + j * 4;
-      return tr((const char*)(base + k * CR + ((col >> 3) ^ col_xor<CR, true, NT>(k))) +
-                    (j & 1) * 8,
-                CR * 16);
+      const int c = wn * (TN / 8) + ni * 2 + ((li & 3) >> 1);
+      return tr((const char*)(base + k * CR + (c ^ col_xor<CR>(k))) + (li & 1) * 8, CR * 16);
     }
   };
   auto compute = [&](int s) __attribute__((always_inline)) {
@@ -364,47 +356,91 @@ __global__ __launch_bounds__(64 * WGM * (BN / 64)) void k_dense_tile(TileArgs t)
 
   // fp32: what the three parts cannot represent is formed again in plain fp32
   // (operands of 2^103 and more, sums of 2^80 and more, infinities, NaN).
-  auto plain = [&](int64_t p, int c) {
-    float z = 0.f;
-    for (int64_t r = r0; r < r1; ++r) {
-      const float x = ((const float*)t.a)[ARS ? r * t.P + p : p * t.R + r];
-      const float y = ((const float*)t.b)[BRS ? r * t.Q + c : c * t.R + r];
-      z = fmaf(x, y, z);
+  auto again = [&](int64_t p, int c, int count, float* v) __attribute__((always_inline)) {
+#pragma unroll
+    for (int k = 0; k < 8; ++k) {
+      if (k >= count || fabsf(v[k]) < INFINITY) continue;
+      float z = 0.f;
+      for (int64_t r = r0; r < r1; ++r) {
+        const float x = ((const float*)t.a)[ARS ? r * t.P + p : p * t.R + r];
+        const float y = ((const float*)t.b)[BRS ? r * t.Q + c + k : (c + k) * t.R + r];
+        z = fmaf(x, y, z);
+      }
+      v[k] = z;
     }
-    return z;
   };
-  auto take = [&](int i, int j, int64_t p, int c, float* v) __attribute__((always_inline)) {
-    const bool bad = F32 && s3_bad(acc[i][j]);
+
+  // Epilogue: the wave's piece to LDS, ROWS rows at a time (16 vectors a row, XORed
+  // by the row), and back with eight columns of a row per lane (with glu, eight of
+  // either half).
+  constexpr int COLS = GLU ? 32 : 64, LR = COLS / 8;  // output columns, lanes a row
+  constexpr int MOST = TM > ROWS ? 2 : 4;  // sums still in registers leave room for fewer
+  constexpr int RI = 64 / LR, U = ROWS / RI < MOST ? ROWS / RI : MOST;
+  static_assert(ROWS % (RI * U) == 0, "whole groups of rows");
+  s3_v4u* const mine = lds + wave * ROWS * 16;
+  const int c = q0 + wn * COLS + lane % LR * 8, cols = n - c;
+  float b0[8] = {}, b1[8] = {};
+  if (t.epi.bias && !t.part && cols > 0) {
+    load8n(t.epi.bias, false, c, cols, b0);
+    if (GLU) load8n(t.epi.bias, false, n + c, cols, b1);
+  }
+  dt_barrier();  // no wave reads operands from LDS any more
 #pragma unroll
-    for (int k = 0; k < 4; ++k) v[k] = F32 ? acc[i][j][k] * kSplitDown : acc[i][j][k];
-    if (F32 && bad)
+  for (int pass = 0; pass < TM / ROWS; ++pass) {
 #pragma unroll
-      for (int k = 0; k < 4; ++k)
-        if (c + k < t.Q && !(fabsf(v[k]) < INFINITY)) v[k] = plain(p, c + k);
-  };
+    for (int i = 0; i < ROWS / 16; ++i)
 #pragma unroll
-  for (int i = 0; i < MI; ++i) {
-    const int64_t p = p0 + wm * TM + i * 16 + li;
-    if (p >= t.P) continue;
+      for (int j = 0; j < NI; ++j)
+        mine[(i * 16 + li) * 16 + ((j * 4 + q) ^ li)] =
+            __builtin_bit_cast(s3_v4u, acc[pass * (ROWS / 16) + i][j]);
+#pragma unroll 1
+    for (int g = 0; g < ROWS / (RI * U); ++g) {
+      float v[U][8], u[U][8];
+      int64_t p[U];
 #pragma unroll
-    for (int h = 0; h < (GLU ? 1 : 2); ++h) {
-      float v[8], u[8];
-      const int c = q0 + (GLU ? wn * (TN / 2) + q * 8 : wn * TN + q * 16 + h * 8);
-      if (c >= n) continue;
-      take(i, 2 * h, p, c, v);
-      take(i, 2 * h + 1, p, c + 4, v + 4);
-      if (GLU) {
-        take(i, 2, p, n + c, u);
-        take(i, 3, p, n + c + 4, u + 4);
+      for (int i = 0; i < U; ++i) {
+        const int row = (g * U + i) * RI + lane / LR;
+        p[i] = p0 + wm * TM + pass * ROWS + row;
+        auto get = [&](int col, float* w) __attribute__((always_inline)) {
+#pragma unroll
+          for (int h = 0; h < 2; ++h) {
+            const s3_v4f x = __builtin_bit_cast(
+                s3_v4f, mine[row * 16 + ((col / 4 + h) ^ (row & 15))]);
+#pragma unroll
+            for (int k = 0; k < 4; ++k) w[h * 4 + k] = F32 ? x[k] * kSplitDown : x[k];
+          }
+        };
+        get(lane % LR * 8, v[i]);
+        if (GLU) get(32 + lane % LR * 8, u[i]);
+      }
+      if (cols <= 0) continue;
+      if (F32) {
+        bool bad = false;
+#pragma unroll
+        for (int i = 0; i < U; ++i)
+#pragma unroll
+          for (int k = 0; k < 8; ++k) {
+            bad |= !(fabsf(v[i][k]) < INFINITY);
+            if (GLU) bad |= !(fabsf(u[i][k]) < INFINITY);
+          }
+        if (bad)
+#pragma unroll
+          for (int i = 0; i < U; ++i)
+            if (p[i] < t.P) {
+              again(p[i], c, cols, v[i]);
+              if (GLU) again(p[i], n + c, cols, u[i]);
+            }
       }
       if (t.part) {
-        float* o = t.part + ((int64_t)pos.split * t.P + p) * t.Q;
-        store8n(o, false, c, n - c, v);
-        if (GLU) store8n(o, false, n + c, n - c, u);
-      } else if (GLU) {
-        epi8_glu(t.epi, p, c, v, u);
+#pragma unroll
+        for (int i = 0; i < U; ++i)
+          if (p[i] < t.P) {
+            float* o = t.part + ((int64_t)pos.split * t.P + p[i]) * t.Q;
+            store8n(o, false, c, cols, v[i]);
+            if (GLU) store8n(o, false, n + c, cols, u[i]);
+          }
       } else {
-        epi8(t.epi, p, c, v);
+        epilogue<U, GLU>(t.epi, p, t.P, c, b0, b1, v, u);
       }
     }
   }
