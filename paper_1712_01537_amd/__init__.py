@@ -888,60 +888,63 @@ def oc_sgd(w, g, v, lr, momentum, decay):
 # --- dense layers and gradient clipping ------------------------------------
 
 
-def _here(**tensors):
-    """Every given tensor is on the current device, whose stream and kernels the
-    call uses."""
-    given = {name: t for name, t in tensors.items() if t is not None}
-    for name, t in given.items():
-        if not isinstance(t, torch.Tensor) or not t.is_cuda:
-            raise OcError(1, f"{name} must be a CUDA (HIP) tensor")
-    d = torch.cuda.current_device()
-    for name, t in given.items():
-        if t.device.index != d:
-            raise OcError(1, f"{name} is on {t.device}, the current device is cuda:{d}")
-
-
-def _ws(nbytes: int, device):
-    return torch.empty(max(int(nbytes), 1), dtype=torch.uint8, device=device)
+def _given(t, name, dev, dtype, shape):
+    """Address of a tensor that has to be contiguous, on the current device dev
+    (whose stream and kernels the call uses), of this dtype and shape; None for
+    None."""
+    if t is None:
+        return None
+    if (t.get_device() == dev and t.dtype is dtype and t.shape == shape and t.is_contiguous()):
+        return t.data_ptr()
+    if t.get_device() != dev:
+        raise OcError(1, f"{name} is on {t.device}, the current device is cuda:{dev}")
+    _dev(t, name, dtype, shape)
+    raise OcError(1, f"{name} does not fit")
 
 
 def _dense_dims(x, w, halves):
+    """Device, rows, cin, cout and columns of w."""
+    for name, t in (("x", x), ("w", w)):
+        if not isinstance(t, torch.Tensor) or not t.is_cuda:
+            raise OcError(1, f"{name} must be a CUDA (HIP) tensor")
     if x.dim() != 2 or w.dim() != 2 or w.shape[0] != x.shape[1] or w.shape[1] % halves:
         raise OcError(1, f"x {tuple(x.shape)} and w {tuple(w.shape)} do not go together")
-    if w.dtype != x.dtype:
-        raise OcError(1, "x and w must share a dtype")
-    return x.shape[0], x.shape[1], w.shape[1] // halves
+    rows, cin = x.shape
+    nz = w.shape[1]
+    return torch._C._cuda_getDevice(), rows, cin, nz // halves, nz
 
 
 def _layer_fwd(glu, x, w, b, res, act, need_pre):
-    _here(x=x, w=w, b=b, res=res)
-    L, dt = load(), _dtype_code(x)
-    rows, cin, cout = _dense_dims(x, w, 2 if glu else 1)
-    nz = w.shape[1]
-    y = torch.empty((rows, cout), dtype=x.dtype, device=x.device)
+    dev, rows, cin, cout, nz = _dense_dims(x, w, 2 if glu else 1)
+    L, t, dt = load(), x.dtype, _dtype_code(x)
+    xp, wp = _given(x, "x", dev, t, (rows, cin)), _given(w, "w", dev, t, (cin, nz))
+    bp = _given(b, "b", dev, torch.float32, (nz,))
+    rp = _given(res, "res", dev, t, (rows, cout))
+    y = torch.empty((rows, cout), dtype=t, device=x.device)
     pre = None
     if need_pre:
         pre = torch.empty((rows, nz), device=x.device,
-                          dtype=x.dtype if act == OC_ACT_RELU and not glu else torch.float32)
+                          dtype=t if act == OC_ACT_RELU and not glu else torch.float32)
+    pp = pre.data_ptr() if need_pre else None
     need = (L.oc_glu_fwd_workspace if glu else L.oc_dense_fwd_workspace)(dt, rows, cin, cout)
-    ws = _ws(need, x.device)
-    bias = _opt(b, "b", dtype=torch.float32, shape=(nz,))
+    ws = torch.empty(need, dtype=torch.uint8, device=x.device) if need else None
+    wsp = ws.data_ptr() if need else None
     if glu:
-        _check(L.oc_glu_fwd(dt, act, rows, cin, cout, _dev(x, "x"), _dev(w, "w"), bias,
-                            _dev(y, "y"), _opt(pre, "pre"), _dev(ws, "ws"), ws.numel(), _stream()))
+        _check(L.oc_glu_fwd(dt, act, rows, cin, cout, xp, wp, bp, y.data_ptr(), pp, wsp, need,
+                            _stream()))
     else:
-        _check(L.oc_dense_fwd(dt, act, rows, cin, cout, _dev(x, "x"), _dev(w, "w"), bias,
-                              _opt(res, "res", dtype=x.dtype, shape=(rows, cout)), _dev(y, "y"),
-                              _opt(pre, "pre"), _dev(ws, "ws"), ws.numel(), _stream()))
+        _check(L.oc_dense_fwd(dt, act, rows, cin, cout, xp, wp, bp, rp, y.data_ptr(), pp, wsp,
+                              need, _stream()))
     return y, pre
 
 
 def _layer_bwd(glu, x, w, dy, pre, act, need_dx, need_dw, need_db, dw, db, dw_dtype):
-    _here(x=x, w=w, dy=dy, pre=pre, dw=dw, db=db)
-    L, dt = load(), _dtype_code(x)
-    rows, cin, cout = _dense_dims(x, w, 2 if glu else 1)
-    nz = w.shape[1]
-    dx = torch.empty_like(x) if need_dx else None
+    dev, rows, cin, cout, nz = _dense_dims(x, w, 2 if glu else 1)
+    L, t, dt = load(), x.dtype, _dtype_code(x)
+    xp, wp = _given(x, "x", dev, t, (rows, cin)), _given(w, "w", dev, t, (cin, nz))
+    dyp = _given(dy, "dy", dev, t, (rows, cout))
+    pp = _given(pre, "pre", dev, t if act == OC_ACT_RELU and not glu else torch.float32, (rows, nz))
+    dx = torch.empty((rows, cin), dtype=t, device=x.device) if need_dx else None
     if dw is None and need_dw:
         dw = torch.empty((cin, nz), dtype=dw_dtype or torch.float32, device=x.device)
     if db is None and need_db:
@@ -949,14 +952,11 @@ def _layer_bwd(glu, x, w, dy, pre, act, need_dx, need_dw, need_db, dw, db, dw_dt
     dw_dt = OC_F32 if dw is None else _dtype_code(dw)
     need = (L.oc_glu_bwd_workspace(dt, rows, cin, cout) if glu
             else L.oc_dense_bwd_workspace(dt, act, rows, cin, cout))
-    ws = _ws(need, x.device)
-    pre_dt = x.dtype if act == OC_ACT_RELU and not glu else torch.float32
+    ws = torch.empty(need, dtype=torch.uint8, device=x.device)
     f = L.oc_glu_bwd if glu else L.oc_dense_bwd
-    _check(f(dt, act, rows, cin, cout, _dev(x, "x"), _dev(w, "w"),
-             _opt(pre, "pre", dtype=pre_dt, shape=(rows, nz)),
-             _dev(dy, "dy", x.dtype, (rows, cout)), _opt(dx, "dx"), dw_dt,
-             _opt(dw, "dw", shape=(cin, nz)), _opt(db, "db", dtype=torch.float32, shape=(nz,)),
-             _dev(ws, "ws"), ws.numel(), _stream()))
+    _check(f(dt, act, rows, cin, cout, xp, wp, pp, dyp, dx.data_ptr() if need_dx else None, dw_dt,
+             _given(dw, "dw", dev, dw.dtype if dw is not None else t, (cin, nz)),
+             _given(db, "db", dev, torch.float32, (nz,)), ws.data_ptr(), need, _stream()))
     return dx, dw, db
 
 
@@ -988,32 +988,39 @@ def oc_glu_bwd(x, w, dy, pre, act=OC_ACT_SILU, need_dx=True, need_dw=True, need_
     return _layer_bwd(True, x, w, dy, pre, act, need_dx, need_dw, need_db, dw, db, dw_dtype)
 
 
-def _grad_list(tensors, name, dtypes):
-    """Host arrays of the tensors' addresses, dtype codes and counts."""
-    d = torch.cuda.current_device() if torch.cuda.is_available() else -1
-    ptrs, dts, counts = [], [], []
+def _grad_list(tensors, name):
+    """Number, and host arrays of the tensors' addresses, dtype codes and counts."""
+    n = len(tensors)
     for i, t in enumerate(tensors):
-        if not t.is_cuda or t.device.index != d or not t.is_contiguous() or t.dtype not in dtypes:
-            raise OcError(1, f"{name}[{i}] must be a contiguous float32 or bfloat16 tensor on "
-                             f"cuda:{d}")
-        ptrs.append(t.data_ptr())
-        dts.append(OC_BF16 if t.dtype is torch.bfloat16 else OC_F32)
-        counts.append(t.numel())
-    n = len(ptrs)
-    return n, (C.c_void_p * n)(*ptrs), (C.c_int * n)(*dts), (C.c_int64 * n)(*counts)
+        if not t.is_cuda:
+            raise OcError(1, f"{name}[{i}] must be a CUDA (HIP) tensor")
+    dev = torch._C._cuda_getDevice()
+    if not all([t.get_device() == dev and t.is_contiguous() for t in tensors]):
+        raise OcError(1, f"{name} must be contiguous tensors on cuda:{dev}")
+    dts = [_GRAD_CODE.get(t.dtype, -1) for t in tensors]
+    if -1 in dts:
+        raise OcError(1, f"{name} must be float32 or bfloat16 tensors")
+    return (n, (C.c_void_p * n)(*[t.data_ptr() for t in tensors]), (C.c_int * n)(*dts),
+            (C.c_int64 * n)(*[t.numel() for t in tensors]))
 
 
-_GRAD_TYPES = (torch.float32, torch.bfloat16)
+def _grad_scratch(L, n, counts):
+    """The norm and the workspace of a call."""
+    dev = torch.device("cuda", torch.cuda.current_device())
+    need = L.oc_grad_workspace(n, counts)
+    return (torch.empty((), dtype=torch.float32, device=dev),
+            torch.empty(need, dtype=torch.uint8, device=dev), need)
+
+
+_GRAD_CODE = {torch.float32: OC_F32, torch.bfloat16: OC_BF16}
 
 
 def oc_grad_norm(grads):
     """The global 2-norm of a list of tensors, as a 0-d device tensor."""
-    n, ptrs, dts, counts = _grad_list(grads, "grads", _GRAD_TYPES)
-    L, dev = load(), torch.device("cuda", torch.cuda.current_device())
-    norm = torch.empty((), dtype=torch.float32, device=dev)
-    ws = _ws(L.oc_grad_workspace(n, counts), dev)
-    _check(L.oc_grad_norm(n, ptrs, dts, counts, _dev(norm, "norm"), _dev(ws, "ws"), ws.numel(),
-                          _stream()))
+    n, ptrs, dts, counts = _grad_list(grads, "grads")
+    L = load()
+    norm, ws, need = _grad_scratch(L, n, counts)
+    _check(L.oc_grad_norm(n, ptrs, dts, counts, norm.data_ptr(), ws.data_ptr(), need, _stream()))
     return norm
 
 
@@ -1021,16 +1028,14 @@ def oc_grad_clip(grads, max_norm, outs=None):
     """Scale the gradients to a global norm of at most max_norm, in place or into
     outs (tensors of float32 or the gradients' own dtype); the norm before that,
     as a 0-d device tensor."""
-    n, ptrs, dts, counts = _grad_list(grads, "grads", _GRAD_TYPES)
-    if outs is None:
-        optrs, odts = ptrs, dts
-    else:
-        m, optrs, odts, ocounts = _grad_list(outs, "outs", _GRAD_TYPES)
-        if m != n or list(ocounts) != list(counts):
+    n, ptrs, dts, counts = _grad_list(grads, "grads")
+    optrs, odts = ptrs, dts
+    if outs is not None:
+        m, optrs, odts, ocounts = _grad_list(outs, "outs")
+        if m != n or bytes(ocounts) != bytes(counts):
             raise OcError(1, "outs and grads differ in number or size")
-    L, dev = load(), torch.device("cuda", torch.cuda.current_device())
-    norm = torch.empty((), dtype=torch.float32, device=dev)
-    ws = _ws(L.oc_grad_workspace(n, counts), dev)
-    _check(L.oc_grad_clip(n, ptrs, dts, counts, max_norm, optrs, odts, _dev(norm, "norm"),
-                          _dev(ws, "ws"), ws.numel(), _stream()))
+    L = load()
+    norm, ws, need = _grad_scratch(L, n, counts)
+    _check(L.oc_grad_clip(n, ptrs, dts, counts, max_norm, optrs, odts, norm.data_ptr(),
+                          ws.data_ptr(), need, _stream()))
     return norm

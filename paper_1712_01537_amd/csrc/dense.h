@@ -60,22 +60,50 @@ __device__ __forceinline__ uint32_t bf_pair(float a, float b) {
 
 // Activations and their slopes in fp32.  SiLU is z s, s = 1 / (1 + e^-z), of
 // slope s (1 + z (1 - s)); GELU is z Phi(z), of slope Phi(z) + z phi(z), Phi
-// and phi the normal distribution and its density.
+// and phi the normal distribution and its density.  The exponential and the
+// reciprocal are the hardware's (one ulp of 2^x; x = z log2 e is off by |z| ulp,
+// where e^z itself is small), and 1 - erf is Hastings' polynomial in t = 1 / (1 +
+// p x) times e^(-x^2) (Abramowitz and Stegun 7.1.26, off by at most 1.5e-7, so Phi
+// by 0.75e-7, about one ulp): some 15 instructions a value instead of 40 for erff,
+// which took 40 of the 107 us of a 35472 x 256 -> 1024 GELU layer.
+__device__ __forceinline__ float exp_fast(float x) {
+  return __builtin_amdgcn_exp2f(x * 1.44269504088896341f);
+}
+__device__ __forceinline__ float sigmoid(float z) {
+  return __builtin_amdgcn_rcpf(1.f + exp_fast(-z));
+}
+// Phi(z); e receives e^(-z^2 / 2).
+__device__ __forceinline__ float normal_cdf(float z, float& e) {
+  const float x = fabsf(z) * 0.70710678118654752f;
+  const float t = __builtin_amdgcn_rcpf(fmaf(0.3275911f, x, 1.f));
+  float p = fmaf(1.061405429f, t, -1.453152027f);
+  p = fmaf(p, t, 1.421413741f);
+  p = fmaf(p, t, -0.284496736f);
+  p = fmaf(p, t, 0.254829592f);
+  e = exp_fast(-0.5f * z * z);
+  const float half = 0.5f * p * t * e;
+  return z < 0.f ? half : 1.f - half;
+}
 __device__ __forceinline__ float act_value(int act, float z) {
   if (act == OC_ACT_RELU) return z > 0.f || z != z ? z : 0.f;
-  if (act == OC_ACT_SILU) return z / (1.f + expf(-z));
-  if (act == OC_ACT_GELU) return 0.5f * z * (1.f + erff(z * 0.70710678118654752f));
+  if (act == OC_ACT_SILU) return z * sigmoid(z);
+  if (act == OC_ACT_GELU) {
+    float e;
+    return z * normal_cdf(z, e);
+  }
   return z;
 }
 __device__ __forceinline__ float act_slope(int act, float z) {
   if (act == OC_ACT_RELU) return z > 0.f ? 1.f : 0.f;
   if (act == OC_ACT_SILU) {
-    const float s = 1.f / (1.f + expf(-z));
-    return s * (1.f + z * (1.f - s));
+    const float s = sigmoid(z);
+    return s * fmaf(z, 1.f - s, 1.f);
   }
-  if (act == OC_ACT_GELU)
-    return 0.5f * (1.f + erff(z * 0.70710678118654752f)) +
-           z * expf(-0.5f * z * z) * 0.39894228040143268f;
+  if (act == OC_ACT_GELU) {
+    float e;
+    const float c = normal_cdf(z, e);
+    return fmaf(z * e, 0.39894228040143268f, c);
+  }
   return 1.f;
 }
 

@@ -43,42 +43,53 @@ DzShape dz_shape(int64_t M, int n) {
 }
 
 // glu 0: z, dz [M][n]; 1: z, dz [M][2 n].  dz NULL: column sums only (dz = dy).
-template <bool GLU>
+template <bool GLU, int ACT>
 __global__ __launch_bounds__(TB) void k_dz(const void* dy, const void* z, bool bf16, bool z_bf16,
-                                           int act, int64_t M, int n, int ct, void* dz,
-                                           float* part) {
+                                           int64_t M, int n, int ct, void* dz, float* part) {
   __shared__ float red[GLU ? 2 : 1][8][TB];
+  constexpr int U = 2;  // rows whose loads are in flight together
   const int tid = threadIdx.x, tc = tid % ct, tr = tid / ct, rl = TB / ct;
   const int nb = gridDim.x, b = blockIdx.x;
   const int64_t r0 = M * b / nb, r1 = M * (b + 1) / nb;
   const int c = (blockIdx.y * ct + tc) * 8, cnt = n - c;
   float s0[8] = {}, s1[8] = {};
   if (cnt > 0)
-    for (int64_t m = r0 + tr; m < r1; m += rl) {
-      float g[8], v[8], u[8];
-      oc::load8n(dy, bf16, m * n + c, cnt, g);
-      if (GLU) {
-        oc::load8n(z, false, m * 2 * n + c, cnt, v);
-        oc::load8n(z, false, m * 2 * n + n + c, cnt, u);
+    for (int64_t m0 = r0 + tr; m0 < r1; m0 += U * rl) {
+      float g[U][8], v[U][8], u[U][8];
+#pragma unroll
+      for (int i = 0; i < U; ++i) {
+        const int64_t m = m0 + i * rl;
+        if (m >= r1) continue;
+        oc::load8n(dy, bf16, m * n + c, cnt, g[i]);
+        if (GLU) {
+          oc::load8n(z, false, m * 2 * n + c, cnt, v[i]);
+          oc::load8n(z, false, m * 2 * n + n + c, cnt, u[i]);
+        } else if (ACT != OC_ACT_NONE) {
+          oc::load8n(z, z_bf16, m * n + c, cnt, v[i]);
+        }
+      }
+#pragma unroll
+      for (int i = 0; i < U; ++i) {
+        const int64_t m = m0 + i * rl;
+        if (m >= r1) continue;
 #pragma unroll
         for (int k = 0; k < 8; ++k) {
-          const float d = g[k];
-          g[k] = d * u[k] * oc::act_slope(act, v[k]);
-          u[k] = d * oc::act_value(act, v[k]);
-          s0[k] += g[k];
-          s1[k] += u[k];
+          const float d = g[i][k];
+          if (GLU) {
+            g[i][k] = d * u[i][k] * oc::act_slope(ACT, v[i][k]);
+            u[i][k] = d * oc::act_value(ACT, v[i][k]);
+            s1[k] += u[i][k];
+          } else if (ACT != OC_ACT_NONE) {
+            g[i][k] = d * oc::act_slope(ACT, v[i][k]);
+          }
+          s0[k] += g[i][k];
         }
-        oc::store8n(dz, bf16, m * 2 * n + c, cnt, g);
-        oc::store8n(dz, bf16, m * 2 * n + n + c, cnt, u);
-      } else {
-        if (act != OC_ACT_NONE) {
-          oc::load8n(z, z_bf16, m * n + c, cnt, v);
-#pragma unroll
-          for (int k = 0; k < 8; ++k) g[k] *= oc::act_slope(act, v[k]);
+        if (GLU) {
+          oc::store8n(dz, bf16, m * 2 * n + c, cnt, g[i]);
+          oc::store8n(dz, bf16, m * 2 * n + n + c, cnt, u[i]);
+        } else if (dz) {
+          oc::store8n(dz, bf16, m * n + c, cnt, g[i]);
         }
-#pragma unroll
-        for (int k = 0; k < 8; ++k) s0[k] += g[k];
-        if (dz) oc::store8n(dz, bf16, m * n + c, cnt, g);
       }
     }
   if (!part) return;
@@ -225,15 +236,25 @@ oc_status bwd(const char* who, bool glu, oc_dtype dt, int32_t act, int64_t rows,
   if (slope || dbias) {
     const DzShape d = dz_shape(rows, cout);
     float* part = dbias ? (float*)(base + o.part) : nullptr;
-    void* out = slope && (dx || dw) ? base + o.dz : nullptr;
-    const dim3 grid(d.nb, d.kb);
-    if (glu)
-      oc::launch(k_dz<true>, grid, dim3(TB), 0, s, dy, pre, bf16, false, act, rows, cout, d.ct,
-                 (void*)(base + o.dz), part);
-    else
-      oc::launch(k_dz<false>, grid, dim3(TB), 0, s, dy, pre, bf16, bf16 && act == OC_ACT_RELU, act,
-                 rows, cout, d.ct, out, part);
-    if (dbias)
+    void* out = glu || (slope && (dx || dw)) ? base + o.dz : nullptr;
+    // the sums of a single block of rows are the result
+    if (dbias && d.nb == 1) part = dbias;
+    const auto run = [&](auto k) {
+      oc::launch(k, dim3(d.nb, d.kb), dim3(TB), 0, s, dy, pre, bf16,
+                 bf16 && act == OC_ACT_RELU && !glu, rows, cout, d.ct, out, part);
+    };
+    if (glu) {
+      if (act == OC_ACT_NONE) run(k_dz<true, OC_ACT_NONE>);
+      else if (act == OC_ACT_RELU) run(k_dz<true, OC_ACT_RELU>);
+      else if (act == OC_ACT_SILU) run(k_dz<true, OC_ACT_SILU>);
+      else run(k_dz<true, OC_ACT_GELU>);
+    } else {
+      if (act == OC_ACT_NONE) run(k_dz<false, OC_ACT_NONE>);
+      else if (act == OC_ACT_RELU) run(k_dz<false, OC_ACT_RELU>);
+      else if (act == OC_ACT_SILU) run(k_dz<false, OC_ACT_SILU>);
+      else run(k_dz<false, OC_ACT_GELU>);
+    }
+    if (dbias && d.nb > 1)
       oc::launch(k_colsum, dim3((unsigned)cdiv(nz, 4)), dim3(TB), 0, s, (const float*)part, d.nb,
                  nz, dbias);
   }

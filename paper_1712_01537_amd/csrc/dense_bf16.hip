@@ -27,12 +27,12 @@ namespace oc {
 
 void tile_bf16(int shape, bool a_rs, bool b_rs, bool direct, bool main, const TileArgs& t,
                hipStream_t s) {
-  switch (shape * 2 + direct) {
-    case 0: return pick<TILE_LARGE, false>(a_rs, b_rs, main, t, s);
+  switch (shape * 2 + direct) {  // (0, 2: not taken, their staging does not fit in registers)
     case 1: return pick<TILE_LARGE, true>(a_rs, b_rs, main, t, s);
-    case 2: return pick<TILE_MEDIUM, false>(a_rs, b_rs, main, t, s);
-    case 3: return pick<TILE_MEDIUM, true>(a_rs, b_rs, main, t, s);
-    case 4: return pick<TILE_SMALL, false>(a_rs, b_rs, main, t, s);
+    case 3: return pick<TILE_TWO, true>(a_rs, b_rs, main, t, s);
+    case 4: return pick<TILE_MEDIUM, false>(a_rs, b_rs, main, t, s);
+    case 5: return pick<TILE_MEDIUM, true>(a_rs, b_rs, main, t, s);
+    case 6: return pick<TILE_SMALL, false>(a_rs, b_rs, main, t, s);
     default: return pick<TILE_SMALL, true>(a_rs, b_rs, main, t, s);
   }
 }

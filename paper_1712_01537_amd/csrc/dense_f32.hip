@@ -28,6 +28,7 @@ namespace oc {
 void tile_f32(int shape, bool a_rs, bool b_rs, bool main, const TileArgs& t, hipStream_t s) {
   switch (shape) {
     case TILE_LARGE: return pick<TILE_LARGE>(a_rs, b_rs, main, t, s);
+    case TILE_TWO: return pick<TILE_TWO>(a_rs, b_rs, main, t, s);
     case TILE_MEDIUM: return pick<TILE_MEDIUM>(a_rs, b_rs, main, t, s);
     default: return pick<TILE_SMALL>(a_rs, b_rs, main, t, s);
   }

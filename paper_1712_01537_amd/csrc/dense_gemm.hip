@@ -77,18 +77,20 @@ struct Plan {
 // of BK terms takes a workgroup `step` microseconds with `fit` of them on a CU,
 // a workgroup 3 more to start and finish; splits write and read their partial
 // sums at 4 TB/s and take another launch of 3.
-Plan plan(oc_dtype dt, int64_t P, int64_t Q, int64_t R, bool glu) {
+// direct: bf16 operands that go straight to LDS; the largest tiles take only those.
+Plan plan(oc_dtype dt, bool direct, int64_t P, int64_t Q, int64_t R, bool glu) {
   struct Cost {
     double step;
     int fit;
   };
-  static const Cost cost[2][oc::TILE_SHAPES] = {{{2.4, 1}, {1.5, 1}, {1.4, 3}},
-                                                {{1.6, 1}, {0.9, 2}, {0.7, 4}}};
+  static const Cost cost[2][oc::TILE_SHAPES] = {{{2.4, 1}, {1.4, 2}, {1.5, 1}, {1.4, 3}},
+                                                {{1.6, 1}, {0.9, 2}, {0.9, 2}, {0.7, 4}}};
   const int cus = oc::cu_count();
   const int64_t n = glu ? Q / 2 : Q;
   Plan best{};
   double least = 1e300;
-  for (int k = 0; k < oc::TILE_SHAPES; ++k) {
+  for (int k = dt == OC_BF16 && !direct ? oc::TILE_MEDIUM : oc::TILE_LARGE; k < oc::TILE_SHAPES;
+       ++k) {
     const oc::TileInfo i = dt == OC_BF16 ? oc::tile_info<uint16_t>(k) : oc::tile_info<float>(k);
     const Cost& c = cost[dt == OC_BF16][k];
     const int64_t ntm = cdiv(P, i.bm), ntn = cdiv(n, glu ? i.bn / 2 : i.bn);
@@ -118,21 +120,22 @@ bool vectors(const void* p, int64_t ld) { return (uintptr_t)p % 16 == 0 && ld % 
 namespace oc {
 
 size_t gemm_ws(oc_dtype dt, int64_t P, int64_t Q, int64_t R, bool, bool, bool glu) {
-  const Plan p = plan(dt, P, Q, R, glu);
-  return p.splits > 1 ? align256((size_t)p.splits * P * Q * 4) : 0;
+  int splits = 1;  // of whichever plan the operands' alignment asks for
+  for (int direct = 0; direct < 2; ++direct) {
+    const Plan p = plan(dt, direct, P, Q, R, glu);
+    if (p.splits > splits) splits = p.splits;
+  }
+  return splits > 1 ? align256((size_t)splits * P * Q * 4) : 0;
 }
 
 void gemm(const Gemm& g, void* ws, bool main, hipStream_t s) {
-  const Plan p = plan(g.dt, g.P, g.Q, g.R, g.epi.glu);
+  const bool direct = g.dt == OC_BF16 && vectors(g.a, g.a_rs ? g.P : g.R) &&
+                      vectors(g.b, g.b_rs ? g.Q : g.R) && (!g.epi.glu || g.epi.n % 8 == 0);
+  const Plan p = plan(g.dt, direct, g.P, g.Q, g.R, g.epi.glu);
   const TileArgs t{g.a, g.b, g.P, g.R, g.Q, p.ntm, p.ntn, p.splits, p.per,
                    p.splits > 1 ? (float*)ws : nullptr, g.epi};
-  if (g.dt == OC_F32) {
-    tile_f32(p.shape, g.a_rs, g.b_rs, main, t, s);
-  } else {
-    const bool direct = vectors(g.a, g.a_rs ? g.P : g.R) && vectors(g.b, g.b_rs ? g.Q : g.R) &&
-                        (!g.epi.glu || g.epi.n % 8 == 0);
-    tile_bf16(p.shape, g.a_rs, g.b_rs, direct, main, t, s);
-  }
+  if (g.dt == OC_F32) tile_f32(p.shape, g.a_rs, g.b_rs, main, t, s);
+  else tile_bf16(p.shape, g.a_rs, g.b_rs, direct, main, t, s);
   if (p.splits == 1) return;
   int lanes = 1;
   while (lanes < 64 && lanes * 4 < p.splits) lanes *= 2;

@@ -44,7 +44,7 @@ struct TileArgs {
 };
 
 // Tile shapes, by type; see gemm() for which is taken.
-enum TileShape { TILE_LARGE, TILE_MEDIUM, TILE_SMALL, TILE_SHAPES };
+enum TileShape { TILE_LARGE, TILE_TWO, TILE_MEDIUM, TILE_SMALL, TILE_SHAPES };
 struct TileInfo {
   int bm, bn, threads, bk;
 };
@@ -52,6 +52,7 @@ template <typename T>
 constexpr TileInfo tile_info(int shape) {
   constexpr bool f32 = sizeof(T) == 4;
   return shape == TILE_LARGE    ? TileInfo{256, f32 ? 128 : 256, 512, f32 ? 32 : 64}
+         : shape == TILE_TWO    ? (f32 ? TileInfo{128, 64, 256, 32} : TileInfo{256, 128, 256, 32})
          : shape == TILE_MEDIUM ? TileInfo{128, 128, f32 ? 512 : 256, f32 ? 32 : 64}
                                 : TileInfo{64, 64, 256, f32 ? 32 : 64};
 }
@@ -119,7 +120,7 @@ __device__ __forceinline__ TilePos tile_pos(const TileArgs& t, uint32_t bid) {
 }
 
 template <typename T, int BM, int BN, int WGM, int BK, bool ARS, bool BRS, bool GLU, bool DIRECT>
-__global__ __launch_bounds__(64 * WGM * (BN / 64)) void k_dense_tile(TileArgs t) {
+__global__ __launch_bounds__(64 * WGM * (BN / 64), 2) void k_dense_tile(TileArgs t) {
   constexpr bool F32 = sizeof(T) == 4;
   static_assert(!(F32 && DIRECT), "fp32 operands are split in registers");
   constexpr int PARTS = F32 ? 3 : 1;
@@ -205,7 +206,8 @@ __global__ __launch_bounds__(64 * WGM * (BN / 64)) void k_dense_tile(TileArgs t)
     }
   };
 
-  // Through registers: load step ks, then split and store it to buffer s.
+  // Through registers: load step ks, then split and store vectors from .. to of it
+  // to buffer s.
   s3_v4u reg[IT][F32 ? 2 : 1];
   bool whole = true;  // every vector of the tile exists, ends of the reduction aside
   if constexpr (!DIRECT) {
@@ -252,9 +254,10 @@ __global__ __launch_bounds__(64 * WGM * (BN / 64)) void k_dense_tile(TileArgs t)
     }
   };
   const SplitK sk = s3_consts();
-  auto stash = [&](int s) __attribute__((always_inline)) {
+  auto stash = [&](int s, int from, int to) __attribute__((always_inline)) {
 #pragma unroll
     for (int i = 0; i < IT; ++i) {
+      if (i < from || i >= to) continue;
       const bool isa = i < ITA;
       const int c = s * STAGE + (isa ? i : i - ITA) * NTHR + tid + (isa ? 0 : PARTS * CA);
       if constexpr (F32) {
@@ -308,49 +311,81 @@ __global__ __launch_bounds__(64 * WGM * (BN / 64)) void k_dense_tile(TileArgs t)
       return tr((const char*)(base + k * CR + (c ^ col_xor<CR>(k))) + (li & 1) * 8, CR * 16);
     }
   };
-  auto compute = [&](int s) __attribute__((always_inline)) {
+
+  // A step is NU units: MI row fragments for each of the BK / 32 sub-steps.  A
+  // unit's row fragment is read AD units ahead and a sub-step's column fragments
+  // ahead of its first unit.  Ahead of the last AD units all of this step's
+  // fragments are in registers: there the workgroup meets, and what follows reads
+  // the next step's buffer and refills this one's, while the matrix cores still
+  // have AD units to do.
+  constexpr int KK = BK / 32, NU = KK * MI, AD = MI >= 4 && !F32 ? 3 : 1;
+  static_assert(AD <= MI, "a sub-step's columns are read within the one before it");
+  s3_v4u a[AD + 1][PARTS], b[2][NI][PARTS];
+  auto read_a = [&](s3_v4u(&f)[PARTS], int s, int u) __attribute__((always_inline)) {
 #pragma unroll
-    for (int kk = 0; kk < BK / 32; ++kk) {
-      s3_v4u b[NI][PARTS];
+    for (int k = 0; k < PARTS; ++k) f[k] = frag_a(s, k, u / MI, u % MI);
+  };
+  auto read_b = [&](s3_v4u(&f)[NI][PARTS], int s, int kk) __attribute__((always_inline)) {
 #pragma unroll
-      for (int j = 0; j < NI; ++j)
+    for (int j = 0; j < NI; ++j)
 #pragma unroll
-        for (int k = 0; k < PARTS; ++k) b[j][k] = frag_b(s, k, kk, j);
-#pragma unroll
-      for (int i = 0; i < MI; ++i) {
-        s3_v4u a[PARTS];
-#pragma unroll
-        for (int k = 0; k < PARTS; ++k) a[k] = frag_a(s, k, kk, i);
-#pragma unroll
-        for (int j = 0; j < NI; ++j) {
-          if constexpr (F32) {
-#pragma unroll
-            for (int x = 0; x < 6; ++x) acc[i][j] = s3_product(x, b[j], a, acc[i][j]);
-          } else {
-            acc[i][j] = s3_mfma(b[j][0], a[0], acc[i][j]);
-          }
-        }
-      }
-    }
+      for (int k = 0; k < PARTS; ++k) f[j][k] = frag_b(s, k, kk, j);
   };
 
   if constexpr (DIRECT) {
     issue(0, 0);
-    for (int ks = 0; ks < nk; ++ks) {
-      dt_wait_vm();  // this wave's loads of step ks have landed
-      dt_barrier();  // everyone's have, and step ks - 1 is no longer read
-      if (ks + 1 < nk) issue(ks + 1, (ks + 1) & 1);
-      compute(ks & 1);
-    }
+    dt_wait_vm();
+    dt_barrier();
+    if (nk > 1) issue(1, 1);
   } else {
     fetch(0);
-    stash(0);
+    stash(0, 0, IT);
     dt_barrier();
-    for (int ks = 0; ks < nk; ++ks) {
-      if (ks + 1 < nk) fetch(ks + 1);
-      compute(ks & 1);
-      if (ks + 1 < nk) stash((ks + 1) & 1);
-      dt_barrier();
+    if (nk > 1) fetch(1);
+  }
+  read_b(b[0], 0, 0);
+#pragma unroll
+  for (int u = 0; u < AD; ++u) read_a(a[u], 0, u);
+  for (int ks = 0; ks < nk; ++ks) {
+    const int s = ks & 1;
+#pragma unroll
+    for (int u = 0; u < NU; ++u) {
+      constexpr int FREE = NU - AD;  // units ahead of the barrier
+      if (!DIRECT && FREE == 0 && u == 0) stash(s ^ 1, 0, IT);
+      if (u == FREE) {
+        // this wave's part of step ks + 1 is in LDS, and it reads step ks no more
+        if (DIRECT) dt_wait_vm();
+        dt_barrier();
+        if (ks + 2 < nk) {
+          if constexpr (DIRECT) issue(ks + 2, s);
+          else fetch(ks + 2);
+        }
+      }
+      // (of the last step: what lies in the other buffer, never used)
+      read_a(a[AD], u + AD < NU ? s : s ^ 1, (u + AD) % NU);
+      if (u % MI == MI - AD) read_b(b[1], u / MI + 1 < KK ? s : s ^ 1, (u / MI + 1) % KK);
+      if (!DIRECT && u < FREE)
+        stash(s ^ 1, IT * u / (FREE ? FREE : 1), IT * (u + 1) / (FREE ? FREE : 1));
+      if constexpr (F32) {
+#pragma unroll
+        for (int x = 0; x < 6; ++x)
+#pragma unroll
+          for (int j = 0; j < NI; ++j)
+            acc[u % MI][j] = s3_product(x, b[0][j], a[0], acc[u % MI][j]);
+      } else {
+#pragma unroll
+        for (int j = 0; j < NI; ++j) acc[u % MI][j] = s3_mfma(b[0][j][0], a[0][0], acc[u % MI][j]);
+      }
+      __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+      for (int i = 0; i < AD; ++i)
+#pragma unroll
+        for (int k = 0; k < PARTS; ++k) a[i][k] = a[i + 1][k];
+      if (u % MI == MI - 1)
+#pragma unroll
+        for (int j = 0; j < NI; ++j)
+#pragma unroll
+          for (int k = 0; k < PARTS; ++k) b[0][j][k] = b[1][j][k];
     }
   }
 

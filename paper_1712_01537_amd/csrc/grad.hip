@@ -13,7 +13,9 @@
 //
 // Tensors come as a table in the kernel's arguments (so that a captured call
 // keeps its own copy), MOST_TENSORS a launch, cut into chunks of CHUNK elements
-// of one tensor; a workgroup takes a contiguous range of chunks.
+// of one tensor; a workgroup takes every gridDim.x-th chunk.  The clipping pass
+// goes backwards, so that it finds what the first pass read last in the last-level
+// cache.
 #include <algorithm>
 #include <cmath>
 
@@ -48,14 +50,13 @@ __device__ __forceinline__ int tensor_of(const Table& t, uint32_t k) {
 }
 
 // f(v, element, count) for the vectors of eight of this thread in the block's chunks.
-template <typename Load, typename F>
+// Back: from the last chunk to the first.
+template <bool BACK, typename Load, typename F>
 __device__ __forceinline__ void for_chunks(const Table& t, Load&& load, F&& f) {
   const uint32_t total = t.first[t.n];
-  const uint32_t k0 = (uint32_t)((uint64_t)total * blockIdx.x / gridDim.x);
-  const uint32_t k1 = (uint32_t)((uint64_t)total * (blockIdx.x + 1) / gridDim.x);
-  int i = -1;
-  for (uint32_t k = k0; k < k1; ++k) {
-    if (i < 0 || k >= t.first[i + 1]) i = tensor_of(t, k);
+  for (uint32_t j = blockIdx.x; j < total; j += gridDim.x) {
+    const uint32_t k = BACK ? total - 1 - j : j;
+    const int i = tensor_of(t, k);
     const int64_t e0 = (int64_t)(k - t.first[i]) * CHUNK + threadIdx.x * 8, n = t.count[i];
     float v[4][8];
 #pragma unroll
@@ -89,7 +90,7 @@ __device__ __forceinline__ double block_sum(double a) {
 
 __global__ __launch_bounds__(TB) void k_sq_sum(Table t, double* part) {
   double a[8] = {};
-  for_chunks(
+  for_chunks<false>(
       t, [&](int i, int64_t e, int64_t n, float(&v)[8]) { load_in(t, i, e, n, v); },
       [&](int, int64_t, int64_t, float(&v)[8]) {
 #pragma unroll
@@ -119,7 +120,7 @@ __global__ __launch_bounds__(TB) void k_clip(Table t, const double* part, int n,
   const double r = sqrt(total_of(part, n));
   if (norm && blockIdx.x == 0 && threadIdx.x == 0) *norm = (float)r;
   const float c = r <= max_norm ? 1.f : (float)(max_norm / r);
-  for_chunks(
+  for_chunks<true>(
       t,
       [&](int i, int64_t e, int64_t cnt, float(&v)[8]) {
         // nothing changes: gradients scaled in place by one
