@@ -30,19 +30,33 @@ struct Epi {
 
 // out [P][Q] = sum over r < R of A(p, r) B(r, q), then `epi` (M = P, nz = Q).
 //   a_rs 0: A is stored [P][R], 1: [R][P].  b_rs 1: B is stored [R][Q], 0: [Q][R].
-// Leading dimensions are those row lengths.  dt: type of A and B.
+//   lda, ldb: elements from row to row; columns between a row's end and there hold
+//   zeros where they lie in its last 16-byte vector.  half: with glu, B's column of
+//   the other half's first.  dt: type of A and B.
 struct Gemm {
   oc_dtype dt;
   int64_t P, R;
   int32_t Q;
   const void *a, *b;
+  int64_t lda, ldb;
+  int32_t half;
   bool a_rs, b_rs;
   Epi epi;
 };
 
+// Whether a layer's bf16 operands are copied to rows of whole 16-byte vectors first:
+// where they are not, and the product is large enough to gain from it (8383 x 513 ->
+// 1027: the forward takes 48 us on rows of any length through registers and 27 with the
+// copies, which take 8; products of 2 GFLOP gain nothing).
+inline bool pads(oc_dtype dt, int64_t rows, int64_t cin, int64_t cout, bool glu) {
+  return dt == OC_BF16 && (cin % 8 || cout % 8) &&
+         2.0 * rows * cin * cout * (glu ? 2 : 1) >= 2e9;
+}
+inline int64_t pad8(int64_t n) { return (n + 7) / 8 * 8; }
+
 // Bytes of workspace the product needs (partial sums of a split reduction);
-// a function of the type, the sizes and the layout alone.
-size_t gemm_ws(oc_dtype dt, int64_t P, int64_t Q, int64_t R, bool a_rs, bool b_rs, bool glu);
+// a function of the type and the sizes alone.
+size_t gemm_ws(oc_dtype dt, int64_t P, int64_t Q, int64_t R, bool glu);
 // Enqueue it.  main: its kernel does the call's main arithmetic (profiling).
 void gemm(const Gemm& g, void* ws, bool main, hipStream_t s);
 
@@ -141,15 +155,23 @@ __device__ __forceinline__ void store1(void* p, bool bf16, int64_t i, float v) {
   else
     ((float*)p)[i] = v;
 }
-// The first cnt (1..8) of them; the others read as zero and are not written.
-__device__ __forceinline__ void load8n(const void* p, bool bf16, int64_t i, int cnt, float (&v)[8]) {
-  if (cnt >= 8) {
+// The first cnt (1..8) of them; the others read as zero.  n: elements in all.  What
+// lies behind them in the array is read and dropped: one vector load, where eight
+// loads under a mask each wait for the one before.
+__device__ __forceinline__ void load8n(const void* p, bool bf16, int64_t i, int cnt, int64_t n,
+                                       float (&v)[8]) {
+  if (i + 8 <= n) {
     load8(p, bf16, i, v);
+    if (cnt < 8) {
+#pragma unroll
+      for (int k = 0; k < 8; ++k) v[k] = k < cnt ? v[k] : 0.f;
+    }
   } else {
 #pragma unroll
-    for (int k = 0; k < 8; ++k) v[k] = k < cnt ? load1(p, bf16, i + k) : 0.f;
+    for (int k = 0; k < 8; ++k) v[k] = k < cnt && i + k < n ? load1(p, bf16, i + k) : 0.f;
   }
 }
+// The first cnt of them; the others are not written.
 __device__ __forceinline__ void store8n(void* p, bool bf16, int64_t i, int cnt,
                                         const float (&v)[8]) {
   if (cnt >= 8) {
@@ -173,7 +195,7 @@ __device__ __forceinline__ void epilogue(const Epi& e, const int64_t (&m)[U], in
   if (!GLU && e.res) {
 #pragma unroll
     for (int i = 0; i < U; ++i)
-      if (m[i] < M) load8n(e.res, e.y_bf16, m[i] * e.n + c, cnt, r[i]);
+      if (m[i] < M) load8n(e.res, e.y_bf16, m[i] * e.n + c, cnt, M * e.n, r[i]);
   }
 #pragma unroll
   for (int i = 0; i < U; ++i)

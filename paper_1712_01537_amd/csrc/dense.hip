@@ -42,10 +42,12 @@ DzShape dz_shape(int64_t M, int n) {
   return d;
 }
 
-// glu 0: z, dz [M][n]; 1: z, dz [M][2 n].  dz NULL: column sums only (dz = dy).
+// glu 0: z, dz [M][n]; 1: z, dz [M][2 n].  dz has rows of ld elements, those past the
+// columns zero (bf16 rows padded to whole vectors); NULL: column sums only (dz = dy).
 template <bool GLU, int ACT>
 __global__ __launch_bounds__(TB) void k_dz(const void* dy, const void* z, bool bf16, bool z_bf16,
-                                           int64_t M, int n, int ct, void* dz, float* part) {
+                                           int64_t M, int n, int ct, void* dz, int64_t ld,
+                                           float* part) {
   __shared__ float red[GLU ? 2 : 1][8][TB];
   constexpr int U = 2;  // rows whose loads are in flight together
   const int tid = threadIdx.x, tc = tid % ct, tr = tid / ct, rl = TB / ct;
@@ -60,12 +62,12 @@ __global__ __launch_bounds__(TB) void k_dz(const void* dy, const void* z, bool b
       for (int i = 0; i < U; ++i) {
         const int64_t m = m0 + i * rl;
         if (m >= r1) continue;
-        oc::load8n(dy, bf16, m * n + c, cnt, g[i]);
+        oc::load8n(dy, bf16, m * n + c, cnt, M * n, g[i]);
         if (GLU) {
-          oc::load8n(z, false, m * 2 * n + c, cnt, v[i]);
-          oc::load8n(z, false, m * 2 * n + n + c, cnt, u[i]);
+          oc::load8n(z, false, m * 2 * n + c, cnt, M * 2 * n, v[i]);
+          oc::load8n(z, false, m * 2 * n + n + c, cnt, M * 2 * n, u[i]);
         } else if (ACT != OC_ACT_NONE) {
-          oc::load8n(z, z_bf16, m * n + c, cnt, v[i]);
+          oc::load8n(z, z_bf16, m * n + c, cnt, M * n, v[i]);
         }
       }
 #pragma unroll
@@ -85,10 +87,12 @@ __global__ __launch_bounds__(TB) void k_dz(const void* dy, const void* z, bool b
           s0[k] += g[i][k];
         }
         if (GLU) {
-          oc::store8n(dz, bf16, m * 2 * n + c, cnt, g[i]);
-          oc::store8n(dz, bf16, m * 2 * n + n + c, cnt, u[i]);
+          oc::store8n(dz, bf16, m * ld + c, cnt, g[i]);
+          oc::store8n(dz, bf16, m * ld + n + c, cnt, u[i]);
+          if (cnt <= 8)
+            for (int64_t k = 2 * n; k < ld; ++k) oc::store1(dz, bf16, m * ld + k, 0.f);
         } else if (dz) {
-          oc::store8n(dz, bf16, m * n + c, cnt, g[i]);
+          oc::store8n(dz, bf16, m * ld + c, (int)(ld - c), g[i]);
         }
       }
     }
@@ -169,10 +173,57 @@ void zero(void* p, oc_dtype dt, int64_t n, hipStream_t s) {
   oc::launch(k_zero16, dim3((unsigned)cdiv(halves, TB)), dim3(TB), 0, s, (uint16_t*)p, halves);
 }
 
+// --- copies to rows of whole vectors ------------------------------------------
+
+// Two bf16 matrices [rows][cols] copied to rows of ld elements (a multiple of
+// eight), zero past the columns; with halves, the columns' second half starts at ld / 2
+// (zero between).  A thread writes one vector; grid y picks the matrix.
+struct Pad {
+  const void* src;
+  uint16_t* dst;
+  int64_t rows, ld;
+  int32_t cols, halves;
+};
+struct Pads {
+  Pad p[2];
+};
+__global__ __launch_bounds__(TB) void k_pad(Pads a) {
+  const Pad p = blockIdx.y ? a.p[1] : a.p[0];
+  const int64_t nv = p.ld / 8, total = p.src ? p.rows * nv : 0;
+  for (int64_t i = (int64_t)blockIdx.x * TB + threadIdx.x; i < total; i += (int64_t)gridDim.x * TB) {
+    const int64_t r = i / nv;
+    int c = (int)(i - r * nv) * 8, lim = p.cols, add = 0;
+    if (p.halves) {
+      lim = p.cols / 2;
+      if (c >= p.ld / 2) c -= (int)(p.ld / 2), add = lim;
+    }
+    float v[8];
+    const int cnt = lim - c < 0 ? 0 : lim - c;
+    oc::load8n(p.src, true, cnt ? r * p.cols + add + c : 0, cnt, p.rows * p.cols, v);
+    oc::store8(p.dst, true, i * 8, v);
+  }
+}
+void pad(const Pads& a, hipStream_t s) {
+  int64_t most = 1;
+  for (const Pad& p : a.p) most = std::max(most, p.src ? p.rows * p.ld / 8 : 0);
+  oc::launch(k_pad, dim3((unsigned)std::min<int64_t>(cdiv(most, TB), 8192), 2), dim3(TB), 0, s, a);
+}
+size_t pad_bytes(int64_t rows, int64_t ld) { return oc::align256((size_t)rows * ld * 2); }
+
 // --- the two layers -----------------------------------------------------------
 
-size_t fwd_ws(oc_dtype dt, int64_t rows, int32_t cin, int32_t cout, bool glu) {
-  return oc::gemm_ws(dt, rows, glu ? 2 * cout : cout, cin, false, true, glu);
+struct FwdWs {
+  size_t x, w, gemm, total;  // offsets, bytes in all
+};
+FwdWs fwd_ws(oc_dtype dt, int64_t rows, int32_t cin, int32_t cout, bool glu) {
+  const int64_t nz = glu ? 2 * cout : cout;
+  const bool pd = oc::pads(dt, rows, cin, cout, glu);
+  FwdWs f;
+  f.x = 0;
+  f.w = pd && cin % 8 ? pad_bytes(rows, oc::pad8(cin)) : 0;
+  f.gemm = f.w + (pd && cout % 8 ? pad_bytes(cin, (glu ? 2 : 1) * oc::pad8(cout)) : 0);
+  f.total = f.gemm + oc::gemm_ws(dt, rows, nz, cin, glu);
+  return f;
 }
 
 oc_status fwd(const char* who, bool glu, oc_dtype dt, int32_t act, int64_t rows, int32_t cin,
@@ -182,29 +233,50 @@ oc_status fwd(const char* who, bool glu, oc_dtype dt, int32_t act, int64_t rows,
   if (st != OC_OK) return st;
   if (rows == 0) return OC_OK;
   if (!x || !w || !y) return oc::fail(OC_ERR_ARG, "%s: NULL buffer", who);
-  st = check_ws(who, ws, ws_bytes, fwd_ws(dt, rows, cin, cout, glu));
+  const FwdWs o = fwd_ws(dt, rows, cin, cout, glu);
+  st = check_ws(who, ws, ws_bytes, o.total);
   if (st != OC_OK) return st;
-  const int32_t bf16 = dt == OC_BF16;
-  oc::Gemm g{dt,    rows, cin,  glu ? 2 * cout : cout, x, w, false, true,
+  const int32_t bf16 = dt == OC_BF16, nz = glu ? 2 * cout : cout;
+  char* base = (char*)ws;
+  int64_t lda = cin, ldb = nz, half = cout;
+  if (oc::pads(dt, rows, cin, cout, glu)) {
+    Pads p{};
+    if (cin % 8) {
+      lda = oc::pad8(cin);
+      p.p[0] = Pad{x, (uint16_t*)(base + o.x), rows, lda, cin, 0};
+      x = base + o.x;
+    }
+    if (cout % 8) {
+      half = oc::pad8(cout);
+      ldb = glu ? 2 * half : half;
+      p.p[1] = Pad{w, (uint16_t*)(base + o.w), cin, ldb, nz, glu};
+      w = base + o.w;
+    }
+    pad(p, s);
+  }
+  oc::Gemm g{dt,    rows, cin, nz, x, w, lda, ldb, (int32_t)half, false, true,
              {act, glu, cout, bf16, bf16 && act == OC_ACT_RELU && !glu, bias, res, y, pre}};
-  oc::gemm(g, ws, true, s);
+  oc::gemm(g, base + o.gemm, true, s);
   OC_LAUNCH_CHECK();
   return OC_OK;
 }
 
 struct BwdWs {
-  size_t dz, part, gemm, total;  // offsets, bytes in all
+  size_t dz, part, x, w, gemm, total;  // offsets, bytes in all
 };
 BwdWs bwd_ws(oc_dtype dt, int32_t act, int64_t rows, int32_t cin, int32_t cout, bool glu) {
   const int64_t nz = glu ? 2 * cout : cout;
   const DzShape d = dz_shape(rows, cout);
+  const bool pd = oc::pads(dt, rows, cin, cout, glu);
   BwdWs b;
   b.dz = 0;
-  b.part = glu || act != OC_ACT_NONE
-               ? oc::align256((size_t)rows * nz * (dt == OC_BF16 ? 2 : 4)) : 0;
-  b.gemm = b.part + oc::align256((size_t)d.nb * nz * 4);
-  b.total = b.gemm + oc::align256(std::max(oc::gemm_ws(dt, rows, cin, nz, false, false, false),
-                                           oc::gemm_ws(dt, cin, nz, rows, true, true, false)));
+  b.part = glu || act != OC_ACT_NONE || (pd && nz % 8)
+               ? oc::align256((size_t)rows * (pd ? oc::pad8(nz) : nz) * (dt == OC_BF16 ? 2 : 4)) : 0;
+  b.x = b.part + oc::align256((size_t)d.nb * nz * 4);
+  b.w = b.x + (pd && cin % 8 ? pad_bytes(rows, oc::pad8(cin)) : 0);
+  b.gemm = b.w + (pd && nz % 8 ? pad_bytes(cin, oc::pad8(nz)) : 0);
+  b.total = b.gemm + oc::align256(std::max(oc::gemm_ws(dt, rows, cin, nz, false),
+                                           oc::gemm_ws(dt, cin, nz, rows, false)));
   return b;
 }
 
@@ -231,17 +303,19 @@ oc_status bwd(const char* who, bool glu, oc_dtype dt, int32_t act, int64_t rows,
   st = check_ws(who, ws, ws_bytes, o.total);
   if (st != OC_OK) return st;
   char* base = (char*)ws;
-  const bool bf16 = dt == OC_BF16;
-  const void* dz = slope ? base + o.dz : dy;
-  if (slope || dbias) {
+  const bool bf16 = dt == OC_BF16, pd = oc::pads(dt, rows, cin, cout, glu);
+  const bool apart = slope || (pd && nz % 8);  // dz is not dy itself
+  const int64_t ldz = pd ? oc::pad8(nz) : nz;
+  const void* dz = apart ? base + o.dz : dy;
+  if (apart || dbias) {
     const DzShape d = dz_shape(rows, cout);
     float* part = dbias ? (float*)(base + o.part) : nullptr;
-    void* out = glu || (slope && (dx || dw)) ? base + o.dz : nullptr;
+    void* out = glu || (apart && (dx || dw)) ? base + o.dz : nullptr;
     // the sums of a single block of rows are the result
     if (dbias && d.nb == 1) part = dbias;
     const auto run = [&](auto k) {
       oc::launch(k, dim3(d.nb, d.kb), dim3(TB), 0, s, dy, pre, bf16,
-                 bf16 && act == OC_ACT_RELU && !glu, rows, cout, d.ct, out, part);
+                 bf16 && act == OC_ACT_RELU && !glu, rows, cout, d.ct, out, ldz, part);
     };
     if (glu) {
       if (act == OC_ACT_NONE) run(k_dz<true, OC_ACT_NONE>);
@@ -258,13 +332,28 @@ oc_status bwd(const char* who, bool glu, oc_dtype dt, int32_t act, int64_t rows,
       oc::launch(k_colsum, dim3((unsigned)cdiv(nz, 4)), dim3(TB), 0, s, (const float*)part, d.nb,
                  nz, dbias);
   }
+  int64_t ldx = cin, ldw = nz;
+  if (pd && ((dw && cin % 8) || (dx && nz % 8))) {
+    Pads p{};
+    if (dw && cin % 8) {
+      ldx = oc::pad8(cin);
+      p.p[0] = Pad{x, (uint16_t*)(base + o.x), rows, ldx, cin, 0};
+      x = base + o.x;
+    }
+    if (dx && nz % 8) {
+      ldw = oc::pad8(nz);
+      p.p[1] = Pad{w, (uint16_t*)(base + o.w), cin, ldw, nz, 0};
+      w = base + o.w;
+    }
+    pad(p, s);
+  }
   if (dx) {
-    oc::Gemm g{dt,    rows, nz, cin, dz, w, false, false,
+    oc::Gemm g{dt,    rows, nz, cin, dz, w, ldz, ldw, 0, false, false,
                {OC_ACT_NONE, 0, cin, bf16, 0, nullptr, nullptr, dx, nullptr}};
     oc::gemm(g, base + o.gemm, true, s);
   }
   if (dw) {
-    oc::Gemm g{dt,    cin, rows, nz, x, dz, true, true,
+    oc::Gemm g{dt,    cin, rows, nz, x, dz, ldx, ldz, 0, true, true,
                {OC_ACT_NONE, 0, nz, dw_dt == OC_BF16, 0, nullptr, nullptr, dw, nullptr}};
     oc::gemm(g, base + o.gemm, !dx, s);
   }
@@ -277,7 +366,7 @@ oc_status bwd(const char* who, bool glu, oc_dtype dt, int32_t act, int64_t rows,
 extern "C" {
 
 size_t oc_dense_fwd_workspace(oc_dtype dt, int64_t rows, int32_t cin, int32_t cout) {
-  return sizes_ok(dt, rows, cin, cout, false) ? fwd_ws(dt, rows, cin, cout, false) : 0;
+  return sizes_ok(dt, rows, cin, cout, false) ? fwd_ws(dt, rows, cin, cout, false).total : 0;
 }
 
 oc_status oc_dense_fwd(oc_dtype dt, int32_t act, int64_t rows, int32_t cin, int32_t cout,
@@ -300,7 +389,7 @@ oc_status oc_dense_bwd(oc_dtype dt, int32_t act, int64_t rows, int32_t cin, int3
 }
 
 size_t oc_glu_fwd_workspace(oc_dtype dt, int64_t rows, int32_t cin, int32_t cout) {
-  return sizes_ok(dt, rows, cin, cout, true) ? fwd_ws(dt, rows, cin, cout, true) : 0;
+  return sizes_ok(dt, rows, cin, cout, true) ? fwd_ws(dt, rows, cin, cout, true).total : 0;
 }
 
 oc_status oc_glu_fwd(oc_dtype dt, int32_t act, int64_t rows, int32_t cin, int32_t cout,

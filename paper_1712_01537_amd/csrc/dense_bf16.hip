@@ -8,7 +8,7 @@ void go(bool main, const oc::TileArgs& t, hipStream_t s) {
   constexpr oc::TileInfo i = oc::tile_info<uint16_t>(SHAPE);
   constexpr int WGM = i.threads / 64 / (i.bn / 64);
   const auto k = oc::k_dense_tile<uint16_t, i.bm, i.bn, WGM, i.bk, ARS, BRS, GLU, DIRECT>;
-  const dim3 grid((unsigned)((int64_t)t.ntm * t.ntn * t.splits));
+  const dim3 grid((unsigned)(t.whole + t.classes * t.members));
   if (main) oc::launch_main(k, grid, dim3(i.threads), s, t);
   else oc::launch(k, grid, dim3(i.threads), 0, s, t);
 }
@@ -27,12 +27,11 @@ namespace oc {
 
 void tile_bf16(int shape, bool a_rs, bool b_rs, bool direct, bool main, const TileArgs& t,
                hipStream_t s) {
-  switch (shape * 2 + direct) {  // (0, 2: not taken, their staging does not fit in registers)
-    case 1: return pick<TILE_LARGE, true>(a_rs, b_rs, main, t, s);
-    case 3: return pick<TILE_TWO, true>(a_rs, b_rs, main, t, s);
-    case 4: return pick<TILE_MEDIUM, false>(a_rs, b_rs, main, t, s);
-    case 5: return pick<TILE_MEDIUM, true>(a_rs, b_rs, main, t, s);
-    case 6: return pick<TILE_SMALL, false>(a_rs, b_rs, main, t, s);
+  if (!direct) return pick<TILE_SMALL, false>(a_rs, b_rs, main, t, s);  // (the only one planned)
+  switch (shape) {
+    case TILE_LARGE: return pick<TILE_LARGE, true>(a_rs, b_rs, main, t, s);
+    case TILE_TWO: return pick<TILE_TWO, true>(a_rs, b_rs, main, t, s);
+    case TILE_MEDIUM: return pick<TILE_MEDIUM, true>(a_rs, b_rs, main, t, s);
     default: return pick<TILE_SMALL, true>(a_rs, b_rs, main, t, s);
   }
 }

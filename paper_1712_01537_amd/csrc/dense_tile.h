@@ -13,9 +13,9 @@
 // + 4 j + i (lane group t, MFMA j, accumulator register i), sixteen of them, and
 // the epilogue reads and writes whole vectors straight from the accumulators.
 //
-// bf16 operands whose rows are whole 16-byte vectors go from memory to LDS
-// directly (buffer_load ... lds; what is out of range reads as zero); others, and
-// fp32 ones, pass through registers, where fp32 values are split in three bf16
+// bf16 operands whose rows are whole 16-byte vectors (of which what is behind a
+// row's end holds zeros) go from memory to LDS directly (buffer_load ... lds; what is
+// out of range reads as zero); others, and fp32 ones, pass through registers, where fp32 values are split in three bf16
 // parts (split3.h), so that each is split once per tile.  fp32: six MFMAs a
 // product.
 //
@@ -35,11 +35,21 @@ namespace oc {
 struct TileArgs {
   const void *a, *b;
   int64_t P, R;
-  int32_t Q;                // B's columns in memory (2 n with glu)
+  int32_t Q;                // columns of the product (2 n with glu)
+  int64_t lda, ldb;         // elements from row to row of A and B in memory
+  int32_t half;             // first column of the other half in B with glu
   int32_t ntm, ntn;         // tiles
-  int32_t splits;           // ranges of the reduction, `per` terms each
-  int64_t per;
-  float* part;              // [splits][P][Q] partial sums, where splits > 1
+  // The first `whole` tiles have a workgroup each.  The rest are shared, in
+  // `members` runs of `run` tiles (member g has tiles whole + g + members j, those
+  // there are): the steps of a run, `steps` a tile, are dealt out to `classes`
+  // workgroups, `share` each (at most a tile's, so of at most two tiles).  So the
+  // members' workgroups of one class walk the same range of the reduction, next to
+  // each other in the order of the tiles, and share what they read in L2.  Sums of
+  // a workgroup (class c, member g) that are not all of its tile j's go to
+  // part[(c + j) members + g][BM][BN].
+  int32_t whole, members, run, classes;
+  int64_t steps, share;
+  float* part;
   Epi epi;
 };
 
@@ -103,20 +113,22 @@ __device__ __forceinline__ dt_sv4 dt_rsrc(const char* p, int64_t bytes) {
                 (int32_t)(bytes < most ? bytes : most), 0x00020000};
 }
 
-// Tile of block `bid`: each XCD (blocks are dealt out to the eight in turn) takes
-// a contiguous range, splits outermost, in groups of eight rows of tiles, so that
-// the tiles an XCD works on at a time share operands in its L2.
+// The place of block i of `total` in the order of the tiles: each XCD (blocks are
+// dealt out to the eight in turn) takes a contiguous range.
+__device__ __forceinline__ uint32_t xcd_order(uint32_t i, uint32_t total) {
+  const uint32_t x = i & 7, per = total >> 3, rem = total & 7;
+  return x * per + (x < rem ? x : rem) + (i >> 3);
+}
+// Row and column of tile i: groups of eight rows of tiles, so that the tiles an XCD
+// works on at a time share operands in its L2.
 struct TilePos {
-  int m, n, split;
+  int m, n;
 };
-__device__ __forceinline__ TilePos tile_pos(const TileArgs& t, uint32_t bid) {
-  const uint32_t total = gridDim.x, x = bid & 7, per = total >> 3, rem = total & 7;
-  const uint32_t idx = x * per + (x < rem ? x : rem) + (bid >> 3);
-  const uint32_t tiles = (uint32_t)t.ntm * t.ntn, split = idx / tiles, i = idx - split * tiles;
-  const uint32_t group = i / (8 * t.ntn), j = i - group * 8 * t.ntn;
-  const uint32_t left = t.ntm - group * 8, rows = left < 8 ? left : 8;
+__host__ __device__ __forceinline__ TilePos tile_pos(int ntm, int ntn, uint32_t i) {
+  const uint32_t group = i / (8 * ntn), j = i - group * 8 * ntn;
+  const uint32_t left = ntm - group * 8, rows = left < 8 ? left : 8;
   const uint32_t n = j / rows;
-  return TilePos{(int)(group * 8 + (j - n * rows)), (int)n, (int)split};
+  return TilePos{(int)(group * 8 + (j - n * rows)), (int)n};
 }
 
 template <typename T, int BM, int BN, int WGM, int BK, bool ARS, bool BRS, bool GLU, bool DIRECT>
@@ -135,16 +147,36 @@ __global__ __launch_bounds__(64 * WGM * (BN / 64), 2) void k_dense_tile(TileArgs
   constexpr int ROWS = TM < 64 ? TM : 64, EPI = WGM * WGN * ROWS * 16;
   __shared__ __attribute__((aligned(16))) s3_v4u lds[2 * STAGE > EPI ? 2 * STAGE : EPI];
 
-  const int tid = threadIdx.x, lane = tid & 63, li = lane & 15, q = lane >> 4;
+  const int n = t.epi.n;
+
+  // this workgroup's tile, or its shares of two
+  const bool shared = blockIdx.x >= (uint32_t)t.whole;
+  const uint32_t w = shared ? xcd_order(blockIdx.x - t.whole, gridDim.x - t.whole)
+                            : xcd_order(blockIdx.x, t.whole);
+  const uint32_t cls = shared ? w / t.members : 0, member = w - cls * t.members;
+  int64_t unit = cls * t.share;
+  const int64_t all = shared ? t.steps * t.run : t.steps;
+  const int64_t unit_end = !shared || unit + t.share > all ? all : unit + t.share;
+#pragma unroll 1
+  while (unit < unit_end) {
+  int tid = threadIdx.x;
+  asm volatile("" : "+v"(tid));  // nothing of a tile is worked out ahead of the loop
+  const int lane = tid & 63, li = lane & 15, q = lane >> 4;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int wm = wave / WGN, wn = wave % WGN;
-  const TilePos pos = tile_pos(t, blockIdx.x);
+  const uint32_t nth = (uint32_t)(unit / t.steps);  // of the run
+  const int64_t s0 = unit - nth * t.steps;
+  const int64_t s1 = s0 + (unit_end - unit) < t.steps ? s0 + (unit_end - unit) : t.steps;
+  unit += s1 - s0;
+  const bool partial = s1 - s0 < t.steps;
+  const uint32_t tile = shared ? t.whole + member + nth * t.members : w;
+  if (tile >= (uint32_t)(t.ntm * t.ntn)) break;  // this member's run is shorter
+  const TilePos pos = tile_pos(t.ntm, t.ntn, tile);
   const int64_t p0 = (int64_t)pos.m * BM;
-  const int n = t.epi.n;
   const int q0 = pos.n * (GLU ? BN / 2 : BN);  // first output column
-  const int64_t r0 = pos.split * t.per;
-  const int64_t r1 = r0 + t.per < t.R ? r0 + t.per : t.R;
-  const int nk = (int)((r1 - r0 + BK - 1) / BK);
+  const int64_t r0 = s0 * BK;
+  const int64_t r1 = s1 * BK < t.R ? s1 * BK : t.R;
+  const int nk = (int)(s1 - s0);
 
   // This thread's vectors: element offset from the operand's tile corner, how
   // many of the eight values exist (rows past the end repeat the last one, whose
@@ -160,7 +192,7 @@ __global__ __launch_bounds__(64 * WGM * (BN / 64), 2) void k_dense_tile(TileArgs
       kof[i] = ((c % CK) ^ row_xor<CK>(row)) * 8;
       const int64_t lim = isa ? t.P - p0 : (int64_t)t.Q - q0;
       const int rr = row < lim ? row : (int)lim - 1;
-      off[i] = (uint32_t)rr * (uint32_t)t.R + kof[i];
+      off[i] = (uint32_t)rr * (uint32_t)(isa ? t.lda : t.ldb) + kof[i];
       cnt[i] = 8;
     } else {
       constexpr int CRA = BM / 8, CRB = BN / 8;
@@ -174,28 +206,29 @@ __global__ __launch_bounds__(64 * WGM * (BN / 64), 2) void k_dense_tile(TileArgs
       } else if (GLU) {
         lim = n - q0;
         e = col / TN * (TN / 2) + col % (TN / 2);
-        add = col % TN >= TN / 2 ? n : 0;
+        add = col % TN >= TN / 2 ? t.half : 0;
       } else {
         lim = t.Q - q0, e = col;
       }
       cnt[i] = lim - e < 0 ? 0 : lim - e < 8 ? lim - e : 8;
-      const uint32_t ld = isa ? (uint32_t)t.P : (uint32_t)t.Q;
+      const uint32_t ld = (uint32_t)(isa ? t.lda : t.ldb);
       off[i] = (uint32_t)kof[i] * ld + (cnt[i] > 0 ? e + add : 0);
     }
   }
-  const char* const abase = (const char*)t.a + (ARS ? r0 * t.P + p0 : p0 * t.R + r0) * sizeof(T);
+  const char* const abase = (const char*)t.a + (ARS ? r0 * t.lda + p0 : p0 * t.lda + r0) * sizeof(T);
   const char* const bbase =
-      (const char*)t.b + (BRS ? r0 * t.Q + q0 : (int64_t)q0 * t.R + r0) * sizeof(T);
-  const int64_t astep = (ARS ? BK * t.P : BK) * sizeof(T);
-  const int64_t bstep = (BRS ? (int64_t)BK * t.Q : BK) * sizeof(T);
+      (const char*)t.b + (BRS ? r0 * t.ldb + q0 : q0 * t.ldb + r0) * sizeof(T);
+  const int64_t astep = (ARS ? BK * t.lda : BK) * sizeof(T);
+  const int64_t bstep = (BRS ? BK * t.ldb : BK) * sizeof(T);
+  const int64_t asize = (ARS ? t.R : t.P) * t.lda, bsize = (BRS ? t.R : (int64_t)t.Q) * t.ldb;
 
   // Direct: start the loads of step ks into buffer s.
   const uint32_t lds0 = __builtin_amdgcn_readfirstlane((uint32_t)(uintptr_t)(dt_lptr)lds);
   auto issue = [&](int ks, int s) __attribute__((always_inline)) {
     const char* pa = abase + ks * astep;
     const char* pb = bbase + ks * bstep;
-    const dt_sv4 ra = dt_rsrc(pa, (const char*)t.a + t.P * t.R * (int64_t)sizeof(T) - pa);
-    const dt_sv4 rb = dt_rsrc(pb, (const char*)t.b + t.R * t.Q * (int64_t)sizeof(T) - pb);
+    const dt_sv4 ra = dt_rsrc(pa, (const char*)t.a + asize * (int64_t)sizeof(T) - pa);
+    const dt_sv4 rb = dt_rsrc(pb, (const char*)t.b + bsize * (int64_t)sizeof(T) - pb);
     const int64_t left = r1 - r0 - (int64_t)ks * BK;
 #pragma unroll
     for (int i = 0; i < IT; ++i) {
@@ -230,16 +263,61 @@ __global__ __launch_bounds__(64 * WGM * (BN / 64), 2) void k_dense_tile(TileArgs
           reg[i][0] = *(const d_v4u_any*)p;
         }
       }
-    } else {
+    } else if ((ARS ? r0 + (int64_t)(ks + 1) * BK < t.R : p0 + BM < t.P || left >= BK) &&
+               (BRS ? r0 + (int64_t)(ks + 1) * BK < t.R : q0 + BN < t.Q || left >= BK)) {
+      // Vectors that do not all exist, none of them the operand's last: read with
+      // what lies behind them, which is then set to zero.
 #pragma unroll
       for (int i = 0; i < IT; ++i) {
         const bool isa = i < ITA;
         const char* p = (isa ? pa : pb) + (uint64_t)off[i] * sizeof(T);
         const int64_t l = left - kof[i];
+        const int m = (isa ? !ARS : !BRS) ? (l < 0 ? 0 : l < 8 ? (int)l : 8) : l <= 0 ? 0 : cnt[i];
+        if (F32) {
+          reg[i][0] = __builtin_bit_cast(s3_v4u, *(const d_v4f_any*)p);
+          reg[i][F32] = __builtin_bit_cast(s3_v4u, *(const d_v4f_any*)(p + 16));
+#pragma unroll
+          for (int k = 0; k < 4; ++k) {
+            reg[i][0][k] = k < m ? reg[i][0][k] : 0u;
+            reg[i][F32][k] = k + 4 < m ? reg[i][F32][k] : 0u;
+          }
+        } else {
+          reg[i][0] = *(const d_v4u_any*)p;
+#pragma unroll
+          for (int k = 0; k < 4; ++k)
+            reg[i][0][k] &= (2 * k < m ? 0xffffu : 0u) | (2 * k + 1 < m ? 0xffff0000u : 0u);
+        }
+      }
+    } else {
+      // The operand's last vectors: those of its end are read as its last eight
+      // elements and moved down.
+#pragma unroll
+      for (int i = 0; i < IT; ++i) {
+        const bool isa = i < ITA;
+        const int64_t size = isa ? asize : bsize;
+        const int64_t at = ((isa ? pa - (const char*)t.a : pb - (const char*)t.b) / (int)sizeof(T)) +
+                           off[i];
+        const int64_t l = left - kof[i];
         int m = l <= 0 ? 0 : cnt[i];
         if ((isa ? !ARS : !BRS) && l < m) m = l < 0 ? 0 : (int)l;
-        float v[8] = {};
-        if (m > 0) load8n(p, !F32, 0, m, v);
+        const void* base = isa ? t.a : t.b;
+        float v[8];
+        if (size >= 8) {
+          const int64_t from = at + 8 <= size ? at : size - 8;
+          const int by = m > 0 ? (int)(at - from) : 0;
+          load8(base, !F32, from, v);
+          if (__any(by > 0)) {
+#pragma unroll
+            for (int h = 4; h > 0; h >>= 1)
+#pragma unroll
+              for (int k = 0; k < 8; ++k) v[k] = by & h ? v[k + h < 8 ? k + h : k] : v[k];
+          }
+        } else {
+#pragma unroll
+          for (int k = 0; k < 8; ++k) v[k] = k < m ? load1(base, !F32, at + k) : 0.f;
+        }
+#pragma unroll
+        for (int k = 0; k < 8; ++k) v[k] = k < m ? v[k] : 0.f;
         if (F32) {
 #pragma unroll
           for (int k = 0; k < 4; ++k) {
@@ -318,7 +396,7 @@ __global__ __launch_bounds__(64 * WGM * (BN / 64), 2) void k_dense_tile(TileArgs
   // fragments are in registers: there the workgroup meets, and what follows reads
   // the next step's buffer and refills this one's, while the matrix cores still
   // have AD units to do.
-  constexpr int KK = BK / 32, NU = KK * MI, AD = MI >= 4 && !F32 ? 3 : 1;
+  constexpr int KK = BK / 32, NU = KK * MI, AD = DIRECT && MI >= 4 ? 3 : 1;
   static_assert(AD <= MI, "a sub-step's columns are read within the one before it");
   s3_v4u a[AD + 1][PARTS], b[2][NI][PARTS];
   auto read_a = [&](s3_v4u(&f)[PARTS], int s, int u) __attribute__((always_inline)) {
@@ -376,6 +454,15 @@ __global__ __launch_bounds__(64 * WGM * (BN / 64), 2) void k_dense_tile(TileArgs
 #pragma unroll
         for (int j = 0; j < NI; ++j) acc[u % MI][j] = s3_mfma(b[0][j][0], a[0][0], acc[u % MI][j]);
       }
+      if constexpr (F32 && TM == 64) {  // the splits and LDS accesses in the shadow of the MFMAs
+#pragma unroll
+        for (int x = 0; x < 24; ++x) {
+          __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
+          __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
+          __builtin_amdgcn_sched_group_barrier(0x002, 3, 0);
+          __builtin_amdgcn_sched_group_barrier(0x200, 1, 0);
+        }
+      }
       __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
       for (int i = 0; i < AD; ++i)
@@ -397,8 +484,8 @@ __global__ __launch_bounds__(64 * WGM * (BN / 64), 2) void k_dense_tile(TileArgs
       if (k >= count || fabsf(v[k]) < INFINITY) continue;
       float z = 0.f;
       for (int64_t r = r0; r < r1; ++r) {
-        const float x = ((const float*)t.a)[ARS ? r * t.P + p : p * t.R + r];
-        const float y = ((const float*)t.b)[BRS ? r * t.Q + c + k : (c + k) * t.R + r];
+        const float x = ((const float*)t.a)[ARS ? r * t.lda + p : p * t.lda + r];
+        const float y = ((const float*)t.b)[BRS ? r * t.ldb + c + k : (c + k) * t.ldb + r];
         z = fmaf(x, y, z);
       }
       v[k] = z;
@@ -415,9 +502,9 @@ __global__ __launch_bounds__(64 * WGM * (BN / 64), 2) void k_dense_tile(TileArgs
   s3_v4u* const mine = lds + wave * ROWS * 16;
   const int c = q0 + wn * COLS + lane % LR * 8, cols = n - c;
   float b0[8] = {}, b1[8] = {};
-  if (t.epi.bias && !t.part && cols > 0) {
-    load8n(t.epi.bias, false, c, cols, b0);
-    if (GLU) load8n(t.epi.bias, false, n + c, cols, b1);
+  if (t.epi.bias && !partial && cols > 0) {
+    load8n(t.epi.bias, false, c, cols, t.Q, b0);
+    if (GLU) load8n(t.epi.bias, false, n + c, cols, t.Q, b1);
   }
   dt_barrier();  // no wave reads operands from LDS any more
 #pragma unroll
@@ -466,18 +553,21 @@ __global__ __launch_bounds__(64 * WGM * (BN / 64), 2) void k_dense_tile(TileArgs
               if (GLU) again(p[i], n + c, cols, u[i]);
             }
       }
-      if (t.part) {
+      if (partial) {
 #pragma unroll
-        for (int i = 0; i < U; ++i)
-          if (p[i] < t.P) {
-            float* o = t.part + ((int64_t)pos.split * t.P + p[i]) * t.Q;
-            store8n(o, false, c, cols, v[i]);
-            if (GLU) store8n(o, false, n + c, cols, u[i]);
-          }
+        for (int i = 0; i < U; ++i) {
+          const int row = (int)(p[i] - p0);
+          const int64_t slot = (int64_t)(cls + nth) * t.members + member;
+          float* o = t.part + (slot * BM + row) * BN + wn * TN + lane % LR * 8;
+          store8(o, false, 0, v[i]);
+          if (GLU) store8(o, false, 32, u[i]);
+        }
       } else {
         epilogue<U, GLU>(t.epi, p, t.P, c, b0, b1, v, u);
       }
     }
+  }
+  dt_barrier();  // the next tile's operands go where the sums were
   }
 }
 

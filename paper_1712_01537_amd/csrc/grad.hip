@@ -69,7 +69,7 @@ __device__ __forceinline__ void for_chunks(const Table& t, Load&& load, F&& f) {
 __device__ __forceinline__ void load_in(const Table& t, int i, int64_t e, int64_t n, float (&v)[8]) {
   const int cnt = (int)(n - e < 8 ? n - e : 8);
   if (cnt > 0) {
-    oc::load8n(t.in[i], t.in_bf16[i], e, cnt, v);
+    oc::load8n(t.in[i], t.in_bf16[i], e, cnt, n, v);
   } else {
 #pragma unroll
     for (int k = 0; k < 8; ++k) v[k] = 0.f;
