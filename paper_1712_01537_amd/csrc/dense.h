@@ -46,13 +46,26 @@ struct Gemm {
 
 // Whether a layer's bf16 operands are copied to rows of whole 16-byte vectors first:
 // where they are not, and the product is large enough to gain from it (8383 x 513 ->
-// 1027: the forward takes 48 us on rows of any length through registers and 27 with the
-// copies, which take 8; products of 2 GFLOP gain nothing).
+// 1027: the forward takes 48 us on rows of any length through registers, in 64 x 64
+// tiles, and 37 with the copies; a product of 2 GFLOP takes some 10 either way).
 inline bool pads(oc_dtype dt, int64_t rows, int64_t cin, int64_t cout, bool glu) {
   return dt == OC_BF16 && (cin % 8 || cout % 8) &&
          2.0 * rows * cin * cout * (glu ? 2 : 1) >= 2e9;
 }
 inline int64_t pad8(int64_t n) { return (n + 7) / 8 * 8; }
+
+// The forward product of few rows: out [rows][Q] = x [rows][R] times w [R][Q], no workspace.
+// Few: where it is faster than the tiles, that is for up to 4 (fp32: 8) rows, and for
+// more while its workgroups (4 rows, 16 columns) have a CU each and the reduction is
+// not long.  With tiles in brackets: fp32 1024 -> 1024, 8 rows 6.1 us (10.5), 16 rows 6.3
+// (10.9); 4096 -> 4096, 8 rows 24 (28), 16 rows 49 (28); bf16 1024 -> 1024, 4 rows 5.7
+// (7.7), 8 rows 5.9 (7.6); 4096 -> 4096, 4 rows 11.7 (13.4), 8 rows 17.0 (13.7).
+inline bool few_rows(oc_dtype dt, int64_t rows, int64_t cin, int64_t cout) {
+  return rows <= (dt == OC_F32 ? 8 : 4) ||
+         (rows <= 64 && cdiv(cout, 16) * cdiv(rows, 4) <= 256 && cin <= 2048);
+}
+void gemm_rows(oc_dtype dt, int32_t rows, int32_t R, int32_t Q, const void* x, const void* w,
+               const Epi& epi, hipStream_t s);
 
 // Bytes of workspace the product needs (partial sums of a split reduction);
 // a function of the type and the sizes alone.
@@ -61,6 +74,13 @@ size_t gemm_ws(oc_dtype dt, int64_t P, int64_t Q, int64_t R, bool glu);
 void gemm(const Gemm& g, void* ws, bool main, hipStream_t s);
 
 // --- device side ---------------------------------------------------------
+
+// The place of block i of `total` in an order of tiles or columns: each XCD (blocks are
+// dealt out to the eight in turn) takes a contiguous range.
+__device__ __forceinline__ uint32_t xcd_order(uint32_t i, uint32_t total) {
+  const uint32_t x = i & 7, per = total >> 3, rem = total & 7;
+  return x * per + (x < rem ? x : rem) + (i >> 3);
+}
 
 __device__ __forceinline__ float bf_up(uint32_t h) {
   return __builtin_bit_cast(float, h << 16);

@@ -217,6 +217,7 @@ struct FwdWs {
 };
 FwdWs fwd_ws(oc_dtype dt, int64_t rows, int32_t cin, int32_t cout, bool glu) {
   const int64_t nz = glu ? 2 * cout : cout;
+  if (oc::few_rows(dt, rows, cin, cout)) return FwdWs{0, 0, 0, 0};
   const bool pd = oc::pads(dt, rows, cin, cout, glu);
   FwdWs f;
   f.x = 0;
@@ -237,6 +238,12 @@ oc_status fwd(const char* who, bool glu, oc_dtype dt, int32_t act, int64_t rows,
   st = check_ws(who, ws, ws_bytes, o.total);
   if (st != OC_OK) return st;
   const int32_t bf16 = dt == OC_BF16, nz = glu ? 2 * cout : cout;
+  const oc::Epi epi{act, glu, cout, bf16, bf16 && act == OC_ACT_RELU && !glu, bias, res, y, pre};
+  if (oc::few_rows(dt, rows, cin, cout)) {
+    oc::gemm_rows(dt, (int32_t)rows, cin, nz, x, w, epi, s);
+    OC_LAUNCH_CHECK();
+    return OC_OK;
+  }
   char* base = (char*)ws;
   int64_t lda = cin, ldb = nz, half = cout;
   if (oc::pads(dt, rows, cin, cout, glu)) {
@@ -254,9 +261,8 @@ oc_status fwd(const char* who, bool glu, oc_dtype dt, int32_t act, int64_t rows,
     }
     pad(p, s);
   }
-  oc::Gemm g{dt,    rows, cin, nz, x, w, lda, ldb, (int32_t)half, false, true,
-             {act, glu, cout, bf16, bf16 && act == OC_ACT_RELU && !glu, bias, res, y, pre}};
-  oc::gemm(g, base + o.gemm, true, s);
+  oc::gemm(oc::Gemm{dt, rows, cin, nz, x, w, lda, ldb, (int32_t)half, false, true, epi},
+           base + o.gemm, true, s);
   OC_LAUNCH_CHECK();
   return OC_OK;
 }

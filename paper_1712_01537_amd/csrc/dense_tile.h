@@ -113,12 +113,6 @@ __device__ __forceinline__ dt_sv4 dt_rsrc(const char* p, int64_t bytes) {
                 (int32_t)(bytes < most ? bytes : most), 0x00020000};
 }
 
-// The place of block i of `total` in the order of the tiles: each XCD (blocks are
-// dealt out to the eight in turn) takes a contiguous range.
-__device__ __forceinline__ uint32_t xcd_order(uint32_t i, uint32_t total) {
-  const uint32_t x = i & 7, per = total >> 3, rem = total & 7;
-  return x * per + (x < rem ? x : rem) + (i >> 3);
-}
 // Row and column of tile i: groups of eight rows of tiles, so that the tiles an XCD
 // works on at a time share operands in its L2.
 struct TilePos {
