@@ -95,9 +95,9 @@ __global__ __launch_bounds__(TB) void k_dense_rows(const void* x, const void* w,
               if (BF16) {
                 wv[2 * m] = oc::bf_up(raw[i][j][h][0][m] & 0xffffu);
                 wv[2 * m + 1] = __builtin_bit_cast(float, raw[i][j][h][0][m] & 0xffff0000u);
-              } else {
-                wv[m] = __builtin_bit_cast(float, raw[i][j][h][0][m]);
-                wv[4 + m] = __builtin_bit_cast(float, raw[i][j][h][V - 1][m]);
+              } else {  // (a bit cast of a vector's element would take the first one's bits)
+                wv[m] = __builtin_bit_cast(oc::d_v4f, raw[i][j][h][0])[m];
+                wv[4 + m] = __builtin_bit_cast(oc::d_v4f, raw[i][j][h][V - 1])[m];
               }
             }
             add(h, one, wv);

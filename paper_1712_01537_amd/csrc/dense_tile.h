@@ -470,22 +470,6 @@ __global__ __launch_bounds__(64 * WGM * (BN / 64), 2) void k_dense_tile(TileArgs
     }
   }
 
-  // fp32: what the three parts cannot represent is formed again in plain fp32
-  // (operands of 2^103 and more, sums of 2^80 and more, infinities, NaN).
-  auto again = [&](int64_t p, int c, int count, float* v) __attribute__((always_inline)) {
-#pragma unroll
-    for (int k = 0; k < 8; ++k) {
-      if (k >= count || fabsf(v[k]) < INFINITY) continue;
-      float z = 0.f;
-      for (int64_t r = r0; r < r1; ++r) {
-        const float x = ((const float*)t.a)[ARS ? r * t.lda + p : p * t.lda + r];
-        const float y = ((const float*)t.b)[BRS ? r * t.ldb + c + k : (c + k) * t.ldb + r];
-        z = fmaf(x, y, z);
-      }
-      v[k] = z;
-    }
-  };
-
   // Epilogue: the wave's piece to LDS, ROWS rows at a time (16 vectors a row, XORed
   // by the row), and back with eight columns of a row per lane (with glu, eight of
   // either half).
@@ -507,8 +491,31 @@ __global__ __launch_bounds__(64 * WGM * (BN / 64), 2) void k_dense_tile(TileArgs
     for (int i = 0; i < ROWS / 16; ++i)
 #pragma unroll
       for (int j = 0; j < NI; ++j)
-        mine[(i * 16 + li) * 16 + ((j * 4 + q) ^ li)] =
-            __builtin_bit_cast(s3_v4u, acc[pass * (ROWS / 16) + i][j]);
+        mine[(i * 16 + li) * 16 + ((j * 4 + q) ^ li)] = __builtin_bit_cast(
+            s3_v4u, F32 ? acc[pass * (ROWS / 16) + i][j] * kSplitDown : acc[pass * (ROWS / 16) + i][j]);
+    if constexpr (F32) {
+      // What the three parts cannot represent is formed again in plain fp32 (operands
+      // of 2^103 and more, sums of 2^80 and more, infinities, NaN).
+      bool bad = false;
+#pragma unroll
+      for (int i = 0; i < ROWS / 16; ++i)
+#pragma unroll
+        for (int j = 0; j < NI; ++j) bad |= s3_bad(acc[pass * (ROWS / 16) + i][j]);
+      if (__any(bad))
+        for (int x = lane; x < ROWS * 64; x += 64) {
+          const int row = x >> 6, col = x & 63;
+          const int64_t p = p0 + wm * TM + pass * ROWS + row;
+          const int cc = GLU ? q0 + wn * 32 + (col & 31) : q0 + wn * 64 + col;
+          float* const v = (float*)&mine[row * 16 + ((col >> 2) ^ (row & 15))] + (col & 3);
+          if (fabsf(*v) < INFINITY || p >= t.P || cc >= n) continue;
+          const int qc = GLU && col >= 32 ? cc + t.half : cc;
+          float z = 0.f;
+          for (int64_t r = r0; r < r1; ++r)
+            z = fmaf(((const float*)t.a)[ARS ? r * t.lda + p : p * t.lda + r],
+                     ((const float*)t.b)[BRS ? r * t.ldb + qc : qc * t.ldb + r], z);
+          *v = z;
+        }
+    }
 #pragma unroll 1
     for (int g = 0; g < ROWS / (RI * U); ++g) {
       float v[U][8], u[U][8];
@@ -523,30 +530,13 @@ __global__ __launch_bounds__(64 * WGM * (BN / 64), 2) void k_dense_tile(TileArgs
             const s3_v4f x = __builtin_bit_cast(
                 s3_v4f, mine[row * 16 + ((col / 4 + h) ^ (row & 15))]);
 #pragma unroll
-            for (int k = 0; k < 4; ++k) w[h * 4 + k] = F32 ? x[k] * kSplitDown : x[k];
+            for (int k = 0; k < 4; ++k) w[h * 4 + k] = x[k];
           }
         };
         get(lane % LR * 8, v[i]);
         if (GLU) get(32 + lane % LR * 8, u[i]);
       }
       if (cols <= 0) continue;
-      if (F32) {
-        bool bad = false;
-#pragma unroll
-        for (int i = 0; i < U; ++i)
-#pragma unroll
-          for (int k = 0; k < 8; ++k) {
-            bad |= !(fabsf(v[i][k]) < INFINITY);
-            if (GLU) bad |= !(fabsf(u[i][k]) < INFINITY);
-          }
-        if (bad)
-#pragma unroll
-          for (int i = 0; i < U; ++i)
-            if (p[i] < t.P) {
-              again(p[i], c, cols, v[i]);
-              if (GLU) again(p[i], n + c, cols, u[i]);
-            }
-      }
       if (partial) {
 #pragma unroll
         for (int i = 0; i < U; ++i) {
