@@ -98,6 +98,26 @@ __device__ __forceinline__ void dt_barrier() {
 // All of this wave's vector memory operations are done.
 __device__ __forceinline__ void dt_wait_vm() { __builtin_amdgcn_s_waitcnt(0x0F70); }
 
+// s3_split8 with the differences as subtractions: the dot products that it forms
+// them with are one instruction where these are two, but issue at a quarter of the
+// rate (a step of the large tile alone on its CU: 2.0 us with them, 1.7 without).
+__device__ __forceinline__ Split8 dt_split8(const s3_v4f& x, const s3_v4f& y) {
+  Split8 r;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    float a = (i < 2 ? x : y)[2 * (i & 1)] * kSplitUp;
+    float b = (i < 2 ? x : y)[2 * (i & 1) + 1] * kSplitUp;
+#pragma unroll
+    for (int k = 0; k < 3; ++k) {
+      const uint32_t h = s3_round2(a, b);
+      r.p[k][i] = h;
+      a -= __builtin_bit_cast(float, h << 16);
+      b -= __builtin_bit_cast(float, h & 0xffff0000u);
+    }
+  }
+  return r;
+}
+
 // Memory to LDS: lane i's 16 bytes at byte `off` of the resource land at lds +
 // 16 i; an offset past the resource's end stores zeros.
 __device__ __forceinline__ void dt_lds_load16(dt_sv4 rsrc, uint32_t off, uint32_t lds) {
@@ -233,107 +253,89 @@ __global__ __launch_bounds__(64 * WGM * (BN / 64), 2) void k_dense_tile(TileArgs
     }
   };
 
-  // Through registers: load step ks, then split and store vectors from .. to of it
-  // to buffer s.
+  // Through registers: load vectors from .. to of step ks, then split and store them
+  // to buffer s.  The first `plain` steps read whole vectors: what such a vector holds
+  // of a column past the end goes to sums that are dropped, and lies inside the
+  // operand as long as its last line is not read or the tile has no such column.
   s3_v4u reg[IT][F32 ? 2 : 1];
-  bool whole = true;  // every vector of the tile exists, ends of the reduction aside
+  int plain = 0;
   if constexpr (!DIRECT) {
+    bool whole = true;
 #pragma unroll
     for (int i = 0; i < IT; ++i) whole = whole && (cnt[i] == 8 || cnt[i] == 0);
     whole = __syncthreads_and(whole);
+    plain = (int)(((whole ? r1 : r1 < t.R ? r1 : t.R - 1) - r0) / BK);
   }
-  auto fetch = [&](int ks) __attribute__((always_inline)) {
+  auto fetch_plain = [&](int ks, int from, int to) __attribute__((always_inline)) {
     const char* pa = abase + ks * astep;
     const char* pb = bbase + ks * bstep;
-    const int64_t left = r1 - r0 - (int64_t)ks * BK;
-    if (whole && left >= BK) {
 #pragma unroll
-      for (int i = 0; i < IT; ++i) {
-        const char* p = (i < ITA ? pa : pb) + (uint64_t)off[i] * sizeof(T);
-        if (F32) {
-          reg[i][0] = __builtin_bit_cast(s3_v4u, *(const d_v4f_any*)p);
-          reg[i][F32] = __builtin_bit_cast(s3_v4u, *(const d_v4f_any*)(p + 16));
-        } else {
-          reg[i][0] = *(const d_v4u_any*)p;
-        }
-      }
-    } else if ((ARS ? r0 + (int64_t)(ks + 1) * BK < t.R : p0 + BM < t.P || left >= BK) &&
-               (BRS ? r0 + (int64_t)(ks + 1) * BK < t.R : q0 + BN < t.Q || left >= BK)) {
-      // Vectors that do not all exist, none of them the operand's last: read with
-      // what lies behind them, which is then set to zero.
-#pragma unroll
-      for (int i = 0; i < IT; ++i) {
-        const bool isa = i < ITA;
-        const char* p = (isa ? pa : pb) + (uint64_t)off[i] * sizeof(T);
-        const int64_t l = left - kof[i];
-        const int m = (isa ? !ARS : !BRS) ? (l < 0 ? 0 : l < 8 ? (int)l : 8) : l <= 0 ? 0 : cnt[i];
-        if (F32) {
-          reg[i][0] = __builtin_bit_cast(s3_v4u, *(const d_v4f_any*)p);
-          reg[i][F32] = __builtin_bit_cast(s3_v4u, *(const d_v4f_any*)(p + 16));
-#pragma unroll
-          for (int k = 0; k < 4; ++k) {
-            reg[i][0][k] = k < m ? reg[i][0][k] : 0u;
-            reg[i][F32][k] = k + 4 < m ? reg[i][F32][k] : 0u;
-          }
-        } else {
-          reg[i][0] = *(const d_v4u_any*)p;
-#pragma unroll
-          for (int k = 0; k < 4; ++k)
-            reg[i][0][k] &= (2 * k < m ? 0xffffu : 0u) | (2 * k + 1 < m ? 0xffff0000u : 0u);
-        }
-      }
-    } else {
-      // The operand's last vectors: those of its end are read as its last eight
-      // elements and moved down.
-#pragma unroll
-      for (int i = 0; i < IT; ++i) {
-        const bool isa = i < ITA;
-        const int64_t size = isa ? asize : bsize;
-        const int64_t at = ((isa ? pa - (const char*)t.a : pb - (const char*)t.b) / (int)sizeof(T)) +
-                           off[i];
-        const int64_t l = left - kof[i];
-        int m = l <= 0 ? 0 : cnt[i];
-        if ((isa ? !ARS : !BRS) && l < m) m = l < 0 ? 0 : (int)l;
-        const void* base = isa ? t.a : t.b;
-        float v[8];
-        if (size >= 8) {
-          const int64_t from = at + 8 <= size ? at : size - 8;
-          const int by = m > 0 ? (int)(at - from) : 0;
-          load8(base, !F32, from, v);
-          if (__any(by > 0)) {
-#pragma unroll
-            for (int h = 4; h > 0; h >>= 1)
-#pragma unroll
-              for (int k = 0; k < 8; ++k) v[k] = by & h ? v[k + h < 8 ? k + h : k] : v[k];
-          }
-        } else {
-#pragma unroll
-          for (int k = 0; k < 8; ++k) v[k] = k < m ? load1(base, !F32, at + k) : 0.f;
-        }
-#pragma unroll
-        for (int k = 0; k < 8; ++k) v[k] = k < m ? v[k] : 0.f;
-        if (F32) {
-#pragma unroll
-          for (int k = 0; k < 4; ++k) {
-            reg[i][0][k] = __builtin_bit_cast(uint32_t, v[k]);
-            reg[i][F32][k] = __builtin_bit_cast(uint32_t, v[4 + k]);
-          }
-        } else {
-          reg[i][0] = s3_v4u{bf_pair(v[0], v[1]), bf_pair(v[2], v[3]), bf_pair(v[4], v[5]),
-                             bf_pair(v[6], v[7])};
-        }
+    for (int i = from; i < to; ++i) {
+      const char* p = (i < ITA ? pa : pb) + (uint32_t)(off[i] * sizeof(T));
+      if (F32) {
+        reg[i][0] = __builtin_bit_cast(s3_v4u, *(const d_v4f_any*)p);
+        reg[i][F32] = __builtin_bit_cast(s3_v4u, *(const d_v4f_any*)(p + 16));
+      } else {
+        reg[i][0] = *(const d_v4u_any*)p;
       }
     }
   };
-  const SplitK sk = s3_consts();
-  auto stash = [&](int s, int from, int to) __attribute__((always_inline)) {
+  // The other steps: what lies behind a vector's end is set to zero, and vectors at
+  // the operand's end are read as its last eight elements and moved down.
+  auto fetch_tail = [&](int ks) __attribute__((always_inline)) {
+    const char* pa = abase + ks * astep;
+    const char* pb = bbase + ks * bstep;
+    const int64_t left = r1 - r0 - (int64_t)ks * BK;
 #pragma unroll
     for (int i = 0; i < IT; ++i) {
-      if (i < from || i >= to) continue;
+      const bool isa = i < ITA;
+      const int64_t size = isa ? asize : bsize;
+      const int64_t at = ((isa ? pa - (const char*)t.a : pb - (const char*)t.b) / (int)sizeof(T)) +
+                         off[i];
+      const int64_t l = left - kof[i];
+      int m = l <= 0 ? 0 : cnt[i];
+      if ((isa ? !ARS : !BRS) && l < m) m = l < 0 ? 0 : (int)l;
+      const void* base = isa ? t.a : t.b;
+      float v[8];
+      if (size >= 8) {
+        const int64_t from = at + 8 <= size ? at : size - 8;
+        const int by = m > 0 ? (int)(at - from) : 0;
+        load8(base, !F32, from, v);
+        if (__any(by > 0)) {
+#pragma unroll
+          for (int h = 4; h > 0; h >>= 1)
+#pragma unroll
+            for (int k = 0; k < 8; ++k) v[k] = by & h ? v[k + h < 8 ? k + h : k] : v[k];
+        }
+      } else {
+#pragma unroll
+        for (int k = 0; k < 8; ++k) v[k] = k < m ? load1(base, !F32, at + k) : 0.f;
+      }
+#pragma unroll
+      for (int k = 0; k < 8; ++k) v[k] = k < m ? v[k] : 0.f;
+      if (F32) {
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+          reg[i][0][k] = __builtin_bit_cast(uint32_t, v[k]);
+          reg[i][F32][k] = __builtin_bit_cast(uint32_t, v[4 + k]);
+        }
+      } else {
+        reg[i][0] = s3_v4u{bf_pair(v[0], v[1]), bf_pair(v[2], v[3]), bf_pair(v[4], v[5]),
+                           bf_pair(v[6], v[7])};
+      }
+    }
+  };
+  auto fetch = [&](int ks) __attribute__((always_inline)) {
+    if (ks < plain) fetch_plain(ks, 0, IT);
+    else fetch_tail(ks);
+  };
+  auto stash = [&](int s, int from, int to) __attribute__((always_inline)) {
+#pragma unroll
+    for (int i = from; i < to; ++i) {
       const bool isa = i < ITA;
       const int c = s * STAGE + (isa ? i : i - ITA) * NTHR + tid + (isa ? 0 : PARTS * CA);
       if constexpr (F32) {
-        const Split8 p = s3_split8(sk, __builtin_bit_cast(s3_v4f, reg[i][0]),
+        const Split8 p = dt_split8(__builtin_bit_cast(s3_v4f, reg[i][0]),
                                    __builtin_bit_cast(s3_v4f, reg[i][F32]));
 #pragma unroll
         for (int k = 0; k < 3; ++k) lds[c + k * (isa ? CA : CB)] = p.p[k];
@@ -404,6 +406,75 @@ __global__ __launch_bounds__(64 * WGM * (BN / 64), 2) void k_dense_tile(TileArgs
       for (int k = 0; k < PARTS; ++k) f[j][k] = frag_b(s, k, kk, j);
   };
 
+  // The large fp32 tile's step: four units of two row and two column fragments, 24
+  // MFMAs and six LDS reads each, every read into registers that the unit before has
+  // done with.  (Row by row, a step's twelve column reads of every wave came at once
+  // after the barrier, and took 960 cycles of the LDS: 2.33 us a step.)
+  constexpr bool QUAD = F32 && MI == 4;
+
+  if constexpr (QUAD) {
+    s3_v4u fa[4][PARTS], fb[4][PARTS];
+    auto read2a = [&](int s, int i) __attribute__((always_inline)) {
+      read_a(fa[i], s, i);
+      read_a(fa[i + 1], s, i + 1);
+    };
+    auto read2b = [&](int s, int j) __attribute__((always_inline)) {
+#pragma unroll
+      for (int x = j; x < j + 2; ++x)
+#pragma unroll
+        for (int k = 0; k < PARTS; ++k) fb[x][k] = frag_b(s, k, 0, x);
+    };
+    auto multiply = [&](int i, int j) __attribute__((always_inline)) {
+#pragma unroll
+      for (int x = 0; x < 6; ++x)
+#pragma unroll
+        for (int m = 0; m < 4; ++m)
+          acc[i + m / 2][j + m % 2] =
+              s3_product(x, fb[j + m % 2], fa[i + m / 2], acc[i + m / 2][j + m % 2]);
+#pragma unroll
+      for (int x = 0; x < 24; ++x) {  // splits and LDS accesses in the shadow of the MFMAs
+        __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
+        __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
+        __builtin_amdgcn_sched_group_barrier(0x002, 3, 0);
+        __builtin_amdgcn_sched_group_barrier(0x200, 1, 0);
+      }
+      __builtin_amdgcn_sched_barrier(0);
+    };
+    static_assert(IT == 3, "a vector for each of the units ahead of the barrier");
+    // Step ks.  ahead(i): load vector i of step ks + 2, right behind its place's use.
+    auto step = [&](int s, auto&& ahead) __attribute__((always_inline)) {
+      read2b(s, 2);
+      stash(s ^ 1, 0, 1);
+      ahead(0);
+      multiply(0, 0);
+      read2a(s, 2);
+      stash(s ^ 1, 1, 2);
+      ahead(1);
+      multiply(0, 2);
+      stash(s ^ 1, 2, 3);
+      ahead(2);
+      multiply(2, 0);
+      dt_barrier();  // step ks + 1 is in LDS, and step ks in registers
+      read2a(s ^ 1, 0);  // (of the last step: what lies there, never used)
+      read2b(s ^ 1, 0);
+      multiply(2, 2);
+    };
+    fetch(0);
+    stash(0, 0, IT);
+    dt_barrier();
+    if (nk > 1) fetch(1);
+    read2a(0, 0);
+    read2b(0, 0);
+    int ks = 0;
+    // no branch between the loads, so that each is waited for by itself
+    for (; ks + 2 < plain; ++ks)
+      step(ks & 1, [&](int i) __attribute__((always_inline)) { fetch_plain(ks + 2, i, i + 1); });
+#pragma unroll 1
+    for (; ks < nk; ++ks) {
+      step(ks & 1, [](int) {});
+      if (ks + 2 < nk) fetch(ks + 2);
+    }
+  } else {
   if constexpr (DIRECT) {
     issue(0, 0);
     dt_wait_vm();
@@ -448,15 +519,6 @@ __global__ __launch_bounds__(64 * WGM * (BN / 64), 2) void k_dense_tile(TileArgs
 #pragma unroll
         for (int j = 0; j < NI; ++j) acc[u % MI][j] = s3_mfma(b[0][j][0], a[0][0], acc[u % MI][j]);
       }
-      if constexpr (F32 && TM == 64) {  // the splits and LDS accesses in the shadow of the MFMAs
-#pragma unroll
-        for (int x = 0; x < 24; ++x) {
-          __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
-          __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
-          __builtin_amdgcn_sched_group_barrier(0x002, 3, 0);
-          __builtin_amdgcn_sched_group_barrier(0x200, 1, 0);
-        }
-      }
       __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
       for (int i = 0; i < AD; ++i)
@@ -468,6 +530,7 @@ __global__ __launch_bounds__(64 * WGM * (BN / 64), 2) void k_dense_tile(TileArgs
 #pragma unroll
           for (int k = 0; k < PARTS; ++k) b[0][j][k] = b[1][j][k];
     }
+  }
   }
 
   // Epilogue: the wave's piece to LDS, ROWS rows at a time (16 vectors a row, XORed
