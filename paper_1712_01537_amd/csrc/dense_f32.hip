@@ -7,7 +7,7 @@ template <int SHAPE, bool ARS, bool BRS, bool GLU>
 void go(bool main, const oc::TileArgs& t, hipStream_t s) {
   constexpr oc::TileInfo i = oc::tile_info<float>(SHAPE);
   constexpr int WGM = i.threads / 64 / (i.bn / 64);
-  const auto k = oc::k_dense_tile<float, i.bm, i.bn, WGM, i.bk, ARS, BRS, GLU, false>;
+  const auto k = oc::k_dense_tile<float, i.bm, i.bn, WGM, i.bk, i.nb, ARS, BRS, GLU, false>;
   const dim3 grid((unsigned)(t.whole + t.classes * t.members));
   if (main) oc::launch_main(k, grid, dim3(i.threads), s, t);
   else oc::launch(k, grid, dim3(i.threads), 0, s, t);

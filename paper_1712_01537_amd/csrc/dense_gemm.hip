@@ -90,8 +90,8 @@ struct Plan {
 // the card; the least is taken.  Measured, in microseconds: a step of BK terms of a
 // workgroup alone on its CU and with all that fit there, and what a workgroup takes
 // to start and finish.  (As many workgroups as fit, all three layouts within 5%: bf16
-// 256x256 1404 TFLOP/s, 256x128 1190, 128x128 1157, 64x64 715; fp32 256x128 220,
-// 128x64 168, 128x128 200, 64x64 143.)  Partial sums are written and read at 4 TB/s
+// 256x256 1430 TFLOP/s, 256x128 1190, 128x128 1180, 64x64 715; fp32 256x128 250,
+// 128x64 168, 128x128 202, 64x64 140.)  Partial sums are written and read at 4 TB/s
 // and take another launch of 4 us.
 // direct: bf16 operands that go straight to LDS; the larger tiles take only those.
 Plan plan(oc_dtype dt, bool direct, int64_t P, int64_t Q, int64_t R, bool glu) {
@@ -101,8 +101,8 @@ Plan plan(oc_dtype dt, bool direct, int64_t P, int64_t Q, int64_t R, bool glu) {
     double ends;
   };
   static const Cost cost[2][oc::TILE_SHAPES] = {
-      {{2.25, 2.33, 1, 9.}, {1.05, 1.6, 2, 5.5}, {1.27, 1.33, 1, 6.}, {0.75, 1.4, 3, 4.}},
-      {{1.35, 1.53, 1, 8.}, {0.64, 0.91, 2, 7.}, {0.62, 0.93, 2, 4.5}, {0.48, 0.75, 4, 2.5}}};
+      {{1.75, 2.16, 1, 9.}, {1.02, 1.6, 2, 5.5}, {1.18, 1.33, 1, 6.}, {0.74, 1.45, 3, 4.}},
+      {{1.22, 1.5, 1, 8.}, {0.6, 0.9, 2, 7.}, {0.64, 0.91, 2, 4.5}, {0.47, 0.74, 4, 2.5}}};
   const int64_t cus = oc::cu_count(), n = glu ? Q / 2 : Q;
   Plan best{};
   double least = 1e300;
@@ -119,8 +119,9 @@ Plan plan(oc_dtype dt, bool direct, int64_t P, int64_t Q, int64_t R, bool glu) {
       const int64_t wgs = members * classes;
       double us = rounds;
       if (rest > 0) {
-        const double crowd = c.fit > 1 && wgs > cus
-                                 ? std::min(1.0, (double)(wgs - cus) / (double)(slots - cus)) : 0.0;
+        const int64_t calm = c.fit > 1 ? cus : cus / 4;  // workgroups that run as if alone
+        const double crowd =
+            wgs > calm ? std::min(1.0, (double)(wgs - calm) / (double)(slots - calm)) : 0.0;
         us += share * (whole > 0 ? c.full : c.step + (c.full - c.step) * crowd) + c.ends;
       }
       if (share < steps)

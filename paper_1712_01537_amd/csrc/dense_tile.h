@@ -6,8 +6,8 @@
 // gradient (x and dz across their rows) without transposing anything in memory.
 //
 // A workgroup owns a BM x BN tile, its waves TM x 64 pieces of it, and walks the
-// reduction BK at a time through two LDS buffers: while one is multiplied the
-// next lands in the other, one barrier a step.  The product is formed transposed
+// reduction BK at a time through two or more LDS buffers: while one is multiplied the
+// next ones land in the others, one barrier a step.  The product is formed transposed
 // (the MFMA's first operand is B), so that a lane ends up with consecutive
 // columns of one row: with the columns of a 64-wide piece dealt out as q = 16 t
 // + 4 j + i (lane group t, MFMA j, accumulator register i), sixteen of them, and
@@ -57,14 +57,15 @@ struct TileArgs {
 enum TileShape { TILE_LARGE, TILE_TWO, TILE_MEDIUM, TILE_SMALL, TILE_SHAPES };
 struct TileInfo {
   int bm, bn, threads, bk;
+  int nb;  // LDS buffers of BK terms (direct operands; others take two)
 };
 template <typename T>
 constexpr TileInfo tile_info(int shape) {
   constexpr bool f32 = sizeof(T) == 4;
-  return shape == TILE_LARGE    ? TileInfo{256, f32 ? 128 : 256, 512, f32 ? 32 : 64}
-         : shape == TILE_TWO    ? (f32 ? TileInfo{128, 64, 256, 32} : TileInfo{256, 128, 256, 32})
-         : shape == TILE_MEDIUM ? TileInfo{128, 128, f32 ? 512 : 256, f32 ? 32 : 64}
-                                : TileInfo{64, 64, 256, f32 ? 32 : 64};
+  return shape == TILE_LARGE    ? (f32 ? TileInfo{256, 128, 512, 32, 2} : TileInfo{256, 256, 512, 64, 2})
+         : shape == TILE_TWO    ? (f32 ? TileInfo{128, 64, 256, 32, 2} : TileInfo{256, 128, 256, 32, 2})
+         : shape == TILE_MEDIUM ? (f32 ? TileInfo{128, 128, 512, 32, 2} : TileInfo{128, 128, 256, 64, 2})
+                                : (f32 ? TileInfo{64, 64, 256, 32, 2} : TileInfo{64, 64, 256, 64, 2});
 }
 
 // Enqueue the tile kernel for fp32 or bf16 operands (dense_f32.hip, dense_bf16.hip).
@@ -95,8 +96,14 @@ __device__ __forceinline__ int col_xor(int k) {
 __device__ __forceinline__ void dt_barrier() {
   asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
 }
-// All of this wave's vector memory operations are done.
-__device__ __forceinline__ void dt_wait_vm() { __builtin_amdgcn_s_waitcnt(0x0F70); }
+// At most N of this wave's vector memory operations are outstanding (they complete
+// in order; the compiler adds none of its own to the loop that counts them, which
+// must not spill).
+template <int N>
+__device__ __forceinline__ void dt_wait_vm() {
+  static_assert(N < 64, "vmcnt range");
+  asm volatile("s_waitcnt vmcnt(%0)" ::"n"(N) : "memory");
+}
 
 // s3_split8 with the differences as subtractions: the dot products that it forms
 // them with are one instruction where these are two, but issue at a quarter of the
@@ -128,9 +135,9 @@ __device__ __forceinline__ void dt_lds_load16(dt_sv4 rsrc, uint32_t off, uint32_
 constexpr uint32_t kPastEnd = 0x80000000u;  // of any resource
 __device__ __forceinline__ dt_sv4 dt_rsrc(const char* p, int64_t bytes) {
   const uint64_t a = (uint64_t)(uintptr_t)p;
-  const int64_t most = 0x7ffffff0;
+  const int64_t most = 0x7ffffff0;  // below kPastEnd; an end before p leaves nothing in range
   return dt_sv4{(int32_t)(uint32_t)a, (int32_t)((a >> 32) & 0xffffu),
-                (int32_t)(bytes < most ? bytes : most), 0x00020000};
+                (int32_t)(bytes < 0 ? 0 : bytes < most ? bytes : most), 0x00020000};
 }
 
 // Row and column of tile i: groups of eight rows of tiles, so that the tiles an XCD
@@ -145,7 +152,7 @@ __host__ __device__ __forceinline__ TilePos tile_pos(int ntm, int ntn, uint32_t 
   return TilePos{(int)(group * 8 + (j - n * rows)), (int)n};
 }
 
-template <typename T, int BM, int BN, int WGM, int BK, bool ARS, bool BRS, bool GLU, bool DIRECT>
+template <typename T, int BM, int BN, int WGM, int BK, int BUFS, bool ARS, bool BRS, bool GLU, bool DIRECT>
 __global__ __launch_bounds__(64 * WGM * (BN / 64), 2) void k_dense_tile(TileArgs t) {
   constexpr bool F32 = sizeof(T) == 4;
   static_assert(!(F32 && DIRECT), "fp32 operands are split in registers");
@@ -156,10 +163,10 @@ __global__ __launch_bounds__(64 * WGM * (BN / 64), 2) void k_dense_tile(TileArgs
   constexpr int ITA = CA / NTHR, ITB = CB / NTHR, IT = ITA + ITB;
   static_assert(CA % NTHR == 0 && CB % NTHR == 0 && TM % 16 == 0, "whole vectors per thread");
   static_assert(!GLU || (!ARS && BRS), "the gated layer is a forward product");
-  constexpr int STAGE = PARTS * (CA + CB);
+  constexpr int STAGE = PARTS * (CA + CB), NB = DIRECT ? BUFS : 2;
   // the epilogue's pieces: ROWS rows of 64 sums per wave at a time
   constexpr int ROWS = TM < 64 ? TM : 64, EPI = WGM * WGN * ROWS * 16;
-  __shared__ __attribute__((aligned(16))) s3_v4u lds[2 * STAGE > EPI ? 2 * STAGE : EPI];
+  __shared__ __attribute__((aligned(16))) s3_v4u lds[NB * STAGE > EPI ? NB * STAGE : EPI];
 
   const int n = t.epi.n;
 
@@ -236,27 +243,30 @@ __global__ __launch_bounds__(64 * WGM * (BN / 64), 2) void k_dense_tile(TileArgs
   const int64_t bstep = (BRS ? BK * t.ldb : BK) * sizeof(T);
   const int64_t asize = (ARS ? t.R : t.P) * t.lda, bsize = (BRS ? t.R : (int64_t)t.Q) * t.ldb;
 
-  // Direct: start the loads of step ks into buffer s.
+  // Direct: start the loads of vectors from .. to of step ks into the buffer at vector
+  // `buf`.  (Of steps past the last: nothing is read, zeros are stored; so a wave's
+  // count of loads is known.)
   const uint32_t lds0 = __builtin_amdgcn_readfirstlane((uint32_t)(uintptr_t)(dt_lptr)lds);
-  auto issue = [&](int ks, int s) __attribute__((always_inline)) {
+  auto issue = [&](int ks, int buf, int from, int to) __attribute__((always_inline)) {
     const char* pa = abase + ks * astep;
     const char* pb = bbase + ks * bstep;
     const dt_sv4 ra = dt_rsrc(pa, (const char*)t.a + asize * (int64_t)sizeof(T) - pa);
     const dt_sv4 rb = dt_rsrc(pb, (const char*)t.b + bsize * (int64_t)sizeof(T) - pb);
     const int64_t left = r1 - r0 - (int64_t)ks * BK;
 #pragma unroll
-    for (int i = 0; i < IT; ++i) {
+    for (int i = from; i < to; ++i) {
       const bool isa = i < ITA;
       const uint32_t o = cnt[i] > 0 && kof[i] < left ? off[i] * 2 : kPastEnd;
       const uint32_t at = (isa ? i : i - ITA) * NTHR + wave * 64 + (isa ? 0 : CA);
-      dt_lds_load16(isa ? ra : rb, o, lds0 + (s * STAGE + at) * 16);
+      dt_lds_load16(isa ? ra : rb, o, lds0 + (buf + at) * 16);
     }
   };
 
   // Through registers: load vectors from .. to of step ks, then split and store them
-  // to buffer s.  The first `plain` steps read whole vectors: what such a vector holds
-  // of a column past the end goes to sums that are dropped, and lies inside the
-  // operand as long as its last line is not read or the tile has no such column.
+  // to the buffer at vector `buf`.  The first `plain` steps read whole vectors: what
+  // such a vector holds of a column past the end goes to sums that are dropped, and lies
+  // inside the operand as long as its last lines are not read or the tile has no such
+  // column.
   s3_v4u reg[IT][F32 ? 2 : 1];
   int plain = 0;
   if constexpr (!DIRECT) {
@@ -264,7 +274,9 @@ __global__ __launch_bounds__(64 * WGM * (BN / 64), 2) void k_dense_tile(TileArgs
 #pragma unroll
     for (int i = 0; i < IT; ++i) whole = whole && (cnt[i] == 8 || cnt[i] == 0);
     whole = __syncthreads_and(whole);
-    plain = (int)(((whole ? r1 : r1 < t.R ? r1 : t.R - 1) - r0) / BK);
+    const int64_t la = ARS ? (t.lda + 7) / t.lda : 0, lb = BRS ? (t.ldb + 7) / t.ldb : 0;
+    const int64_t end = t.R - (la > lb ? la : lb);  // lines that a vector leaves room behind
+    plain = (int)(((whole || r1 < end ? r1 : end) - r0) / BK);
   }
   auto fetch_plain = [&](int ks, int from, int to) __attribute__((always_inline)) {
     const char* pa = abase + ks * astep;
@@ -329,11 +341,11 @@ __global__ __launch_bounds__(64 * WGM * (BN / 64), 2) void k_dense_tile(TileArgs
     if (ks < plain) fetch_plain(ks, 0, IT);
     else fetch_tail(ks);
   };
-  auto stash = [&](int s, int from, int to) __attribute__((always_inline)) {
+  auto stash = [&](int buf, int from, int to) __attribute__((always_inline)) {
 #pragma unroll
     for (int i = from; i < to; ++i) {
       const bool isa = i < ITA;
-      const int c = s * STAGE + (isa ? i : i - ITA) * NTHR + tid + (isa ? 0 : PARTS * CA);
+      const int c = buf + (isa ? i : i - ITA) * NTHR + tid + (isa ? 0 : PARTS * CA);
       if constexpr (F32) {
         const Split8 p = dt_split8(__builtin_bit_cast(s3_v4f, reg[i][0]),
                                    __builtin_bit_cast(s3_v4f, reg[i][F32]));
@@ -360,8 +372,8 @@ __global__ __launch_bounds__(64 * WGM * (BN / 64), 2) void k_dense_tile(TileArgs
         s3_v2u, __builtin_amdgcn_ds_read_tr16_b64_v4i16((dt_lds_v4s*)(a + 4 * line)));
     return s3_v4u{lo[0], lo[1], hi[0], hi[1]};
   };
-  auto frag_a = [&](int s, int part, int kk, int mi) __attribute__((always_inline)) {
-    const s3_v4u* base = lds + s * STAGE + part * CA;
+  auto frag_a = [&](int buf, int part, int kk, int mi) __attribute__((always_inline)) {
+    const s3_v4u* base = lds + buf + part * CA;
     if constexpr (!ARS) {
       const int row = wm * TM + mi * 16 + li;
       return base[row * CK + ((kk * 4 + q) ^ row_xor<CK>(li))];
@@ -373,8 +385,8 @@ __global__ __launch_bounds__(64 * WGM * (BN / 64), 2) void k_dense_tile(TileArgs
                 CR * 16);
     }
   };
-  auto frag_b = [&](int s, int part, int kk, int ni) __attribute__((always_inline)) {
-    const s3_v4u* base = lds + s * STAGE + PARTS * CA + part * CB;
+  auto frag_b = [&](int buf, int part, int kk, int ni) __attribute__((always_inline)) {
+    const s3_v4u* base = lds + buf + PARTS * CA + part * CB;
     if constexpr (!BRS) {
       const int row = wn * TN + ni * 16 + li;
       return base[row * CK + ((kk * 4 + q) ^ row_xor<CK>(li))];
@@ -442,21 +454,21 @@ __global__ __launch_bounds__(64 * WGM * (BN / 64), 2) void k_dense_tile(TileArgs
     };
     static_assert(IT == 3, "a vector for each of the units ahead of the barrier");
     // Step ks.  ahead(i): load vector i of step ks + 2, right behind its place's use.
-    auto step = [&](int s, auto&& ahead) __attribute__((always_inline)) {
+    auto step = [&](int s, int nx, auto&& ahead) __attribute__((always_inline)) {
       read2b(s, 2);
-      stash(s ^ 1, 0, 1);
+      stash(nx, 0, 1);
       ahead(0);
       multiply(0, 0);
       read2a(s, 2);
-      stash(s ^ 1, 1, 2);
+      stash(nx, 1, 2);
       ahead(1);
       multiply(0, 2);
-      stash(s ^ 1, 2, 3);
+      stash(nx, 2, 3);
       ahead(2);
       multiply(2, 0);
       dt_barrier();  // step ks + 1 is in LDS, and step ks in registers
-      read2a(s ^ 1, 0);  // (of the last step: what lies there, never used)
-      read2b(s ^ 1, 0);
+      read2a(nx, 0);  // (of the last step: what lies there, never used)
+      read2b(nx, 0);
       multiply(2, 2);
     };
     fetch(0);
@@ -468,18 +480,24 @@ __global__ __launch_bounds__(64 * WGM * (BN / 64), 2) void k_dense_tile(TileArgs
     int ks = 0;
     // no branch between the loads, so that each is waited for by itself
     for (; ks + 2 < plain; ++ks)
-      step(ks & 1, [&](int i) __attribute__((always_inline)) { fetch_plain(ks + 2, i, i + 1); });
+      step((ks & 1) * STAGE, (~ks & 1) * STAGE, [&](int i) __attribute__((always_inline)) { fetch_plain(ks + 2, i, i + 1); });
 #pragma unroll 1
     for (; ks < nk; ++ks) {
-      step(ks & 1, [](int) {});
+      step((ks & 1) * STAGE, (~ks & 1) * STAGE, [](int) {});
       if (ks + 2 < nk) fetch(ks + 2);
     }
   } else {
+  // Loads are started LP a unit from the barrier on, so that no wave stands still
+  // while a whole step's worth of them finds its way into the memory pipeline (input
+  // gradient, 256x256 tiles: 1493 TFLOP/s, all at once 1430).  The small tile's few
+  // steps wait for their arrival instead (alone on a CU 0.48 us a step, two a unit 0.6).
+  constexpr int LP = TM >= 128 ? 2 : MI >= 4 ? 4 : IT;
+  constexpr int AHEAD = LP * AD < IT ? LP * AD : IT;  // ahead of the next step's first unit
   if constexpr (DIRECT) {
-    issue(0, 0);
-    dt_wait_vm();
+#pragma unroll
+    for (int k = 0; k < NB; ++k) issue(k, k * STAGE, 0, k < NB - 1 ? IT : AHEAD);
+    dt_wait_vm<(NB - 2) * IT + AHEAD>();
     dt_barrier();
-    if (nk > 1) issue(1, 1);
   } else {
     fetch(0);
     stash(0, 0, IT);
@@ -489,26 +507,31 @@ __global__ __launch_bounds__(64 * WGM * (BN / 64), 2) void k_dense_tile(TileArgs
   read_b(b[0], 0, 0);
 #pragma unroll
   for (int u = 0; u < AD; ++u) read_a(a[u], 0, u);
+  int buf = 0, last = (NB - 1) * STAGE;  // buffers of steps ks and ks - 1
   for (int ks = 0; ks < nk; ++ks) {
-    const int s = ks & 1;
+    const int nx = buf == (NB - 1) * STAGE ? 0 : buf + STAGE;
 #pragma unroll
     for (int u = 0; u < NU; ++u) {
       constexpr int FREE = NU - AD;  // units ahead of the barrier
-      if (!DIRECT && FREE == 0 && u == 0) stash(s ^ 1, 0, IT);
+      if (!DIRECT && FREE == 0 && u == 0) stash(nx, 0, IT);
       if (u == FREE) {
         // this wave's part of step ks + 1 is in LDS, and it reads step ks no more
-        if (DIRECT) dt_wait_vm();
+        if (DIRECT) dt_wait_vm<(NB - 2) * IT>();
         dt_barrier();
-        if (ks + 2 < nk) {
-          if constexpr (DIRECT) issue(ks + 2, s);
-          else fetch(ks + 2);
-        }
+        if constexpr (!DIRECT)
+          if (ks + 2 < nk) fetch(ks + 2);
+      }
+      if constexpr (DIRECT) {
+        const int from = LP * (u < FREE ? u + AD : u - FREE);
+        if (from < IT)
+          issue(u < FREE ? ks - 1 + NB : ks + NB, u < FREE ? last : buf, from,
+                from + LP < IT ? from + LP : IT);
       }
       // (of the last step: what lies in the other buffer, never used)
-      read_a(a[AD], u + AD < NU ? s : s ^ 1, (u + AD) % NU);
-      if (u % MI == MI - AD) read_b(b[1], u / MI + 1 < KK ? s : s ^ 1, (u / MI + 1) % KK);
+      read_a(a[AD], u + AD < NU ? buf : nx, (u + AD) % NU);
+      if (u % MI == MI - AD) read_b(b[1], u / MI + 1 < KK ? buf : nx, (u / MI + 1) % KK);
       if (!DIRECT && u < FREE)
-        stash(s ^ 1, IT * u / (FREE ? FREE : 1), IT * (u + 1) / (FREE ? FREE : 1));
+        stash(nx, IT * u / (FREE ? FREE : 1), IT * (u + 1) / (FREE ? FREE : 1));
       if constexpr (F32) {
 #pragma unroll
         for (int x = 0; x < 6; ++x)
@@ -530,7 +553,10 @@ __global__ __launch_bounds__(64 * WGM * (BN / 64), 2) void k_dense_tile(TileArgs
 #pragma unroll
           for (int k = 0; k < PARTS; ++k) b[0][j][k] = b[1][j][k];
     }
+    last = buf;
+    buf = nx;
   }
+  if (DIRECT) dt_wait_vm<0>();  // nothing lands in LDS any more
   }
 
   // Epilogue: the wave's piece to LDS, ROWS rows at a time (16 vectors a row, XORed
@@ -614,7 +640,8 @@ __global__ __launch_bounds__(64 * WGM * (BN / 64), 2) void k_dense_tile(TileArgs
       }
     }
   }
-  dt_barrier();  // the next tile's operands go where the sums were
+  if (DIRECT) dt_wait_vm<0>();  // stores are not counted among the next tile's loads
+  dt_barrier();                 // whose operands go where the sums were
   }
 }
 
