@@ -578,8 +578,9 @@ oc_status oc_sgd(int64_t n, float* w, const float* g, float* v, float lr, float 
  *           is done), cin, cout 1 .. 65536.
  *   bias    dev f32 [cout] or NULL.  res dev [rows][cout] or NULL; may be y.
  *   y       dev [rows][cout].
- *   pre     dev [rows][cout] or NULL: receives x w + bias for the backward, in
- *           fp32; for OC_ACT_RELU in the type dt.
+ *   pre     dev or NULL: receives what the backward needs of x w + bias: f32
+ *           [rows][cout] itself; for OC_ACT_RELU u8 [rows][(cout + 7) / 8], bit k of
+ *           byte j being [x w + bias > 0] at column 8 j + k.
  *   ws      dev workspace of at least oc_dense_fwd_workspace() bytes (may be NULL
  *           when that is 0).
  * Buffers need the alignment of their elements only.  Deterministic: no
@@ -596,9 +597,10 @@ oc_status oc_dense_fwd(oc_dtype dt, int32_t act, int64_t rows, int32_t cin, int3
 /* Gradients of oc_dense_fwd: with dz = dy act'(x w + bias),
  *   dx = dz w^T, dw = x^T dz, dbias = the sum of dz over the rows
  * (the residual's gradient is dy itself).
- *   pre     what oc_dense_fwd left there; may be NULL for OC_ACT_NONE.  A ReLU's
- *           slope is [pre > 0], so the output y of a forward without a residual
- *           does as well.
+ *   pre     what oc_dense_fwd left there; not read for OC_ACT_NONE.
+ *   y       for OC_ACT_RELU, in place of pre (then NULL): dev [rows][cout], the
+ *           output of a forward without a residual, positive where x w + bias is;
+ *           otherwise not read.
  *   dy      dev [rows][cout] and dx dev [rows][cin] or NULL, of type dt.
  *   dw      dev [cin][cout] or NULL, of type dw_dt: OC_F32 or dt.
  *   dbias   dev f32 [cout] or NULL.
@@ -607,9 +609,9 @@ oc_status oc_dense_fwd(oc_dtype dt, int32_t act, int64_t rows, int32_t cin, int3
  * are 0. */
 size_t oc_dense_bwd_workspace(oc_dtype dt, int32_t act, int64_t rows, int32_t cin, int32_t cout);
 oc_status oc_dense_bwd(oc_dtype dt, int32_t act, int64_t rows, int32_t cin, int32_t cout,
-                       const void* x, const void* w, const void* pre, const void* dy, void* dx,
-                       oc_dtype dw_dt, void* dw, float* dbias, void* ws, size_t ws_bytes,
-                       hipStream_t stream);
+                       const void* x, const void* w, const void* pre, const void* y,
+                       const void* dy, void* dx, oc_dtype dw_dt, void* dw, float* dbias, void* ws,
+                       size_t ws_bytes, hipStream_t stream);
 
 /* Gated layer: both projections, the activation and the product in one kernel,
  *   y = act(g) u,  g = (x w + bias)[:, :cout],  u = (x w + bias)[:, cout:]

@@ -223,7 +223,7 @@ def load():
         "oc_dense_fwd_workspace": ([C.c_int, i64, i32, i32], sz),
         "oc_dense_fwd": ([C.c_int, i32, i64, i32, i32, p, p, p, p, p, p, p, sz, p], C.c_int),
         "oc_dense_bwd_workspace": ([C.c_int, i32, i64, i32, i32], sz),
-        "oc_dense_bwd": ([C.c_int, i32, i64, i32, i32, p, p, p, p, p, C.c_int, p, p, p, sz, p],
+        "oc_dense_bwd": ([C.c_int, i32, i64, i32, i32, p, p, p, p, p, p, C.c_int, p, p, p, sz, p],
                          C.c_int),
         "oc_glu_fwd_workspace": ([C.c_int, i64, i32, i32], sz),
         "oc_glu_fwd": ([C.c_int, i32, i64, i32, i32, p, p, p, p, p, p, sz, p], C.c_int),
@@ -914,6 +914,13 @@ def _dense_dims(x, w, halves):
     return torch._C._cuda_getDevice(), rows, cin, nz // halves, nz
 
 
+def _pre_kind(glu, act, rows, nz):
+    """dtype and shape of what a forward keeps for its backward."""
+    if act == OC_ACT_RELU and not glu:
+        return torch.uint8, (rows, (nz + 7) // 8)
+    return torch.float32, (rows, nz)
+
+
 def _layer_fwd(glu, x, w, b, res, act, need_pre):
     dev, rows, cin, cout, nz = _dense_dims(x, w, 2 if glu else 1)
     L, t, dt = load(), x.dtype, _dtype_code(x)
@@ -923,8 +930,8 @@ def _layer_fwd(glu, x, w, b, res, act, need_pre):
     y = torch.empty((rows, cout), dtype=t, device=x.device)
     pre = None
     if need_pre:
-        pre = torch.empty((rows, nz), device=x.device,
-                          dtype=t if act == OC_ACT_RELU and not glu else torch.float32)
+        pt, pshape = _pre_kind(glu, act, rows, nz)
+        pre = torch.empty(pshape, dtype=pt, device=x.device)
     pp = pre.data_ptr() if need_pre else None
     need = (L.oc_glu_fwd_workspace if glu else L.oc_dense_fwd_workspace)(dt, rows, cin, cout)
     ws = torch.empty(need, dtype=torch.uint8, device=x.device) if need else None
@@ -943,7 +950,11 @@ def _layer_bwd(glu, x, w, dy, pre, act, need_dx, need_dw, need_db, dw, db, dw_dt
     L, t, dt = load(), x.dtype, _dtype_code(x)
     xp, wp = _given(x, "x", dev, t, (rows, cin)), _given(w, "w", dev, t, (cin, nz))
     dyp = _given(dy, "dy", dev, t, (rows, cout))
-    pp = _given(pre, "pre", dev, t if act == OC_ACT_RELU and not glu else torch.float32, (rows, nz))
+    pp = yp = None
+    if pre is not None and act == OC_ACT_RELU and not glu and pre.dtype is t:
+        yp = _given(pre, "pre", dev, t, (rows, nz))  # the forward's output
+    else:
+        pp = _given(pre, "pre", dev, *_pre_kind(glu, act, rows, nz))
     dx = torch.empty((rows, cin), dtype=t, device=x.device) if need_dx else None
     if dw is None and need_dw:
         dw = torch.empty((cin, nz), dtype=dw_dtype or torch.float32, device=x.device)
@@ -953,16 +964,17 @@ def _layer_bwd(glu, x, w, dy, pre, act, need_dx, need_dw, need_db, dw, db, dw_dt
     need = (L.oc_glu_bwd_workspace(dt, rows, cin, cout) if glu
             else L.oc_dense_bwd_workspace(dt, act, rows, cin, cout))
     ws = torch.empty(need, dtype=torch.uint8, device=x.device)
+    saved = (pp,) if glu else (pp, yp)
     f = L.oc_glu_bwd if glu else L.oc_dense_bwd
-    _check(f(dt, act, rows, cin, cout, xp, wp, pp, dyp, dx.data_ptr() if need_dx else None, dw_dt,
-             _given(dw, "dw", dev, dw.dtype if dw is not None else t, (cin, nz)),
+    _check(f(dt, act, rows, cin, cout, xp, wp, *saved, dyp, dx.data_ptr() if need_dx else None,
+             dw_dt, _given(dw, "dw", dev, dw.dtype if dw is not None else t, (cin, nz)),
              _given(db, "db", dev, torch.float32, (nz,)), ws.data_ptr(), need, _stream()))
     return dx, dw, db
 
 
 def oc_dense_fwd(x, w, b=None, res=None, act=OC_ACT_NONE, need_pre=False):
-    """y = act(x w + b) + res over the rows of x: (y, pre), pre the values ahead of
-    the activation for the backward (fp32; of x's dtype for OC_ACT_RELU) or None.
+    """y = act(x w + b) + res over the rows of x: (y, pre), pre what the backward needs
+    of x w + b (its values, float32; for OC_ACT_RELU their signs, one bit each) or None.
     x, w, res and y share a dtype (float32 or bfloat16); b is float32."""
     return _layer_fwd(False, x, w, b, res, act, need_pre)
 
@@ -970,7 +982,7 @@ def oc_dense_fwd(x, w, b=None, res=None, act=OC_ACT_NONE, need_pre=False):
 def oc_dense_bwd(x, w, dy, act=OC_ACT_NONE, pre=None, need_dx=True, need_dw=True, need_db=True,
                  dw=None, db=None, dw_dtype=None):
     """(dx, dw, db) of oc_dense_fwd (None where not needed).  pre: as the forward
-    returned it; for OC_ACT_RELU without a residual y does as well.  dw, db:
+    returned it; for OC_ACT_RELU the y of a forward without a residual does as well.  dw, db:
     optional caller tensors to write into; a new dw is of dw_dtype (float32 if
     not given, or x's dtype)."""
     return _layer_bwd(False, x, w, dy, pre, act, need_dx, need_dw, need_db, dw, db, dw_dtype)

@@ -16,12 +16,12 @@ typedef d_v4u d_v4u_any __attribute__((aligned(2)));
 // What becomes of the product z [M][nz] (nz = n, or 2 n when glu):
 //   glu 0: y[m][c] = act(z[m][c] + bias[c]) + res[m][c]
 //   glu 1: y[m][c] = act(z[m][c] + bias[c]) (z[m][n + c] + bias[n + c])
-// pre (if any) receives z + bias.  y and res are bf16 when y_bf16, pre when
-// pre_bf16, else fp32.  A residual may be y itself: a lane reads its elements
-// before it writes them.
+// pre (if any) receives z + bias in fp32, or with pre_bits the bits [z + bias > 0],
+// eight columns a byte, (n + 7) / 8 bytes a row.  y and res are bf16 when y_bf16, else
+// fp32.  A residual may be y itself: a lane reads its elements before it writes them.
 struct Epi {
   int32_t act, glu, n;
-  int32_t y_bf16, pre_bf16;
+  int32_t y_bf16, pre_bits;
   const float* bias;
   const void* res;
   void* y;
@@ -229,8 +229,15 @@ __device__ __forceinline__ void epilogue(const Epi& e, const int64_t (&m)[U], in
     for (int i = 0; i < U; ++i)
       if (m[i] < M) {
         const int64_t at = m[i] * (GLU ? 2 : 1) * e.n + c;
-        store8n(e.pre, e.pre_bf16, at, cnt, z[i]);
-        if (GLU) store8n(e.pre, e.pre_bf16, at + e.n, cnt, u[i]);
+        if (!GLU && e.pre_bits) {
+          uint32_t bits = 0;
+#pragma unroll
+          for (int k = 0; k < 8; ++k) bits |= (z[i][k] > 0.f ? 1u : 0u) << k;
+          ((uint8_t*)e.pre)[m[i] * ((e.n + 7) / 8) + c / 8] = (uint8_t)bits;
+        } else {
+          store8n(e.pre, false, at, cnt, z[i]);
+          if (GLU) store8n(e.pre, false, at + e.n, cnt, u[i]);
+        }
       }
   }
   if (e.act == OC_ACT_RELU) {

@@ -44,10 +44,12 @@ DzShape dz_shape(int64_t M, int n) {
 
 // glu 0: z, dz [M][n]; 1: z, dz [M][2 n].  dz has rows of ld elements, those past the
 // columns zero (bf16 rows padded to whole vectors); NULL: column sums only (dz = dy).
-template <bool GLU, int ACT>
-__global__ __launch_bounds__(TB) void k_dz(const void* dy, const void* z, bool bf16, bool z_bf16,
-                                           int64_t M, int n, int ct, void* dz, int64_t ld,
-                                           float* part) {
+// A ReLU's slope comes from the forward's bits (Z_BITS) or from its output, of dy's type
+// (Z_OUT); the others' from z.
+enum { Z_F32, Z_OUT, Z_BITS };
+template <bool GLU, int ACT, int Z>
+__global__ __launch_bounds__(TB) void k_dz(const void* dy, const void* z, bool bf16, int64_t M,
+                                           int n, int ct, void* dz, int64_t ld, float* part) {
   __shared__ float red[GLU ? 2 : 1][8][TB];
   constexpr int U = 2;  // rows whose loads are in flight together
   const int tid = threadIdx.x, tc = tid % ct, tr = tid / ct, rl = TB / ct;
@@ -66,8 +68,12 @@ __global__ __launch_bounds__(TB) void k_dz(const void* dy, const void* z, bool b
         if (GLU) {
           oc::load8n(z, false, m * 2 * n + c, cnt, M * 2 * n, v[i]);
           oc::load8n(z, false, m * 2 * n + n + c, cnt, M * 2 * n, u[i]);
+        } else if (Z == Z_BITS) {
+          const uint32_t bits = ((const uint8_t*)z)[m * ((n + 7) / 8) + c / 8];
+#pragma unroll
+          for (int k = 0; k < 8; ++k) v[i][k] = bits >> k & 1 ? 1.f : 0.f;
         } else if (ACT != OC_ACT_NONE) {
-          oc::load8n(z, z_bf16, m * n + c, cnt, M * n, v[i]);
+          oc::load8n(z, Z == Z_OUT && bf16, m * n + c, cnt, M * n, v[i]);
         }
       }
 #pragma unroll
@@ -238,7 +244,7 @@ oc_status fwd(const char* who, bool glu, oc_dtype dt, int32_t act, int64_t rows,
   st = check_ws(who, ws, ws_bytes, o.total);
   if (st != OC_OK) return st;
   const int32_t bf16 = dt == OC_BF16, nz = glu ? 2 * cout : cout;
-  const oc::Epi epi{act, glu, cout, bf16, bf16 && act == OC_ACT_RELU && !glu, bias, res, y, pre};
+  const oc::Epi epi{act, glu, cout, bf16, act == OC_ACT_RELU && !glu, bias, res, y, pre};
   if (oc::few_rows(dt, rows, cin, cout)) {
     oc::gemm_rows(dt, (int32_t)rows, cin, nz, x, w, epi, s);
     OC_LAUNCH_CHECK();
@@ -287,9 +293,9 @@ BwdWs bwd_ws(oc_dtype dt, int32_t act, int64_t rows, int32_t cin, int32_t cout, 
 }
 
 oc_status bwd(const char* who, bool glu, oc_dtype dt, int32_t act, int64_t rows, int32_t cin,
-              int32_t cout, const void* x, const void* w, const void* pre, const void* dy,
-              void* dx, oc_dtype dw_dt, void* dw, float* dbias, void* ws, size_t ws_bytes,
-              hipStream_t s) {
+              int32_t cout, const void* x, const void* w, const void* pre, const void* y,
+              const void* dy, void* dx, oc_dtype dw_dt, void* dw, float* dbias, void* ws,
+              size_t ws_bytes, hipStream_t s) {
   oc_status st = check(who, dt, act, glu, rows, cin, cout);
   if (st != OC_OK) return st;
   if (dw && dw_dt != OC_F32 && dw_dt != dt)
@@ -302,7 +308,9 @@ oc_status bwd(const char* who, bool glu, oc_dtype dt, int32_t act, int64_t rows,
     return OC_OK;
   }
   const bool slope = glu || act != OC_ACT_NONE;
-  if (!dy || (slope && !pre) || (dx && !w) || (dw && !x))
+  const bool from_y = !glu && act == OC_ACT_RELU && y;
+  if (pre && from_y) return oc::fail(OC_ERR_ARG, "%s: both pre and y", who);
+  if (!dy || (slope && !pre && !from_y) || (dx && !w) || (dw && !x))
     return oc::fail(OC_ERR_ARG, "%s: NULL buffer", who);
   if (!dx && !dw && !dbias) return OC_OK;
   const BwdWs o = bwd_ws(dt, act, rows, cin, cout, glu);
@@ -320,19 +328,20 @@ oc_status bwd(const char* who, bool glu, oc_dtype dt, int32_t act, int64_t rows,
     // the sums of a single block of rows are the result
     if (dbias && d.nb == 1) part = dbias;
     const auto run = [&](auto k) {
-      oc::launch(k, dim3(d.nb, d.kb), dim3(TB), 0, s, dy, pre, bf16,
-                 bf16 && act == OC_ACT_RELU && !glu, rows, cout, d.ct, out, ldz, part);
+      oc::launch(k, dim3(d.nb, d.kb), dim3(TB), 0, s, dy, from_y ? y : pre, bf16, rows, cout, d.ct,
+                 out, ldz, part);
     };
     if (glu) {
-      if (act == OC_ACT_NONE) run(k_dz<true, OC_ACT_NONE>);
-      else if (act == OC_ACT_RELU) run(k_dz<true, OC_ACT_RELU>);
-      else if (act == OC_ACT_SILU) run(k_dz<true, OC_ACT_SILU>);
-      else run(k_dz<true, OC_ACT_GELU>);
+      if (act == OC_ACT_NONE) run(k_dz<true, OC_ACT_NONE, Z_F32>);
+      else if (act == OC_ACT_RELU) run(k_dz<true, OC_ACT_RELU, Z_F32>);
+      else if (act == OC_ACT_SILU) run(k_dz<true, OC_ACT_SILU, Z_F32>);
+      else run(k_dz<true, OC_ACT_GELU, Z_F32>);
     } else {
-      if (act == OC_ACT_NONE) run(k_dz<false, OC_ACT_NONE>);
-      else if (act == OC_ACT_RELU) run(k_dz<false, OC_ACT_RELU>);
-      else if (act == OC_ACT_SILU) run(k_dz<false, OC_ACT_SILU>);
-      else run(k_dz<false, OC_ACT_GELU>);
+      if (act == OC_ACT_NONE) run(k_dz<false, OC_ACT_NONE, Z_F32>);
+      else if (from_y) run(k_dz<false, OC_ACT_RELU, Z_OUT>);
+      else if (act == OC_ACT_RELU) run(k_dz<false, OC_ACT_RELU, Z_BITS>);
+      else if (act == OC_ACT_SILU) run(k_dz<false, OC_ACT_SILU, Z_F32>);
+      else run(k_dz<false, OC_ACT_GELU, Z_F32>);
     }
     if (dbias && d.nb > 1)
       oc::launch(k_colsum, dim3((unsigned)cdiv(nz, 4)), dim3(TB), 0, s, (const float*)part, d.nb,
@@ -387,11 +396,11 @@ size_t oc_dense_bwd_workspace(oc_dtype dt, int32_t act, int64_t rows, int32_t ci
 }
 
 oc_status oc_dense_bwd(oc_dtype dt, int32_t act, int64_t rows, int32_t cin, int32_t cout,
-                       const void* x, const void* w, const void* pre, const void* dy, void* dx,
-                       oc_dtype dw_dt, void* dw, float* dbias, void* ws, size_t ws_bytes,
-                       hipStream_t s) {
-  return bwd("oc_dense_bwd", false, dt, act, rows, cin, cout, x, w, pre, dy, dx, dw_dt, dw, dbias,
-             ws, ws_bytes, s);
+                       const void* x, const void* w, const void* pre, const void* y,
+                       const void* dy, void* dx, oc_dtype dw_dt, void* dw, float* dbias, void* ws,
+                       size_t ws_bytes, hipStream_t s) {
+  return bwd("oc_dense_bwd", false, dt, act, rows, cin, cout, x, w, pre, y, dy, dx, dw_dt, dw,
+             dbias, ws, ws_bytes, s);
 }
 
 size_t oc_glu_fwd_workspace(oc_dtype dt, int64_t rows, int32_t cin, int32_t cout) {
@@ -414,8 +423,8 @@ oc_status oc_glu_bwd(oc_dtype dt, int32_t act, int64_t rows, int32_t cin, int32_
                      const void* x, const void* w, const float* pre, const void* dy, void* dx,
                      oc_dtype dw_dt, void* dw, float* dbias, void* ws, size_t ws_bytes,
                      hipStream_t s) {
-  return bwd("oc_glu_bwd", true, dt, act, rows, cin, cout, x, w, pre, dy, dx, dw_dt, dw, dbias, ws,
-             ws_bytes, s);
+  return bwd("oc_glu_bwd", true, dt, act, rows, cin, cout, x, w, pre, nullptr, dy, dx, dw_dt, dw,
+             dbias, ws, ws_bytes, s);
 }
 
 }  // extern "C"

@@ -92,10 +92,12 @@ def run_and_check(c, act, glu, dt, bwd=True, dw_dtype=None):
         yr, z = D.dense_fwd(x, w, b, _np(c["res"]), act)
         r = 0.0 if c["res"] is None else _abs(_np(c["res"]))
         ty = 1.13 * tz + 8 * U * (_abs(z) + r + _abs(yr))
-    pre_bf = not f32 and act == "relu" and not glu
-    check(pre, z, tz + (BF * _abs(z) if pre_bf else 0), "pre")
     check(y, yr, ty + rnd * (_abs(yr) + ty), "y")
-    if not pre_bf:
+    if act == "relu" and not glu:  # signs, eight columns a byte
+        bits = np.unpackbits(pre.cpu().numpy(), axis=1, bitorder="little")
+        np.testing.assert_array_equal(bits[:, :z.shape[1]], z > 0)
+    else:
+        check(pre, z, tz, "pre")
         check_norm(pre, z, np.sqrt(np.square(x) @ np.square(w)), cin, "pre")
     if not bwd:
         return
@@ -284,7 +286,7 @@ def test_what_is_behind_stays(rows, cin, cout, dt):
     ws2 = torch.full((int(L.oc_dense_bwd_workspace(code, 3, rows, cin, cout)) + 256,), 5,
                      dtype=torch.uint8, device="cuda")
     assert L.oc_dense_bwd(code, 3, rows, cin, cout, c["x"].data_ptr(), c["w"].data_ptr(),
-                          pre.data_ptr(), c["dy"].data_ptr(), dx.data_ptr(), 0, dw.data_ptr(),
+                          pre.data_ptr(), None, c["dy"].data_ptr(), dx.data_ptr(), 0, dw.data_ptr(),
                           db.data_ptr(), ws2.data_ptr(), ws2.numel() - 256, oc._stream()) == 0
     for buf, v in ((yb, y), (pb, pre), (dxb, dx), (dwb, dw), (dbb, db)):
         assert (buf[v.numel():] == 11.0).all()
@@ -403,9 +405,12 @@ def test_more_than_4_gib():
     y, pre = oc.oc_dense_fwd(c["x"], c["w"], c["b"], act=1, need_pre=True)
     at = torch.tensor([0, 1, 131071, 524287, 524288, 1048575, 1048576, rows - 1], device="cuda")
     z = c["x"][at].double() @ c["w"].double() + c["b"].double()
-    assert torch.equal(pre[at].double(), z) and torch.equal(y[at].double(), torch.relu(z))
-    del y
-    dx, dw, db = oc.oc_dense_bwd(c["x"], c["w"], c["dy"], act=1, pre=pre)
+    assert torch.equal(y[at].double(), torch.relu(z))
+    bit = torch.arange(cout, device="cuda")
+    assert torch.equal((pre[at][:, bit // 8] >> (bit % 8) & 1).bool(), z > 0)
+    dx, dw, db = oc.oc_dense_bwd(c["x"], c["w"], c["dy"], act=1, pre=y)
+    for p, q in zip(oc.oc_dense_bwd(c["x"], c["w"], c["dy"], act=1, pre=pre), (dx, dw, db)):
+        assert torch.equal(p, q)
     dz = c["dy"][at].double() * (z > 0)
     w = c["w"].double()
     tol = (cout + 4) * U * (dz.abs() @ w.abs().t())
@@ -414,7 +419,7 @@ def test_more_than_4_gib():
     dbr, S = torch.zeros(cout, dtype=torch.float64, device="cuda"), torch.zeros_like(dwr)
     for i in range(0, rows, 100_000):
         x, d = c["x"][i:i + 100_000].double(), c["dy"][i:i + 100_000].double()
-        d = d * (pre[i:i + 100_000] > 0)
+        d = d * (y[i:i + 100_000] > 0)
         dwr += x.t() @ d
         S += x.abs().t() @ d.abs()
         dbr += d.sum(0)
@@ -439,6 +444,9 @@ def test_refusals_of_tensors():
                  lambda: oc.oc_dense_fwd(c["x"], c["w"], act=7),
                  lambda: oc.oc_dense_fwd(c["x"].half(), c["w"].half()),
                  lambda: oc.oc_dense_bwd(c["x"], c["w"], c["dy"], act=2),
+                 lambda: oc.oc_dense_bwd(c["x"], c["w"], c["dy"], act=1),
+                 lambda: oc.oc_dense_bwd(c["x"], c["w"], c["dy"], act=2, pre=c["dy"].byte()),
+                 lambda: oc.oc_dense_bwd(c["x"], c["w"], c["dy"], act=1, pre=c["dy"].byte()),
                  lambda: oc.oc_dense_bwd(c["x"], c["w"], c["dy"][:2]),
                  lambda: oc.oc_dense_bwd(c["x"], c["w"], c["dy"], dw_dtype=torch.bfloat16),
                  lambda: oc.oc_glu_fwd(c["x"], c["w"][:, :15].contiguous()),

@@ -106,9 +106,11 @@ def test_dense_refusals():
         assert L.oc_dense_fwd_workspace(*bad) == 0
         assert L.oc_dense_bwd_workspace(bad[0], 0, *bad[1:]) == 0
 
-    def bwd(dt=0, act=2, rows=4, pre=P, dy=P, dx=P, dw_dt=0, dw=P, db=P, x=P, w=P, ws=P, n=1 << 30):
-        return L.oc_dense_bwd(dt, act, rows, 3, 5, x, w, pre, dy, dx, dw_dt, dw, db, ws, n, None)
+    def bwd(dt=0, act=2, rows=4, pre=P, y=None, dy=P, dx=P, dw_dt=0, dw=P, db=P, x=P, w=P, ws=P,
+            n=1 << 30):
+        return L.oc_dense_bwd(dt, act, rows, 3, 5, x, w, pre, y, dy, dx, dw_dt, dw, db, ws, n, None)
 
+    assert bwd(act=1, y=P) == 1 and bwd(act=1, pre=None) == 1 and bwd(pre=None, y=P) == 1
     assert bwd(pre=None) == 1 and bwd(dy=None) == 1 and bwd(w=None) == 1 and bwd(x=None) == 1
     assert bwd(dw_dt=1) == 1 and bwd(dw_dt=7) == 1 and bwd(dt=1, dw_dt=7) == 1
     assert bwd(act=9) == 1 and bwd(rows=-2) == 1
