@@ -574,16 +574,22 @@ oc_status oc_sgd(int64_t n, float* w, const float* g, float* v, float lr, float 
  *           bias is fp32.  Sums are fp32; an OC_BF16 result is rounded once.
  *   act     OC_ACT_NONE, OC_ACT_RELU, OC_ACT_SILU (z / (1 + e^-z)) or
  *           OC_ACT_GELU (z Phi(z), Phi the normal distribution function).
- *   x       dev [rows][cin].  w dev [cin][cout].  rows 0 .. 2^31 - 1 (0: nothing
- *           is done), cin, cout 1 .. 65536.
+ *   x       dev [rows][cin].  w dev [cin][cout].  rows 0 .. 2^28 - 1 (0: nothing
+ *           is done), cin, cout 1 .. 65536; OC_ERR_UNSUPPORTED from 2^36 values of x
+ *           or y on (2^24 tiles of 64 x 64).
  *   bias    dev f32 [cout] or NULL.  res dev [rows][cout] or NULL; may be y.
  *   y       dev [rows][cout].
  *   pre     dev or NULL: receives what the backward needs of x w + bias: f32
  *           [rows][cout] itself; for OC_ACT_RELU u8 [rows][(cout + 7) / 8], bit k of
  *           byte j being [x w + bias > 0] at column 8 j + k.
- *   ws      dev workspace of at least oc_dense_fwd_workspace() bytes (may be NULL
- *           when that is 0).
- * Buffers need the alignment of their elements only.  Deterministic: no
+ *   ws      dev workspace of at least oc_dense_fwd_workspace() bytes, 16-byte
+ *           aligned (may be NULL when that is 0): partial sums of reductions split
+ *           across workgroups, added in a fixed order; for large OC_BF16 layers with
+ *           channel counts that are no multiples of 8, copies of x and w in padded
+ *           rows; in the backward dz and the partial sums of dbias.
+ * OC_F32 products are formed and their range is treated as in oc_conv_fwd (six bf16
+ * matrix products each; for up to 64 rows also plain fp32 ones).  Other buffers need
+ * the alignment of their elements only.  Deterministic: no
  * floating-point atomics. */
 #define OC_ACT_NONE 0
 #define OC_ACT_RELU 1
@@ -637,7 +643,7 @@ oc_status oc_glu_bwd(oc_dtype dt, int32_t act, int64_t rows, int32_t cin, int32_
  * value of n tensors, squares and sums in double.  Host arrays: grads (device
  * pointers), dts (OC_F32 or OC_BF16 each), counts (values each, 0 allowed); they
  * are read during the call.  ws: dev, at least oc_grad_workspace(n, counts)
- * bytes.  n 0: norm = 0. */
+ * bytes, 8-byte aligned.  n 0: norm = 0. */
 size_t oc_grad_workspace(int32_t n, const int64_t* counts);
 oc_status oc_grad_norm(int32_t n, const void* const* grads, const oc_dtype* dts,
                        const int64_t* counts, float* norm, void* ws, size_t ws_bytes,

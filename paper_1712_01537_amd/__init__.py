@@ -13,6 +13,7 @@ If ``liboc.so`` is missing or cannot be loaded, every entry point raises
 from __future__ import annotations
 
 import ctypes as C
+import functools
 import os
 
 import torch
@@ -914,6 +915,17 @@ def _dense_dims(x, w, halves):
     return torch._C._cuda_getDevice(), rows, cin, nz // halves, nz
 
 
+@functools.lru_cache(maxsize=1024)
+def _layer_ws(bwd, glu, dev, dt, act, rows, cin, cout):
+    """Workspace bytes of a call on device dev, a function of its sizes."""
+    L = load()
+    if glu:
+        return (L.oc_glu_bwd_workspace if bwd else L.oc_glu_fwd_workspace)(dt, rows, cin, cout)
+    if bwd:
+        return L.oc_dense_bwd_workspace(dt, act, rows, cin, cout)
+    return L.oc_dense_fwd_workspace(dt, rows, cin, cout)
+
+
 def _pre_kind(glu, act, rows, nz):
     """dtype and shape of what a forward keeps for its backward."""
     if act == OC_ACT_RELU and not glu:
@@ -933,7 +945,7 @@ def _layer_fwd(glu, x, w, b, res, act, need_pre):
         pt, pshape = _pre_kind(glu, act, rows, nz)
         pre = torch.empty(pshape, dtype=pt, device=x.device)
     pp = pre.data_ptr() if need_pre else None
-    need = (L.oc_glu_fwd_workspace if glu else L.oc_dense_fwd_workspace)(dt, rows, cin, cout)
+    need = _layer_ws(False, glu, dev, dt, act, rows, cin, cout)
     ws = torch.empty(need, dtype=torch.uint8, device=x.device) if need else None
     wsp = ws.data_ptr() if need else None
     if glu:
@@ -961,8 +973,7 @@ def _layer_bwd(glu, x, w, dy, pre, act, need_dx, need_dw, need_db, dw, db, dw_dt
     if db is None and need_db:
         db = torch.empty(nz, dtype=torch.float32, device=x.device)
     dw_dt = OC_F32 if dw is None else _dtype_code(dw)
-    need = (L.oc_glu_bwd_workspace(dt, rows, cin, cout) if glu
-            else L.oc_dense_bwd_workspace(dt, act, rows, cin, cout))
+    need = _layer_ws(True, glu, dev, dt, act, rows, cin, cout)
     ws = torch.empty(need, dtype=torch.uint8, device=x.device)
     saved = (pp,) if glu else (pp, yp)
     f = L.oc_glu_bwd if glu else L.oc_dense_bwd
@@ -1046,6 +1057,9 @@ def oc_grad_clip(grads, max_norm, outs=None):
         m, optrs, odts, ocounts = _grad_list(outs, "outs")
         if m != n or bytes(ocounts) != bytes(counts):
             raise OcError(1, "outs and grads differ in number or size")
+    written = [p for p, c in zip(optrs, counts) if c]
+    if len(set(written)) != len(written):
+        raise OcError(1, "a tensor is to be written twice")
     L = load()
     norm, ws, need = _grad_scratch(L, n, counts)
     _check(L.oc_grad_clip(n, ptrs, dts, counts, max_norm, optrs, odts, norm.data_ptr(),

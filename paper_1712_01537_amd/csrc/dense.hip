@@ -26,7 +26,8 @@ constexpr int TB = 256;
 // (b, k) has rows M b / nb .. and columns 8 ct k ..  Column sums: per thread
 // fp32 over its rows (about 30), then the row lanes in order through LDS into
 // part[b][column], then k_colsum in double over the blocks: a fixed order.
-// Bound by memory: dy and z read, dz written.
+// Bound by memory: dy and z read, dz written (65536 x 4096 bf16 ReLU from y 346 us, 4.4
+// TB/s; 32768 x 2816 bf16 gated 288 us, 4.5 TB/s).
 struct DzShape {
   int ct, rl, kb, nb;  // column threads, row lanes, column blocks, row blocks
 };
@@ -51,7 +52,7 @@ template <bool GLU, int ACT, int Z>
 __global__ __launch_bounds__(TB) void k_dz(const void* dy, const void* z, bool bf16, int64_t M,
                                            int n, int ct, void* dz, int64_t ld, float* part) {
   __shared__ float red[GLU ? 2 : 1][8][TB];
-  constexpr int U = 2;  // rows whose loads are in flight together
+  constexpr int U = GLU ? 2 : 4;  // rows whose loads are in flight together
   const int tid = threadIdx.x, tc = tid % ct, tr = tid / ct, rl = TB / ct;
   const int nb = gridDim.x, b = blockIdx.x;
   const int64_t r0 = M * b / nb, r1 = M * (b + 1) / nb;
@@ -142,8 +143,12 @@ __global__ __launch_bounds__(TB) void k_colsum(const float* part, int nb, int nz
 
 // --- arguments ---------------------------------------------------------------
 
-constexpr int64_t MOST_ROWS = (int64_t)1 << 31;
+constexpr int64_t MOST_ROWS = (int64_t)1 << 28;
 constexpr int32_t MOST_COLS = 1 << 16;
+// A launch has fewer than 2^32 threads: 64x64 tiles of the largest product.
+bool too_many_tiles(int64_t rows, int64_t cin, int64_t nz) {
+  return cdiv(rows, 64) * cdiv(std::max(cin, nz), 64) >= (int64_t)1 << 24;
+}
 
 oc_status check(const char* who, oc_dtype dt, int32_t act, bool glu, int64_t rows, int32_t cin,
                 int32_t cout) {
@@ -154,29 +159,36 @@ oc_status check(const char* who, oc_dtype dt, int32_t act, bool glu, int64_t row
   if (rows < 0 || rows >= MOST_ROWS || cin < 1 || cin > MOST_COLS || cout < 1 || cout > most)
     return oc::fail(OC_ERR_ARG, "%s: %lld rows, %d -> %d channels", who, (long long)rows, cin,
                     cout);
+  if (too_many_tiles(rows, cin, glu ? 2 * cout : cout))
+    return oc::fail(OC_ERR_UNSUPPORTED, "%s: %lld rows of %d -> %d channels are too many", who,
+                    (long long)rows, cin, cout);
   return OC_OK;
 }
 
 bool sizes_ok(oc_dtype dt, int64_t rows, int32_t cin, int32_t cout, bool glu) {
   return (dt == OC_F32 || dt == OC_BF16) && rows > 0 && rows < MOST_ROWS && cin >= 1 &&
-         cin <= MOST_COLS && cout >= 1 && cout <= (glu ? MOST_COLS / 2 : MOST_COLS);
+         cin <= MOST_COLS && cout >= 1 && cout <= (glu ? MOST_COLS / 2 : MOST_COLS) &&
+         !too_many_tiles(rows, cin, glu ? 2 * cout : cout);
 }
 
 oc_status check_ws(const char* who, const void* ws, size_t have, size_t need) {
   if (need && (!ws || have < need))
     return oc::fail(OC_ERR_ARG, "%s: workspace %zu bytes < %zu", who, ws ? have : 0, need);
+  if (need && (uintptr_t)ws % 16)
+    return oc::fail(OC_ERR_ARG, "%s: the workspace is not 16-byte aligned", who);
   return OC_OK;
 }
 
 // n values of the type set to zero (two bytes a thread: bf16 buffers are not
 // aligned to four).
 __global__ __launch_bounds__(TB) void k_zero16(uint16_t* p, int64_t n) {
-  const int64_t i = (int64_t)blockIdx.x * TB + threadIdx.x;
-  if (i < n) p[i] = 0;
+  for (int64_t i = (int64_t)blockIdx.x * TB + threadIdx.x; i < n; i += (int64_t)gridDim.x * TB)
+    p[i] = 0;
 }
 void zero(void* p, oc_dtype dt, int64_t n, hipStream_t s) {
   const int64_t halves = dt == OC_F32 ? 2 * n : n;
-  oc::launch(k_zero16, dim3((unsigned)cdiv(halves, TB)), dim3(TB), 0, s, (uint16_t*)p, halves);
+  oc::launch(k_zero16, dim3((unsigned)std::min<int64_t>(cdiv(halves, TB), 4096)), dim3(TB), 0, s,
+             (uint16_t*)p, halves);
 }
 
 // --- copies to rows of whole vectors ------------------------------------------

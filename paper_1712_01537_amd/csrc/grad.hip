@@ -205,6 +205,8 @@ oc_status check_ws(const char* who, int32_t n, const int64_t* counts, const void
   const size_t need = oc_grad_workspace(n, counts);
   if (!ws || have < need)
     return oc::fail(OC_ERR_ARG, "%s: workspace %zu bytes < %zu", who, ws ? have : 0, need);
+  if ((uintptr_t)ws % 8)
+    return oc::fail(OC_ERR_ARG, "%s: the workspace is not 8-byte aligned", who);
   return OC_OK;
 }
 

@@ -200,6 +200,55 @@ def test_large(i, dt, glu):
         assert far <= 64 * most, (what, far, most)
 
 
+@pytest.mark.parametrize("dt", ["f32", "bf16"])
+@pytest.mark.parametrize("rows,cin,cout,glu", [(70, 65536, 3, False), (70, 3, 65536, False),
+                                               (3, 65536, 5, False), (2, 5, 65536, False),
+                                               (9, 4, 32768, True), (1, 12, 32768, True)])
+def test_longest_rows(rows, cin, cout, glu, dt):
+    run_and_check(make(rows, cin, cout, dt, "silu", glu), "silu", glu, dt)
+
+
+@pytest.mark.parametrize("act", ["silu", "gelu"])
+@pytest.mark.parametrize("glu", [False, True])
+def test_gradients_against_differences(glu, act):
+    """Central differences of the kernels' own forward along random directions.
+    With h = 2^-7 a direction of unit mean square changes z by some h; the third
+    derivative's term is h^2 / 6 < 1.1e-5 of the slope's, a few times more where
+    products of two changes enter; fp32 outputs of size 1 are off by some 2^-23 each,
+    so a sum of n of them by 2^-23 sqrt(n), over 2 h 2^-17 sqrt(n), while a derivative
+    is of size sqrt(n): 1e-3 of the gradient's norm covers both."""
+    c = make(90, 40, 48, "f32", act, glu, res=False)
+    a, f = ACT[act], oc.oc_glu_fwd if glu else oc.oc_dense_fwd
+    _, pre = f(c["x"], c["w"], c["b"], act=a, need_pre=True)
+    grads = (oc.oc_glu_bwd(c["x"], c["w"], c["dy"], pre, act=a) if glu
+             else oc.oc_dense_bwd(c["x"], c["w"], c["dy"], act=a, pre=pre))
+    g = torch.Generator(device="cuda")
+    g.manual_seed(3)
+    h = 2.0 ** -7
+    for k, grad in zip("xwb", grads):
+        v = torch.empty_like(grad).normal_(generator=g)
+        scale = 1.0 if k != "w" else 40 ** -0.5
+        ends = []
+        for s in (h * scale, -h * scale):
+            t = {q: c[q] + s * v if q == k else c[q] for q in "xwb"}
+            ends.append(float((f(t["x"], t["w"], t["b"], act=a)[0].double() * c["dy"].double()).sum()))
+        num = (ends[0] - ends[1]) / (2 * h * scale)
+        want = float((grad.double() * v.double()).sum())
+        assert abs(num - want) <= 1e-3 * float(grad.double().norm()), (k, num, want)
+
+
+@pytest.mark.parametrize("dt", ["f32", "bf16"])
+def test_a_row_does_not_depend_on_the_others(dt):
+    """The same row among few, some and many: within the bounds of its own sums
+    (other kernels and orders), whatever the rest holds."""
+    c = make(700, 136, 72, dt, "gelu", False)
+    z = D.product(_np(c["x"]), _np(c["w"]), _np(c["b"]))
+    S = _abs(_np(c["x"])) @ _abs(_np(c["w"])) + _abs(_np(c["b"]))
+    for rows in (1, 3, 4, 5, 8, 9, 16, 17, 64, 65, 130, 700):
+        pre = oc.oc_dense_fwd(c["x"][:rows].contiguous(), c["w"], c["b"], act=3, need_pre=True)[1]
+        check(pre, z[:rows], (136 + 4) * U * S[:rows], rows)
+
+
 def _view(t, shift):
     """A contiguous copy of t whose first element is `shift` elements into its buffer."""
     buf = torch.full((t.numel() + 16,), 7.0, dtype=t.dtype, device=t.device)

@@ -136,6 +136,7 @@ def test_refusals_of_tensors():
     g = torch.ones(10, device="cuda")
     for call in (lambda: oc.oc_grad_norm([g.double()]), lambda: oc.oc_grad_norm([g[::2]]),
                  lambda: oc.oc_grad_clip([g], -1.0), lambda: oc.oc_grad_clip([g], math.nan),
+                 lambda: oc.oc_grad_clip([g, g], 1.0), lambda: oc.oc_grad_clip([g, g[:3]], 1.0),
                  lambda: oc.oc_grad_clip([g], 1.0, outs=[]),
                  lambda: oc.oc_grad_clip([g], 1.0, outs=[g[:5]]),
                  lambda: oc.oc_grad_clip([g], 1.0, outs=[g.to(torch.bfloat16)])):

@@ -97,11 +97,13 @@ def _fwd(dt=0, act=0, rows=4, cin=3, cout=5, x=P, w=P, y=P, ws=None, n=0):
 def test_dense_refusals():
     L = oc.load()
     for bad in (dict(dt=2), dict(dt=-1), dict(act=4), dict(act=-1), dict(rows=-1),
-                dict(rows=1 << 31), dict(cin=0), dict(cin=65537), dict(cout=0),
+                dict(rows=1 << 28), dict(cin=0), dict(cin=65537), dict(cout=0),
                 dict(cout=65537), dict(x=None), dict(w=None), dict(y=None)):
         assert _fwd(**bad) == 1, bad
         assert b"oc_dense_fwd" in L.oc_last_error()
     assert _fwd(rows=0, x=None, w=None, y=None) == 0  # nothing to do
+    assert _fwd(rows=1 << 24, cout=4096) == 5 and _fwd(rows=1 << 24, cin=4096) == 5
+    assert L.oc_dense_fwd_workspace(0, 1 << 24, 3, 4096) == 0
     for bad in ((2, 4, 3, 5), (0, 0, 3, 5), (0, 4, 0, 5), (0, 4, 3, 65537)):
         assert L.oc_dense_fwd_workspace(*bad) == 0
         assert L.oc_dense_bwd_workspace(bad[0], 0, *bad[1:]) == 0
@@ -115,6 +117,7 @@ def test_dense_refusals():
     assert bwd(dw_dt=1) == 1 and bwd(dw_dt=7) == 1 and bwd(dt=1, dw_dt=7) == 1
     assert bwd(act=9) == 1 and bwd(rows=-2) == 1
     need = L.oc_dense_bwd_workspace(0, 2, 4, 3, 5)
+    assert bwd(ws=C.c_void_p(264)) == 1 and b"aligned" in L.oc_last_error()
     assert need > 0 and bwd(n=need - 1) == 1 and bwd(ws=None) == 1
     assert b"workspace" in L.oc_last_error()
     assert bwd(dx=None, dw=None, db=None) == 0  # nothing asked for
@@ -154,7 +157,7 @@ def test_grad_refusals():
     assert clip(o=None) == 1 and clip(od=None) == 1
     assert clip(od=(C.c_int * 2)(1, 1)) == 1   # fp32 into bf16
     assert clip(od=(C.c_int * 2)(0, 0)) == 1   # in place, in another type
-    assert clip(ws=None) == 1 and clip(nb=need - 1) == 1
+    assert clip(ws=C.c_void_p(260)) == 1 and clip(ws=None) == 1 and clip(nb=need - 1) == 1
     assert L.oc_grad_norm(2, ptrs, dts, counts, None, P, need, None) == 1
     assert L.oc_grad_norm(2, ptrs, dts, counts, P, P, need - 1, None) == 1
     assert L.oc_grad_workspace(-1, counts) == 0 and L.oc_grad_workspace(1, None) == 0
