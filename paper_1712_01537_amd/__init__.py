@@ -1012,24 +1012,28 @@ def oc_glu_bwd(x, w, dy, pre, act=OC_ACT_SILU, need_dx=True, need_dw=True, need_
 
 
 def _grad_list(tensors, name):
-    """Number, and host arrays of the tensors' addresses, dtype codes and counts."""
+    """Number, and host arrays of the tensors' addresses, dtype codes and counts.
+    (Per tensor this is what a call costs on the host: one pass for each.)"""
     n = len(tensors)
-    for i, t in enumerate(tensors):
-        if not t.is_cuda:
-            raise OcError(1, f"{name}[{i}] must be a CUDA (HIP) tensor")
+    devs = {t.get_device() for t in tensors}
+    if -1 in devs:
+        raise OcError(1, f"{name} must be CUDA (HIP) tensors")
     dev = torch._C._cuda_getDevice()
-    if not all([t.get_device() == dev and t.is_contiguous() for t in tensors]):
-        raise OcError(1, f"{name} must be contiguous tensors on cuda:{dev}")
-    dts = [_GRAD_CODE.get(t.dtype, -1) for t in tensors]
-    if -1 in dts:
-        raise OcError(1, f"{name} must be float32 or bfloat16 tensors")
+    if not devs <= {dev}:
+        raise OcError(1, f"{name} must be on cuda:{dev}, the current device")
+    if False in [t.is_contiguous() for t in tensors]:
+        raise OcError(1, f"{name} must be contiguous")
+    try:
+        dts = [_GRAD_CODE[t.dtype] for t in tensors]
+    except KeyError:
+        raise OcError(1, f"{name} must be float32 or bfloat16 tensors") from None
     return (n, (C.c_void_p * n)(*[t.data_ptr() for t in tensors]), (C.c_int * n)(*dts),
             (C.c_int64 * n)(*[t.numel() for t in tensors]))
 
 
 def _grad_scratch(L, n, counts):
     """The norm and the workspace of a call."""
-    dev = torch.device("cuda", torch.cuda.current_device())
+    dev = torch.device("cuda", torch._C._cuda_getDevice())
     need = L.oc_grad_workspace(n, counts)
     return (torch.empty((), dtype=torch.float32, device=dev),
             torch.empty(need, dtype=torch.uint8, device=dev), need)
@@ -1057,9 +1061,10 @@ def oc_grad_clip(grads, max_norm, outs=None):
         m, optrs, odts, ocounts = _grad_list(outs, "outs")
         if m != n or bytes(ocounts) != bytes(counts):
             raise OcError(1, "outs and grads differ in number or size")
-    written = [p for p, c in zip(optrs, counts) if c]
-    if len(set(written)) != len(written):
-        raise OcError(1, "a tensor is to be written twice")
+    if len(set(optrs)) != n:  # (empty tensors may share an address)
+        written = [p for p, c in zip(optrs, counts) if c]
+        if len(set(written)) != len(written):
+            raise OcError(1, "a tensor is to be written twice")
     L = load()
     norm, ws, need = _grad_scratch(L, n, counts)
     _check(L.oc_grad_clip(n, ptrs, dts, counts, max_norm, optrs, odts, norm.data_ptr(),
