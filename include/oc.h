@@ -603,7 +603,10 @@ oc_status oc_dense_fwd(oc_dtype dt, int32_t act, int64_t rows, int32_t cin, int3
 /* Gradients of oc_dense_fwd: with dz = dy act'(x w + bias),
  *   dx = dz w^T, dw = x^T dz, dbias = the sum of dz over the rows
  * (the residual's gradient is dy itself).
- *   pre     what oc_dense_fwd left there; not read for OC_ACT_NONE.
+ *   pre     what oc_dense_fwd left there; not read for OC_ACT_NONE.  NULL: x w +
+ *           bias is formed once more, which needs no memory between the passes and
+ *           for few input channels and many values less time.
+ *   bias    the forward's; read only when x w + bias is formed once more.
  *   y       for OC_ACT_RELU, in place of pre (then NULL): dev [rows][cout], the
  *           output of a forward without a residual, positive where x w + bias is;
  *           otherwise not read.
@@ -615,9 +618,9 @@ oc_status oc_dense_fwd(oc_dtype dt, int32_t act, int64_t rows, int32_t cin, int3
  * are 0. */
 size_t oc_dense_bwd_workspace(oc_dtype dt, int32_t act, int64_t rows, int32_t cin, int32_t cout);
 oc_status oc_dense_bwd(oc_dtype dt, int32_t act, int64_t rows, int32_t cin, int32_t cout,
-                       const void* x, const void* w, const void* pre, const void* y,
-                       const void* dy, void* dx, oc_dtype dw_dt, void* dw, float* dbias, void* ws,
-                       size_t ws_bytes, hipStream_t stream);
+                       const void* x, const void* w, const float* bias, const void* pre,
+                       const void* y, const void* dy, void* dx, oc_dtype dw_dt, void* dw,
+                       float* dbias, void* ws, size_t ws_bytes, hipStream_t stream);
 
 /* Gated layer: both projections, the activation and the product in one kernel,
  *   y = act(g) u,  g = (x w + bias)[:, :cout],  u = (x w + bias)[:, cout:]
@@ -632,12 +635,12 @@ oc_status oc_glu_fwd(oc_dtype dt, int32_t act, int64_t rows, int32_t cin, int32_
                      void* ws, size_t ws_bytes, hipStream_t stream);
 
 /* Gradients of oc_glu_fwd: dz = [dy u act'(g) | dy act(g)] [rows][2 cout], then
- * dx, dw [cin][2 cout] and dbias [2 cout] as oc_dense_bwd. */
+ * dx, dw [cin][2 cout] and dbias [2 cout] as oc_dense_bwd, pre and bias likewise. */
 size_t oc_glu_bwd_workspace(oc_dtype dt, int64_t rows, int32_t cin, int32_t cout);
 oc_status oc_glu_bwd(oc_dtype dt, int32_t act, int64_t rows, int32_t cin, int32_t cout,
-                     const void* x, const void* w, const float* pre, const void* dy, void* dx,
-                     oc_dtype dw_dt, void* dw, float* dbias, void* ws, size_t ws_bytes,
-                     hipStream_t stream);
+                     const void* x, const void* w, const float* bias, const float* pre,
+                     const void* dy, void* dx, oc_dtype dw_dt, void* dw, float* dbias, void* ws,
+                     size_t ws_bytes, hipStream_t stream);
 
 /* norm (dev f32 scalar) = the square root of the sum of the squares of every
  * value of n tensors, squares and sums in double.  Host arrays: grads (device

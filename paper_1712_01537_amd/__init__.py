@@ -224,12 +224,12 @@ def load():
         "oc_dense_fwd_workspace": ([C.c_int, i64, i32, i32], sz),
         "oc_dense_fwd": ([C.c_int, i32, i64, i32, i32, p, p, p, p, p, p, p, sz, p], C.c_int),
         "oc_dense_bwd_workspace": ([C.c_int, i32, i64, i32, i32], sz),
-        "oc_dense_bwd": ([C.c_int, i32, i64, i32, i32, p, p, p, p, p, p, C.c_int, p, p, p, sz, p],
+        "oc_dense_bwd": ([C.c_int, i32, i64, i32, i32, p, p, p, p, p, p, p, C.c_int, p, p, p, sz, p],
                          C.c_int),
         "oc_glu_fwd_workspace": ([C.c_int, i64, i32, i32], sz),
         "oc_glu_fwd": ([C.c_int, i32, i64, i32, i32, p, p, p, p, p, p, sz, p], C.c_int),
         "oc_glu_bwd_workspace": ([C.c_int, i64, i32, i32], sz),
-        "oc_glu_bwd": ([C.c_int, i32, i64, i32, i32, p, p, p, p, p, C.c_int, p, p, p, sz, p],
+        "oc_glu_bwd": ([C.c_int, i32, i64, i32, i32, p, p, p, p, p, p, C.c_int, p, p, p, sz, p],
                        C.c_int),
         "oc_grad_workspace": ([i32, p], sz),
         "oc_grad_norm": ([i32, p, p, p, p, p, sz, p], C.c_int),
@@ -933,18 +933,45 @@ def _pre_kind(glu, act, rows, nz):
     return torch.float32, (rows, nz)
 
 
-def _layer_fwd(glu, x, w, b, res, act, need_pre):
+class Again:
+    """What a forward keeps where the backward is to form x w + b once more: the bias
+    b itself, which, like x and w, is not to change before the backward."""
+
+    def __init__(self, b):
+        self.b = b
+
+
+def _again(glu, act, dt, rows, cin, cout):
+    """Whether forming x w + b once more takes less time than keeping it: where the
+    kept values outgrow the last-level cache (256 MB) and the product is short.
+    Forward and backward, kept and formed again, us:
+      bf16 gated: 32768 x 64 -> 2 x 1024 296, 193; 65536 x 256 -> 2 x 2048 1174, 980;
+      bf16 GELU: 65536 x 64 -> 2048 587, 542; x 128 -> 4096 1148, 1105; x 256 -> 4096
+      1240, 1297; 35472 x 256 -> 1024 (145 MB) 229, 243;
+      fp32: gated 46295 x 64 -> 2 x 3552 1994, 1892, from 128 channels 2408, 2501;
+      GELU 65536 x 64 -> 4096 1883, 1782, from 128 channels 2199, 2276.
+    Rows off 16 bytes are kept (bf16 17505 x 32 -> 2 x 839: 168, 210)."""
+    most = 64 if dt == OC_F32 else 256 if glu else 128
+    kept = 4 * rows * cout * (2 if glu else 1)
+    return ((glu or act in (OC_ACT_SILU, OC_ACT_GELU)) and kept >= 256 << 20
+            and cin <= most and cin % 8 == 0 and cout % 8 == 0)
+
+
+def _layer_fwd(glu, x, w, b, res, act, need_pre, again):
     dev, rows, cin, cout, nz = _dense_dims(x, w, 2 if glu else 1)
     L, t, dt = load(), x.dtype, _dtype_code(x)
     xp, wp = _given(x, "x", dev, t, (rows, cin)), _given(w, "w", dev, t, (cin, nz))
     bp = _given(b, "b", dev, torch.float32, (nz,))
     rp = _given(res, "res", dev, t, (rows, cout))
     y = torch.empty((rows, cout), dtype=t, device=x.device)
-    pre = None
+    pre = pp = None
     if need_pre:
-        pt, pshape = _pre_kind(glu, act, rows, nz)
-        pre = torch.empty(pshape, dtype=pt, device=x.device)
-    pp = pre.data_ptr() if need_pre else None
+        if _again(glu, act, dt, rows, cin, cout) if again is None else again:
+            pre = Again(b)
+        else:
+            pt, pshape = _pre_kind(glu, act, rows, nz)
+            pre = torch.empty(pshape, dtype=pt, device=x.device)
+            pp = pre.data_ptr()
     need = _layer_ws(False, glu, dev, dt, act, rows, cin, cout)
     ws = torch.empty(need, dtype=torch.uint8, device=x.device) if need else None
     wsp = ws.data_ptr() if need else None
@@ -962,8 +989,12 @@ def _layer_bwd(glu, x, w, dy, pre, act, need_dx, need_dw, need_db, dw, db, dw_dt
     L, t, dt = load(), x.dtype, _dtype_code(x)
     xp, wp = _given(x, "x", dev, t, (rows, cin)), _given(w, "w", dev, t, (cin, nz))
     dyp = _given(dy, "dy", dev, t, (rows, cout))
-    pp = yp = None
-    if pre is not None and act == OC_ACT_RELU and not glu and pre.dtype is t:
+    pp = yp = bp = None
+    if isinstance(pre, Again):
+        bp = _given(pre.b, "b", dev, torch.float32, (nz,))
+    elif pre is None and (glu or act != OC_ACT_NONE):
+        raise OcError(1, "the backward needs pre, as the forward returned it")
+    elif pre is not None and act == OC_ACT_RELU and not glu and pre.dtype is t:
         yp = _given(pre, "pre", dev, t, (rows, nz))  # the forward's output
     else:
         pp = _given(pre, "pre", dev, *_pre_kind(glu, act, rows, nz))
@@ -975,7 +1006,7 @@ def _layer_bwd(glu, x, w, dy, pre, act, need_dx, need_dw, need_db, dw, db, dw_dt
     dw_dt = OC_F32 if dw is None else _dtype_code(dw)
     need = _layer_ws(True, glu, dev, dt, act, rows, cin, cout)
     ws = torch.empty(need, dtype=torch.uint8, device=x.device)
-    saved = (pp,) if glu else (pp, yp)
+    saved = (bp, pp) if glu else (bp, pp, yp)
     f = L.oc_glu_bwd if glu else L.oc_dense_bwd
     _check(f(dt, act, rows, cin, cout, xp, wp, *saved, dyp, dx.data_ptr() if need_dx else None,
              dw_dt, _given(dw, "dw", dev, dw.dtype if dw is not None else t, (cin, nz)),
@@ -983,26 +1014,28 @@ def _layer_bwd(glu, x, w, dy, pre, act, need_dx, need_dw, need_db, dw, db, dw_dt
     return dx, dw, db
 
 
-def oc_dense_fwd(x, w, b=None, res=None, act=OC_ACT_NONE, need_pre=False):
+def oc_dense_fwd(x, w, b=None, res=None, act=OC_ACT_NONE, need_pre=False, again=None):
     """y = act(x w + b) + res over the rows of x: (y, pre), pre what the backward needs
-    of x w + b (its values, float32; for OC_ACT_RELU their signs, one bit each) or None.
+    of x w + b, to be handed on to it, or None.  That is its values (float32), for
+    OC_ACT_RELU their signs (one bit each), or an Again where the backward is to form
+    them once more (again: True, False, or None for whichever is faster).
     x, w, res and y share a dtype (float32 or bfloat16); b is float32."""
-    return _layer_fwd(False, x, w, b, res, act, need_pre)
+    return _layer_fwd(False, x, w, b, res, act, need_pre, again)
 
 
 def oc_dense_bwd(x, w, dy, act=OC_ACT_NONE, pre=None, need_dx=True, need_dw=True, need_db=True,
                  dw=None, db=None, dw_dtype=None):
     """(dx, dw, db) of oc_dense_fwd (None where not needed).  pre: as the forward
-    returned it; for OC_ACT_RELU the y of a forward without a residual does as well.  dw, db:
-    optional caller tensors to write into; a new dw is of dw_dtype (float32 if
-    not given, or x's dtype)."""
+    returned it; for OC_ACT_RELU the y of a forward without a residual does as well.
+    dw, db: optional caller tensors to write into; a new dw is of dw_dtype (float32
+    if not given, or x's dtype)."""
     return _layer_bwd(False, x, w, dy, pre, act, need_dx, need_dw, need_db, dw, db, dw_dtype)
 
 
-def oc_glu_fwd(x, w, b=None, act=OC_ACT_SILU, need_pre=False):
-    """y = act(g) u, [g | u] = x w + b, w [cin][2 cout]: (y, pre), pre [rows][2 cout]
-    float32 for the backward or None."""
-    return _layer_fwd(True, x, w, b, None, act, need_pre)
+def oc_glu_fwd(x, w, b=None, act=OC_ACT_SILU, need_pre=False, again=None):
+    """y = act(g) u, [g | u] = x w + b, w [cin][2 cout]: (y, pre), pre (values
+    [rows][2 cout] or an Again) and again as oc_dense_fwd's."""
+    return _layer_fwd(True, x, w, b, None, act, need_pre, again)
 
 
 def oc_glu_bwd(x, w, dy, pre, act=OC_ACT_SILU, need_dx=True, need_dw=True, need_db=True, dw=None,

@@ -26,6 +26,12 @@ struct Epi {
   const void* res;
   void* y;
   void* pre;
+  // The backward's dz from a product formed again instead (dy given; type y_bf16):
+  // y receives dz = dy act'(z) (gated [dy u act'(g) | dy act(g)]) in rows of ldz
+  // elements, zero past the columns, and colsum [row tiles][nz], if any, its column sums.
+  const void* dy;
+  int64_t ldz;
+  float* colsum;
 };
 
 // out [P][Q] = sum over r < R of A(p, r) B(r, q), then `epi` (M = P, nz = Q).
@@ -67,6 +73,12 @@ inline bool few_rows(oc_dtype dt, int64_t rows, int64_t cin, int64_t cout) {
 void gemm_rows(oc_dtype dt, int32_t rows, int32_t R, int32_t Q, const void* x, const void* w,
                const Epi& epi, hipStream_t s);
 
+// Row tiles of a product that forms dz.
+int64_t gemm_dz_tiles(oc_dtype dt, bool direct, int64_t P, int64_t Q, int64_t R, bool glu);
+// Whether its operands go straight to LDS.
+bool gemm_direct(oc_dtype dt, const void* a, int64_t lda, const void* b, int64_t ldb, bool glu,
+                 int64_t half);
+
 // Bytes of workspace the product needs (partial sums of a split reduction);
 // a function of the type and the sizes alone.
 size_t gemm_ws(oc_dtype dt, int64_t P, int64_t Q, int64_t R, bool glu);
@@ -106,24 +118,23 @@ __device__ __forceinline__ float exp_fast(float x) {
 __device__ __forceinline__ float sigmoid(float z) {
   return __builtin_amdgcn_rcpf(1.f + exp_fast(-z));
 }
-// Phi(z); e receives e^(-z^2 / 2).
-__device__ __forceinline__ float normal_cdf(float z, float& e) {
-  const float x = fabsf(z) * 0.70710678118654752f;
-  const float t = __builtin_amdgcn_rcpf(fmaf(0.3275911f, x, 1.f));
-  float p = fmaf(1.061405429f, t, -1.453152027f);
-  p = fmaf(p, t, 1.421413741f);
-  p = fmaf(p, t, -0.284496736f);
-  p = fmaf(p, t, 0.254829592f);
+// Half of 1 - erf(|z| / sqrt(2)), that is Phi(-|z|); e receives e^(-z^2 / 2).
+__device__ __forceinline__ float normal_tail(float z, float& e) {
+  const float t = __builtin_amdgcn_rcpf(fmaf(0.3275911f * 0.70710678118654752f, fabsf(z), 1.f));
+  float p = fmaf(0.5f * 1.061405429f, t, 0.5f * -1.453152027f);
+  p = fmaf(p, t, 0.5f * 1.421413741f);
+  p = fmaf(p, t, 0.5f * -0.284496736f);
+  p = fmaf(p, t, 0.5f * 0.254829592f);
   e = exp_fast(-0.5f * z * z);
-  const float half = 0.5f * p * t * e;
-  return z < 0.f ? half : 1.f - half;
+  return p * t * e;
 }
 __device__ __forceinline__ float act_value(int act, float z) {
-  if (act == OC_ACT_RELU) return z > 0.f || z != z ? z : 0.f;
+  if (act == OC_ACT_RELU) return z < 0.f ? 0.f : z;  // (NaN stays NaN)
   if (act == OC_ACT_SILU) return z * sigmoid(z);
   if (act == OC_ACT_GELU) {
+    // z Phi(z) = max(z, 0) - |z| Phi(-|z|); the tail is 0 well before |z| = 16
     float e;
-    return z * normal_cdf(z, e);
+    return fmaf(-fminf(fabsf(z), 16.f), normal_tail(z, e), fmaxf(z, 0.f));
   }
   return z;
 }
@@ -135,8 +146,8 @@ __device__ __forceinline__ float act_slope(int act, float z) {
   }
   if (act == OC_ACT_GELU) {
     float e;
-    const float c = normal_cdf(z, e);
-    return fmaf(z * e, 0.39894228040143268f, c);
+    const float q = normal_tail(z, e);
+    return fmaf(z * e, 0.39894228040143268f, z < 0.f ? q : 1.f - q);
   }
   return 1.f;
 }
@@ -270,6 +281,58 @@ __device__ __forceinline__ void epilogue(const Epi& e, const int64_t (&m)[U], in
 #pragma unroll
   for (int i = 0; i < U; ++i)
     if (m[i] < M) store8n(e.y, e.y_bf16, m[i] * e.n + c, cnt, z[i]);
+}
+
+// Likewise for dz: u and z become its halves (without GLU, z becomes dz).
+template <int ACT, int U, bool GLU>
+__device__ __forceinline__ void slopes(const float (&d)[U][8], float (&z)[U][8], float (&u)[U][8]) {
+#pragma unroll
+  for (int i = 0; i < U; ++i)
+#pragma unroll
+    for (int k = 0; k < 8; ++k) {
+      const float g = z[i][k];
+      z[i][k] = d[i][k] * (GLU ? u[i][k] * act_slope(ACT, g) : act_slope(ACT, g));
+      if (GLU) u[i][k] = d[i][k] * act_value(ACT, g);
+    }
+}
+template <int U, bool GLU>
+__device__ __forceinline__ void epilogue_dz(const Epi& e, const int64_t (&m)[U], int64_t M, int c,
+                                            const float (&b0)[8], const float (&b1)[8],
+                                            float (&z)[U][8], float (&u)[U][8], float (&s0)[8],
+                                            float (&s1)[8]) {
+  const int cnt = e.n - c;
+  float d[U][8];
+#pragma unroll
+  for (int i = 0; i < U; ++i) {
+    if (m[i] < M) load8n(e.dy, e.y_bf16, m[i] * e.n + c, cnt, M * e.n, d[i]);
+#pragma unroll
+    for (int k = 0; k < 8; ++k) {
+      z[i][k] += b0[k];
+      if (GLU) u[i][k] += b1[k];
+    }
+  }
+  if (e.act == OC_ACT_NONE) slopes<OC_ACT_NONE, U, GLU>(d, z, u);
+  else if (e.act == OC_ACT_RELU) slopes<OC_ACT_RELU, U, GLU>(d, z, u);
+  else if (e.act == OC_ACT_SILU) slopes<OC_ACT_SILU, U, GLU>(d, z, u);
+  else slopes<OC_ACT_GELU, U, GLU>(d, z, u);
+#pragma unroll
+  for (int i = 0; i < U; ++i) {
+    if (m[i] >= M) continue;
+#pragma unroll
+    for (int k = 0; k < 8; ++k) {
+      if (k >= cnt) z[i][k] = u[i][k] = 0.f;  // (of columns that are not there)
+      s0[k] += z[i][k];
+      if (GLU) s1[k] += u[i][k];
+    }
+    if (GLU) {
+      store8n(e.y, e.y_bf16, m[i] * e.ldz + c, cnt, z[i]);
+      store8n(e.y, e.y_bf16, m[i] * e.ldz + e.n + c, cnt, u[i]);
+      if (cnt <= 8)
+        for (int64_t k = 2 * e.n; k < e.ldz; ++k) store1(e.y, e.y_bf16, m[i] * e.ldz + k, 0.f);
+    } else {
+      store8n(e.y, e.y_bf16, m[i] * e.ldz + c, (int)(e.ldz - c), z[i]);
+    }
+  }
 }
 
 }  // namespace oc

@@ -230,6 +230,33 @@ size_t pad_bytes(int64_t rows, int64_t ld) { return oc::align256((size_t)rows * 
 
 // --- the two layers -----------------------------------------------------------
 
+// x and w as the forward's product takes them, copied to xp and wp where they are padded.
+struct Operands {
+  const void *x, *w;
+  int64_t lda, ldb;
+  int32_t half;
+};
+Operands operands(oc_dtype dt, int64_t rows, int32_t cin, int32_t cout, bool glu, const void* x,
+                  const void* w, void* xp, void* wp, hipStream_t s) {
+  const int32_t nz = glu ? 2 * cout : cout;
+  Operands f{x, w, cin, nz, cout};
+  if (!oc::pads(dt, rows, cin, cout, glu)) return f;
+  Pads p{};
+  if (cin % 8) {
+    f.lda = oc::pad8(cin);
+    f.x = xp;
+    p.p[0] = Pad{x, (uint16_t*)xp, rows, f.lda, cin, 0};
+  }
+  if (cout % 8) {
+    f.half = (int32_t)oc::pad8(cout);
+    f.ldb = glu ? 2 * f.half : f.half;
+    f.w = wp;
+    p.p[1] = Pad{w, (uint16_t*)wp, cin, f.ldb, nz, glu};
+  }
+  pad(p, s);
+  return f;
+}
+
 struct FwdWs {
   size_t x, w, gemm, total;  // offsets, bytes in all
 };
@@ -256,30 +283,16 @@ oc_status fwd(const char* who, bool glu, oc_dtype dt, int32_t act, int64_t rows,
   st = check_ws(who, ws, ws_bytes, o.total);
   if (st != OC_OK) return st;
   const int32_t bf16 = dt == OC_BF16, nz = glu ? 2 * cout : cout;
-  const oc::Epi epi{act, glu, cout, bf16, act == OC_ACT_RELU && !glu, bias, res, y, pre};
+  const oc::Epi epi{act, glu, cout, bf16, act == OC_ACT_RELU && !glu, bias, res, y, pre, nullptr, 0,
+                    nullptr};
   if (oc::few_rows(dt, rows, cin, cout)) {
     oc::gemm_rows(dt, (int32_t)rows, cin, nz, x, w, epi, s);
     OC_LAUNCH_CHECK();
     return OC_OK;
   }
   char* base = (char*)ws;
-  int64_t lda = cin, ldb = nz, half = cout;
-  if (oc::pads(dt, rows, cin, cout, glu)) {
-    Pads p{};
-    if (cin % 8) {
-      lda = oc::pad8(cin);
-      p.p[0] = Pad{x, (uint16_t*)(base + o.x), rows, lda, cin, 0};
-      x = base + o.x;
-    }
-    if (cout % 8) {
-      half = oc::pad8(cout);
-      ldb = glu ? 2 * half : half;
-      p.p[1] = Pad{w, (uint16_t*)(base + o.w), cin, ldb, nz, glu};
-      w = base + o.w;
-    }
-    pad(p, s);
-  }
-  oc::gemm(oc::Gemm{dt, rows, cin, nz, x, w, lda, ldb, (int32_t)half, false, true, epi},
+  const Operands f = operands(dt, rows, cin, cout, glu, x, w, base + o.x, base + o.w, s);
+  oc::gemm(oc::Gemm{dt, rows, cin, nz, f.x, f.w, f.lda, f.ldb, f.half, false, true, epi},
            base + o.gemm, true, s);
   OC_LAUNCH_CHECK();
   return OC_OK;
@@ -296,18 +309,20 @@ BwdWs bwd_ws(oc_dtype dt, int32_t act, int64_t rows, int32_t cin, int32_t cout, 
   b.dz = 0;
   b.part = glu || act != OC_ACT_NONE || (pd && nz % 8)
                ? oc::align256((size_t)rows * (pd ? oc::pad8(nz) : nz) * (dt == OC_BF16 ? 2 : 4)) : 0;
-  b.x = b.part + oc::align256((size_t)d.nb * nz * 4);
+  // (a product formed again leaves a sum for each tile of 64 rows or more)
+  b.x = b.part + oc::align256((size_t)std::max<int64_t>(d.nb, cdiv(rows, 64)) * nz * 4);
   b.w = b.x + (pd && cin % 8 ? pad_bytes(rows, oc::pad8(cin)) : 0);
   b.gemm = b.w + (pd && nz % 8 ? pad_bytes(cin, oc::pad8(nz)) : 0);
-  b.total = b.gemm + oc::align256(std::max(oc::gemm_ws(dt, rows, cin, nz, false),
-                                           oc::gemm_ws(dt, cin, nz, rows, false)));
+  const size_t again = pd && cout % 8 ? pad_bytes(cin, (glu ? 2 : 1) * oc::pad8(cout)) : 0;
+  b.total = b.gemm + oc::align256(std::max({oc::gemm_ws(dt, rows, cin, nz, false),
+                                            oc::gemm_ws(dt, cin, nz, rows, false), again}));
   return b;
 }
 
 oc_status bwd(const char* who, bool glu, oc_dtype dt, int32_t act, int64_t rows, int32_t cin,
-              int32_t cout, const void* x, const void* w, const void* pre, const void* y,
-              const void* dy, void* dx, oc_dtype dw_dt, void* dw, float* dbias, void* ws,
-              size_t ws_bytes, hipStream_t s) {
+              int32_t cout, const void* x, const void* w, const float* bias, const void* pre,
+              const void* y, const void* dy, void* dx, oc_dtype dw_dt, void* dw, float* dbias,
+              void* ws, size_t ws_bytes, hipStream_t s) {
   oc_status st = check(who, dt, act, glu, rows, cin, cout);
   if (st != OC_OK) return st;
   if (dw && dw_dt != OC_F32 && dw_dt != dt)
@@ -322,7 +337,8 @@ oc_status bwd(const char* who, bool glu, oc_dtype dt, int32_t act, int64_t rows,
   const bool slope = glu || act != OC_ACT_NONE;
   const bool from_y = !glu && act == OC_ACT_RELU && y;
   if (pre && from_y) return oc::fail(OC_ERR_ARG, "%s: both pre and y", who);
-  if (!dy || (slope && !pre && !from_y) || (dx && !w) || (dw && !x))
+  const bool again = slope && !pre && !from_y;  // x w + bias is formed once more
+  if (!dy || ((dx || again) && !w) || ((dw || again) && !x))
     return oc::fail(OC_ERR_ARG, "%s: NULL buffer", who);
   if (!dx && !dw && !dbias) return OC_OK;
   const BwdWs o = bwd_ws(dt, act, rows, cin, cout, glu);
@@ -333,9 +349,21 @@ oc_status bwd(const char* who, bool glu, oc_dtype dt, int32_t act, int64_t rows,
   const bool apart = slope || (pd && nz % 8);  // dz is not dy itself
   const int64_t ldz = pd ? oc::pad8(nz) : nz;
   const void* dz = apart ? base + o.dz : dy;
-  if (apart || dbias) {
+  float* part = dbias ? (float*)(base + o.part) : nullptr;
+  if (again) {
+    const Operands f =
+        operands(dt, rows, cin, cout, glu, x, w, base + o.x, base + o.gemm, s);
+    const int64_t tiles = oc::gemm_dz_tiles(
+        dt, oc::gemm_direct(dt, f.x, f.lda, f.w, f.ldb, glu, f.half), rows, nz, cin, glu);
+    oc::gemm(oc::Gemm{dt, rows, cin, nz, f.x, f.w, f.lda, f.ldb, f.half, false, true,
+                      {act, glu, cout, bf16, 0, bias, nullptr, base + o.dz, nullptr, dy, ldz,
+                       part}},
+             nullptr, false, s);
+    if (dbias)
+      oc::launch(k_colsum, dim3((unsigned)cdiv(nz, 4)), dim3(TB), 0, s, (const float*)part,
+                 (int)tiles, nz, dbias);
+  } else if (apart || dbias) {
     const DzShape d = dz_shape(rows, cout);
-    float* part = dbias ? (float*)(base + o.part) : nullptr;
     void* out = glu || (apart && (dx || dw)) ? base + o.dz : nullptr;
     // the sums of a single block of rows are the result
     if (dbias && d.nb == 1) part = dbias;
@@ -364,7 +392,7 @@ oc_status bwd(const char* who, bool glu, oc_dtype dt, int32_t act, int64_t rows,
     Pads p{};
     if (dw && cin % 8) {
       ldx = oc::pad8(cin);
-      p.p[0] = Pad{x, (uint16_t*)(base + o.x), rows, ldx, cin, 0};
+      if (!again) p.p[0] = Pad{x, (uint16_t*)(base + o.x), rows, ldx, cin, 0};
       x = base + o.x;
     }
     if (dx && nz % 8) {
@@ -376,12 +404,13 @@ oc_status bwd(const char* who, bool glu, oc_dtype dt, int32_t act, int64_t rows,
   }
   if (dx) {
     oc::Gemm g{dt,    rows, nz, cin, dz, w, ldz, ldw, 0, false, false,
-               {OC_ACT_NONE, 0, cin, bf16, 0, nullptr, nullptr, dx, nullptr}};
+               {OC_ACT_NONE, 0, cin, bf16, 0, nullptr, nullptr, dx, nullptr, nullptr, 0, nullptr}};
     oc::gemm(g, base + o.gemm, true, s);
   }
   if (dw) {
     oc::Gemm g{dt,    cin, rows, nz, x, dz, ldx, ldz, 0, true, true,
-               {OC_ACT_NONE, 0, nz, dw_dt == OC_BF16, 0, nullptr, nullptr, dw, nullptr}};
+               {OC_ACT_NONE, 0, nz, dw_dt == OC_BF16, 0, nullptr, nullptr, dw, nullptr, nullptr, 0,
+                nullptr}};
     oc::gemm(g, base + o.gemm, !dx, s);
   }
   OC_LAUNCH_CHECK();
@@ -408,11 +437,11 @@ size_t oc_dense_bwd_workspace(oc_dtype dt, int32_t act, int64_t rows, int32_t ci
 }
 
 oc_status oc_dense_bwd(oc_dtype dt, int32_t act, int64_t rows, int32_t cin, int32_t cout,
-                       const void* x, const void* w, const void* pre, const void* y,
-                       const void* dy, void* dx, oc_dtype dw_dt, void* dw, float* dbias, void* ws,
-                       size_t ws_bytes, hipStream_t s) {
-  return bwd("oc_dense_bwd", false, dt, act, rows, cin, cout, x, w, pre, y, dy, dx, dw_dt, dw,
-             dbias, ws, ws_bytes, s);
+                       const void* x, const void* w, const float* bias, const void* pre,
+                       const void* y, const void* dy, void* dx, oc_dtype dw_dt, void* dw,
+                       float* dbias, void* ws, size_t ws_bytes, hipStream_t s) {
+  return bwd("oc_dense_bwd", false, dt, act, rows, cin, cout, x, w, bias, pre, y, dy, dx, dw_dt,
+             dw, dbias, ws, ws_bytes, s);
 }
 
 size_t oc_glu_fwd_workspace(oc_dtype dt, int64_t rows, int32_t cin, int32_t cout) {
@@ -432,11 +461,11 @@ size_t oc_glu_bwd_workspace(oc_dtype dt, int64_t rows, int32_t cin, int32_t cout
 }
 
 oc_status oc_glu_bwd(oc_dtype dt, int32_t act, int64_t rows, int32_t cin, int32_t cout,
-                     const void* x, const void* w, const float* pre, const void* dy, void* dx,
-                     oc_dtype dw_dt, void* dw, float* dbias, void* ws, size_t ws_bytes,
-                     hipStream_t s) {
-  return bwd("oc_glu_bwd", true, dt, act, rows, cin, cout, x, w, pre, nullptr, dy, dx, dw_dt, dw,
-             dbias, ws, ws_bytes, s);
+                     const void* x, const void* w, const float* bias, const float* pre,
+                     const void* dy, void* dx, oc_dtype dw_dt, void* dw, float* dbias, void* ws,
+                     size_t ws_bytes, hipStream_t s) {
+  return bwd("oc_glu_bwd", true, dt, act, rows, cin, cout, x, w, bias, pre, nullptr, dy, dx,
+             dw_dt, dw, dbias, ws, ws_bytes, s);
 }
 
 }  // extern "C"

@@ -3,11 +3,11 @@
 
 namespace {
 
-template <int SHAPE, bool ARS, bool BRS, bool GLU, bool DIRECT>
+template <int SHAPE, bool ARS, bool BRS, bool GLU, bool DIRECT, bool DZ>
 void go(bool main, const oc::TileArgs& t, hipStream_t s) {
   constexpr oc::TileInfo i = oc::tile_info<uint16_t>(SHAPE);
   constexpr int WGM = i.threads / 64 / (i.bn / 64);
-  const auto k = oc::k_dense_tile<uint16_t, i.bm, i.bn, WGM, i.bk, i.nb, ARS, BRS, GLU, DIRECT>;
+  const auto k = oc::k_dense_tile<uint16_t, i.bm, i.bn, WGM, i.bk, i.nb, ARS, BRS, GLU, DIRECT, DZ>;
   const dim3 grid((unsigned)(t.whole + t.classes * t.members));
   if (main) oc::launch_main(k, grid, dim3(i.threads), s, t);
   else oc::launch(k, grid, dim3(i.threads), 0, s, t);
@@ -15,10 +15,12 @@ void go(bool main, const oc::TileArgs& t, hipStream_t s) {
 
 template <int SHAPE, bool DIRECT>
 void pick(bool a_rs, bool b_rs, bool main, const oc::TileArgs& t, hipStream_t s) {
-  if (a_rs) go<SHAPE, true, true, false, DIRECT>(main, t, s);
-  else if (!b_rs) go<SHAPE, false, false, false, DIRECT>(main, t, s);
-  else if (t.epi.glu) go<SHAPE, false, true, true, DIRECT>(main, t, s);
-  else go<SHAPE, false, true, false, DIRECT>(main, t, s);
+  if (a_rs) go<SHAPE, true, true, false, DIRECT, false>(main, t, s);
+  else if (!b_rs) go<SHAPE, false, false, false, DIRECT, false>(main, t, s);
+  else if (t.epi.dy && t.epi.glu) go<SHAPE, false, true, true, DIRECT, true>(main, t, s);
+  else if (t.epi.dy) go<SHAPE, false, true, false, DIRECT, true>(main, t, s);
+  else if (t.epi.glu) go<SHAPE, false, true, true, DIRECT, false>(main, t, s);
+  else go<SHAPE, false, true, false, DIRECT, false>(main, t, s);
 }
 
 }  // namespace

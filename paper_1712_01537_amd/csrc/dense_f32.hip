@@ -3,11 +3,11 @@
 
 namespace {
 
-template <int SHAPE, bool ARS, bool BRS, bool GLU>
+template <int SHAPE, bool ARS, bool BRS, bool GLU, bool DZ>
 void go(bool main, const oc::TileArgs& t, hipStream_t s) {
   constexpr oc::TileInfo i = oc::tile_info<float>(SHAPE);
   constexpr int WGM = i.threads / 64 / (i.bn / 64);
-  const auto k = oc::k_dense_tile<float, i.bm, i.bn, WGM, i.bk, i.nb, ARS, BRS, GLU, false>;
+  const auto k = oc::k_dense_tile<float, i.bm, i.bn, WGM, i.bk, i.nb, ARS, BRS, GLU, false, DZ>;
   const dim3 grid((unsigned)(t.whole + t.classes * t.members));
   if (main) oc::launch_main(k, grid, dim3(i.threads), s, t);
   else oc::launch(k, grid, dim3(i.threads), 0, s, t);
@@ -15,10 +15,12 @@ void go(bool main, const oc::TileArgs& t, hipStream_t s) {
 
 template <int SHAPE>
 void pick(bool a_rs, bool b_rs, bool main, const oc::TileArgs& t, hipStream_t s) {
-  if (a_rs) go<SHAPE, true, true, false>(main, t, s);
-  else if (!b_rs) go<SHAPE, false, false, false>(main, t, s);
-  else if (t.epi.glu) go<SHAPE, false, true, true>(main, t, s);
-  else go<SHAPE, false, true, false>(main, t, s);
+  if (a_rs) go<SHAPE, true, true, false, false>(main, t, s);
+  else if (!b_rs) go<SHAPE, false, false, false, false>(main, t, s);
+  else if (t.epi.dy && t.epi.glu) go<SHAPE, false, true, true, true>(main, t, s);
+  else if (t.epi.dy) go<SHAPE, false, true, false, true>(main, t, s);
+  else if (t.epi.glu) go<SHAPE, false, true, true, false>(main, t, s);
+  else go<SHAPE, false, true, false, false>(main, t, s);
 }
 
 }  // namespace

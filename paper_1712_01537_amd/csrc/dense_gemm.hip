@@ -94,7 +94,9 @@ struct Plan {
 // 128x64 168, 128x128 202, 64x64 140.)  Partial sums are written and read at 4 TB/s
 // and take another launch of 4 us.
 // direct: bf16 operands that go straight to LDS; the larger tiles take only those.
-Plan plan(oc_dtype dt, bool direct, int64_t P, int64_t Q, int64_t R, bool glu) {
+// apart: every tile has a workgroup (for dz, whose epilogue is the tile kernel's alone).
+Plan plan(oc_dtype dt, bool direct, int64_t P, int64_t Q, int64_t R, bool glu,
+          bool apart = false) {
   struct Cost {
     double step, full;
     int fit;
@@ -134,7 +136,7 @@ Plan plan(oc_dtype dt, bool direct, int64_t P, int64_t Q, int64_t R, bool glu) {
       }
     };
     offer(1, steps);
-    for (int64_t run = 1; run <= 8 && run <= rest; ++run) {
+    for (int64_t run = 1; run <= 8 && run <= rest && !apart; ++run) {
       const int64_t members = cdiv(rest, run);
       for (int64_t classes = slots / members; classes > run; classes = classes * 3 / 4) {
         const int64_t share = cdiv(run * steps, classes);
@@ -159,10 +161,18 @@ size_t gemm_ws(oc_dtype dt, int64_t P, int64_t Q, int64_t R, bool glu) {
   return std::max(a, b);
 }
 
+bool gemm_direct(oc_dtype dt, const void* a, int64_t lda, const void* b, int64_t ldb, bool glu,
+                 int64_t half) {
+  return dt == OC_BF16 && vectors(a, lda) && vectors(b, ldb) && (!glu || half % 8 == 0);
+}
+
+int64_t gemm_dz_tiles(oc_dtype dt, bool direct, int64_t P, int64_t Q, int64_t R, bool glu) {
+  return plan(dt, direct, P, Q, R, glu, true).ntm;
+}
+
 void gemm(const Gemm& g, void* ws, bool main, hipStream_t s) {
-  const bool direct = g.dt == OC_BF16 && vectors(g.a, g.lda) && vectors(g.b, g.ldb) &&
-                      (!g.epi.glu || g.half % 8 == 0);
-  const Plan p = plan(g.dt, direct, g.P, g.Q, g.R, g.epi.glu);
+  const bool direct = gemm_direct(g.dt, g.a, g.lda, g.b, g.ldb, g.epi.glu, g.half);
+  const Plan p = plan(g.dt, direct, g.P, g.Q, g.R, g.epi.glu, g.epi.dy != nullptr);
   const TileArgs t{g.a,     g.b,       g.P,   g.R,       g.Q,     g.lda,   g.ldb,      g.half, p.ntm,
                    p.ntn,   p.whole,   p.members, p.run, p.classes, p.steps, p.share, (float*)ws,
                    g.epi};

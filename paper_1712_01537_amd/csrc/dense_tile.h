@@ -152,7 +152,8 @@ __host__ __device__ __forceinline__ TilePos tile_pos(int ntm, int ntn, uint32_t 
   return TilePos{(int)(group * 8 + (j - n * rows)), (int)n};
 }
 
-template <typename T, int BM, int BN, int WGM, int BK, int BUFS, bool ARS, bool BRS, bool GLU, bool DIRECT>
+template <typename T, int BM, int BN, int WGM, int BK, int BUFS, bool ARS, bool BRS, bool GLU, bool DIRECT,
+          bool DZ>
 __global__ __launch_bounds__(64 * WGM * (BN / 64), 2) void k_dense_tile(TileArgs t) {
   constexpr bool F32 = sizeof(T) == 4;
   static_assert(!(F32 && DIRECT), "fp32 operands are split in registers");
@@ -162,7 +163,7 @@ __global__ __launch_bounds__(64 * WGM * (BN / 64), 2) void k_dense_tile(TileArgs
   constexpr int CK = BK / 8, CA = BM * CK, CB = BN * CK;
   constexpr int ITA = CA / NTHR, ITB = CB / NTHR, IT = ITA + ITB;
   static_assert(CA % NTHR == 0 && CB % NTHR == 0 && TM % 16 == 0, "whole vectors per thread");
-  static_assert(!GLU || (!ARS && BRS), "the gated layer is a forward product");
+  static_assert(!(GLU || DZ) || (!ARS && BRS), "the forward's layout");
   constexpr int STAGE = PARTS * (CA + CB), NB = DIRECT ? BUFS : 2;
   // the epilogue's pieces: ROWS rows of 64 sums per wave at a time
   constexpr int ROWS = TM < 64 ? TM : 64, EPI = WGM * WGN * ROWS * 16;
@@ -573,6 +574,7 @@ __global__ __launch_bounds__(64 * WGM * (BN / 64), 2) void k_dense_tile(TileArgs
     load8n(t.epi.bias, false, c, cols, t.Q, b0);
     if (GLU) load8n(t.epi.bias, false, n + c, cols, t.Q, b1);
   }
+  float c0[8] = {}, c1[8] = {};  // DZ: column sums of this lane's rows
   dt_barrier();  // no wave reads operands from LDS any more
 #pragma unroll
   for (int pass = 0; pass < TM / ROWS; ++pass) {
@@ -635,8 +637,38 @@ __global__ __launch_bounds__(64 * WGM * (BN / 64), 2) void k_dense_tile(TileArgs
           store8(o, false, 0, v[i]);
           if (GLU) store8(o, false, 32, u[i]);
         }
+      } else if constexpr (DZ) {
+        epilogue_dz<U, GLU>(t.epi, p, t.P, c, b0, b1, v, u, c0, c1);
       } else {
         epilogue<U, GLU>(t.epi, p, t.P, c, b0, b1, v, u);
+      }
+    }
+  }
+  if constexpr (DZ) {
+    // the tile's column sums: a wave's lanes, then its row of waves, in a fixed order
+    if (t.epi.colsum) {
+      float* const cs = (float*)lds;
+#pragma unroll
+      for (int m = LR; m < 64; m <<= 1)
+#pragma unroll
+        for (int k = 0; k < 8; ++k) {
+          c0[k] += __shfl_xor(c0[k], m);
+          if (GLU) c1[k] += __shfl_xor(c1[k], m);
+        }
+      dt_barrier();
+      if (lane < LR)
+#pragma unroll
+        for (int k = 0; k < 8; ++k) {
+          cs[wave * 64 + lane * 8 + k] = c0[k];
+          if (GLU) cs[wave * 64 + 32 + lane * 8 + k] = c1[k];
+        }
+      dt_barrier();
+      if (tid < BN) {
+        const int col = tid & 63, g = tid >> 6;
+        const int cc = q0 + (GLU ? g * 32 + (col & 31) : tid);
+        float a = 0.f;
+        for (int m = 0; m < WGM; ++m) a += cs[(m * WGN + g) * 64 + col];
+        if (cc < n) t.epi.colsum[(int64_t)pos.m * t.Q + (GLU && col >= 32 ? n + cc : cc)] = a;
       }
     }
   }

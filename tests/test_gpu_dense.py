@@ -70,7 +70,7 @@ def check_norm(got, ref, scale, R, what):
     assert err <= most, (what, err, most)
 
 
-def run_and_check(c, act, glu, dt, bwd=True, dw_dtype=None):
+def run_and_check(c, act, glu, dt, bwd=True, dw_dtype=None, again=False):
     a = ACT[act]
     x, w = _np(c["x"]), _np(c["w"])
     rows, cin = x.shape
@@ -80,7 +80,7 @@ def run_and_check(c, act, glu, dt, bwd=True, dw_dtype=None):
     S = _abs(x) @ _abs(w) + (0 if b is None else _abs(b))
     tz = (cin + 4) * U * S + 1e-38
     if glu:
-        y, pre = oc.oc_glu_fwd(c["x"], c["w"], c["b"], act=a, need_pre=True)
+        y, pre = oc.oc_glu_fwd(c["x"], c["w"], c["b"], act=a, need_pre=True, again=again)
         yr, z = D.glu_fwd(x, w, b, act)
         n = z.shape[1] // 2
         g, u = z[:, :n], z[:, n:]
@@ -88,12 +88,15 @@ def run_and_check(c, act, glu, dt, bwd=True, dw_dtype=None):
         tag = 1.13 * tz[:, :n] + 8 * U * (_abs(g) + _abs(ag))
         ty = tag * (_abs(u) + tz[:, n:]) + _abs(ag) * tz[:, n:] + 2 * U * _abs(yr)
     else:
-        y, pre = oc.oc_dense_fwd(c["x"], c["w"], c["b"], res=c["res"], act=a, need_pre=True)
+        y, pre = oc.oc_dense_fwd(c["x"], c["w"], c["b"], res=c["res"], act=a, need_pre=True,
+                                 again=again)
         yr, z = D.dense_fwd(x, w, b, _np(c["res"]), act)
         r = 0.0 if c["res"] is None else _abs(_np(c["res"]))
         ty = 1.13 * tz + 8 * U * (_abs(z) + r + _abs(yr))
     check(y, yr, ty + rnd * (_abs(yr) + ty), "y")
-    if act == "relu" and not glu:  # signs, eight columns a byte
+    if again:
+        assert isinstance(pre, oc.Again)
+    elif act == "relu" and not glu:  # signs, eight columns a byte
         bits = np.unpackbits(pre.cpu().numpy(), axis=1, bitorder="little")
         np.testing.assert_array_equal(bits[:, :z.shape[1]], z > 0)
     else:
@@ -157,14 +160,48 @@ def test_glu(i, dt):
                   dw_dtype=torch.bfloat16 if dt == "bf16" and i % 2 else None)
 
 
+@pytest.mark.parametrize("dt", ["f32", "bf16"])
+@pytest.mark.parametrize("glu", [False, True])
+@pytest.mark.parametrize("i", range(len(SIZES)))
+def test_formed_again(i, glu, dt):
+    """The backward from x and w alone: within the same bounds."""
+    rows, cin, cout = SIZES[i]
+    act = list(ACT)[1 + i % 3]
+    print(f"[again] {dt} glu {glu} {rows}x{cin}->{cout} {act}", flush=True)
+    run_and_check(make(rows, cin, cout, dt, act, glu, bias=i % 3 != 1), act, glu, dt, again=True)
+
+
+def test_which_is_formed_again():
+    """Left to the rule: 32768 x 64 -> 2 x 1024 would keep 256 MB, the last-level
+    cache's size, and is formed again; 8 rows fewer are kept.  The gradients agree."""
+    g = torch.Generator().manual_seed(5)
+    w = (torch.randn(64, 2048, generator=g) / 8).bfloat16().cuda()
+    x = torch.randn(32768, 64, generator=g).bfloat16().cuda()
+    dy = torch.randn(32768, 1024, generator=g).bfloat16().cuda()
+    assert isinstance(oc.oc_glu_fwd(x[8:], w, need_pre=True)[1], torch.Tensor)
+    assert oc.oc_glu_fwd(x, w)[1] is None
+    got = []
+    for again in (None, False):
+        y, pre = oc.oc_glu_fwd(x, w, need_pre=True, again=again)
+        assert isinstance(pre, oc.Again if again is None else torch.Tensor)
+        got.append((y,) + tuple(oc.oc_glu_bwd(x, w, dy, pre)))
+    assert torch.equal(got[0][0], got[1][0])
+    # The slopes may be contracted differently, so that a dz now and then rounds to the
+    # neighbouring bf16 value (2^-7 of it apart), and dx and dw (2^-7 apart) after it:
+    # with the terms' signs at random, at most twice 2^-7 of the root of the squares.
+    for a, b in zip(got[0][1:], got[1][1:]):
+        assert (a.double() - b.double()).norm() <= 2.0**-6 * b.double().norm()
+
+
 LARGE = [(70_000, 72, 520, "relu"), (9000, 1032, 2056, "silu"), (40_001, 264, 1000, "gelu"),
          (5000, 520, 4104, "none"), (33_000, 515, 260, "silu"), (6000, 2051, 777, "gelu")]
 
 
+@pytest.mark.parametrize("again", [False, True])
 @pytest.mark.parametrize("glu", [False, True])
 @pytest.mark.parametrize("dt", ["f32", "bf16"])
 @pytest.mark.parametrize("i", range(len(LARGE)))
-def test_large(i, dt, glu):
+def test_large(i, dt, glu, again):
     """Sizes of the large tiles, aligned and not.  The error's 2-norm against that
     of the result: 2^-9 for each rounding to bf16 (its mean square is below a third
     of half a step's), and a random walk of fp32 roundings of the root of the
@@ -181,11 +218,12 @@ def test_large(i, dt, glu):
           "gelu": torch.nn.functional.gelu}[act]
     z = x @ w + b
     if glu:
-        y, pre = oc.oc_glu_fwd(c["x"], c["w"], c["b"], act=a, need_pre=True)
+        y, pre = oc.oc_glu_fwd(c["x"], c["w"], c["b"], act=a, need_pre=True, again=again)
         got = oc.oc_glu_bwd(c["x"], c["w"], c["dy"], pre, act=a, dw_dtype=DT[dt])
         yr = fn(z[:, :cout]) * z[:, cout:]
     else:
-        y, pre = oc.oc_dense_fwd(c["x"], c["w"], c["b"], res=c["res"], act=a, need_pre=True)
+        y, pre = oc.oc_dense_fwd(c["x"], c["w"], c["b"], res=c["res"], act=a, need_pre=True,
+                                 again=again)
         got = oc.oc_dense_bwd(c["x"], c["w"], c["dy"], act=a, pre=pre, dw_dtype=DT[dt])
         yr = fn(z) + c["res"].double()
     ref = torch.autograd.grad(yr, (x, w, b), dy)
@@ -205,7 +243,8 @@ def test_large(i, dt, glu):
                                                (3, 65536, 5, False), (2, 5, 65536, False),
                                                (9, 4, 32768, True), (1, 12, 32768, True)])
 def test_longest_rows(rows, cin, cout, glu, dt):
-    run_and_check(make(rows, cin, cout, dt, "silu", glu), "silu", glu, dt)
+    for again in (False, True):
+        run_and_check(make(rows, cin, cout, dt, "silu", glu), "silu", glu, dt, again=again)
 
 
 @pytest.mark.parametrize("act", ["silu", "gelu"])
@@ -263,8 +302,9 @@ def _view(t, shift):
 def test_any_alignment(rows, glu, dt):
     """Buffers at any element's address give what aligned ones give."""
     c = make(rows, 72, 40, dt, "gelu", glu)
-    run_and_check({k: None if v is None else _view(v, 1 + i) for i, (k, v) in enumerate(c.items())},
-                  "gelu", glu, dt)
+    for again in (False, True):
+        run_and_check({k: None if v is None else _view(v, 1 + i)
+                       for i, (k, v) in enumerate(c.items())}, "gelu", glu, dt, again=again)
 
 
 def test_relu_backward_takes_the_output():
@@ -281,13 +321,14 @@ def test_parts_asked_for(dt):
     """Each gradient alone equals the one of the whole call; none of them asked
     for touches nothing."""
     c = make(200, 48, 80, dt, "silu", False)
-    _, pre = oc.oc_dense_fwd(c["x"], c["w"], c["b"], act=2, need_pre=True)
-    every = oc.oc_dense_bwd(c["x"], c["w"], c["dy"], act=2, pre=pre)
-    for k in range(3):
-        need = [j == k for j in range(3)]
-        got = oc.oc_dense_bwd(c["x"], c["w"], c["dy"], act=2, pre=pre, need_dx=need[0],
-                              need_dw=need[1], need_db=need[2])
-        assert torch.equal(got[k], every[k]) and sum(g is not None for g in got) == 1
+    for again in (False, True):
+        _, pre = oc.oc_dense_fwd(c["x"], c["w"], c["b"], act=2, need_pre=True, again=again)
+        every = oc.oc_dense_bwd(c["x"], c["w"], c["dy"], act=2, pre=pre)
+        for k in range(3):
+            need = [j == k for j in range(3)]
+            got = oc.oc_dense_bwd(c["x"], c["w"], c["dy"], act=2, pre=pre, need_dx=need[0],
+                                  need_dw=need[1], need_db=need[2])
+            assert torch.equal(got[k], every[k]) and sum(g is not None for g in got) == 1
 
 
 @pytest.mark.parametrize("dt", ["f32", "bf16"])
@@ -335,8 +376,9 @@ def test_what_is_behind_stays(rows, cin, cout, dt):
     ws2 = torch.full((int(L.oc_dense_bwd_workspace(code, 3, rows, cin, cout)) + 256,), 5,
                      dtype=torch.uint8, device="cuda")
     assert L.oc_dense_bwd(code, 3, rows, cin, cout, c["x"].data_ptr(), c["w"].data_ptr(),
-                          pre.data_ptr(), None, c["dy"].data_ptr(), dx.data_ptr(), 0, dw.data_ptr(),
-                          db.data_ptr(), ws2.data_ptr(), ws2.numel() - 256, oc._stream()) == 0
+                          None, pre.data_ptr(), None, c["dy"].data_ptr(), dx.data_ptr(), 0,
+                          dw.data_ptr(), db.data_ptr(), ws2.data_ptr(), ws2.numel() - 256,
+                          oc._stream()) == 0
     for buf, v in ((yb, y), (pb, pre), (dxb, dx), (dwb, dw), (dbb, db)):
         assert (buf[v.numel():] == 11.0).all()
     assert (ws[-256:] == 5).all() and (ws2[-256:] == 5).all()
@@ -399,14 +441,15 @@ def test_same_bits_again(dt):
     for rows, cin, cout in ((1, 1024, 640), (40, 512, 72), (3000, 128, 264)):
         for glu in (False, True):
             c = make(rows, cin, cout, dt, "silu", glu)
-            def once():
+            def once(again):
                 if glu:
-                    y, pre = oc.oc_glu_fwd(c["x"], c["w"], c["b"], need_pre=True)
-                    return (y, pre) + tuple(oc.oc_glu_bwd(c["x"], c["w"], c["dy"], pre))
-                y, pre = oc.oc_dense_fwd(c["x"], c["w"], c["b"], act=2, need_pre=True)
-                return (y, pre) + tuple(oc.oc_dense_bwd(c["x"], c["w"], c["dy"], act=2, pre=pre))
-            for p, q in zip(once(), once()):
-                assert torch.equal(p, q)
+                    y, pre = oc.oc_glu_fwd(c["x"], c["w"], c["b"], need_pre=True, again=again)
+                    return (y,) + tuple(oc.oc_glu_bwd(c["x"], c["w"], c["dy"], pre))
+                y, pre = oc.oc_dense_fwd(c["x"], c["w"], c["b"], act=2, need_pre=True, again=again)
+                return (y,) + tuple(oc.oc_dense_bwd(c["x"], c["w"], c["dy"], act=2, pre=pre))
+            for again in (False, True):
+                for p, q in zip(once(again), once(again)):
+                    assert torch.equal(p, q)
 
 
 def test_other_stream_and_graphs():

@@ -110,10 +110,12 @@ def test_dense_refusals():
 
     def bwd(dt=0, act=2, rows=4, pre=P, y=None, dy=P, dx=P, dw_dt=0, dw=P, db=P, x=P, w=P, ws=P,
             n=1 << 30):
-        return L.oc_dense_bwd(dt, act, rows, 3, 5, x, w, pre, y, dy, dx, dw_dt, dw, db, ws, n, None)
+        return L.oc_dense_bwd(dt, act, rows, 3, 5, x, w, None, pre, y, dy, dx, dw_dt, dw, db, ws, n,
+                              None)
 
-    assert bwd(act=1, y=P) == 1 and bwd(act=1, pre=None) == 1 and bwd(pre=None, y=P) == 1
-    assert bwd(pre=None) == 1 and bwd(dy=None) == 1 and bwd(w=None) == 1 and bwd(x=None) == 1
+    assert bwd(act=1, y=P) == 1  # both pre and y
+    assert bwd(pre=None, x=None, dw=None) == 1 and bwd(pre=None, w=None, dx=None) == 1
+    assert bwd(dy=None) == 1 and bwd(w=None) == 1 and bwd(x=None) == 1
     assert bwd(dw_dt=1) == 1 and bwd(dw_dt=7) == 1 and bwd(dt=1, dw_dt=7) == 1
     assert bwd(act=9) == 1 and bwd(rows=-2) == 1
     need = L.oc_dense_bwd_workspace(0, 2, 4, 3, 5)
@@ -137,8 +139,8 @@ def test_glu_refusals():
     assert L.oc_glu_fwd_workspace(0, 4, 3, 32769) == 0
     assert L.oc_glu_bwd_workspace(0, 4, 3, 32769) == 0
     need = L.oc_glu_bwd_workspace(0, 4, 3, 5)
-    for pre, dy, n in ((None, P, need), (P, None, need), (P, P, need - 1)):
-        assert L.oc_glu_bwd(0, 2, 4, 3, 5, P, P, pre, dy, P, 0, P, P, P, n, None) == 1
+    for x, pre, dy, n in ((None, None, P, need), (P, P, None, need), (P, P, P, need - 1)):
+        assert L.oc_glu_bwd(0, 2, 4, 3, 5, x, P, None, pre, dy, P, 0, None, P, P, n, None) == 1
 
 
 def test_grad_refusals():
