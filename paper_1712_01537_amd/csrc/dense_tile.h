@@ -15,9 +15,9 @@
 //
 // bf16 operands whose rows are whole 16-byte vectors (of which what is behind a
 // row's end holds zeros) go from memory to LDS directly (buffer_load ... lds; what is
-// out of range reads as zero); others, and fp32 ones, pass through registers, where fp32 values are split in three bf16
-// parts (split3.h), so that each is split once per tile.  fp32: six MFMAs a
-// product.
+// out of range reads as zero); others, and fp32 ones, pass through registers, where
+// fp32 values are split in three bf16 parts (split3.h), so that each is split once
+// per tile.  fp32: six MFMAs a product.
 //
 // LDS layouts, in 16-byte vectors: a row operand keeps its rows (BK values) with
 // the vectors of a row rotated by XOR, a column operand keeps [BK][BM or BN] the
@@ -152,8 +152,8 @@ __host__ __device__ __forceinline__ TilePos tile_pos(int ntm, int ntn, uint32_t 
   return TilePos{(int)(group * 8 + (j - n * rows)), (int)n};
 }
 
-template <typename T, int BM, int BN, int WGM, int BK, int BUFS, bool ARS, bool BRS, bool GLU, bool DIRECT,
-          bool DZ>
+template <typename T, int BM, int BN, int WGM, int BK, int BUFS, bool ARS, bool BRS, bool GLU,
+          bool DIRECT, bool DZ>
 __global__ __launch_bounds__(64 * WGM * (BN / 64), 2) void k_dense_tile(TileArgs t) {
   constexpr bool F32 = sizeof(T) == 4;
   static_assert(!(F32 && DIRECT), "fp32 operands are split in registers");
