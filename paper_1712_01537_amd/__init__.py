@@ -1098,6 +1098,11 @@ def oc_grad_clip(grads, max_norm, outs=None):
         written = [p for p, c in zip(optrs, counts) if c]
         if len(set(written)) != len(written):
             raise OcError(1, "a tensor is to be written twice")
+    if outs is not None:
+        both = set(optrs).intersection(ptrs)
+        if both - {None} and any(c and p in both and p != q
+                                 for p, q, c in zip(optrs, ptrs, counts)):
+            raise OcError(1, "an output is another tensor's gradient")
     L = load()
     norm, ws, need = _grad_scratch(L, n, counts)
     _check(L.oc_grad_clip(n, ptrs, dts, counts, max_norm, optrs, odts, norm.data_ptr(),

@@ -162,7 +162,7 @@ oc_status check_list(const char* who, int32_t n, const void* const* grads, const
       return oc::fail(OC_ERR_ARG, "%s: tensor %d is NULL or has a bad count", who, i);
   }
   for (int32_t i = 0; i < n; i += MOST_TENSORS)
-    if (chunks_of(i, n, counts) > (int64_t)0xffffffff)
+    if (chunks_of(i, n, counts) > (int64_t)0x7fffffff)  // (indices step on by gridDim.x)
       return oc::fail(OC_ERR_ARG, "%s: too many values", who);
   return OC_OK;
 }

@@ -132,6 +132,22 @@ def test_same_bits_streams_and_graphs():
         assert torch.equal(n, norm) and all(torch.equal(a, b) for a, b in zip(want, outs)), rep
 
 
+def test_outputs_among_the_gradients():
+    """Gradients may be their own outputs beside others that are not; empty tensors
+    share an address (or none); another tensor's gradient is refused."""
+    g, h, o = (torch.full((10,), v, device="cuda") for v in (1.0, 2.0, 0.0))
+    e = [torch.empty(0, device="cuda") for _ in range(4)]
+    with pytest.raises(oc.OcError):
+        oc.oc_grad_clip([g, h], 1.0, outs=[h, g])
+    with pytest.raises(oc.OcError):
+        oc.oc_grad_clip([g, h], 1.0, outs=[o, g])
+    n = oc.oc_grad_clip([g, e[0], h, e[1]], 1.0, outs=[o, e[2], h, e[3]])
+    norm = math.sqrt(50.0)
+    assert abs(n.item() - norm) <= 2.0**-23 * norm
+    for t, v in ((g, 1.0), (o, 1.0 / norm), (h, 2.0 / norm)):
+        assert (t - v).abs().max().item() <= 2.0**-22 * v
+
+
 def test_refusals_of_tensors():
     g = torch.ones(10, device="cuda")
     for call in (lambda: oc.oc_grad_norm([g.double()]), lambda: oc.oc_grad_norm([g[::2]]),

@@ -160,6 +160,10 @@ def test_grad_refusals():
     assert clip(od=(C.c_int * 2)(1, 1)) == 1   # fp32 into bf16
     assert clip(od=(C.c_int * 2)(0, 0)) == 1   # in place, in another type
     assert clip(ws=C.c_void_p(260)) == 1 and clip(ws=None) == 1 and clip(nb=need - 1) == 1
+    # more chunks (of 8192 values) in a launch's 128 tensors than an index counts
+    many = (C.c_void_p * 128)(*[256] * 128), (C.c_int * 128)(), (C.c_int64 * 128)(*[1 << 37] * 128)
+    assert L.oc_grad_norm(128, *many, P, P, 1 << 40, None) == 1
+    assert b"too many values" in L.oc_last_error()
     assert L.oc_grad_norm(2, ptrs, dts, counts, None, P, need, None) == 1
     assert L.oc_grad_norm(2, ptrs, dts, counts, P, P, need - 1, None) == 1
     assert L.oc_grad_workspace(-1, counts) == 0 and L.oc_grad_workspace(1, None) == 0
