@@ -26,7 +26,7 @@ constexpr int TB = 256;
 // (b, k) has rows M b / nb .. and columns 8 ct k ..  Column sums: per thread
 // fp32 over its rows (about 30), then the row lanes in order through LDS into
 // part[b][column], then k_colsum in double over the blocks: a fixed order.
-// Bound by memory: dy and z read, dz written (65536 x 4096 bf16 ReLU from y 346 us, 4.4
+// Bound by memory: dy and z read, dz written (65536 x 4096 bf16 ReLU from y 346 us, 4.7
 // TB/s; 32768 x 2816 bf16 gated 288 us, 4.5 TB/s).
 struct DzShape {
   int ct, rl, kb, nb;  // column threads, row lanes, column blocks, row blocks

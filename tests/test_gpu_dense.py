@@ -452,7 +452,8 @@ def test_same_bits_again(dt):
                     assert torch.equal(p, q)
 
 
-def test_other_stream_and_graphs():
+@pytest.mark.parametrize("again", [False, True])
+def test_other_stream_and_graphs(again):
     """On a stream of its own, and in two captured graphs replayed in turn with
     eager work between, each with new inputs: the eager call's bits."""
     cs = [make(150, 64, 72, dt, "gelu", glu, seed=k)
@@ -460,9 +461,10 @@ def test_other_stream_and_graphs():
 
     def step(c, glu):
         if glu:
-            y, pre = oc.oc_glu_fwd(c["x"], c["w"], c["b"], act=3, need_pre=True)
+            y, pre = oc.oc_glu_fwd(c["x"], c["w"], c["b"], act=3, need_pre=True, again=again)
             return (y,) + tuple(oc.oc_glu_bwd(c["x"], c["w"], c["dy"], pre, act=3))
-        y, pre = oc.oc_dense_fwd(c["x"], c["w"], c["b"], res=c["res"], act=3, need_pre=True)
+        y, pre = oc.oc_dense_fwd(c["x"], c["w"], c["b"], res=c["res"], act=3, need_pre=True,
+                                 again=again)
         return (y,) + tuple(oc.oc_dense_bwd(c["x"], c["w"], c["dy"], act=3, pre=pre))
 
     side = torch.cuda.Stream()
