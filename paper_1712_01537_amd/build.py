@@ -48,7 +48,7 @@ COUNTED_WAIT = re.compile(r"s_waitcnt vmcnt\(%")
 # hold 64-bit addresses beside these and may spill.  The dense layers' tiles spill
 # inside their main loop when the epilogue needs too many registers (65536 x 1024
 # -> 4096 bf16, input gradient: 903 us instead of 475).
-IN_REGISTERS = re.compile(r"k_conv_(?:sp3|dws)I(?:L[ib]\d+E)*Lb0EE+v|k_dense_tileI")
+IN_REGISTERS = re.compile(r"k_conv_(?:sp3|dws)I(?:L[ib]\d+E)*Lb0EE+v|k_dense_tile(?:s2)?I")
 
 
 def _scratch_by_kernel(remarks: str) -> dict:

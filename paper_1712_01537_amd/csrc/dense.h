@@ -82,8 +82,12 @@ bool gemm_direct(oc_dtype dt, const void* a, int64_t lda, const void* b, int64_t
 // Bytes of workspace the product needs (partial sums of a split reduction);
 // a function of the type and the sizes alone.
 size_t gemm_ws(oc_dtype dt, int64_t P, int64_t Q, int64_t R, bool glu);
+// Likewise of gemm2.
+size_t gemm2_ws(oc_dtype dt, int64_t rows, int64_t cin, int64_t nz);
 // Enqueue it.  main: its kernel does the call's main arithmetic (profiling).
 void gemm(const Gemm& g, void* ws, bool main, hipStream_t s);
+// Both products of a backward: dx [rows][cin] over nz terms, dw [cin][nz] over the rows.
+void gemm2(const Gemm& dx, const Gemm& dw, void* ws, hipStream_t s);
 
 // --- device side ---------------------------------------------------------
 

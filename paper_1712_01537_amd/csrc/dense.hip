@@ -315,7 +315,8 @@ BwdWs bwd_ws(oc_dtype dt, int32_t act, int64_t rows, int32_t cin, int32_t cout, 
   b.gemm = b.w + (pd && nz % 8 ? pad_bytes(cin, oc::pad8(nz)) : 0);
   const size_t again = pd && cout % 8 ? pad_bytes(cin, (glu ? 2 : 1) * oc::pad8(cout)) : 0;
   b.total = b.gemm + oc::align256(std::max({oc::gemm_ws(dt, rows, cin, nz, false),
-                                            oc::gemm_ws(dt, cin, nz, rows, false), again}));
+                                            oc::gemm_ws(dt, cin, nz, rows, false),
+                                            oc::gemm2_ws(dt, rows, cin, nz), again}));
   return b;
 }
 
@@ -402,17 +403,15 @@ oc_status bwd(const char* who, bool glu, oc_dtype dt, int32_t act, int64_t rows,
     }
     pad(p, s);
   }
-  if (dx) {
-    oc::Gemm g{dt,    rows, nz, cin, dz, w, ldz, ldw, 0, false, false,
-               {OC_ACT_NONE, 0, cin, bf16, 0, nullptr, nullptr, dx, nullptr, nullptr, 0, nullptr}};
-    oc::gemm(g, base + o.gemm, true, s);
-  }
-  if (dw) {
-    oc::Gemm g{dt,    cin, rows, nz, x, dz, ldx, ldz, 0, true, true,
-               {OC_ACT_NONE, 0, nz, dw_dt == OC_BF16, 0, nullptr, nullptr, dw, nullptr, nullptr, 0,
-                nullptr}};
-    oc::gemm(g, base + o.gemm, !dx, s);
-  }
+  const oc::Gemm gx{dt, rows, nz, cin, dz, w, ldz, ldw, 0, false, false,
+                    {OC_ACT_NONE, 0, cin, bf16, 0, nullptr, nullptr, dx, nullptr, nullptr, 0,
+                     nullptr}};
+  const oc::Gemm gw{dt, cin, rows, nz, x, dz, ldx, ldz, 0, true, true,
+                    {OC_ACT_NONE, 0, nz, dw_dt == OC_BF16, 0, nullptr, nullptr, dw, nullptr,
+                     nullptr, 0, nullptr}};
+  if (dx && dw) oc::gemm2(gx, gw, base + o.gemm, s);
+  else if (dx) oc::gemm(gx, base + o.gemm, true, s);
+  else if (dw) oc::gemm(gw, base + o.gemm, true, s);
   OC_LAUNCH_CHECK();
   return OC_OK;
 }

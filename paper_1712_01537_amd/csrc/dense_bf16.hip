@@ -23,6 +23,15 @@ void pick(bool a_rs, bool b_rs, bool main, const oc::TileArgs& t, hipStream_t s)
   else go<SHAPE, false, true, false, DIRECT, false>(main, t, s);
 }
 
+template <int SHAPE, bool DIRECT>
+void go2(const oc::TileArgs& dx, const oc::TileArgs& dw, bool swapped, hipStream_t s) {
+  constexpr oc::TileInfo i = oc::tile_info<uint16_t>(SHAPE);
+  constexpr int WGM = i.threads / 64 / (i.bn / 64);
+  const unsigned n = dx.whole + dx.classes * dx.members, m = dw.whole + dw.classes * dw.members;
+  oc::launch_main(oc::k_dense_tiles2<uint16_t, i.bm, i.bn, WGM, i.bk, i.nb, DIRECT>, dim3(n + m),
+                  dim3(i.threads), s, dx, dw, (uint32_t)(swapped ? n : m), swapped);
+}
+
 }  // namespace
 
 namespace oc {
@@ -35,6 +44,17 @@ void tile_bf16(int shape, bool a_rs, bool b_rs, bool direct, bool main, const Ti
     case TILE_TWO: return pick<TILE_TWO, true>(a_rs, b_rs, main, t, s);
     case TILE_MEDIUM: return pick<TILE_MEDIUM, true>(a_rs, b_rs, main, t, s);
     default: return pick<TILE_SMALL, true>(a_rs, b_rs, main, t, s);
+  }
+}
+
+void tiles2_bf16(int shape, bool direct, const TileArgs& dx, const TileArgs& dw, bool swapped,
+                 hipStream_t s) {
+  if (!direct) return go2<TILE_SMALL, false>(dx, dw, swapped, s);
+  switch (shape) {
+    case TILE_LARGE: return go2<TILE_LARGE, true>(dx, dw, swapped, s);
+    case TILE_TWO: return go2<TILE_TWO, true>(dx, dw, swapped, s);
+    case TILE_MEDIUM: return go2<TILE_MEDIUM, true>(dx, dw, swapped, s);
+    default: return go2<TILE_SMALL, true>(dx, dw, swapped, s);
   }
 }
 

@@ -23,6 +23,15 @@ void pick(bool a_rs, bool b_rs, bool main, const oc::TileArgs& t, hipStream_t s)
   else go<SHAPE, false, true, false, false>(main, t, s);
 }
 
+template <int SHAPE>
+void go2(const oc::TileArgs& dx, const oc::TileArgs& dw, bool swapped, hipStream_t s) {
+  constexpr oc::TileInfo i = oc::tile_info<float>(SHAPE);
+  constexpr int WGM = i.threads / 64 / (i.bn / 64);
+  const unsigned n = dx.whole + dx.classes * dx.members, m = dw.whole + dw.classes * dw.members;
+  oc::launch_main(oc::k_dense_tiles2<float, i.bm, i.bn, WGM, i.bk, i.nb, false>, dim3(n + m),
+                  dim3(i.threads), s, dx, dw, (uint32_t)(swapped ? n : m), swapped);
+}
+
 }  // namespace
 
 namespace oc {
@@ -33,6 +42,15 @@ void tile_f32(int shape, bool a_rs, bool b_rs, bool main, const TileArgs& t, hip
     case TILE_TWO: return pick<TILE_TWO>(a_rs, b_rs, main, t, s);
     case TILE_MEDIUM: return pick<TILE_MEDIUM>(a_rs, b_rs, main, t, s);
     default: return pick<TILE_SMALL>(a_rs, b_rs, main, t, s);
+  }
+}
+
+void tiles2_f32(int shape, const TileArgs& dx, const TileArgs& dw, bool swapped, hipStream_t s) {
+  switch (shape) {
+    case TILE_LARGE: return go2<TILE_LARGE>(dx, dw, swapped, s);
+    case TILE_TWO: return go2<TILE_TWO>(dx, dw, swapped, s);
+    case TILE_MEDIUM: return go2<TILE_MEDIUM>(dx, dw, swapped, s);
+    default: return go2<TILE_SMALL>(dx, dw, swapped, s);
   }
 }
 

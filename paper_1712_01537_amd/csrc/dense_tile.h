@@ -72,6 +72,9 @@ constexpr TileInfo tile_info(int shape) {
 void tile_f32(int shape, bool a_rs, bool b_rs, bool main, const TileArgs& t, hipStream_t s);
 void tile_bf16(int shape, bool a_rs, bool b_rs, bool direct, bool main, const TileArgs& t,
                hipStream_t s);
+void tiles2_f32(int shape, const TileArgs& dx, const TileArgs& dw, bool swapped, hipStream_t s);
+void tiles2_bf16(int shape, bool direct, const TileArgs& dx, const TileArgs& dw, bool swapped,
+                 hipStream_t s);
 
 // --- device side ---------------------------------------------------------
 
@@ -152,9 +155,21 @@ __host__ __device__ __forceinline__ TilePos tile_pos(int ntm, int ntn, uint32_t 
   return TilePos{(int)(group * 8 + (j - n * rows)), (int)n};
 }
 
+// LDS of a workgroup, in 16-byte vectors: the operands' buffers, or the epilogue's
+// pieces, ROWS rows of 64 sums per wave at a time.
+template <typename T, int BM, int BN, int WGM, int BK, int BUFS, bool DIRECT>
+constexpr int tile_lds() {
+  constexpr int TM = BM / WGM, STAGE = (sizeof(T) == 4 ? 3 : 1) * (BM + BN) * (BK / 8);
+  constexpr int ROWS = TM < 64 ? TM : 64, EPI = WGM * (BN / 64) * ROWS * 16;
+  constexpr int OPS = (DIRECT ? BUFS : 2) * STAGE;
+  return OPS > EPI ? OPS : EPI;
+}
+
+// The work of workgroup `block` of the `blocks` of a product.
 template <typename T, int BM, int BN, int WGM, int BK, int BUFS, bool ARS, bool BRS, bool GLU,
           bool DIRECT, bool DZ>
-__global__ __launch_bounds__(64 * WGM * (BN / 64), 2) void k_dense_tile(TileArgs t) {
+__device__ __forceinline__ void tile_run(const TileArgs& t, uint32_t block, uint32_t blocks,
+                                         s3_v4u* lds) {
   constexpr bool F32 = sizeof(T) == 4;
   static_assert(!(F32 && DIRECT), "fp32 operands are split in registers");
   constexpr int PARTS = F32 ? 3 : 1;
@@ -165,16 +180,14 @@ __global__ __launch_bounds__(64 * WGM * (BN / 64), 2) void k_dense_tile(TileArgs
   static_assert(CA % NTHR == 0 && CB % NTHR == 0 && TM % 16 == 0, "whole vectors per thread");
   static_assert(!(GLU || DZ) || (!ARS && BRS), "the forward's layout");
   constexpr int STAGE = PARTS * (CA + CB), NB = DIRECT ? BUFS : 2;
-  // the epilogue's pieces: ROWS rows of 64 sums per wave at a time
-  constexpr int ROWS = TM < 64 ? TM : 64, EPI = WGM * WGN * ROWS * 16;
-  __shared__ __attribute__((aligned(16))) s3_v4u lds[NB * STAGE > EPI ? NB * STAGE : EPI];
+  constexpr int ROWS = TM < 64 ? TM : 64;  // of the epilogue's pieces
 
   const int n = t.epi.n;
 
   // this workgroup's tile, or its shares of two
-  const bool shared = blockIdx.x >= (uint32_t)t.whole;
-  const uint32_t w = shared ? xcd_order(blockIdx.x - t.whole, gridDim.x - t.whole)
-                            : xcd_order(blockIdx.x, t.whole);
+  const bool shared = block >= (uint32_t)t.whole;
+  const uint32_t w = shared ? xcd_order(block - t.whole, blocks - t.whole)
+                            : xcd_order(block, t.whole);
   const uint32_t cls = shared ? w / t.members : 0, member = w - cls * t.members;
   int64_t unit = cls * t.share;
   const int64_t all = shared ? t.steps * t.run : t.steps;
@@ -675,6 +688,29 @@ __global__ __launch_bounds__(64 * WGM * (BN / 64), 2) void k_dense_tile(TileArgs
   if (DIRECT) dt_wait_vm<0>();  // stores are not counted among the next tile's loads
   dt_barrier();                 // whose operands go where the sums were
   }
+}
+
+template <typename T, int BM, int BN, int WGM, int BK, int BUFS, bool ARS, bool BRS, bool GLU,
+          bool DIRECT, bool DZ>
+__global__ __launch_bounds__(64 * WGM * (BN / 64), 2) void k_dense_tile(TileArgs t) {
+  __shared__ __attribute__((aligned(16))) s3_v4u lds[tile_lds<T, BM, BN, WGM, BK, BUFS, DIRECT>()];
+  tile_run<T, BM, BN, WGM, BK, BUFS, ARS, BRS, GLU, DIRECT, DZ>(t, blockIdx.x, gridDim.x, lds);
+}
+
+// Both products of a backward in one launch: the first `split` workgroups are the
+// weight gradient's (swapped: the input gradient's), the others the other one's.
+template <typename T, int BM, int BN, int WGM, int BK, int BUFS, bool DIRECT>
+__global__ __launch_bounds__(64 * WGM * (BN / 64), 2) void k_dense_tiles2(TileArgs dx, TileArgs dw,
+                                                                          uint32_t split,
+                                                                          bool swapped) {
+  __shared__ __attribute__((aligned(16))) s3_v4u lds[tile_lds<T, BM, BN, WGM, BK, BUFS, DIRECT>()];
+  const bool head = blockIdx.x < split;
+  const uint32_t block = head ? blockIdx.x : blockIdx.x - split;
+  const uint32_t blocks = head ? split : gridDim.x - split;
+  if (head != swapped)
+    tile_run<T, BM, BN, WGM, BK, BUFS, true, true, false, DIRECT, false>(dw, block, blocks, lds);
+  else
+    tile_run<T, BM, BN, WGM, BK, BUFS, false, false, false, DIRECT, false>(dx, block, blocks, lds);
 }
 
 }  // namespace oc

@@ -318,8 +318,10 @@ def test_relu_backward_takes_the_output():
 
 @pytest.mark.parametrize("dt", ["f32", "bf16"])
 def test_parts_asked_for(dt):
-    """Each gradient alone equals the one of the whole call; none of them asked
-    for touches nothing."""
+    """Each gradient alone is that of the whole call, but for the order of its sums
+    (of at most 200 terms: each side within test_large's bound of the exact value);
+    none of them asked for touches nothing."""
+    most = 2 * (U * (4 + 2 * 200 ** 0.5) + (2.0 ** -9 if dt == "bf16" else 0.0))
     c = make(200, 48, 80, dt, "silu", False)
     for again in (False, True):
         _, pre = oc.oc_dense_fwd(c["x"], c["w"], c["b"], act=2, need_pre=True, again=again)
@@ -328,7 +330,8 @@ def test_parts_asked_for(dt):
             need = [j == k for j in range(3)]
             got = oc.oc_dense_bwd(c["x"], c["w"], c["dy"], act=2, pre=pre, need_dx=need[0],
                                   need_dw=need[1], need_db=need[2])
-            assert torch.equal(got[k], every[k]) and sum(g is not None for g in got) == 1
+            assert sum(g is not None for g in got) == 1
+            assert (got[k].double() - every[k].double()).norm() <= most * every[k].double().norm()
 
 
 @pytest.mark.parametrize("dt", ["f32", "bf16"])
