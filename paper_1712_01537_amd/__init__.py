@@ -12,6 +12,7 @@ If ``liboc.so`` is missing or cannot be loaded, every entry point raises
 """
 from __future__ import annotations
 
+import array
 import ctypes as C
 import functools
 import os
@@ -1046,28 +1047,37 @@ def oc_glu_bwd(x, w, dy, pre, act=OC_ACT_SILU, need_dx=True, need_dw=True, need_
 
 def _grad_list(tensors, name):
     """Number, and host arrays of the tensors' addresses, dtype codes and counts.
-    (Per tensor this is what a call costs on the host: one pass for each.)"""
-    n = len(tensors)
-    devs = {t.get_device() for t in tensors}
+    (Per tensor this is what a call costs on the host: one pass in C for each.)"""
+    T = torch.Tensor
+    try:
+        devs = set(map(T.get_device, tensors))
+        contiguous = all(map(T.is_contiguous, tensors))
+    except TypeError:
+        raise OcError(1, f"{name} must be a list of tensors") from None
     if -1 in devs:
         raise OcError(1, f"{name} must be CUDA (HIP) tensors")
     dev = torch._C._cuda_getDevice()
     if not devs <= {dev}:
         raise OcError(1, f"{name} must be on cuda:{dev}, the current device")
-    if False in [t.is_contiguous() for t in tensors]:
+    if not contiguous:
         raise OcError(1, f"{name} must be contiguous")
     try:
-        dts = [_GRAD_CODE[t.dtype] for t in tensors]
+        dts = array.array("i", [_GRAD_CODE[t.dtype] for t in tensors])
     except KeyError:
         raise OcError(1, f"{name} must be float32 or bfloat16 tensors") from None
-    return (n, (C.c_void_p * n)(*[t.data_ptr() for t in tensors]), (C.c_int * n)(*dts),
-            (C.c_int64 * n)(*[t.numel() for t in tensors]))
+    return (len(tensors), array.array("Q", map(T.data_ptr, tensors)), dts,
+            array.array("q", map(T.numel, tensors)))
+
+
+def _at(a):
+    """Address of a host array (kept alive by the caller)."""
+    return a.buffer_info()[0]
 
 
 def _grad_scratch(L, n, counts):
     """The norm and the workspace of a call."""
     dev = torch.device("cuda", torch._C._cuda_getDevice())
-    need = L.oc_grad_workspace(n, counts)
+    need = L.oc_grad_workspace(n, _at(counts))
     return (torch.empty((), dtype=torch.float32, device=dev),
             torch.empty(need, dtype=torch.uint8, device=dev), need)
 
@@ -1080,7 +1090,8 @@ def oc_grad_norm(grads):
     n, ptrs, dts, counts = _grad_list(grads, "grads")
     L = load()
     norm, ws, need = _grad_scratch(L, n, counts)
-    _check(L.oc_grad_norm(n, ptrs, dts, counts, norm.data_ptr(), ws.data_ptr(), need, _stream()))
+    _check(L.oc_grad_norm(n, _at(ptrs), _at(dts), _at(counts), norm.data_ptr(), ws.data_ptr(),
+                          need, _stream()))
     return norm
 
 
@@ -1092,19 +1103,19 @@ def oc_grad_clip(grads, max_norm, outs=None):
     optrs, odts = ptrs, dts
     if outs is not None:
         m, optrs, odts, ocounts = _grad_list(outs, "outs")
-        if m != n or bytes(ocounts) != bytes(counts):
+        if m != n or ocounts != counts:
             raise OcError(1, "outs and grads differ in number or size")
-    if len(set(optrs)) != n:  # (empty tensors may share an address)
-        written = [p for p, c in zip(optrs, counts) if c]
-        if len(set(written)) != len(written):
+    written = set(optrs)
+    if len(written) != n:  # (empty tensors may share an address)
+        some = [p for p, c in zip(optrs, counts) if c]
+        if len(set(some)) != len(some):
             raise OcError(1, "a tensor is to be written twice")
-    if outs is not None:
-        both = set(optrs).intersection(ptrs)
-        if both - {None} and any(c and p in both and p != q
-                                 for p, q, c in zip(optrs, ptrs, counts)):
+    if outs is not None and not written.isdisjoint(ptrs):
+        read = set(ptrs)
+        if any(c and p != q and p in read for p, q, c in zip(optrs, ptrs, counts)):
             raise OcError(1, "an output is another tensor's gradient")
     L = load()
     norm, ws, need = _grad_scratch(L, n, counts)
-    _check(L.oc_grad_clip(n, ptrs, dts, counts, max_norm, optrs, odts, norm.data_ptr(),
-                          ws.data_ptr(), need, _stream()))
+    _check(L.oc_grad_clip(n, _at(ptrs), _at(dts), _at(counts), max_norm, _at(optrs), _at(odts),
+                          norm.data_ptr(), ws.data_ptr(), need, _stream()))
     return norm
