@@ -909,10 +909,11 @@ def _dense_dims(x, w, halves):
     for name, t in (("x", x), ("w", w)):
         if not isinstance(t, torch.Tensor) or not t.is_cuda:
             raise OcError(1, f"{name} must be a CUDA (HIP) tensor")
-    if x.dim() != 2 or w.dim() != 2 or w.shape[0] != x.shape[1] or w.shape[1] % halves:
-        raise OcError(1, f"x {tuple(x.shape)} and w {tuple(w.shape)} do not go together")
-    rows, cin = x.shape
-    nz = w.shape[1]
+    xs, ws = x.shape, w.shape
+    if len(xs) != 2 or len(ws) != 2 or ws[0] != xs[1] or ws[1] % halves:
+        raise OcError(1, f"x {tuple(xs)} and w {tuple(ws)} do not go together")
+    rows, cin = xs
+    nz = ws[1]
     return torch._C._cuda_getDevice(), rows, cin, nz // halves, nz
 
 
@@ -964,7 +965,7 @@ def _layer_fwd(glu, x, w, b, res, act, need_pre, again):
     xp, wp = _given(x, "x", dev, t, (rows, cin)), _given(w, "w", dev, t, (cin, nz))
     bp = _given(b, "b", dev, torch.float32, (nz,))
     rp = _given(res, "res", dev, t, (rows, cout))
-    y = torch.empty((rows, cout), dtype=t, device=x.device)
+    y = x.new_empty((rows, cout))
     pre = pp = None
     if need_pre:
         if _again(glu, act, dt, rows, cin, cout) if again is None else again:
@@ -999,7 +1000,7 @@ def _layer_bwd(glu, x, w, dy, pre, act, need_dx, need_dw, need_db, dw, db, dw_dt
         yp = _given(pre, "pre", dev, t, (rows, nz))  # the forward's output
     else:
         pp = _given(pre, "pre", dev, *_pre_kind(glu, act, rows, nz))
-    dx = torch.empty((rows, cin), dtype=t, device=x.device) if need_dx else None
+    dx = x.new_empty((rows, cin)) if need_dx else None
     if dw is None and need_dw:
         dw = torch.empty((cin, nz), dtype=dw_dtype or torch.float32, device=x.device)
     if db is None and need_db:

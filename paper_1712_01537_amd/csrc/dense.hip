@@ -6,7 +6,7 @@
 // | du]) is written once, in the type of the products' operands, and read by
 // both of them: dx = dz w^T and dw = x^T dz.  Forming dz inside the products
 // instead would read z (fp32) and dy once per tile column of each.  In bf16
-// that rounds dz once (half a step, 2^-9), as the matrix cores' operand has to
+// that rounds dz once (half a step, 2^-8), as the matrix cores' operand has to
 // be; z itself is kept in fp32, since a rounded z would move the slope and so
 // round the gradients a second time.  dbias is summed from the unrounded dz in
 // the same pass.
