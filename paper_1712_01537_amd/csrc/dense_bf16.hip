@@ -52,7 +52,6 @@ void tiles2_bf16(int shape, bool direct, const TileArgs& dx, const TileArgs& dw,
   if (!direct) return go2<TILE_SMALL, false>(dx, dw, swapped, s);
   switch (shape) {
     case TILE_LARGE: return go2<TILE_LARGE, true>(dx, dw, swapped, s);
-    case TILE_TWO: return go2<TILE_TWO, true>(dx, dw, swapped, s);
     case TILE_MEDIUM: return go2<TILE_MEDIUM, true>(dx, dw, swapped, s);
     default: return go2<TILE_SMALL, true>(dx, dw, swapped, s);
   }

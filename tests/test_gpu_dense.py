@@ -238,6 +238,38 @@ def test_large(i, dt, glu, again):
         assert far <= 64 * most, (what, far, most)
 
 
+# Backwards whose two products share a launch: the tile shapes and, of either product,
+# whole and split reductions, in both orders (on a card of 256 CUs).
+TOGETHER = [("bf16", 26680, 1968, 3664), ("bf16", 20680, 960, 2272), ("bf16", 2137, 1200, 1672),
+            ("bf16", 934, 1744, 1480), ("bf16", 2597, 976, 96), ("bf16", 6055, 360, 208),
+            ("bf16", 71, 936, 2288), ("bf16", 4612, 120, 2776), ("bf16", 35, 8, 88),
+            ("bf16", 718, 8, 72), ("bf16", 35, 96, 624), ("bf16", 33, 1656, 1648),
+            ("bf16", 2125, 8, 1040), ("bf16", 2177, 24, 2936), ("bf16", 1500, 203, 77),
+            ("f32", 4151, 920, 3288), ("f32", 1355, 1504, 1640), ("f32", 1640, 1992, 264),
+            ("f32", 1296, 2000, 216), ("f32", 221, 880, 3200), ("f32", 155, 1960, 1704),
+            ("f32", 1168, 200, 1824), ("f32", 1467, 240, 2176), ("f32", 801, 1760, 592),
+            ("f32", 426, 1904, 920), ("f32", 3092, 456, 8), ("f32", 1731, 784, 416),
+            ("f32", 242, 1168, 1136), ("f32", 405, 80, 1760), ("f32", 1178, 1872, 728),
+            ("f32", 895, 1808, 80), ("f32", 1428, 848, 216), ("f32", 116, 1632, 1096),
+            ("f32", 625, 224, 1384), ("f32", 2071, 504, 1288), ("f32", 33, 8, 104),
+            ("f32", 238, 24, 40), ("f32", 35, 448, 3640), ("f32", 678, 24, 1152),
+            ("f32", 397, 33, 205)]
+
+
+@pytest.mark.parametrize("dt,rows,cin,cout", TOGETHER)
+def test_both_products(dt, rows, cin, cout):
+    """test_large's bounds, one rounding of each result (dz is dy)."""
+    c = make(rows, cin, cout, dt, "none", False)
+    x, w, dy = c["x"].double(), c["w"].double(), c["dy"].double()
+    got = oc.oc_dense_bwd(c["x"], c["w"], c["dy"], dw_dtype=DT[dt])
+    for p, r, terms in ((got[0], dy @ w.T, cout), (got[1], x.T @ dy, rows),
+                        (got[2], dy.sum(0), 0)):
+        most = U * (4 + 2 * (terms or rows) ** 0.5) + (2.0 ** -9 if dt == "bf16" and terms else 0.0)
+        assert float((p.double() - r).norm() / r.norm()) <= most
+        far = float((p.double() - r).abs().max() / (r.abs() + r.square().mean().sqrt()).max())
+        assert far <= 64 * most
+
+
 @pytest.mark.parametrize("dt", ["f32", "bf16"])
 @pytest.mark.parametrize("rows,cin,cout,glu", [(70, 65536, 3, False), (70, 3, 65536, False),
                                                (3, 65536, 5, False), (2, 5, 65536, False),
