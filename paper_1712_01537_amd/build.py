@@ -78,6 +78,43 @@ def scratch_fault(text: str, remarks: str) -> str:
     return ""
 
 
+def _asm_statements(text: str) -> list:
+    """A source's assembly statements, to their closing brackets (strings hold none
+    that count)."""
+    out = []
+    for m in re.finditer(r"\basm\b(?:\s+volatile)?\s*\(", text):
+        depth, end = 1, m.end()
+        for t in re.finditer(r'"(?:[^"\\]|\\.)*"|[()]', text[m.end():]):
+            depth += {"(": 1, ")": -1}.get(t.group(), 0)
+            if depth == 0:
+                end = m.end() + t.end()
+                break
+        out.append(text[m.start():end])
+    return out
+
+
+def asm_fault(text: str) -> str:
+    """What is wrong with a source's assembly statements; "" for nothing.  One that
+    writes m0 (the address of a load to LDS) has to say so: the compiler keeps values
+    of its own there, and would go on using one across the statement."""
+    for a in _asm_statements(text):
+        if re.search(r"\bs_\w+ m0\b", a) and '"m0"' not in a:
+            return f"writes m0 without declaring it: {' '.join(a.split())}"
+    return ""
+
+
+def _sources() -> list:
+    return sorted(glob.glob(os.path.join(CSRC, "*.hip")) + glob.glob(os.path.join(CSRC, "*.h")))
+
+
+def check_asm() -> None:
+    for src in _sources():
+        with open(src) as fh:
+            why = asm_fault(fh.read())
+        if why:
+            raise RuntimeError(f"{src}: {why}")
+
+
 def _compile(src: str) -> str:
     obj = os.path.join(OBJ, os.path.basename(src) + ".o")
     cmd = [HIPCC, *FLAGS, "-Rpass-analysis=kernel-resource-usage", "-c", src, "-o", obj]
@@ -93,6 +130,7 @@ def _compile(src: str) -> str:
 
 
 def build(verbose: bool = False) -> str:
+    check_asm()
     os.makedirs(OBJ, exist_ok=True)
     srcs = sorted(glob.glob(os.path.join(CSRC, "*.hip")))
     with cf.ThreadPoolExecutor(max_workers=min(8, len(srcs))) as ex:
