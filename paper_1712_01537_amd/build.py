@@ -96,10 +96,16 @@ def _asm_statements(text: str) -> list:
 def asm_fault(text: str) -> str:
     """What is wrong with a source's assembly statements; "" for nothing.  One that
     writes m0 (the address of a load to LDS) has to say so: the compiler keeps values
-    of its own there, and would go on using one across the statement."""
+    of its own there, and would go on using one across the statement.  And a load to LDS
+    needs an instruction between the write of m0 and itself: the hardware does not wait,
+    and the compiler, which puts an s_nop between its own, does not look into statements."""
     for a in _asm_statements(text):
         if re.search(r"\bs_\w+ m0\b", a) and '"m0"' not in a:
             return f"writes m0 without declaring it: {' '.join(a.split())}"
+        lines = "".join(re.findall(r'"((?:[^"\\]|\\.)*)"', a)).replace("\\t", " ").split("\\n")
+        for first, then in zip(lines, lines[1:]):
+            if re.match(r"\s*s_\w+ m0\b", first) and re.search(r" lds|_lds_", then):
+                return f"loads to LDS right behind the write of m0: {' '.join(a.split())}"
     return ""
 
 

@@ -75,7 +75,7 @@ __device__ __forceinline__ uint32_t lds_addr(const void* lds) {
 // the compiler's wait counting stays exact for the code around it; the
 // caller waits for completion (vm_wait0) before other waves read the data.
 __device__ __forceinline__ void lds_load16(const void* src, uint32_t lds) {
-  asm volatile("s_mov_b32 m0, %0\n\tglobal_load_lds_dwordx4 %1, off" ::"s"(lds), "v"(src)
+  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off" ::"s"(lds), "v"(src)
                : "memory", "m0");
 }
 // Buffer resource over `bytes` bytes at p (raw: offsets in bytes, no stride);
@@ -94,13 +94,13 @@ __device__ __forceinline__ sv4 buf_rsrc(const void* p, uint32_t bytes) {
 // offset off of the resource land at lds + 16 i; an offset past the end
 // stores zeros.
 __device__ __forceinline__ void lds_bload16(sv4 rsrc, uint32_t off, uint32_t lds) {
-  asm volatile("s_mov_b32 m0, %0\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds" ::"s"(lds), "v"(off),
-               "s"(rsrc)
+  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds" ::"s"(lds),
+               "v"(off), "s"(rsrc)
                : "memory", "m0");
 }
 // The same for 4 bytes per lane (lane i's dword lands at lds + 4 i).
 __device__ __forceinline__ void lds_load4(const void* src, uint32_t lds) {
-  asm volatile("s_mov_b32 m0, %0\n\tglobal_load_lds_dword %1, off" ::"s"(lds), "v"(src)
+  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dword %1, off" ::"s"(lds), "v"(src)
                : "memory", "m0");
 }
 // s_waitcnt vmcnt(0): all of this wave's vector memory operations are done.

@@ -49,15 +49,15 @@ __device__ __forceinline__ uint32_t lds_addr(const void* lds) {
 // Direct global->LDS loads: lane i's bytes land at LDS byte address
 // lds + 16 i (16 or 12 bytes) or lds + 4 i (4 bytes); lds is wave-uniform.
 __device__ __forceinline__ void lds_load16(const void* src, uint32_t lds) {
-  asm volatile("s_mov_b32 m0, %0\n\tglobal_load_lds_dwordx4 %1, off" ::"s"(lds), "v"(src)
+  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off" ::"s"(lds), "v"(src)
                : "memory", "m0");
 }
 __device__ __forceinline__ void lds_load12(const void* src, uint32_t lds) {
-  asm volatile("s_mov_b32 m0, %0\n\tglobal_load_lds_dwordx3 %1, off" ::"s"(lds), "v"(src)
+  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx3 %1, off" ::"s"(lds), "v"(src)
                : "memory", "m0");
 }
 __device__ __forceinline__ void lds_load4(const void* src, uint32_t lds) {
-  asm volatile("s_mov_b32 m0, %0\n\tglobal_load_lds_dword %1, off" ::"s"(lds), "v"(src)
+  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dword %1, off" ::"s"(lds), "v"(src)
                : "memory", "m0");
 }
 // 16-byte store from inline assembly (counted like the loads by the waits).

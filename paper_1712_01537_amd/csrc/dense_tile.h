@@ -131,8 +131,8 @@ __device__ __forceinline__ Split8 dt_split8(const s3_v4f& x, const s3_v4f& y) {
 // Memory to LDS: lane i's 16 bytes at byte `off` of the resource land at lds +
 // 16 i; an offset past the resource's end stores zeros.
 __device__ __forceinline__ void dt_lds_load16(dt_sv4 rsrc, uint32_t off, uint32_t lds) {
-  asm volatile("s_mov_b32 m0, %0\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds" ::"s"(lds), "v"(off),
-               "s"(rsrc)
+  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds" ::"s"(lds),
+               "v"(off), "s"(rsrc)
                : "memory", "m0");
 }
 constexpr uint32_t kPastEnd = 0x80000000u;  // of any resource

@@ -3,8 +3,8 @@ import pytest
 
 from paper_1712_01537_amd import build
 
-LOAD = ('asm volatile("s_mov_b32 m0, %%0\\n\\tbuffer_load_dwordx4 %%1, %%2, 0 offen lds" ::"s"(lds), '
-        '"v"(off),\n               "s"(f(rsrc))\n               : "memory"%s);')
+LOAD = ('asm volatile("s_mov_b32 m0, %%0\\n\\ts_nop 0\\n\\tbuffer_load_dwordx4 %%1, %%2, 0 offen lds" '
+        '::"s"(lds), "v"(off),\n               "s"(f(rsrc))\n               : "memory"%s);')
 
 
 @pytest.mark.parametrize("text,word", [
@@ -18,6 +18,15 @@ LOAD = ('asm volatile("s_mov_b32 m0, %%0\\n\\tbuffer_load_dwordx4 %%1, %%2, 0 of
 def test_m0_is_declared(text, word):
     why = build.asm_fault(text)
     assert bool(why) == bool(word) and word in why
+
+
+@pytest.mark.parametrize("load", ["buffer_load_dwordx4 %1, %2, 0 offen lds",
+                                  "global_load_lds_dword %1, off"])
+def test_a_wait_state_behind_m0(load):
+    text = 'asm volatile("s_mov_b32 m0, %0\\n\\t" "' + load + '" ::"s"(a), "v"(b) : "m0");'
+    assert "right behind" in build.asm_fault(text)
+    assert build.asm_fault(text.replace('\\n\\t" "', '\\n\\ts_nop 0\\n\\t"\n"')) == ""
+    assert build.asm_fault('asm("s_mov_b32 m0, %0\\n\\tv_mov_b32 %1, 0" ::"s"(a) : "m0");') == ""
 
 
 def test_every_source():
