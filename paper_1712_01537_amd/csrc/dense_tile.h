@@ -143,6 +143,18 @@ __device__ __forceinline__ dt_sv4 dt_rsrc(const char* p, int64_t bytes) {
                 (int32_t)(bytes < 0 ? 0 : bytes < most ? bytes : most), 0x00020000};
 }
 
+// Terms r .. r + 3 of row or column `at` of an fp32 operand (RS: stored across the
+// reduction); those from `end` on read as zero.
+template <bool RS>
+__device__ __forceinline__ s3_v4f dt_terms(const float* m, int64_t ld, int64_t at, int64_t r,
+                                           int64_t end) {
+  if (!RS && r + 4 <= end) return *(const d_v4f_any*)(m + at * ld + r);
+  s3_v4f v;
+#pragma unroll
+  for (int e = 0; e < 4; ++e) v[e] = r + e < end ? m[RS ? (r + e) * ld + at : at * ld + r + e] : 0.f;
+  return v;
+}
+
 // Row and column of tile i: groups of eight rows of tiles, so that the tiles an XCD
 // works on at a time share operands in its L2.
 struct TilePos {
@@ -599,26 +611,70 @@ __device__ __forceinline__ void tile_run(const TileArgs& t, uint32_t block, uint
             s3_v4u, F32 ? acc[pass * (ROWS / 16) + i][j] * kSplitDown : acc[pass * (ROWS / 16) + i][j]);
     if constexpr (F32) {
       // What the three parts cannot represent is formed again in plain fp32 (operands
-      // of 2^103 and more, sums of 2^80 and more, infinities, NaN).
+      // of 2^103 and more, sums of 2^80 and more, infinities, NaN): sixteen rows that hold
+      // such a sum by 64 columns at a time, with fp32 MFMAs, and of those results the ones
+      // that are not finite replaced.  (35472 x 512 -> 1024 with one NaN weight, which
+      // every row tile meets: forward 399 us, 224 without; a lane a result took 4340.)
       bool bad = false;
 #pragma unroll
       for (int i = 0; i < ROWS / 16; ++i)
 #pragma unroll
         for (int j = 0; j < NI; ++j) bad |= s3_bad(acc[pass * (ROWS / 16) + i][j]);
-      if (__any(bad))
-        for (int x = lane; x < ROWS * 64; x += 64) {
-          const int row = x >> 6, col = x & 63;
-          const int64_t p = p0 + wm * TM + pass * ROWS + row;
-          const int cc = GLU ? q0 + wn * 32 + (col & 31) : q0 + wn * 64 + col;
-          float* const v = (float*)&mine[row * 16 + ((col >> 2) ^ (row & 15))] + (col & 3);
-          if (fabsf(*v) < INFINITY || p >= t.P || cc >= n) continue;
-          const int qc = GLU && col >= 32 ? cc + t.half : cc;
-          float z = 0.f;
-          for (int64_t r = r0; r < r1; ++r)
-            z = fmaf(((const float*)t.a)[ARS ? r * t.lda + p : p * t.lda + r],
-                     ((const float*)t.b)[BRS ? r * t.ldb + qc : qc * t.ldb + r], z);
-          *v = z;
+      if (__any(bad)) {
+        const int64_t p = p0 + wm * TM + pass * ROWS + li;
+        int cols16[NI];  // this lane's first column of an MFMA's sixteen, and in B column li
+        int64_t bcol[NI];
+#pragma unroll
+        for (int j = 0; j < NI; ++j) {
+          const int first = GLU ? q0 + wn * 32 + (j & 1) * 16 : q0 + wn * 64 + j * 16;
+          cols16[j] = first + 4 * q;
+          bcol[j] = (first + li < n ? first + li : n - 1) + (GLU && j > 1 ? t.half : 0);
         }
+#pragma unroll 1
+        for (int i = 0; i < ROWS / 16; ++i) {
+          const auto at = [&](int j) __attribute__((always_inline)) {
+            return (i * 16 + li) * 16 + ((j * 4 + q) ^ li);
+          };
+          bool again = false;
+#pragma unroll
+          for (int j = 0; j < NI; ++j)
+#pragma unroll
+            for (int k = 0; k < 4; ++k)
+              again |= p + i * 16 < t.P && cols16[j] + k < n &&
+                       !(fabsf(__builtin_bit_cast(s3_v4f, mine[at(j)])[k]) < INFINITY);
+          if (!__any(again)) continue;
+          const int64_t row = p + i * 16 < t.P ? p + i * 16 : t.P - 1;
+          s3_v4f sum[NI], fa, fb[NI], na, nb[NI];
+          const auto load = [&](int64_t r, s3_v4f& x, s3_v4f(&y)[NI]) __attribute__((always_inline)) {
+            x = dt_terms<ARS>((const float*)t.a, t.lda, row, r + 4 * q, r1);
+#pragma unroll
+            for (int j = 0; j < NI; ++j)
+              y[j] = dt_terms<BRS>((const float*)t.b, t.ldb, bcol[j], r + 4 * q, r1);
+          };
+#pragma unroll
+          for (int j = 0; j < NI; ++j) sum[j] = s3_v4f{0.f, 0.f, 0.f, 0.f};
+          load(r0, fa, fb);
+#pragma unroll 1
+          for (int64_t r = r0; r < r1; r += 16) {  // term 4 q + e of the sixteen in MFMA e
+            load(r + 16, na, nb);
+#pragma unroll
+            for (int e = 0; e < 4; ++e)
+#pragma unroll
+              for (int j = 0; j < NI; ++j)
+                sum[j] = __builtin_amdgcn_mfma_f32_16x16x4f32(fb[j][e], fa[e], sum[j], 0, 0, 0);
+            fa = na;
+#pragma unroll
+            for (int j = 0; j < NI; ++j) fb[j] = nb[j];
+          }
+#pragma unroll
+          for (int j = 0; j < NI; ++j) {
+            s3_v4f v = __builtin_bit_cast(s3_v4f, mine[at(j)]);
+#pragma unroll
+            for (int k = 0; k < 4; ++k) v[k] = fabsf(v[k]) < INFINITY ? v[k] : sum[j][k];
+            mine[at(j)] = __builtin_bit_cast(s3_v4u, v);
+          }
+        }
+      }
     }
 #pragma unroll 1
     for (int g = 0; g < ROWS / (RI * U); ++g) {

@@ -1,0 +1,89 @@
+"""GPU tests of the dense layers and of clipping at their edges: operands that are not
+finite or far from 1, small results, long sums, overlapping outputs, calls from two threads.
+
+Bounds as in test_gpu_dense.py (u = 2^-24): a sum of R products in fp32, in any order, is
+off by at most (R + 4) u S, S the sum of the products' absolute values."""
+import math
+
+import pytest
+import torch
+
+import paper_1712_01537_amd as oc
+
+pytestmark = pytest.mark.gpu
+
+U = 2.0 ** -24
+
+
+def normal(shape, seed, scale=1.0):
+    g = torch.Generator(device="cuda")
+    g.manual_seed(seed)
+    return torch.empty(shape, device="cuda").normal_(generator=g) * scale
+
+
+def product_check(got, a, b, what):
+    """got against a b in 64 bits: NaN and infinities where those are, else within the
+    bound."""
+    ref = a.double() @ b.double()
+    tol = (a.shape[1] + 4) * U * (a.double().abs() @ b.double().abs())
+    assert torch.equal(torch.isnan(got), torch.isnan(ref)), what
+    inf = torch.isinf(ref)
+    assert torch.equal(got[inf].double(), ref[inf]), what
+    fin = torch.isfinite(ref)
+    assert ((got.double() - ref)[fin].abs() <= tol[fin]).all(), what
+
+
+# Sizes of every tile shape, with whole and shared reductions and ragged edges.
+ODD = [(70, 37, 50), (300, 72, 65), (517, 130, 259), (2100, 96, 200), (1300, 520, 1031),
+       (9000, 48, 130), (12000, 515, 260)]
+
+
+@pytest.mark.parametrize("rows,cin,cout", ODD)
+def test_fp32_operands_that_no_parts_hold(rows, cin, cout):
+    """Infinities, NaN and values of 2^110 here and there: each result is what its own
+    sum is in fp32, in y, dx and dw."""
+    x, w = normal((rows, cin), 1), normal((cin, cout), 2, cin ** -0.5)
+    dy = normal((rows, cout), 3)
+    for t, big in ((x, 2.0 ** 110), (w, 2.0 ** -12), (dy, -(2.0 ** 12))):
+        at = torch.randint(0, t.numel(), (3,), generator=torch.Generator().manual_seed(rows))
+        t.view(-1)[at[0]] = big
+        t.view(-1)[at[1]] = -math.inf
+        t.view(-1)[at[2]] = math.nan
+    x[rows - 1, cin - 1] = 2.0 ** 110
+    y, _ = oc.oc_dense_fwd(x, w)
+    product_check(y, x, w, "y")
+    dx, dw, _ = oc.oc_dense_bwd(x, w, dy)
+    product_check(dx, dy, w.t().contiguous(), "dx")
+    product_check(dw, x.t().contiguous(), dy, "dw")
+    if cout % 2 == 0:  # gated: y = g u with no activation
+        z = x.double() @ w.double()
+        ref = z[:, :cout // 2] * z[:, cout // 2:]
+        got = oc.oc_glu_fwd(x, w, act=oc.OC_ACT_NONE)[0]
+        # (a product of two sums of 2^110 and more passes fp32's largest value)
+        ref = torch.where(ref.abs() > 3.4e38, ref.sign() * math.inf, ref)
+        assert torch.equal(torch.isnan(got), torch.isnan(ref))
+        assert torch.equal(torch.isinf(got), torch.isinf(ref))
+
+
+def micros(f):
+    f()
+    best = math.inf
+    for _ in range(5):
+        a, b = (torch.cuda.Event(enable_timing=True) for _ in range(2))
+        a.record()
+        f()
+        b.record()
+        torch.cuda.synchronize()
+        best = min(best, a.elapsed_time(b) * 1e3)
+    return best
+
+
+def test_one_nan_weight_does_not_hold_up_a_layer():
+    """Forming a column's results again is a few times the layer's work at most (one
+    lane a result took 40 times the forward and 30 times the backward)."""
+    x, w, dy = normal((8192, 256), 1), normal((256, 512), 2, 0.0625), normal((8192, 512), 3)
+    for f in (lambda: oc.oc_dense_fwd(x, w), lambda: oc.oc_dense_bwd(x, w, dy)):
+        w[3, 5] = 0.5
+        plain = micros(f)
+        w[3, 5] = math.nan
+        assert micros(f) <= 10 * plain
