@@ -87,3 +87,31 @@ def test_one_nan_weight_does_not_hold_up_a_layer():
         plain = micros(f)
         w[3, 5] = math.nan
         assert micros(f) <= 10 * plain
+
+
+@pytest.mark.parametrize("dt", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("rows", [6, 40_000])
+def test_gelu_keeps_the_digits_of_small_values(rows, dt):
+    """z Phi(z) and its slope relative to themselves at negative z.  One channel of weight
+    1 makes z exactly x, and dx exactly dz = dy act'(z) with dy = 1.
+
+    Phi(-|z|) is off by at most (22 + 1.5 z^2) u of itself: the reciprocal and its operand
+    3 u, stretched by at most 0.8 / 0.3; the fit 3 u; eight steps of a polynomial whose
+    terms sum to at most twice its value 5 u; e^(-z^2/2) 2 u and 3 u of z^2 / 2; products
+    2 u.  y adds one more rounding, the slope's two terms two each."""
+    x = -torch.linspace(0.02, 12.0, rows, device="cuda")[:, None].to(dt)
+    one, dy = torch.ones((1, 1), device="cuda", dtype=dt), torch.ones_like(x)
+    z = x.double()
+    phi = torch.exp(-0.5 * z * z) / math.sqrt(2.0 * math.pi)
+    tail = 0.5 * torch.special.erfc(-z * math.sqrt(0.5))
+    rnd = 2.0 ** -8 if dt == torch.bfloat16 else 0.0
+    rel = (24 + 2 * z * z) * U
+    y, pre = oc.oc_dense_fwd(x, one, act=oc.OC_ACT_GELU, need_pre=True, again=False)
+    ref = z * tail
+    assert ((y.double() - ref).abs() <= (rel + rnd + rel * rnd) * ref.abs()).all()
+    for kept in (pre, oc.Again(None)):
+        dx, dw, db = oc.oc_dense_bwd(x, one, dy, act=oc.OC_ACT_GELU, pre=kept)
+        ref = tail + z * phi
+        off = rel * (tail + z.abs() * phi)
+        # (bf16: dz is rounded, dx holds it)
+        assert ((dx.double() - ref).abs() <= off + rnd * (ref.abs() + off)).all()
