@@ -119,19 +119,24 @@ __global__ __launch_bounds__(TB) void k_clip(Table t, const double* part, int n,
                                              float* norm) {
   const double r = sqrt(total_of(part, n));
   if (norm && blockIdx.x == 0 && threadIdx.x == 0) *norm = (float)r;
-  const float c = r <= max_norm ? 1.f : (float)(max_norm / r);
+  // The factor as c 2^e, 0.5 <= c < 1 (or 1, 0, NaN): one below fp32's normal numbers (a
+  // norm of 10^37 clipped to 0.1) would have few bits or none as an fp32 value.
+  const bool within = r <= max_norm;
+  const double factor = max_norm / r;
+  const int e2 = within ? 0 : __builtin_amdgcn_frexp_exp(factor);
+  const float c = within ? 1.f : (float)__builtin_amdgcn_frexp_mant(factor);
   for_chunks<true>(
       t,
       [&](int i, int64_t e, int64_t cnt, float(&v)[8]) {
         // nothing changes: gradients scaled in place by one
-        if (c == 1.f && t.in[i] == t.out[i]) return;
+        if (within && t.in[i] == t.out[i]) return;
         load_in(t, i, e, cnt, v);
       },
       [&](int i, int64_t e, int64_t cnt, float(&v)[8]) {
-        if ((c == 1.f && t.in[i] == t.out[i]) || e >= cnt) return;
-        if (c != 1.f) {
+        if ((within && t.in[i] == t.out[i]) || e >= cnt) return;
+        if (!within) {
 #pragma unroll
-          for (int k = 0; k < 8; ++k) v[k] *= c;
+          for (int k = 0; k < 8; ++k) v[k] = __builtin_amdgcn_ldexpf(v[k] * c, e2);
         }
         oc::store8n(t.out[i], t.out_bf16[i], e, (int)(cnt - e < 8 ? cnt - e : 8), v);
       });

@@ -115,3 +115,25 @@ def test_gelu_keeps_the_digits_of_small_values(rows, dt):
         off = rel * (tail + z.abs() * phi)
         # (bf16: dz is rounded, dx holds it)
         assert ((dx.double() - ref).abs() <= off + rnd * (ref.abs() + off)).all()
+
+
+@pytest.mark.parametrize("most", [0.1, 1e-6, 1e-20])
+@pytest.mark.parametrize("size", [1e37, 1e38, 3e38])
+def test_clipping_of_huge_gradients(size, most):
+    """max_norm / norm lies below fp32's normal numbers, or below all of its numbers,
+    while the clipped values are ordinary: off by the rounding of the factor and of the
+    product (in fp32 by 2 u, in double by 1)."""
+    n = 10_007
+    g = torch.Generator("cuda").manual_seed(1)
+    base = [torch.empty(n, device="cuda").uniform_(-1, 1, generator=g) * size,
+            normal(300, 2, size / 8).to(torch.bfloat16), torch.full((3,), size, device="cuda")]
+    norm = torch.cat([g.double() for g in base]).norm()
+    for place in (False, True):
+        grads = [g.clone() for g in base]
+        outs = grads if place else [torch.empty(g.numel(), device="cuda") for g in grads]
+        oc.oc_grad_clip(grads, most, outs=None if place else outs)
+        for g, o in zip(base, outs):
+            ref = g.double() * (most / norm)
+            rnd = 2.0 ** -8 if o.dtype == torch.bfloat16 else 0.0
+            # (values below fp32's normal numbers are off by half of its smallest one)
+            assert ((o.double() - ref).abs() <= (2.1 * U + rnd) * ref.abs() + 1e-45).all()
