@@ -614,7 +614,8 @@ oc_status oc_dense_fwd(oc_dtype dt, int32_t act, int64_t rows, int32_t cin, int3
  *   dw      dev [cin][cout] or NULL, of type dw_dt: OC_F32 or dt.
  *   dbias   dev f32 [cout] or NULL.
  * OC_BF16: dz is rounded to bf16 (the operand of dx and dw), as oc_conv_bwd's dy
- * is; dbias is summed from the values before that.  With rows 0, dw and dbias
+ * is; dbias is summed from the values before that.  dbias is summed in fp32 over at
+ * most 64 rows at a time and in double from there.  With rows 0, dw and dbias
  * are 0. */
 size_t oc_dense_bwd_workspace(oc_dtype dt, int32_t act, int64_t rows, int32_t cin, int32_t cout);
 oc_status oc_dense_bwd(oc_dtype dt, int32_t act, int64_t rows, int32_t cin, int32_t cout,

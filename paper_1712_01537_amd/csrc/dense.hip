@@ -24,10 +24,12 @@ constexpr int TB = 256;
 //
 // A thread has eight columns and every rl-th row of the block's range; block
 // (b, k) has rows M b / nb .. and columns 8 ct k ..  Column sums: per thread
-// fp32 over its rows (about 30), then the row lanes in order through LDS into
-// part[b][column], then k_colsum in double over the blocks: a fixed order.
+// fp32 over its rows (at most MOST_ADDED, whatever M is: as many blocks as that takes),
+// then in double the row lanes in order through LDS into part[b][column] and, by
+// k_colsum, the blocks: a fixed order.
 // Bound by memory: dy and z read, dz written (65536 x 4096 bf16 ReLU from y 346 us, 4.7
 // TB/s; 32768 x 2816 bf16 gated 288 us, 4.5 TB/s).
+constexpr int64_t MOST_ADDED = 64;
 struct DzShape {
   int ct, rl, kb, nb;  // column threads, row lanes, column blocks, row blocks
 };
@@ -39,7 +41,7 @@ DzShape dz_shape(int64_t M, int n) {
   d.rl = TB / d.ct;
   d.kb = (int)cdiv(chunks, d.ct);
   const int64_t most = std::max<int64_t>(64, 2048 / d.kb);
-  d.nb = (int)std::max<int64_t>(1, std::min<int64_t>(most, cdiv(M, 4 * d.rl)));
+  d.nb = (int)std::max(std::min<int64_t>(most, cdiv(M, 4 * d.rl)), cdiv(M, MOST_ADDED * d.rl));
   return d;
 }
 
@@ -115,9 +117,9 @@ __global__ __launch_bounds__(TB) void k_dz(const void* dy, const void* z, bool b
     const int cc = blockIdx.y * ct * 8 + i;
     if (cc >= n) continue;
     for (int h = 0; h < (GLU ? 2 : 1); ++h) {
-      float a = 0.f;
-      for (int r = 0; r < rl; ++r) a += red[h][i & 7][r * ct + (i >> 3)];
-      part[(int64_t)b * nz + h * n + cc] = a;
+      double a = 0.0;
+      for (int r = 0; r < rl; ++r) a += (double)red[h][i & 7][r * ct + (i >> 3)];
+      part[(int64_t)b * nz + h * n + cc] = (float)a;
     }
   }
 }

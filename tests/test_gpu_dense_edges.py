@@ -137,3 +137,15 @@ def test_clipping_of_huge_gradients(size, most):
             rnd = 2.0 ** -8 if o.dtype == torch.bfloat16 else 0.0
             # (values below fp32's normal numbers are off by half of its smallest one)
             assert ((o.double() - ref).abs() <= (2.1 * U + rnd) * ref.abs() + 1e-45).all()
+
+
+def test_dbias_of_very_many_rows():
+    """At most 64 values are added up in fp32 (63 roundings), the rest in double (each
+    partial sum and the result rounded once).  The value is one whose sum in fp32 loses
+    2^-16 with every term from the 256th on: 500 in a row are off by 125 u."""
+    rows = 500 * 2048 * 256
+    v = 1.0 + 2.0 ** -16 - 2.0 ** -23
+    x = torch.zeros((rows, 1), device="cuda")
+    dy = torch.full((rows, 1), v, device="cuda")
+    db = oc.oc_dense_bwd(x, x[:1], dy, need_dx=False, need_dw=False)[2]
+    assert abs(float(db.double()) - rows * v) <= 65 * U * rows * v
