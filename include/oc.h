@@ -602,7 +602,8 @@ oc_status oc_dense_fwd(oc_dtype dt, int32_t act, int64_t rows, int32_t cin, int3
 
 /* Gradients of oc_dense_fwd: with dz = dy act'(x w + bias),
  *   dx = dz w^T, dw = x^T dz, dbias = the sum of dz over the rows
- * (the residual's gradient is dy itself).
+ * (the residual's gradient is dy itself).  OC_ACT_RELU masks: dz is dy where x w +
+ * bias > 0 and 0 elsewhere, whatever dy holds there.
  *   pre     what oc_dense_fwd left there; not read for OC_ACT_NONE.  NULL: x w +
  *           bias is formed once more, which needs no memory between the passes and
  *           for few input channels and many values less time.

@@ -108,7 +108,7 @@ __device__ __forceinline__ uint32_t bf_pair(float a, float b) {
   return __builtin_bit_cast(uint32_t, __builtin_convertvector((v2f){a, b}, v2bf));
 }
 
-// Activations and their slopes in fp32.  SiLU is z s, s = 1 / (1 + e^-z), of
+// Activations and their gradients in fp32.  SiLU is z s, s = 1 / (1 + e^-z), of
 // slope s (1 + z (1 - s)); GELU is z Phi(z), of slope Phi(z) + z phi(z), Phi
 // and phi the normal distribution and its density.  The exponential and the
 // reciprocal are the hardware's (one ulp of 2^x; x = z log2 e is off by |z| ulp,
@@ -147,18 +147,20 @@ __device__ __forceinline__ float act_value(int act, float z) {
   }
   return z;
 }
-__device__ __forceinline__ float act_slope(int act, float z) {
-  if (act == OC_ACT_RELU) return z > 0.f ? 1.f : 0.f;
+// d act'(z).  A ReLU's is a mask, as the convolutions' is: where z is not positive it is 0
+// whatever d holds (an infinity times 0 would be NaN).
+__device__ __forceinline__ float act_grad(int act, float d, float z) {
+  if (act == OC_ACT_RELU) return z > 0.f ? d : 0.f;
   if (act == OC_ACT_SILU) {
     const float s = sigmoid(z);
-    return s * fmaf(z, 1.f - s, 1.f);
+    return d * (s * fmaf(z, 1.f - s, 1.f));
   }
   if (act == OC_ACT_GELU) {
     float e;
     const float q = normal_tail(z, e);
-    return fmaf(z * e, 0.39894228040143268f, z < 0.f ? q : 1.f - q);
+    return d * fmaf(z * e, 0.39894228040143268f, z < 0.f ? q : 1.f - q);
   }
-  return 1.f;
+  return d;
 }
 
 // Eight consecutive elements i .. i + 7 of an fp32 or bf16 array.
@@ -300,7 +302,7 @@ __device__ __forceinline__ void slopes(const float (&d)[U][8], float (&z)[U][8],
 #pragma unroll
     for (int k = 0; k < 8; ++k) {
       const float g = z[i][k];
-      z[i][k] = d[i][k] * (GLU ? u[i][k] * act_slope(ACT, g) : act_slope(ACT, g));
+      z[i][k] = act_grad(ACT, GLU ? d[i][k] * u[i][k] : d[i][k], g);
       if (GLU) u[i][k] = d[i][k] * act_value(ACT, g);
     }
 }

@@ -87,11 +87,11 @@ __global__ __launch_bounds__(TB) void k_dz(const void* dy, const void* z, bool b
         for (int k = 0; k < 8; ++k) {
           const float d = g[i][k];
           if (GLU) {
-            g[i][k] = d * u[i][k] * oc::act_slope(ACT, v[i][k]);
+            g[i][k] = oc::act_grad(ACT, d * u[i][k], v[i][k]);
             u[i][k] = d * oc::act_value(ACT, v[i][k]);
             s1[k] += u[i][k];
           } else if (ACT != OC_ACT_NONE) {
-            g[i][k] = d * oc::act_slope(ACT, v[i][k]);
+            g[i][k] = oc::act_grad(ACT, d, v[i][k]);
           }
           s0[k] += g[i][k];
         }

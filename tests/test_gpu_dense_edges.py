@@ -149,3 +149,36 @@ def test_dbias_of_very_many_rows():
     dy = torch.full((rows, 1), v, device="cuda")
     db = oc.oc_dense_bwd(x, x[:1], dy, need_dx=False, need_dw=False)[2]
     assert abs(float(db.double()) - rows * v) <= 65 * U * rows * v
+
+
+@pytest.mark.parametrize("dt", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("rows,cin,cout", [(3, 16, 24), (300, 40, 72), (1100, 33, 65)])
+def test_relu_masks_what_is_not_finite(rows, cin, cout, dt):
+    """Infinities and NaN in dy where the unit is not active leave the bits of zeros
+    there, from the forward's bits, its output or x w + b formed again."""
+    x, w = normal((rows, cin), 1).to(dt), normal((cin, cout), 2, cin ** -0.5).to(dt)
+    dy = normal((rows, cout), 3).to(dt)
+    y, bits = oc.oc_dense_fwd(x, w, act=oc.OC_ACT_RELU, need_pre=True, again=False)
+    off = y == 0
+    zero, bad = dy.masked_fill(off, 0.0), dy.masked_fill(off, math.inf)
+    bad[off & (torch.arange(cout, device="cuda") % 3 == 0)] = math.nan
+    for pre in (bits, y, oc.Again(None)):
+        want = oc.oc_dense_bwd(x, w, zero, act=oc.OC_ACT_RELU, pre=pre)
+        got = oc.oc_dense_bwd(x, w, bad, act=oc.OC_ACT_RELU, pre=pre)
+        assert all(torch.isfinite(p).all() and torch.equal(p, q) for p, q in zip(got, want))
+
+
+@pytest.mark.parametrize("dt", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("rows,cin,cout", [(3, 16, 24), (300, 40, 72), (1100, 33, 65)])
+def test_gated_relu_masks_what_is_not_finite(rows, cin, cout, dt):
+    """A dy u that passes the largest value, where the gate is not active."""
+    x, w = normal((rows, cin), 1).to(dt), normal((cin, 2 * cout), 2, cin ** -0.5).to(dt)
+    w[:, cout:] *= 2.0 ** 65
+    dy = normal((rows, cout), 3).to(dt)
+    pre = oc.oc_glu_fwd(x, w, act=oc.OC_ACT_RELU, need_pre=True, again=False)[1]
+    off = pre[:, :cout] < -0.01  # (formed again, a value next to 0 may change sides)
+    dy = torch.where(off, dy * 2.0 ** 75, torch.zeros_like(dy))
+    assert torch.isinf(dy.float() * pre[:, cout:]).any()
+    for kept in (pre, oc.Again(None)):
+        for g in oc.oc_glu_bwd(x, w, dy, kept, act=oc.OC_ACT_RELU):
+            assert (g == 0).all()
