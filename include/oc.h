@@ -657,8 +657,9 @@ oc_status oc_grad_norm(int32_t n, const void* const* grads, const oc_dtype* dts,
 /* Clipping by the global norm, ahead of oc_sgd: outs[i] = c grads[i], c = 1 where
  * norm <= max_norm, else max_norm / norm (max_norm >= 0; infinity only copies).
  *   outs    host array of device pointers, of types out_dts: OC_F32 or the
- *           gradient's own.  outs[i] may be grads[i] (same type); otherwise no
- *           output overlaps a gradient or another output.
+ *           gradient's own.  outs[i] may be grads[i] (same type); otherwise an
+ *           output that overlaps a gradient or another output is refused.
+ *           (Gradients may overlap each other.)
  *   norm    dev f32 scalar, the norm before clipping, or NULL.
  * A NaN gradient makes every output NaN; an infinite one (and no NaN) makes
  * itself NaN and every finite one 0. */

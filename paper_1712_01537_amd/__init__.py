@@ -1099,22 +1099,14 @@ def oc_grad_norm(grads):
 def oc_grad_clip(grads, max_norm, outs=None):
     """Scale the gradients to a global norm of at most max_norm, in place or into
     outs (tensors of float32 or the gradients' own dtype); the norm before that,
-    as a 0-d device tensor."""
+    as a 0-d device tensor.  No output may overlap another output, or a gradient that
+    is not its own as a whole."""
     n, ptrs, dts, counts = _grad_list(grads, "grads")
     optrs, odts = ptrs, dts
     if outs is not None:
         m, optrs, odts, ocounts = _grad_list(outs, "outs")
         if m != n or ocounts != counts:
             raise OcError(1, "outs and grads differ in number or size")
-    written = set(optrs)
-    if len(written) != n:  # (empty tensors may share an address)
-        some = [p for p, c in zip(optrs, counts) if c]
-        if len(set(some)) != len(some):
-            raise OcError(1, "a tensor is to be written twice")
-    if outs is not None and not written.isdisjoint(ptrs):
-        read = set(ptrs)
-        if any(c and p != q and p in read for p, q, c in zip(optrs, ptrs, counts)):
-            raise OcError(1, "an output is another tensor's gradient")
     L = load()
     norm, ws, need = _grad_scratch(L, n, counts)
     _check(L.oc_grad_clip(n, _at(ptrs), _at(dts), _at(counts), max_norm, _at(optrs), _at(odts),

@@ -18,6 +18,8 @@
 // cache.
 #include <algorithm>
 #include <cmath>
+#include <memory>
+#include <new>
 
 #include "dense.h"
 
@@ -205,6 +207,38 @@ int sq_sums(int32_t n, const void* const* grads, const oc_dtype* dts, const int6
   return at;
 }
 
+// Every output apart from the other outputs and from every gradient, but for its own as a
+// whole: a workgroup would read what another has written, or both would write.
+oc_status check_outputs(int32_t n, const void* const* grads, const oc_dtype* dts,
+                        const int64_t* counts, void* const* outs, const oc_dtype* out_dts) {
+  struct Span {
+    uintptr_t from, to;
+    int32_t i;
+  };
+  const auto span = [&](const void* p, oc_dtype t, int32_t i) {
+    return Span{(uintptr_t)p, (uintptr_t)p + (uintptr_t)counts[i] * (t == OC_BF16 ? 2 : 4), i};
+  };
+  const auto before = [](const Span& a, const Span& b) { return a.from < b.from; };
+  const std::unique_ptr<Span[]> all(new (std::nothrow) Span[n > 0 ? n : 1]);
+  if (!all) return oc::fail(OC_ERR_NOMEM, "oc_grad_clip: %d tensors", n);
+  Span *const first = all.get(), *last = first;
+  for (int32_t i = 0; i < n; ++i)
+    if (counts[i] > 0) *last++ = span(outs[i], out_dts[i], i);
+  if (!std::is_sorted(first, last, before)) std::sort(first, last, before);
+  for (const Span* s = first; s + 1 < last; ++s)
+    if (s[1].from < s->to)
+      return oc::fail(OC_ERR_ARG, "oc_grad_clip: outputs %d and %d overlap", s->i, s[1].i);
+  for (int32_t i = 0; i < n; ++i) {
+    if (counts[i] == 0 || outs[i] == grads[i]) continue;
+    const Span g = span(grads[i], dts[i], i);
+    // the first output that ends behind the gradient's start (they are apart and in order)
+    const Span* s = std::partition_point(first, last, [&](const Span& o) { return o.to <= g.from; });
+    if (s < last && s->from < g.to)
+      return oc::fail(OC_ERR_ARG, "oc_grad_clip: output %d overlaps gradient %d", s->i, i);
+  }
+  return OC_OK;
+}
+
 oc_status check_ws(const char* who, int32_t n, const int64_t* counts, const void* ws,
                    size_t have) {
   const size_t need = oc_grad_workspace(n, counts);
@@ -259,6 +293,8 @@ oc_status oc_grad_clip(int32_t n, const void* const* grads, const oc_dtype* dts,
     if (counts[i] > 0 && outs[i] == grads[i] && out_dts[i] != dts[i])
       return oc::fail(OC_ERR_ARG, "oc_grad_clip: output %d is its gradient in another type", i);
   }
+  st = check_outputs(n, grads, dts, counts, outs, out_dts);
+  if (st != OC_OK) return st;
   st = check_ws("oc_grad_clip", n, counts, ws, ws_bytes);
   if (st != OC_OK) return st;
   double* part = (double*)ws;

@@ -182,3 +182,24 @@ def test_gated_relu_masks_what_is_not_finite(rows, cin, cout, dt):
     for kept in (pre, oc.Again(None)):
         for g in oc.oc_glu_bwd(x, w, dy, kept, act=oc.OC_ACT_RELU):
             assert (g == 0).all()
+
+
+def test_clipping_into_views():
+    """Views that overlap are refused and untouched; views end to end and a gradient
+    listed twice are not."""
+    buf = torch.full((1000,), 2.0, device="cuda")
+    for grads, outs in (([buf[:600], buf[599:]], None), ([buf[:500]], [buf[1:501]]),
+                        ([buf[:10], buf[500:510]], [buf[20:30], buf[29:39]]),
+                        ([buf[:10], buf[500:510]], [buf[505:515], buf[20:30]])):
+        with pytest.raises(oc.OcError):
+            oc.oc_grad_clip(grads, 1.0, outs=outs)
+    assert (buf == 2.0).all()
+    out = torch.zeros(600, device="cuda")
+    norm = oc.oc_grad_clip([buf[:300], buf[:300]], 1.0, outs=[out[:300], out[300:]])
+    want = math.sqrt(600 * 4.0)
+    assert abs(float(norm) - want) <= 1.01 * U * want
+    assert ((out.double() - 2.0 / want).abs() <= 2.1 * U * 2.0 / want).all()
+    assert (buf == 2.0).all()
+    oc.oc_grad_clip([buf[:600], buf[600:]], 1.0)
+    want = 2.0 / math.sqrt(4000.0)
+    assert ((buf.double() - want).abs() <= 2.1 * U * want).all()
