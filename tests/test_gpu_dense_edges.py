@@ -203,3 +203,63 @@ def test_clipping_into_views():
     oc.oc_grad_clip([buf[:600], buf[600:]], 1.0)
     want = 2.0 / math.sqrt(4000.0)
     assert ((buf.double() - want).abs() <= 2.1 * U * want).all()
+
+
+@pytest.mark.parametrize("dt", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("rows,cin,cout", [(2, 96, 40), (70, 160, 72), (600, 520, 264),
+                                           (5000, 520, 1032), (300, 75, 67)])
+def test_what_is_not_finite_stays_in_its_row_and_column(rows, cin, cout, dt):
+    """Values are split in parts one by one: next to an infinity or NaN every other row's
+    and column's bits are as they were, its neighbours' too."""
+    x, w = normal((rows, cin), 1).to(dt), normal((cin, cout), 2, cin ** -0.5).to(dt)
+    dy = normal((rows, cout), 3).to(dt)
+    y0, (dx0, dw0, db0) = oc.oc_dense_fwd(x, w)[0], oc.oc_dense_bwd(x, w, dy)
+    r, k, n = rows - 1, cin // 2, cout - 1
+    x[r, k], dy[r, n] = math.inf, math.nan
+    y, (dx, dw, db) = oc.oc_dense_fwd(x, w)[0], oc.oc_dense_bwd(x, w, dy)
+    i, j, m = (torch.arange(v, device="cuda") for v in (rows, cin, cout))
+    assert torch.equal(y[i != r], y0[i != r]) and torch.equal(dx[i != r], dx0[i != r])
+    assert torch.equal(db[m != n], db0[m != n])
+    assert torch.equal(dw[j != k][:, m != n], dw0[j != k][:, m != n])
+    assert torch.isnan(dx[r]).all() and torch.isnan(dw[:, n]).all() and torch.isnan(db[n])
+    assert torch.isinf(y[r]).all() and torch.isinf(dw[k, m != n]).all()
+
+
+def test_two_threads():
+    """Calls from two threads at once, each on a stream of its own, over sizes whose plans
+    both threads work out: the bits of a single thread."""
+    import threading
+
+    sizes = [(300 + 64 * i, 40 + 24 * (i % 5), 96 + 8 * i) for i in range(12)]
+    data = [(normal((r, k), i).to(t), normal((k, 2 * n), i + 50, k ** -0.5).to(t), normal((r, n), i + 99).to(t))
+            for t in (torch.float32, torch.bfloat16) for i, (r, k, n) in enumerate(sizes)]
+
+    def step(x, w, dy):
+        y, pre = oc.oc_glu_fwd(x, w, need_pre=True)
+        dx, dw, db = oc.oc_glu_bwd(x, w, dy, pre)
+        outs = [torch.empty_like(g) for g in (dw, db)]
+        return (y, dx, dw, db, oc.oc_grad_clip([dw, db], 0.5, outs=outs), *outs)
+
+    want = [step(*d) for d in data]
+    torch.cuda.synchronize()
+    failed = []
+
+    def work(order):
+        try:
+            with torch.cuda.stream(torch.cuda.Stream()):
+                for _ in range(5):
+                    got = [(i, step(*data[i])) for i in order]
+                    torch.cuda.current_stream().synchronize()
+                    for i, g in got:
+                        if not all(torch.equal(p, q) for p, q in zip(want[i], g)):
+                            failed.append(i)
+        except Exception as e:
+            failed.append(e)
+
+    threads = [threading.Thread(target=work, args=(o,))
+               for o in (list(range(len(data))), list(reversed(range(len(data)))))]
+    for t in threads:
+        t.start()
+    for t in threads:
+        t.join()
+    assert not failed
