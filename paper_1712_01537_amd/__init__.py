@@ -1051,6 +1051,7 @@ def _grad_list(tensors, name):
     (Per tensor this is what a call costs on the host: one pass in C for each.)"""
     T = torch.Tensor
     try:
+        n = len(tensors)  # (a generator would be used up by the first pass)
         devs = set(map(T.get_device, tensors))
         contiguous = all(map(T.is_contiguous, tensors))
     except TypeError:
@@ -1066,7 +1067,7 @@ def _grad_list(tensors, name):
         dts = array.array("i", [_GRAD_CODE[t.dtype] for t in tensors])
     except KeyError:
         raise OcError(1, f"{name} must be float32 or bfloat16 tensors") from None
-    return (len(tensors), array.array("Q", map(T.data_ptr, tensors)), dts,
+    return (n, array.array("Q", map(T.data_ptr, tensors)), dts,
             array.array("q", map(T.numel, tensors)))
 
 

@@ -1,4 +1,5 @@
-"""Outputs of oc_grad_clip that overlap are refused before any device work."""
+"""Lists that oc_grad_norm and oc_grad_clip refuse before any device work: outputs that
+overlap, and what is no list."""
 import ctypes as C
 
 import pytest
@@ -47,3 +48,10 @@ def test_overlaps(grads, outs, counts, dts, out_dts):
 def test_apart(grads, outs, counts, dts, out_dts):
     assert clip(grads, outs, counts, dts, out_dts) == 1
     assert b"workspace" in oc.load().oc_last_error()
+
+
+@pytest.mark.parametrize("what", [iter([]), (t for t in ()), None, 3])
+def test_no_list(what):
+    for call in (lambda: oc.oc_grad_norm(what), lambda: oc.oc_grad_clip(what, 1.0)):
+        with pytest.raises(oc.OcError, match="list of tensors"):
+            call()
