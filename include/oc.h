@@ -610,7 +610,8 @@ oc_status oc_dense_fwd(oc_dtype dt, int32_t act, int64_t rows, int32_t cin, int3
  *   bias    the forward's; read only when x w + bias is formed once more.
  *   y       for OC_ACT_RELU, in place of pre (then NULL): dev [rows][cout], the
  *           output of a forward without a residual, positive where x w + bias is;
- *           otherwise not read.
+ *           otherwise not read.  It saves the memory of the bits, which are the faster
+ *           of the two: 1/16 (OC_F32: 1/32) of y's bytes.
  *   dy      dev [rows][cout] and dx dev [rows][cin] or NULL, of type dt.
  *   dw      dev [cin][cout] or NULL, of type dw_dt: OC_F32 or dt.
  *   dbias   dev f32 [cout] or NULL.

@@ -1020,7 +1020,10 @@ def oc_dense_fwd(x, w, b=None, res=None, act=OC_ACT_NONE, need_pre=False, again=
     """y = act(x w + b) + res over the rows of x: (y, pre), pre what the backward needs
     of x w + b, to be handed on to it, or None.  That is its values (float32), for
     OC_ACT_RELU their signs (one bit each), or an Again where the backward is to form
-    them once more (again: True, False, or None for whichever is faster).
+    them once more (again: True, False, or None for whichever is faster, a matter of the
+    sizes).  An Again reads x, w and b once more, so with again other than False none of
+    the three, b included, may change before the backward.  For OC_ACT_NONE no pre is
+    needed (need_pre costs a write of 4 bytes a value).
     x, w, res and y share a dtype (float32 or bfloat16); b is float32."""
     return _layer_fwd(False, x, w, b, res, act, need_pre, again)
 
@@ -1028,7 +1031,8 @@ def oc_dense_fwd(x, w, b=None, res=None, act=OC_ACT_NONE, need_pre=False, again=
 def oc_dense_bwd(x, w, dy, act=OC_ACT_NONE, pre=None, need_dx=True, need_dw=True, need_db=True,
                  dw=None, db=None, dw_dtype=None):
     """(dx, dw, db) of oc_dense_fwd (None where not needed).  pre: as the forward
-    returned it; for OC_ACT_RELU the y of a forward without a residual does as well.
+    returned it; for OC_ACT_RELU the y of a forward without a residual does as well (it
+    needs no memory between the passes, and 16 or 32 times the bits' reading).
     dw, db: optional caller tensors to write into; a new dw is of dw_dtype (float32
     if not given, or x's dtype)."""
     return _layer_bwd(False, x, w, dy, pre, act, need_dx, need_dw, need_db, dw, db, dw_dtype)
@@ -1036,7 +1040,8 @@ def oc_dense_bwd(x, w, dy, act=OC_ACT_NONE, pre=None, need_dx=True, need_dw=True
 
 def oc_glu_fwd(x, w, b=None, act=OC_ACT_SILU, need_pre=False, again=None):
     """y = act(g) u, [g | u] = x w + b, w [cin][2 cout]: (y, pre), pre (values
-    [rows][2 cout] or an Again) and again as oc_dense_fwd's."""
+    [rows][2 cout] or an Again) and again as oc_dense_fwd's: with again other than False,
+    x, w and b may not change before the backward."""
     return _layer_fwd(True, x, w, b, None, act, need_pre, again)
 
 

@@ -88,13 +88,6 @@ struct Plan {
   }
 };
 
-// Expected time of each shape, and of each way to deal out the tiles that do not fill
-// the card; the least is taken.  Measured, in microseconds: a step of BK terms of a
-// workgroup alone on its CU and with all that fit there, and what a workgroup takes
-// to start and finish.  (As many workgroups as fit, all three layouts within 5%: bf16
-// 256x256 1430 TFLOP/s, 256x128 1190, 128x128 1180, 64x64 715; fp32 256x128 250,
-// 128x64 168, 128x128 202, 64x64 140.)  Partial sums are written and read at 4 TB/s
-// and take another launch of 4 us.
 // What make() returns for these sizes on this device: the plans of a call's products are
 // asked for by its workspace and by its launches, and took the host 6 us a backward in
 // all (bf16 2048 x 256 -> 256: 22 us a call, its kernels 15).  Every thread remembers the
@@ -120,6 +113,20 @@ V remembered(oc_dtype dt, int flags, int64_t P, int64_t Q, int64_t R, F&& make) 
   return value[at];
 }
 
+// Expected time of each shape, and of each way to deal out the tiles that do not fill
+// the card; the least is taken.  Measured, in microseconds: a step of BK terms of a
+// workgroup alone on its CU (step) and with all that fit there (full), and what a
+// workgroup takes to start and finish (ends).  (As many workgroups as fit, all three
+// layouts within 5%: bf16 256x256 1430 TFLOP/s, 256x128 1190, 128x128 1180, 64x64 715;
+// fp32 256x128 250, 128x64 168, 128x128 202, 64x64 140.)  Partial sums are written and
+// read at 4 TB/s and take another launch of 4 us.
+// There is no term for what the epilogue writes and reads, so the expectation holds where
+// the reduction is long (35472 x 512 -> 1024 fp32, dx and dw: 199 and 181 us, measured 202
+// and 187; 65536 x 1024 -> 4096 bf16: 416 and 430, measured 436 and 440) and is too short
+// where the epilogue moves much (the forwards of these 216 and 512, measured 281 and 557;
+// 35472 x 256 -> 1024 bf16 GELU with its fp32 values kept 41, measured 74; the gated
+// 32768 x 1024 -> 2 x 2816 352, measured 458).  There shapes that differ by less than that
+// are in an order of no meaning.
 struct Cost {
   double step, full;
   int fit;

@@ -8,10 +8,9 @@
 // A workgroup owns a BM x BN tile, its waves TM x 64 pieces of it, and walks the
 // reduction BK at a time through two or more LDS buffers: while one is multiplied the
 // next ones land in the others, one barrier a step.  The product is formed transposed
-// (the MFMA's first operand is B), so that a lane ends up with consecutive
-// columns of one row: with the columns of a 64-wide piece dealt out as q = 16 t
-// + 4 j + i (lane group t, MFMA j, accumulator register i), sixteen of them, and
-// the epilogue reads and writes whole vectors straight from the accumulators.
+// (the MFMA's first operand is B), so that a lane ends up with four consecutive columns
+// of one row.  The epilogue passes the sums through LDS, so that a lane has eight columns
+// of a row and reads and writes whole vectors.
 //
 // bf16 operands whose rows are whole 16-byte vectors (of which what is behind a
 // row's end holds zeros) go from memory to LDS directly (buffer_load ... lds; what is
