@@ -669,6 +669,104 @@ oc_status oc_grad_clip(int32_t n, const void* const* grads, const oc_dtype* dts,
                        const oc_dtype* out_dts, float* norm, void* ws, size_t ws_bytes,
                        hipStream_t stream);
 
+/* ---- Row operators around dense layers: rows are octants of a depth (or whole
+ * shapes), contiguous, c channels each.  rows 0 .. 2^28 - 1 (0: nothing is done but
+ * that sums over the rows are 0), c 1 .. 65536, fewer than 2^40 values.  dt OC_F32 or
+ * OC_BF16 is the type of the feature maps; gamma, beta, their gradients, mean and invstd
+ * are fp32.  Sums are fp32 over at most 64 rows and double from there; each OC_BF16
+ * result is rounded once.  Buffers need the alignment of their elements only, but for
+ * workspaces (16 bytes) and generator states (8).  An output that overlaps another
+ * buffer is refused, but for those named below, which may be the same buffer as a whole.
+ * Deterministic: no floating-point atomics.
+ *
+ * Layer norm over the channels of each row:
+ *   y = (x - mean) invstd gamma + beta,  invstd = 1 / sqrt(var + eps)
+ * with the biased variance.
+ *   x, y    dev [rows][c]; y may be x.
+ *   gamma, beta  dev f32 [c], each or NULL (1, 0).  eps > 0.
+ *   mean, invstd dev f32 [rows], written for the backward, each or NULL.
+ * A row that holds an infinity or a NaN becomes NaN; so do its dx and its share of the
+ * sums over rows.  Deviations from 2^63 on have an infinite variance: y is beta. */
+oc_status oc_ln_fwd(oc_dtype dt, int64_t rows, int32_t c, const void* x, const float* gamma,
+                    const float* beta, float eps, void* y, float* mean, float* invstd,
+                    hipStream_t stream);
+
+/* Gradients of oc_ln_fwd: with z = (x - mean) invstd and g = dy gamma,
+ *   dx = invstd (g - the row's mean of g - z times the row's mean of g z),
+ *   dgamma = the sum of dy z, dbeta = the sum of dy over the rows.
+ *   dx      dev [rows][c] or NULL.  dgamma, dbeta dev f32 [c], each or NULL.
+ *   ws      dev workspace of at least oc_ln_bwd_workspace() bytes; may be NULL when
+ *           neither dgamma nor dbeta is asked for. */
+size_t oc_ln_bwd_workspace(int64_t rows, int32_t c);
+oc_status oc_ln_bwd(oc_dtype dt, int64_t rows, int32_t c, const void* x, const void* dy,
+                    const float* gamma, const float* mean, const float* invstd, void* dx,
+                    float* dgamma, float* dbeta, void* ws, size_t ws_bytes, hipStream_t stream);
+
+/* Dropout with ratio p in [0, 1) whose mask is drawn inside: y = keep ? x / q : 0, q =
+ * T / 2^32, T = (1 - p) 2^32 rounded (p keeping nothing by that rounding is refused;
+ * one keeping everything copies).  The mask is a function of the generator's state, the
+ * site, the row and the column (and of c) alone, whatever dt is; it is never stored, and
+ * the backward is the same call on dy.  oc_dropout takes a mask that the caller draws.
+ *   rng     dev u64 [2], {seed, step}, read when the kernel runs: a captured call draws
+ *           another mask once the caller has changed the step.  Not read (may be NULL)
+ *           where p keeps everything.
+ *   site    0 .. 32767: calls of one step with different sites have independent masks.
+ *   y       dev [rows][c]; may be x.
+ * The mask: group g of eight columns of row r has the index i = r ceil(c / 8) + g.
+ * Philox4x32-10 (Salmon et al., SC 2011) with the key {seed low, seed high} and the
+ * counter {i low, i high + 2^16 site, step low, step high} gives four words; their
+ * halves, low before high, are the high 16 bits of the columns' 32-bit numbers, and those
+ * of the words with 2^31 added to the counter's second word are the low ones.  A value
+ * is kept where its number is below T. */
+oc_status oc_dropout_rng(oc_dtype dt, int64_t rows, int32_t c, const void* x, double p,
+                         const uint64_t* rng, int32_t site, void* y, hipStream_t stream);
+
+/* Residual step: h = res + dropout(x), y = the layer norm of h, in one kernel; dropout as
+ * oc_dropout_rng, layer norm as oc_ln_fwd.  y, mean and invstd are formed from h before
+ * it is rounded to dt.
+ *   res     dev [rows][c] or NULL (0).
+ *   h       dev [rows][c], written for the layers above and the backward; may be res.
+ *   y       dev [rows][c]; may be x. */
+oc_status oc_drop_ln_fwd(oc_dtype dt, int64_t rows, int32_t c, const void* x, const void* res,
+                         double p, const uint64_t* rng, int32_t site, const float* gamma,
+                         const float* beta, float eps, void* h, void* y, float* mean,
+                         float* invstd, hipStream_t stream);
+
+/* Gradients of oc_drop_ln_fwd: dres = dh + oc_ln_bwd's dx at h for dy, dx = dropout's mask
+ * and scale on dres (before its rounding), dgamma and dbeta as oc_ln_bwd.
+ *   dh      dev [rows][c], the gradient that reaches h from the layers above, or NULL (0).
+ *   dx, dres  dev [rows][c], each or NULL.
+ *   rng     the state as the forward read it.
+ *   ws      as oc_ln_bwd's. */
+oc_status oc_drop_ln_bwd(oc_dtype dt, int64_t rows, int32_t c, const void* h, const void* dy,
+                         const void* dh, double p, const uint64_t* rng, int32_t site,
+                         const float* gamma, const float* mean, const float* invstd, void* dx,
+                         void* dres, float* dgamma, float* dbeta, void* ws, size_t ws_bytes,
+                         hipStream_t stream);
+
+/* Table rows by id: y[r] = scale table[id[r]]; 0 where the id is outside the table (as a
+ * padded row's may be).
+ *   flags   0 or OC_IDS_KEYS: the ids are shuffle keys (oc_level's keys), whose shape
+ *           index in bits 24..31 is dropped: the row of an octant of depth l is its place
+ *           in the cube, of a table of 8^l rows.
+ *   ids     dev i32 [rows].  table dev [num][c], num 1 .. 2^28 - 1, fewer than 2^40
+ *           values.  y dev [rows][c]. */
+#define OC_IDS_KEYS 1
+oc_status oc_embed_fwd(oc_dtype dt, int32_t flags, int64_t rows, int64_t num, int32_t c,
+                       const int32_t* ids, const void* table, float scale, void* y,
+                       hipStream_t stream);
+
+/* Gradient of oc_embed_fwd: dtable[v] = scale times the sum of dy[r] over the rows r whose
+ * id is v, in a fixed order; every row of the table is written (0 where no id names it).
+ * Ids outside the table add to nothing.
+ *   dtable  dev [num][c], of type dtable_dt: OC_F32 or dt.
+ *   ws      dev workspace of at least oc_embed_bwd_workspace() bytes (may be NULL when
+ *           that is 0): the rows sorted by id, and partial sums. */
+size_t oc_embed_bwd_workspace(int64_t rows, int64_t num, int32_t c);
+oc_status oc_embed_bwd(oc_dtype dt, int32_t flags, int64_t rows, int64_t num, int32_t c,
+                       const int32_t* ids, const void* dy, float scale, oc_dtype dtable_dt,
+                       void* dtable, void* ws, size_t ws_bytes, hipStream_t stream);
+
 /* Profiling: the next launch, on the calling thread, of the kernel that does
  * the main work of an entry point (the kernel oc_conv_kernel names for a
  * convolution pass; the pooling, routing or unpooling kernel of oc_pool_* /

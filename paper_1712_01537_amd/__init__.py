@@ -63,6 +63,14 @@ __all__ = [
     "oc_glu_bwd",
     "oc_grad_norm",
     "oc_grad_clip",
+    "oc_ln_fwd",
+    "oc_ln_bwd",
+    "oc_dropout_rng",
+    "oc_drop_ln_fwd",
+    "oc_drop_ln_bwd",
+    "oc_embed_fwd",
+    "oc_embed_bwd",
+    "OC_IDS_KEYS",
     "OC_ACT_NONE",
     "OC_ACT_RELU",
     "OC_ACT_SILU",
@@ -75,6 +83,7 @@ OC_FUSE_RELU = 1
 OC_DEFER_DW = 2
 OC_POOL_MAX, OC_POOL_AVG = 0, 1
 OC_ACT_NONE, OC_ACT_RELU, OC_ACT_SILU, OC_ACT_GELU = 0, 1, 2, 3
+OC_IDS_KEYS = 1
 OC_F32, OC_BF16 = 0, 1
 STATUS = {0: "OC_OK", 1: "OC_ERR_ARG", 2: "OC_ERR_RANGE", 3: "OC_ERR_NOMEM", 4: "OC_ERR_DEVICE",
           5: "OC_ERR_UNSUPPORTED"}
@@ -94,6 +103,8 @@ EXPORTS = (
     "oc_dense_fwd", "oc_dense_fwd_workspace", "oc_dense_bwd", "oc_dense_bwd_workspace",
     "oc_glu_fwd", "oc_glu_fwd_workspace", "oc_glu_bwd", "oc_glu_bwd_workspace",
     "oc_grad_workspace", "oc_grad_norm", "oc_grad_clip",
+    "oc_ln_fwd", "oc_ln_bwd_workspace", "oc_ln_bwd", "oc_dropout_rng", "oc_drop_ln_fwd",
+    "oc_drop_ln_bwd", "oc_embed_fwd", "oc_embed_bwd_workspace", "oc_embed_bwd",
 )
 
 
@@ -235,6 +246,18 @@ def load():
         "oc_grad_workspace": ([i32, p], sz),
         "oc_grad_norm": ([i32, p, p, p, p, p, sz, p], C.c_int),
         "oc_grad_clip": ([i32, p, p, p, C.c_double, p, p, p, p, sz, p], C.c_int),
+        "oc_ln_fwd": ([C.c_int, i64, i32, p, p, p, C.c_float, p, p, p, p], C.c_int),
+        "oc_ln_bwd_workspace": ([i64, i32], sz),
+        "oc_ln_bwd": ([C.c_int, i64, i32, p, p, p, p, p, p, p, p, p, sz, p], C.c_int),
+        "oc_dropout_rng": ([C.c_int, i64, i32, p, C.c_double, p, i32, p, p], C.c_int),
+        "oc_drop_ln_fwd": ([C.c_int, i64, i32, p, p, C.c_double, p, i32, p, p, C.c_float, p, p, p,
+                            p, p], C.c_int),
+        "oc_drop_ln_bwd": ([C.c_int, i64, i32, p, p, p, C.c_double, p, i32, p, p, p, p, p, p, p,
+                            p, sz, p], C.c_int),
+        "oc_embed_fwd": ([C.c_int, i32, i64, i64, i32, p, p, C.c_float, p, p], C.c_int),
+        "oc_embed_bwd_workspace": ([i64, i64, i32], sz),
+        "oc_embed_bwd": ([C.c_int, i32, i64, i64, i32, p, p, C.c_float, C.c_int, p, p, sz, p],
+                         C.c_int),
     }
     for name, (args, res) in sigs.items():
         f = getattr(L, name)
@@ -1118,3 +1141,183 @@ def oc_grad_clip(grads, max_norm, outs=None):
     _check(L.oc_grad_clip(n, _at(ptrs), _at(dts), _at(counts), max_norm, _at(optrs), _at(odts),
                           norm.data_ptr(), ws.data_ptr(), need, _stream()))
     return norm
+
+
+# --- row operators: layer norm, dropout from a counter, table rows ----------
+
+
+def _rows_of(x, name):
+    """Current device, dtype code, rows and channels of a feature map."""
+    if not isinstance(x, torch.Tensor) or not x.is_cuda:
+        raise OcError(1, f"{name} must be a CUDA (HIP) tensor")
+    if x.dim() != 2:
+        raise OcError(1, f"{name} must have rows and channels, has shape {tuple(x.shape)}")
+    rows, c = x.shape
+    return torch._C._cuda_getDevice(), _dtype_code(x), rows, c
+
+
+def _rng_state(rng, dev, p):
+    """Address of a generator's state {seed, step}; None where no mask is drawn."""
+    if rng is None and p == 0:
+        return None
+    if not isinstance(rng, torch.Tensor):
+        raise OcError(1, "rng must be a tensor of two int64: seed and step")
+    return _given(rng, "rng", dev, torch.int64, (2,))
+
+
+@functools.lru_cache(maxsize=1024)
+def _ln_ws(rows, c):
+    return load().oc_ln_bwd_workspace(rows, c)
+
+
+def _stats(x, rows, need):
+    """mean and invstd of the rows (one allocation), or None twice."""
+    if not need:
+        return None, None, None, None
+    st = torch.empty((2, rows), dtype=torch.float32, device=x.device)
+    return st[0], st[1], st.data_ptr(), st.data_ptr() + 4 * rows
+
+
+def _norm_sums(x, dev, rows, c, dgamma, dbeta, need_dgamma, need_dbeta):
+    """dgamma and dbeta with their addresses, and the workspace for them."""
+    if dgamma is None and need_dgamma:
+        dgamma = torch.empty(c, dtype=torch.float32, device=x.device)
+    if dbeta is None and need_dbeta:
+        dbeta = torch.empty(c, dtype=torch.float32, device=x.device)
+    need = _ln_ws(rows, c) if dgamma is not None or dbeta is not None else 0
+    ws = torch.empty(need, dtype=torch.uint8, device=x.device) if need else None
+    return (dgamma, dbeta, _given(dgamma, "dgamma", dev, torch.float32, (c,)),
+            _given(dbeta, "dbeta", dev, torch.float32, (c,)), ws,
+            ws.data_ptr() if need else None, need)
+
+
+def oc_ln_fwd(x, gamma=None, beta=None, eps=1e-5, need_stats=False):
+    """Layer norm over the channels of each row of x [rows][c] (float32 or bfloat16):
+    (y, mean, invstd), the last two None unless need_stats (the backward's).  gamma, beta:
+    float32 [c] or None."""
+    dev, dt, rows, c = _rows_of(x, "x")
+    y = x.new_empty((rows, c))
+    mean, invstd, mp, ip = _stats(x, rows, need_stats)
+    _check(load().oc_ln_fwd(dt, rows, c, _given(x, "x", dev, x.dtype, (rows, c)),
+                            _given(gamma, "gamma", dev, torch.float32, (c,)),
+                            _given(beta, "beta", dev, torch.float32, (c,)), eps, y.data_ptr(), mp,
+                            ip, _stream()))
+    return y, mean, invstd
+
+
+def oc_ln_bwd(x, dy, gamma, mean, invstd, need_dx=True, need_dgamma=True, need_dbeta=True,
+              dgamma=None, dbeta=None):
+    """(dx, dgamma, dbeta) of oc_ln_fwd (None where not needed); dgamma, dbeta: optional
+    caller tensors to write into."""
+    dev, dt, rows, c = _rows_of(x, "x")
+    dx = x.new_empty((rows, c)) if need_dx else None
+    dgamma, dbeta, gp, bp, ws, wsp, need = _norm_sums(x, dev, rows, c, dgamma, dbeta, need_dgamma,
+                                                      need_dbeta)
+    _check(load().oc_ln_bwd(dt, rows, c, _given(x, "x", dev, x.dtype, (rows, c)),
+                            _given(dy, "dy", dev, x.dtype, (rows, c)),
+                            _given(gamma, "gamma", dev, torch.float32, (c,)),
+                            _given(mean, "mean", dev, torch.float32, (rows,)),
+                            _given(invstd, "invstd", dev, torch.float32, (rows,)),
+                            dx.data_ptr() if need_dx else None, gp, bp, wsp, need, _stream()))
+    return dx, dgamma, dbeta
+
+
+def oc_dropout_rng(x, p, rng, site=0, y=None):
+    """Dropout of ratio p on x [rows][c] with a mask drawn from the generator's state rng,
+    an int64 device tensor {seed, step} that the kernel reads as it runs (rng[1] += 1 goes
+    on to the next step, in a captured graph too); site tells the calls of a step apart.
+    The backward is the same call on dy.  y: where to write, may be x."""
+    dev, dt, rows, c = _rows_of(x, "x")
+    xp = _given(x, "x", dev, x.dtype, (rows, c))
+    rp = _rng_state(rng, dev, p)
+    if y is None:
+        y = x.new_empty((rows, c))
+    _check(load().oc_dropout_rng(dt, rows, c, xp, p, rp, site,
+                                 _given(y, "y", dev, x.dtype, (rows, c)), _stream()))
+    return y
+
+
+def oc_drop_ln_fwd(x, res, p, rng, gamma=None, beta=None, site=0, eps=1e-5, need_stats=False,
+                   h=None):
+    """The residual step h = res + dropout(x), y = the layer norm of h: (h, y, mean,
+    invstd), the last two None unless need_stats.  res: as x, or None (0).  p, rng, site as
+    oc_dropout_rng's (rng may be None for p = 0).  h: where to write it, may be res."""
+    dev, dt, rows, c = _rows_of(x, "x")
+    xp = _given(x, "x", dev, x.dtype, (rows, c))
+    rp = _rng_state(rng, dev, p)
+    if h is None:
+        h = x.new_empty((rows, c))
+    y = x.new_empty((rows, c))
+    mean, invstd, mp, ip = _stats(x, rows, need_stats)
+    _check(load().oc_drop_ln_fwd(dt, rows, c, xp, _given(res, "res", dev, x.dtype, (rows, c)), p,
+                                 rp, site, _given(gamma, "gamma", dev, torch.float32, (c,)),
+                                 _given(beta, "beta", dev, torch.float32, (c,)), eps,
+                                 _given(h, "h", dev, x.dtype, (rows, c)), y.data_ptr(), mp, ip,
+                                 _stream()))
+    return h, y, mean, invstd
+
+
+def oc_drop_ln_bwd(h, dy, p, rng, gamma, mean, invstd, dh=None, site=0, need_dx=True,
+                   need_dres=True, need_dgamma=True, need_dbeta=True, dgamma=None, dbeta=None):
+    """(dx, dres, dgamma, dbeta) of oc_drop_ln_fwd (None where not needed).  dh: the gradient
+    that reaches h from the layers above, or None; rng holds what the forward read."""
+    dev, dt, rows, c = _rows_of(h, "h")
+    t = h.dtype
+    dx = h.new_empty((rows, c)) if need_dx else None
+    dres = h.new_empty((rows, c)) if need_dres else None
+    dgamma, dbeta, gp, bp, ws, wsp, need = _norm_sums(h, dev, rows, c, dgamma, dbeta, need_dgamma,
+                                                      need_dbeta)
+    _check(load().oc_drop_ln_bwd(dt, rows, c, _given(h, "h", dev, t, (rows, c)),
+                                 _given(dy, "dy", dev, t, (rows, c)),
+                                 _given(dh, "dh", dev, t, (rows, c)), p, _rng_state(rng, dev, p),
+                                 site, _given(gamma, "gamma", dev, torch.float32, (c,)),
+                                 _given(mean, "mean", dev, torch.float32, (rows,)),
+                                 _given(invstd, "invstd", dev, torch.float32, (rows,)),
+                                 dx.data_ptr() if need_dx else None,
+                                 dres.data_ptr() if need_dres else None, gp, bp, wsp, need,
+                                 _stream()))
+    return dx, dres, dgamma, dbeta
+
+
+@functools.lru_cache(maxsize=1024)
+def _embed_ws(rows, num, c):
+    return load().oc_embed_bwd_workspace(rows, num, c)
+
+
+def _ids_of(ids, dev):
+    if not isinstance(ids, torch.Tensor) or ids.dim() != 1:
+        raise OcError(1, "ids must be a tensor of one dimension")
+    return ids.shape[0], _given(ids, "ids", dev, torch.int32, ids.shape)
+
+
+def oc_embed_fwd(ids, table, scale=1.0, keys=False):
+    """y[r] = scale table[ids[r]], 0 where the id is outside the table.  ids: int32; with
+    keys they are shuffle keys (Octree.keys), whose shape index is dropped.  table [num][c]:
+    float32 or bfloat16, as y."""
+    dev, dt, num, c = _rows_of(table, "table")
+    rows, idp = _ids_of(ids, dev)
+    y = table.new_empty((rows, c))
+    _check(load().oc_embed_fwd(dt, OC_IDS_KEYS if keys else 0, rows, num, c, idp,
+                               _given(table, "table", dev, table.dtype, (num, c)), scale,
+                               y.data_ptr(), _stream()))
+    return y
+
+
+def oc_embed_bwd(ids, dy, num, scale=1.0, keys=False, dtable=None, dtype=None):
+    """The gradient [num][c] of oc_embed_fwd's table for dy, every row of it written.
+    dtable: optional caller tensor to write into; a new one is of dtype (float32 if not
+    given, or dy's)."""
+    dev, dt, rows, c = _rows_of(dy, "dy")
+    n, idp = _ids_of(ids, dev)
+    if n != rows:
+        raise OcError(1, f"{n} ids for {rows} rows")
+    dyp = _given(dy, "dy", dev, dy.dtype, (rows, c))
+    if dtable is None:
+        dtable = torch.empty((num, c), dtype=dtype or torch.float32, device=dy.device)
+    need = _embed_ws(rows, num, c)
+    ws = torch.empty(need, dtype=torch.uint8, device=dy.device) if need else None
+    _check(load().oc_embed_bwd(dt, OC_IDS_KEYS if keys else 0, rows, num, c, idp, dyp, scale,
+                               _dtype_code(dtable),
+                               _given(dtable, "dtable", dev, dtable.dtype, (num, c)),
+                               ws.data_ptr() if need else None, need, _stream()))
+    return dtable
