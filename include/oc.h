@@ -725,8 +725,9 @@ oc_status oc_dropout_rng(oc_dtype dt, int64_t rows, int32_t c, const void* x, do
  * oc_dropout_rng, layer norm as oc_ln_fwd.  y, mean and invstd are formed from h before
  * it is rounded to dt.
  *   res     dev [rows][c] or NULL (0).
- *   h       dev [rows][c], written for the layers above and the backward; may be res.
- *   y       dev [rows][c]; may be x. */
+ *   h       dev [rows][c], the residual of the layers above; may be res.
+ *   y       dev [rows][c]; may be x.
+ * The backward reads x and res again: where it is to run, h is not res and y is not x. */
 oc_status oc_drop_ln_fwd(oc_dtype dt, int64_t rows, int32_t c, const void* x, const void* res,
                          double p, const uint64_t* rng, int32_t site, const float* gamma,
                          const float* beta, float eps, void* h, void* y, float* mean,
@@ -734,15 +735,17 @@ oc_status oc_drop_ln_fwd(oc_dtype dt, int64_t rows, int32_t c, const void* x, co
 
 /* Gradients of oc_drop_ln_fwd: dres = dh + oc_ln_bwd's dx at h for dy, dx = dropout's mask
  * and scale on dres (before its rounding), dgamma and dbeta as oc_ln_bwd.
+ *   x, res  the forward's, from which h is formed once more (the OC_BF16 h that it wrote is
+ *           rounded, which would cost dgamma, an fp32 sum, all but some 9 of its bits).
  *   dh      dev [rows][c], the gradient that reaches h from the layers above, or NULL (0).
  *   dx, dres  dev [rows][c], each or NULL.
  *   rng     the state as the forward read it.
  *   ws      as oc_ln_bwd's. */
-oc_status oc_drop_ln_bwd(oc_dtype dt, int64_t rows, int32_t c, const void* h, const void* dy,
-                         const void* dh, double p, const uint64_t* rng, int32_t site,
-                         const float* gamma, const float* mean, const float* invstd, void* dx,
-                         void* dres, float* dgamma, float* dbeta, void* ws, size_t ws_bytes,
-                         hipStream_t stream);
+oc_status oc_drop_ln_bwd(oc_dtype dt, int64_t rows, int32_t c, const void* x, const void* res,
+                         const void* dy, const void* dh, double p, const uint64_t* rng,
+                         int32_t site, const float* gamma, const float* mean,
+                         const float* invstd, void* dx, void* dres, float* dgamma, float* dbeta,
+                         void* ws, size_t ws_bytes, hipStream_t stream);
 
 /* Table rows by id: y[r] = scale table[id[r]]; 0 where the id is outside the table (as a
  * padded row's may be).

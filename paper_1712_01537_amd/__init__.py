@@ -252,8 +252,8 @@ def load():
         "oc_dropout_rng": ([C.c_int, i64, i32, p, C.c_double, p, i32, p, p], C.c_int),
         "oc_drop_ln_fwd": ([C.c_int, i64, i32, p, p, C.c_double, p, i32, p, p, C.c_float, p, p, p,
                             p, p], C.c_int),
-        "oc_drop_ln_bwd": ([C.c_int, i64, i32, p, p, p, C.c_double, p, i32, p, p, p, p, p, p, p,
-                            p, sz, p], C.c_int),
+        "oc_drop_ln_bwd": ([C.c_int, i64, i32, p, p, p, p, C.c_double, p, i32, p, p, p, p, p, p,
+                            p, p, sz, p], C.c_int),
         "oc_embed_fwd": ([C.c_int, i32, i64, i64, i32, p, p, C.c_float, p, p], C.c_int),
         "oc_embed_bwd_workspace": ([i64, i64, i32], sz),
         "oc_embed_bwd": ([C.c_int, i32, i64, i64, i32, p, p, C.c_float, C.c_int, p, p, sz, p],
@@ -1241,7 +1241,8 @@ def oc_drop_ln_fwd(x, res, p, rng, gamma=None, beta=None, site=0, eps=1e-5, need
                    h=None):
     """The residual step h = res + dropout(x), y = the layer norm of h: (h, y, mean,
     invstd), the last two None unless need_stats.  res: as x, or None (0).  p, rng, site as
-    oc_dropout_rng's (rng may be None for p = 0).  h: where to write it, may be res."""
+    oc_dropout_rng's (rng may be None for p = 0).  h: where to write it; may be res where no
+    backward follows, which reads x and res again."""
     dev, dt, rows, c = _rows_of(x, "x")
     xp = _given(x, "x", dev, x.dtype, (rows, c))
     rp = _rng_state(rng, dev, p)
@@ -1257,17 +1258,19 @@ def oc_drop_ln_fwd(x, res, p, rng, gamma=None, beta=None, site=0, eps=1e-5, need
     return h, y, mean, invstd
 
 
-def oc_drop_ln_bwd(h, dy, p, rng, gamma, mean, invstd, dh=None, site=0, need_dx=True,
+def oc_drop_ln_bwd(x, res, dy, p, rng, gamma, mean, invstd, dh=None, site=0, need_dx=True,
                    need_dres=True, need_dgamma=True, need_dbeta=True, dgamma=None, dbeta=None):
-    """(dx, dres, dgamma, dbeta) of oc_drop_ln_fwd (None where not needed).  dh: the gradient
-    that reaches h from the layers above, or None; rng holds what the forward read."""
-    dev, dt, rows, c = _rows_of(h, "h")
-    t = h.dtype
-    dx = h.new_empty((rows, c)) if need_dx else None
-    dres = h.new_empty((rows, c)) if need_dres else None
-    dgamma, dbeta, gp, bp, ws, wsp, need = _norm_sums(h, dev, rows, c, dgamma, dbeta, need_dgamma,
+    """(dx, dres, dgamma, dbeta) of oc_drop_ln_fwd (None where not needed).  x, res: the
+    forward's (its h is formed again); dh: the gradient that reaches h from the layers
+    above, or None; rng holds what the forward read."""
+    dev, dt, rows, c = _rows_of(x, "x")
+    t = x.dtype
+    dx = x.new_empty((rows, c)) if need_dx else None
+    dres = x.new_empty((rows, c)) if need_dres else None
+    dgamma, dbeta, gp, bp, ws, wsp, need = _norm_sums(x, dev, rows, c, dgamma, dbeta, need_dgamma,
                                                       need_dbeta)
-    _check(load().oc_drop_ln_bwd(dt, rows, c, _given(h, "h", dev, t, (rows, c)),
+    _check(load().oc_drop_ln_bwd(dt, rows, c, _given(x, "x", dev, t, (rows, c)),
+                                 _given(res, "res", dev, t, (rows, c)),
                                  _given(dy, "dy", dev, t, (rows, c)),
                                  _given(dh, "dh", dev, t, (rows, c)), p, _rng_state(rng, dev, p),
                                  site, _given(gamma, "gamma", dev, torch.float32, (c,)),

@@ -25,7 +25,11 @@ __global__ __launch_bounds__(TB) void k_drop_rng(Drop d, const void* x, bool bf1
     const int col = (int)(i - row * nv) * 8;
     float v[8];
     oc::load8n(x, bf16, row * c + col, c - col, n, v);
-    if (d.on) oc::drop8(d, key, (uint64_t)i, v);
+    if (d.on) {
+      bool k[8];
+      oc::keep8(d, key, (uint64_t)i, k);
+      oc::drop8(d, k, v);
+    }
     oc::store8n(y, bf16, row * c + col, c - col, v);
   }
 }

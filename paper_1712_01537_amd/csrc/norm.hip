@@ -14,38 +14,18 @@
 // deviations from 2^63 on has an infinite variance and a y of beta.
 #include <algorithm>
 
-#include "rows.h"
+#include "norm.h"
 
 namespace {
 
 using oc::cdiv;
 using oc::Drop;
+using oc::MOST_ADDED;
+using oc::Norm;
+using oc::NormBwd;
 
 constexpr int TB = 256;
 constexpr int64_t MOST_BLOCKS = (int64_t)1 << 22;  // (a launch has fewer than 2^32 threads)
-
-struct Norm {
-  const void *x, *res;  // res: the residual step's, or NULL
-  void *h, *y;          // h: the residual step's
-  const float *gamma, *beta;
-  float *mean, *invstd;
-  int64_t rows;
-  int c;
-  bool bf16;
-  float eps;
-  Drop drop;
-};
-
-struct NormBwd {
-  const void *h, *dy, *dh;
-  void *dx, *dres;  // dx: behind the dropout; dres: in front of it (a plain norm's dx)
-  const float *gamma, *mean, *invstd;
-  float* delta;  // [rows], for the column sums of rows too long for registers
-  int64_t rows;
-  int c;
-  bool bf16;
-  Drop drop;
-};
 
 // The sums of K values over the block's threads, in every thread: lanes first, then the
 // waves in order.  Two calls in a row need different halves of `red`.
@@ -69,13 +49,17 @@ __device__ __forceinline__ void block_sums(float (&v)[K], float (*red)[K]) {
 // --- rows of any length ----------------------------------------------------------
 // One workgroup a row, which it reads once a pass.
 
-// The values 8 i .. 8 i + 7 of a row's h.
-__device__ __forceinline__ void load_h(const Norm& a, const oc::DropKey& key, int64_t row, int i,
-                                       float (&v)[8]) {
+// The values 8 i .. 8 i + 7 of a row's h; keep: which of them dropout has kept.
+template <typename Args>
+__device__ __forceinline__ void load_h(const Args& a, const oc::DropKey& key, int64_t row, int i,
+                                       float (&v)[8], bool (&keep)[8]) {
   const int c = i * 8, cnt = a.c - c;
   const int64_t at = row * a.c + c, n = a.rows * a.c;
   oc::load8n(a.x, a.bf16, at, cnt, n, v);
-  if (a.drop.on) oc::drop8(a.drop, key, (uint64_t)row * ((a.c + 7) / 8) + i, v);
+  if (a.drop.on) {
+    oc::keep8(a.drop, key, (uint64_t)row * ((a.c + 7) / 8) + i, keep);
+    oc::drop8(a.drop, keep, v);
+  }
   if (a.res) {
     float r[8];
     oc::load8n(a.res, a.bf16, at, cnt, n, r);
@@ -91,16 +75,17 @@ __global__ __launch_bounds__(TB) void k_ln_fwd_any(Norm a) {
   const float rc = 1.f / (float)a.c;
   for (int64_t row = blockIdx.x; row < a.rows; row += gridDim.x) {
   float v[8];
+  bool keep[8];
   float m[1] = {0.f};
   for (int i = threadIdx.x; i < nv; i += TB) {
-    load_h(a, key, row, i, v);
+    load_h(a, key, row, i, v, keep);
 #pragma unroll
     for (int k = 0; k < 8; ++k) m[0] = fmaf(v[k], rc, m[0]);
   }
   block_sums(m, red0);
   float s[2] = {0.f, 0.f};
   for (int i = threadIdx.x; i < nv; i += TB) {
-    load_h(a, key, row, i, v);
+    load_h(a, key, row, i, v, keep);
 #pragma unroll
     for (int k = 0; k < 8; ++k) {
       const float d = i * 8 + k < a.c ? v[k] - m[0] : 0.f;
@@ -114,7 +99,7 @@ __global__ __launch_bounds__(TB) void k_ln_fwd_any(Norm a) {
   if (var < 0.f) var = 0.f;  // (NaN stays NaN)
   const float invstd = 1.f / sqrtf(var + a.eps);
   for (int i = threadIdx.x; i < nv; i += TB) {
-    load_h(a, key, row, i, v);
+    load_h(a, key, row, i, v, keep);
     const int c = i * 8, cnt = a.c - c;
     const int64_t at = row * a.c + c;
     if (a.h) oc::store8n(a.h, a.bf16, at, cnt, v);
@@ -142,9 +127,10 @@ __global__ __launch_bounds__(TB) void k_ln_bwd_any(NormBwd a) {
   __syncthreads();  // the sums of the row before have been read
   const float m = a.mean[row], r = a.invstd[row], rc = 1.f / (float)a.c;
   float d[8], g[8];
+  bool keep[8];
   const auto load = [&](int i) {
     const int c = i * 8, cnt = a.c - c;
-    oc::load8n(a.h, a.bf16, row * a.c + c, cnt, n, d);
+    load_h(a, key, row, i, d, keep);
     oc::load8n(a.dy, a.bf16, row * a.c + c, cnt, n, g);
 #pragma unroll
     for (int k = 0; k < 8; ++k) {
@@ -179,7 +165,7 @@ __global__ __launch_bounds__(TB) void k_ln_bwd_any(NormBwd a) {
     }
     if (a.dres) oc::store8n(a.dres, a.bf16, at, cnt, g);
     if (a.dx) {
-      if (a.drop.on) oc::drop8(a.drop, key, (uint64_t)row * nv + i, g);
+      if (a.drop.on) oc::drop8(a.drop, keep, g);
       oc::store8n(a.dx, a.bf16, at, cnt, g);
     }
   }
@@ -189,7 +175,6 @@ __global__ __launch_bounds__(TB) void k_ln_bwd_any(NormBwd a) {
 // Sums over the rows: a thread has eight columns and every rl-th row of the block's
 // range, at most MOST_ADDED of them, in fp32; the row lanes are added in double, and
 // k_ln_colsum adds the blocks' part[b][2][c] (dgamma, dbeta), in a fixed order.
-constexpr int64_t MOST_ADDED = 64;
 struct ColShape {
   int ct, rl, kb;  // column threads, row lanes, column blocks
   int64_t nb;      // row blocks
@@ -211,11 +196,13 @@ __global__ __launch_bounds__(TB) void k_ln_cols_any(NormBwd a, int ct, float* pa
   const int64_t nb = gridDim.x, b = blockIdx.x;
   const int64_t r0 = a.rows * b / nb, r1 = a.rows * (b + 1) / nb, n = a.rows * a.c;
   const int c = (blockIdx.y * ct + tc) * 8, cnt = a.c - c;
+  const oc::DropKey key = a.drop.on ? oc::drop_key(a.drop) : oc::DropKey{};
   float sg[8] = {}, sb[8] = {};
   if (cnt > 0)
     for (int64_t r = r0 + tr; r < r1; r += rl) {
       float x[8], g[8];
-      oc::load8n(a.h, a.bf16, r * a.c + c, cnt, n, x);
+      bool keep[8];
+      load_h(a, key, r, c / 8, x, keep);
       oc::load8n(a.dy, a.bf16, r * a.c + c, cnt, n, g);
       const float m = a.mean[r], is = a.invstd[r], de = a.delta[r];
 #pragma unroll
@@ -265,26 +252,33 @@ __global__ __launch_bounds__(TB) void k_ln_colsum(const float* part, int64_t nb,
 // --- the calls ---------------------------------------------------------------------
 
 struct BwdWs {
-  size_t part, delta, total;
+  int64_t blocks;
+  size_t delta, total;
 };
 BwdWs bwd_ws(int64_t rows, int c) {
   BwdWs w{};
-  const ColShape d = col_shape(rows, c);
-  w.delta = oc::align256((size_t)d.nb * 2 * c * sizeof(float));
-  w.total = w.delta + oc::align256((size_t)rows * sizeof(float));
+  const bool rows_fit = c <= oc::NORM_ROWS_MOST;
+  w.blocks = rows_fit ? oc::norm_rows_blocks(rows, c) : col_shape(rows, c).nb;
+  w.delta = oc::align256((size_t)w.blocks * 2 * c * sizeof(float));
+  w.total = w.delta + (rows_fit ? 0 : oc::align256((size_t)rows * sizeof(float)));
   return w;
 }
 
 void fwd(const Norm& a, hipStream_t s) {
-  oc::launch_main(k_ln_fwd_any, dim3((unsigned)std::min(a.rows, MOST_BLOCKS)), dim3(TB), s, a);
+  if (a.c <= oc::NORM_ROWS_MOST)
+    oc::norm_rows_fwd(a, s);
+  else
+    oc::launch_main(k_ln_fwd_any, dim3((unsigned)std::min(a.rows, MOST_BLOCKS)), dim3(TB), s, a);
 }
 
 void bwd(NormBwd a, float* dgamma, float* dbeta, void* ws, hipStream_t s) {
   const BwdWs w = bwd_ws(a.rows, a.c);
   const bool cols = dgamma || dbeta;
-  const ColShape d = col_shape(a.rows, a.c);
-  float* part = (float*)ws;
-  if (a.rows > 0) {
+  float* part = cols ? (float*)ws : nullptr;
+  if (a.rows > 0 && a.c <= oc::NORM_ROWS_MOST) {
+    oc::norm_rows_bwd(a, part, s);
+  } else if (a.rows > 0) {
+    const ColShape d = col_shape(a.rows, a.c);
     a.delta = cols ? (float*)((char*)ws + w.delta) : nullptr;
     oc::launch_main(k_ln_bwd_any, dim3((unsigned)std::min(a.rows, MOST_BLOCKS)), dim3(TB), s, a);
     if (cols)
@@ -293,7 +287,7 @@ void bwd(NormBwd a, float* dgamma, float* dbeta, void* ws, hipStream_t s) {
   }
   if (cols)
     oc::launch(k_ln_colsum, dim3((unsigned)cdiv(2 * (int64_t)a.c, 4)), dim3(TB), 0, s,
-               (const float*)part, d.nb, a.c, dgamma, dbeta);
+               (const float*)part, a.rows > 0 ? w.blocks : 0, a.c, dgamma, dbeta);
 }
 
 }  // namespace
@@ -372,23 +366,23 @@ oc_status oc_ln_bwd(oc_dtype dt, int64_t rows, int32_t c, const void* x, const v
                          {"invstd", invstd, nr, false, nullptr}};
   OC_TRY(oc::check_spans(who, sp));
   if ((rows == 0 || !dx) && !dgamma && !dbeta) return OC_OK;
-  bwd(NormBwd{x, dy, nullptr, nullptr, dx, gamma, mean, invstd, nullptr, rows, c, dt == OC_BF16,
+  bwd(NormBwd{x, nullptr, dy, nullptr, nullptr, dx, gamma, mean, invstd, nullptr, rows, c, dt == OC_BF16,
               Drop{}},
       dgamma, dbeta, ws, s);
   OC_LAUNCH_CHECK();
   return OC_OK;
 }
 
-oc_status oc_drop_ln_bwd(oc_dtype dt, int64_t rows, int32_t c, const void* h, const void* dy,
-                         const void* dh, double p, const uint64_t* rng, int32_t site,
-                         const float* gamma, const float* mean, const float* invstd, void* dx,
-                         void* dres, float* dgamma, float* dbeta, void* ws, size_t ws_bytes,
-                         hipStream_t s) {
+oc_status oc_drop_ln_bwd(oc_dtype dt, int64_t rows, int32_t c, const void* x, const void* res,
+                         const void* dy, const void* dh, double p, const uint64_t* rng,
+                         int32_t site, const float* gamma, const float* mean,
+                         const float* invstd, void* dx, void* dres, float* dgamma, float* dbeta,
+                         void* ws, size_t ws_bytes, hipStream_t s) {
   const char* who = "oc_drop_ln_bwd";
   OC_TRY(oc::check_rows(who, dt, rows, c));
   Drop drop;
   OC_TRY(oc::make_drop(who, p, rng, site, &drop));
-  if (rows > 0 && (!h || !dy || !mean || !invstd))
+  if (rows > 0 && (!x || !dy || !mean || !invstd))
     return oc::fail(OC_ERR_ARG, "%s: NULL buffer", who);
   const size_t need = dgamma || dbeta ? oc_ln_bwd_workspace(rows, c) : 0;
   OC_TRY(oc::check_row_ws(who, ws, ws_bytes, need));
@@ -398,7 +392,8 @@ oc_status oc_drop_ln_bwd(oc_dtype dt, int64_t rows, int32_t c, const void* h, co
                          {"dgamma", dgamma, nc, true, nullptr},
                          {"dbeta", dbeta, nc, true, nullptr},
                          {"the workspace", need ? ws : nullptr, need, true, nullptr},
-                         {"h", h, n, false, nullptr},
+                         {"x", x, n, false, nullptr},
+                         {"res", res, n, false, nullptr},
                          {"dy", dy, n, false, nullptr},
                          {"dh", dh, n, false, nullptr},
                          {"gamma", gamma, nc, false, nullptr},
@@ -407,7 +402,7 @@ oc_status oc_drop_ln_bwd(oc_dtype dt, int64_t rows, int32_t c, const void* h, co
                          {"rng", rng, drop.on ? (size_t)16 : 0, false, nullptr}};
   OC_TRY(oc::check_spans(who, sp));
   if ((rows == 0 || (!dx && !dres)) && !dgamma && !dbeta) return OC_OK;
-  bwd(NormBwd{h, dy, dh, dx, dres, gamma, mean, invstd, nullptr, rows, c, dt == OC_BF16, drop},
+  bwd(NormBwd{x, res, dy, dh, dx, dres, gamma, mean, invstd, nullptr, rows, c, dt == OC_BF16, drop},
       dgamma, dbeta, ws, s);
   OC_LAUNCH_CHECK();
   return OC_OK;

@@ -1,0 +1,469 @@
+// Layer norm and the residual step on rows that fit in registers: TPR threads hold a row,
+// NV vectors of eight channels each, so that each row is read once.
+#include <algorithm>
+
+#include "norm.h"
+
+namespace {
+
+using oc::cdiv;
+using oc::d_v4f;
+using oc::d_v4f_any;
+using oc::d_v4u;
+using oc::d_v4u_any;
+using oc::MOST_ADDED;
+using oc::Norm;
+using oc::NormBwd;
+
+// Eight values as they lie in memory, so that a load can be in flight while the row
+// before is worked on.
+template <bool BF>
+struct Raw;
+template <>
+struct Raw<true> {
+  d_v4u u;
+};
+template <>
+struct Raw<false> {
+  d_v4f a, b;
+};
+__device__ __forceinline__ void raw_load(Raw<true>& r, const void* p, int64_t i, int64_t n) {
+  if (i + 8 <= n) {
+    r.u = *(const d_v4u_any*)((const uint16_t*)p + i);
+  } else {
+    uint32_t h[8];
+#pragma unroll
+    for (int k = 0; k < 8; ++k) h[k] = i + k < n ? ((const uint16_t*)p)[i + k] : 0;
+    r.u = d_v4u{h[0] | h[1] << 16, h[2] | h[3] << 16, h[4] | h[5] << 16, h[6] | h[7] << 16};
+  }
+}
+__device__ __forceinline__ void raw_load(Raw<false>& r, const void* p, int64_t i, int64_t n) {
+  if (i + 8 <= n) {
+    r.a = *(const d_v4f_any*)((const float*)p + i);
+    r.b = *(const d_v4f_any*)((const float*)p + i + 4);
+  } else {
+    float v[8];
+#pragma unroll
+    for (int k = 0; k < 8; ++k) v[k] = i + k < n ? ((const float*)p)[i + k] : 0.f;
+    r.a = d_v4f{v[0], v[1], v[2], v[3]};
+    r.b = d_v4f{v[4], v[5], v[6], v[7]};
+  }
+}
+__device__ __forceinline__ void unpack(const Raw<true>& r, float (&v)[8]) {
+#pragma unroll
+  for (int k = 0; k < 4; ++k) {
+    v[2 * k] = oc::bf_up(r.u[k] & 0xffffu);
+    v[2 * k + 1] = __builtin_bit_cast(float, r.u[k] & 0xffff0000u);
+  }
+}
+__device__ __forceinline__ void unpack(const Raw<false>& r, float (&v)[8]) {
+#pragma unroll
+  for (int k = 0; k < 4; ++k) v[k] = r.a[k], v[4 + k] = r.b[k];
+}
+
+// (A vector's element goes by value: __builtin_bit_cast of v[1] itself takes v[0].)
+__device__ __forceinline__ float float_of(uint32_t u) { return __builtin_bit_cast(float, u); }
+
+// v of another lane by data-parallel primitives (no trip through LDS).
+template <int CTRL>
+__device__ __forceinline__ float dpp(float v) {
+  return __builtin_bit_cast(
+      float, __builtin_amdgcn_update_dpp(0, __builtin_bit_cast(int, v), CTRL, 0xf, 0xf, true));
+}
+// The sum over groups of L lanes (a power of two up to 64), in each of them: pairs, then
+// pairs of pairs, ...  Each step adds the same two values in both halves, so that the
+// lanes agree in every bit.
+template <int L>
+__device__ __forceinline__ float lanes_sum(float v) {
+  if (L >= 2) v += dpp<0xB1>(v);   // quad_perm 1 0 3 2
+  if (L >= 4) v += dpp<0x4E>(v);   // quad_perm 2 3 0 1
+  if (L >= 8) v += dpp<0x141>(v);  // row_half_mirror: the other four of eight
+  if (L >= 16) v += dpp<0x140>(v); // row_mirror: the other eight of sixteen
+  if (L >= 32) {
+    const uint32_t u = __builtin_bit_cast(uint32_t, v);
+    const auto r = __builtin_amdgcn_permlane16_swap(u, u, false, false);
+    v = float_of(r[0]) + float_of(r[1]);
+  }
+  if (L >= 64) {
+    const uint32_t u = __builtin_bit_cast(uint32_t, v);
+    const auto r = __builtin_amdgcn_permlane32_swap(u, u, false, false);
+    v = float_of(r[0]) + float_of(r[1]);
+  }
+  return v;
+}
+
+// (one row a workgroup where its waves share sums: they pass the barriers together)
+constexpr int block_of(int tpr) { return tpr <= 64 ? 256 : tpr; }
+
+// The row's h from what lies in memory; values behind the row's end are 0.
+template <bool BF, bool STEP>
+__device__ __forceinline__ void form_h(const Raw<BF>& x, const Raw<BF>& res, bool has_res,
+                                       const oc::Drop& drop, const oc::DropKey& key,
+                                       uint64_t index, int cnt, float (&v)[8], bool (&keep)[8]) {
+  unpack(x, v);
+  if (STEP) {
+    if (drop.on) {
+      oc::keep8(drop, key, index, keep);
+      oc::drop8(drop, keep, v);
+    }
+    if (has_res) {
+      float r[8];
+      unpack(res, r);
+#pragma unroll
+      for (int k = 0; k < 8; ++k) v[k] += r[k];
+    }
+  }
+  if (cnt < 8) {
+#pragma unroll
+    for (int k = 0; k < 8; ++k) v[k] = k < cnt ? v[k] : 0.f;
+  }
+}
+
+// The sums over the waves of a row (at most 16), wave by wave.  Rows in turn use the two
+// halves of `red`: a wave that has passed a row's barrier has read the row's before.
+//
+// Forward.  The lanes of a wave find their mean m by one sum, then delta = mean of v - m
+// and the squares of v - m by two more; waves are joined by Chan et al.'s formula for
+// counts, means and sums of squared deviations, relative to the first wave's mean.
+template <bool BF, int TPR, int NV, bool STEP>
+__global__ __launch_bounds__(block_of(TPR)) void k_ln_rows(Norm a) {
+  constexpr int BLK = block_of(TPR), G = BLK / TPR, L = TPR < 64 ? TPR : 64, W = TPR / L;
+  __shared__ float red[2][BLK / 64][3];
+  const int t = threadIdx.x % TPR, g = threadIdx.x / TPR;
+  const int nv = (a.c + 7) / 8;
+  const int64_t n = a.rows * a.c, stride = (int64_t)gridDim.x * G;
+  const oc::DropKey key = STEP && a.drop.on ? oc::drop_key(a.drop) : oc::DropKey{};
+  const bool has_res = STEP && a.res;
+  int cnt[NV];
+  float gam[NV][8], bet[NV][8];
+#pragma unroll
+  for (int j = 0; j < NV; ++j) {
+    const int col = (j * TPR + t) * 8;
+    cnt[j] = a.c - col;
+#pragma unroll
+    for (int k = 0; k < 8; ++k) gam[j][k] = 1.f, bet[j][k] = 0.f;
+    if (a.gamma && cnt[j] > 0) oc::load8n(a.gamma, false, col, cnt[j], a.c, gam[j]);
+    if (a.beta && cnt[j] > 0) oc::load8n(a.beta, false, col, cnt[j], a.c, bet[j]);
+  }
+  // channels of this wave's part of a row
+  const auto channels = [&](int w) {
+    int have = 0;
+#pragma unroll
+    for (int j = 0; j < NV; ++j) {
+      const int left = a.c - (j * TPR + w * L) * 8;
+      have += left < 0 ? 0 : left < L * 8 ? left : L * 8;
+    }
+    return (float)have;
+  };
+  const int w0 = t / L;
+  const float own = channels(w0), r_own = own > 0.f ? 1.f / own : 0.f, rc = 1.f / (float)a.c;
+  Raw<BF> x[NV], res[NV];
+  const auto load = [&](int64_t row) {
+#pragma unroll
+    for (int j = 0; j < NV; ++j)
+      if (cnt[j] > 0) {
+        const int64_t at = row * a.c + (j * TPR + t) * 8;
+        raw_load(x[j], a.x, at, n);
+        if (has_res) raw_load(res[j], a.res, at, n);
+      }
+  };
+  int64_t row = (int64_t)blockIdx.x * G + g;
+  if (row < a.rows) load(row);
+  for (int par = 0; row < a.rows; row += stride, par ^= 1) {
+    float v[NV][8];
+    bool keep[8];
+#pragma unroll
+    for (int j = 0; j < NV; ++j) {
+      if (cnt[j] > 0)
+        form_h<BF, STEP>(x[j], res[j], has_res, a.drop, key,
+                         (uint64_t)row * nv + (j * TPR + t), cnt[j], v[j], keep);
+      else
+#pragma unroll
+        for (int k = 0; k < 8; ++k) v[j][k] = 0.f;
+    }
+    if (row + stride < a.rows) load(row + stride);
+    if (STEP) {
+#pragma unroll
+      for (int j = 0; j < NV; ++j)
+        if (cnt[j] > 0) oc::store8n(a.h, BF, row * a.c + (j * TPR + t) * 8, cnt[j], v[j]);
+    }
+    float m = 0.f;
+#pragma unroll
+    for (int j = 0; j < NV; ++j)
+#pragma unroll
+      for (int k = 0; k < 8; ++k) m = fmaf(v[j][k], r_own, m);
+    m = lanes_sum<L>(m);
+    float s1 = 0.f, s2 = 0.f;
+#pragma unroll
+    for (int j = 0; j < NV; ++j)
+#pragma unroll
+      for (int k = 0; k < 8; ++k) {
+        v[j][k] = k < cnt[j] ? v[j][k] - m : 0.f;
+        s1 += v[j][k];
+        s2 = fmaf(v[j][k], v[j][k], s2);
+      }
+    s1 = lanes_sum<L>(s1);
+    s2 = lanes_sum<L>(s2);
+    float delta = s1 * r_own, m2 = fmaf(-delta, s1, s2), mean = m + delta;
+    if (W > 1) {
+      if ((t & 63) == 0) {
+        red[par][w0][0] = m;
+        red[par][w0][1] = delta;
+        red[par][w0][2] = m2;
+      }
+      __syncthreads();
+      const float m0 = red[par][0][0];
+      float far = 0.f;  // the row's mean - m0
+#pragma unroll
+      for (int w = 0; w < W; ++w)
+        far = fmaf(channels(w) * rc, (red[par][w][0] - m0) + red[par][w][1], far);
+      m2 = 0.f;
+#pragma unroll
+      for (int w = 0; w < W; ++w) {
+        const float d = ((red[par][w][0] - m0) + red[par][w][1]) - far, nw = channels(w);
+        m2 += nw > 0.f ? fmaf(nw * d, d, red[par][w][2]) : 0.f;
+      }
+      delta = far - (m - m0);  // of this wave's deviations
+      mean = m0 + far;
+    }
+    float var = m2 * rc;
+    if (var < 0.f) var = 0.f;  // (NaN stays NaN)
+    const float invstd = 1.f / sqrtf(var + a.eps);
+#pragma unroll
+    for (int j = 0; j < NV; ++j) {
+      if (cnt[j] <= 0) continue;
+#pragma unroll
+      for (int k = 0; k < 8; ++k)
+        v[j][k] = fmaf((v[j][k] - delta) * invstd, gam[j][k], bet[j][k]);
+      oc::store8n(a.y, BF, row * a.c + (j * TPR + t) * 8, cnt[j], v[j]);
+    }
+    if (t == 0) {
+      if (a.mean) a.mean[row] = mean;
+      if (a.invstd) a.invstd[row] = invstd;
+    }
+  }
+}
+
+// Backward: one reduction of three sums a row.  dgamma's and dbeta's sums stay in
+// registers over the group's rows, at most MOST_ADDED; the workgroup's groups are then
+// added in double through LDS, and its sums written for the sum over the workgroups.
+template <bool BF, int TPR, int NV, bool STEP>
+__global__ __launch_bounds__(block_of(TPR)) void k_ln_rows_bwd(NormBwd a, float* part) {
+  constexpr int BLK = block_of(TPR), G = BLK / TPR, L = TPR < 64 ? TPR : 64, W = TPR / L;
+  __shared__ float red[2][BLK / 64][3];
+  __shared__ float cols[G > 1 ? 2 : 1][G > 1 ? 8 : 1][G > 1 ? BLK : 1];
+  const int t = threadIdx.x % TPR, g = threadIdx.x / TPR;
+  const int nv = (a.c + 7) / 8;
+  const int64_t n = a.rows * a.c, nb = gridDim.x, b = blockIdx.x;
+  const int64_t r0 = a.rows * b / nb, r1 = a.rows * (b + 1) / nb;
+  const oc::DropKey key = STEP && a.drop.on ? oc::drop_key(a.drop) : oc::DropKey{};
+  const bool has_res = STEP && a.res, has_dh = STEP && a.dh;
+  const float rc = 1.f / (float)a.c;
+  int cnt[NV];
+  float gam[NV][8], sg[NV][8], sb[NV][8];
+#pragma unroll
+  for (int j = 0; j < NV; ++j) {
+    const int col = (j * TPR + t) * 8;
+    cnt[j] = a.c - col;
+#pragma unroll
+    for (int k = 0; k < 8; ++k) gam[j][k] = 1.f, sg[j][k] = sb[j][k] = 0.f;
+    if (a.gamma && cnt[j] > 0) oc::load8n(a.gamma, false, col, cnt[j], a.c, gam[j]);
+  }
+  Raw<BF> x[NV], res[NV], dy[NV], dh[NV];
+  float mean = 0.f, invstd = 0.f;
+  const auto load = [&](int64_t row) {
+    mean = a.mean[row];
+    invstd = a.invstd[row];
+#pragma unroll
+    for (int j = 0; j < NV; ++j)
+      if (cnt[j] > 0) {
+        const int64_t at = row * a.c + (j * TPR + t) * 8;
+        raw_load(x[j], a.x, at, n);
+        raw_load(dy[j], a.dy, at, n);
+        if (has_res) raw_load(res[j], a.res, at, n);
+        if (has_dh) raw_load(dh[j], a.dh, at, n);
+      }
+  };
+  int64_t row = r0 + g;
+  if (row < r1) load(row);
+  for (int par = 0; row < r1; row += G, par ^= 1) {
+    float d[NV][8], e[NV][8], u[NV][8];
+    bool keep[NV][8];
+    const float m = mean, r = invstd;
+    float s[3] = {0.f, 0.f, 0.f};
+#pragma unroll
+    for (int j = 0; j < NV; ++j) {
+      if (cnt[j] > 0) {
+        form_h<BF, STEP>(x[j], res[j], has_res, a.drop, key,
+                         (uint64_t)row * nv + (j * TPR + t), cnt[j], d[j], keep[j]);
+        unpack(dy[j], e[j]);
+        if (has_dh) unpack(dh[j], u[j]);
+      }
+#pragma unroll
+      for (int k = 0; k < 8; ++k) {
+        d[j][k] = k < cnt[j] ? d[j][k] - m : 0.f;
+        e[j][k] = k < cnt[j] ? e[j][k] : 0.f;
+        const float q = e[j][k] * gam[j][k];
+        s[0] += q;
+        s[1] = fmaf(q, d[j][k], s[1]);
+        s[2] += d[j][k];
+      }
+    }
+    if (row + G < r1) load(row + G);
+#pragma unroll
+    for (int k = 0; k < 3; ++k) s[k] = lanes_sum<L>(s[k]);
+    if (W > 1) {
+      if ((t & 63) == 0) {
+#pragma unroll
+        for (int k = 0; k < 3; ++k) red[par][t / 64][k] = s[k];
+      }
+      __syncthreads();
+#pragma unroll
+      for (int k = 0; k < 3; ++k) {
+        s[k] = red[par][0][k];
+#pragma unroll
+        for (int w = 1; w < W; ++w) s[k] += red[par][w][k];
+      }
+    }
+    const float delta = s[2] * rc, gm = s[0] * rc, zm = fmaf(-delta, s[0], s[1]) * rc * r;
+#pragma unroll
+    for (int j = 0; j < NV; ++j) {
+#pragma unroll
+      for (int k = 0; k < 8; ++k) {
+        const float z = (d[j][k] - delta) * r;
+        sg[j][k] = fmaf(e[j][k], z, sg[j][k]);
+        sb[j][k] += e[j][k];
+        e[j][k] = r * fmaf(-z, zm, fmaf(e[j][k], gam[j][k], -gm));
+        if (has_dh) e[j][k] += u[j][k];
+      }
+      if (cnt[j] <= 0) continue;
+      const int64_t at = row * a.c + (j * TPR + t) * 8;
+      if (a.dres) oc::store8n(a.dres, BF, at, cnt[j], e[j]);
+      if (STEP && a.dx) {
+        if (a.drop.on) oc::drop8(a.drop, keep[j], e[j]);
+        oc::store8n(a.dx, BF, at, cnt[j], e[j]);
+      }
+    }
+  }
+  if (!part) return;
+  if (G == 1) {
+#pragma unroll
+    for (int j = 0; j < NV; ++j) {
+      if (cnt[j] <= 0) continue;
+      const int col = (j * TPR + t) * 8;
+      oc::store8n(part, false, b * 2 * a.c + col, cnt[j], sg[j]);
+      oc::store8n(part, false, (b * 2 + 1) * a.c + col, cnt[j], sb[j]);
+    }
+    return;
+  }
+#pragma unroll
+  for (int j = 0; j < NV; ++j) {
+    __syncthreads();
+#pragma unroll
+    for (int k = 0; k < 8; ++k) {
+      cols[0][k][threadIdx.x] = sg[j][k];
+      cols[G > 1][k][threadIdx.x] = sb[j][k];
+    }
+    __syncthreads();
+    for (int i = threadIdx.x; i < TPR * 16; i += BLK) {
+      const int h = i / (TPR * 8), q = i % (TPR * 8), col = j * TPR * 8 + q;
+      if (col >= a.c) continue;
+      double sum = 0.0;
+#pragma unroll
+      for (int w = 0; w < G; ++w) sum += (double)cols[h][q & 7][w * TPR + (q >> 3)];
+      part[(b * 2 + h) * a.c + col] = (float)sum;
+    }
+  }
+}
+
+// Threads of a row of c channels with v vectors each, at least as many as a power of two
+// up to a wave takes.
+int threads_of(int c, int v) {
+  const int nv = (int)cdiv(c, 8);
+  int t = 1;
+  while (t < 64 && t < nv) t *= 2;
+  while (v * t < nv) t *= 2;
+  return t;
+}
+int threads_bwd(int c) { return threads_of(c, c <= 8192 ? 1 : 2); }
+
+// f(threads of a row, vectors of a thread), both as constants.
+template <int V>
+using Int = std::integral_constant<int, V>;
+template <typename F>
+void with_small(int t, F&& f) {
+  switch (t) {
+    case 1: return f(Int<1>{}, Int<1>{});
+    case 2: return f(Int<2>{}, Int<1>{});
+    case 4: return f(Int<4>{}, Int<1>{});
+    case 8: return f(Int<8>{}, Int<1>{});
+    case 16: return f(Int<16>{}, Int<1>{});
+    case 32: return f(Int<32>{}, Int<1>{});
+    default: return f(Int<64>{}, Int<1>{});
+  }
+}
+template <typename F>
+void with_fwd(int c, F&& f) {
+  const int t = threads_of(c, 2);
+  if (c <= 512) return with_small(t, f);
+  switch (t) {
+    case 64: return f(Int<64>{}, Int<2>{});
+    case 128: return f(Int<128>{}, Int<2>{});
+    case 256: return f(Int<256>{}, Int<2>{});
+    case 512: return f(Int<512>{}, Int<2>{});
+    default: return f(Int<1024>{}, Int<2>{});
+  }
+}
+template <typename F>
+void with_bwd(int c, F&& f) {
+  const int t = threads_bwd(c);
+  if (c <= 512) return with_small(t, f);
+  if (c > 8192) return f(Int<1024>{}, Int<2>{});
+  switch (t) {
+    case 128: return f(Int<128>{}, Int<1>{});
+    case 256: return f(Int<256>{}, Int<1>{});
+    case 512: return f(Int<512>{}, Int<1>{});
+    default: return f(Int<1024>{}, Int<1>{});
+  }
+}
+
+}  // namespace
+
+namespace oc {
+
+void norm_rows_fwd(const Norm& a, hipStream_t s) {
+  with_fwd(a.c, [&](auto t, auto v) {
+    constexpr int TPR = decltype(t)::value, NV = decltype(v)::value, BLK = block_of(TPR);
+    const int64_t blocks = std::min<int64_t>(cdiv(a.rows, BLK / TPR), 2048 * 256 / BLK);
+    const auto go = [&](auto kernel) {
+      launch_main(kernel, dim3((unsigned)blocks), dim3(BLK), s, a);
+    };
+    if (a.h)
+      a.bf16 ? go(k_ln_rows<true, TPR, NV, true>) : go(k_ln_rows<false, TPR, NV, true>);
+    else
+      a.bf16 ? go(k_ln_rows<true, TPR, NV, false>) : go(k_ln_rows<false, TPR, NV, false>);
+  });
+}
+
+int64_t norm_rows_blocks(int64_t rows, int32_t c) {
+  const int tpr = threads_bwd(c), g = block_of(tpr) / tpr;
+  const int64_t most = 2048 * 256 / block_of(tpr);
+  return std::max(std::min<int64_t>(cdiv(rows, 4 * g), most), cdiv(rows, MOST_ADDED * g));
+}
+
+void norm_rows_bwd(const NormBwd& a, float* part, hipStream_t s) {
+  const int64_t blocks = norm_rows_blocks(a.rows, a.c);
+  with_bwd(a.c, [&](auto t, auto v) {
+    constexpr int TPR = decltype(t)::value, NV = decltype(v)::value;
+    const auto go = [&](auto kernel) {
+      launch_main(kernel, dim3((unsigned)blocks), dim3(block_of(TPR)), s, a, part);
+    };
+    if (a.drop.on || a.res || a.dx || a.dh)
+      a.bf16 ? go(k_ln_rows_bwd<true, TPR, NV, true>) : go(k_ln_rows_bwd<false, TPR, NV, true>);
+    else
+      a.bf16 ? go(k_ln_rows_bwd<true, TPR, NV, false>)
+             : go(k_ln_rows_bwd<false, TPR, NV, false>);
+  });
+}
+
+}  // namespace oc

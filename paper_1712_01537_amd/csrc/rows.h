@@ -68,10 +68,7 @@ __device__ __forceinline__ void keep8(const Drop& d, const DropKey& key, uint64_
     }
   }
 }
-__device__ __forceinline__ void drop8(const Drop& d, const DropKey& key, uint64_t index,
-                                      float (&v)[8]) {
-  bool k[8];
-  keep8(d, key, index, k);
+__device__ __forceinline__ void drop8(const Drop& d, const bool (&k)[8], float (&v)[8]) {
 #pragma unroll
   for (int j = 0; j < 8; ++j) v[j] = k[j] ? v[j] * d.scale : 0.f;
 }

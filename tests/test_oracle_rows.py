@@ -120,11 +120,11 @@ def _drop_ln_fwd(dt=F32, rows=4, c=8, x=1, res=2, p=0.5, rng=3, site=0, gamma=4,
                                     *a[5:], None)
 
 
-def _drop_ln_bwd(dt=F32, rows=4, c=8, h=1, dy=2, dh=3, p=0.5, rng=4, site=0, gamma=5, mean=6,
+def _drop_ln_bwd(dt=F32, rows=4, c=8, x=1, res=13, dy=2, dh=3, p=0.5, rng=4, site=0, gamma=5, mean=6,
                  invstd=7, dx=8, dres=9, dg=10, db=11, ws=12, ws_bytes=1 << 20):
     a = [None if v is None else _at(v)
-         for v in (h, dy, dh, rng, gamma, mean, invstd, dx, dres, dg, db, ws)]
-    return oc.load().oc_drop_ln_bwd(dt, rows, c, a[0], a[1], a[2], p, a[3], site, *a[4:],
+         for v in (x, res, dy, dh, rng, gamma, mean, invstd, dx, dres, dg, db, ws)]
+    return oc.load().oc_drop_ln_bwd(dt, rows, c, *a[:4], p, a[4], site, *a[5:],
                                     ws_bytes, None)
 
 
@@ -160,7 +160,7 @@ REFUSED = [
     (_drop_ln_fwd, dict(p=1.5)), (_drop_ln_fwd, dict(eps=-1.0)), (_drop_ln_fwd, dict(h=None)),
     (_drop_ln_fwd, dict(x=None)), (_drop_ln_fwd, dict(y=None)), (_drop_ln_fwd, dict(rng=None)),
     (_drop_ln_fwd, dict(h=1)), (_drop_ln_fwd, dict(y=2)), (_drop_ln_fwd, dict(h=7)),
-    (_drop_ln_bwd, dict(p=1.0)), (_drop_ln_bwd, dict(h=None)), (_drop_ln_bwd, dict(dx=9)),
+    (_drop_ln_bwd, dict(p=1.0)), (_drop_ln_bwd, dict(x=None)), (_drop_ln_bwd, dict(dx=13)), (_drop_ln_bwd, dict(dx=9)),
     (_drop_ln_bwd, dict(dres=3)), (_drop_ln_bwd, dict(dx=2)), (_drop_ln_bwd, dict(rng=None)),
     (_drop_ln_bwd, dict(ws_bytes=0)), (_drop_ln_bwd, dict(site=1 << 20)),
     (_embed_fwd, dict(flags=2)), (_embed_fwd, dict(num=0)), (_embed_fwd, dict(num=1 << 28)),
@@ -219,6 +219,6 @@ def test_binding_refuses_what_is_no_device_tensor():
                  lambda: oc.oc_embed_fwd(torch.zeros(2, dtype=torch.int32), x),
                  lambda: oc.oc_embed_bwd(torch.zeros(2, dtype=torch.int32), x, 4),
                  lambda: oc.oc_ln_bwd(x, x, None, x[0], x[0]),
-                 lambda: oc.oc_drop_ln_bwd(x, x, 0.0, None, None, x[0], x[0])):
+                 lambda: oc.oc_drop_ln_bwd(x, x, x, 0.0, None, None, x[0], x[0])):
         with pytest.raises(oc.OcError):
             call()
