@@ -328,8 +328,8 @@ def _own(s):
     out = {"h": h, "y": y}
     if not train:
         return out
-    dx, dres, dg, db = oc.oc_drop_ln_bwd(h, s["dy"], c["p"], s["rng"], s["gamma"], mean, invstd,
-                                         dh=s["dh"], site=c["site"], need_dres=c["res"])
+    dx, dres, dg, db = oc.oc_drop_ln_bwd(x, s["res"], s["dy"], c["p"], s["rng"], s["gamma"], mean,
+                                         invstd, dh=s["dh"], site=c["site"], need_dres=c["res"])
     out.update(dx=dx, dgamma=dg, dbeta=db)
     return dict(out, dres=dres) if c["res"] else out
 
