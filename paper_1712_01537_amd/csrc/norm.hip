@@ -224,20 +224,22 @@ __global__ __launch_bounds__(TB) void k_ln_cols_any(NormBwd a, int ct, float* pa
 }
 
 // dgamma[c], dbeta[c] = the sums of part[b][0 / 1][c] over the nb blocks, in double: 64
-// lanes a column take every 64th block, then a fixed tree through LDS.
-__global__ __launch_bounds__(TB) void k_ln_colsum(const float* part, int64_t nb, int c,
+// lanes a column take every 64th block, then a fixed tree through LDS.  A workgroup has 16
+// columns (64 bytes of a row of part).
+constexpr int CB = 1024, CC = 16;
+__global__ __launch_bounds__(CB) void k_ln_colsum(const float* part, int64_t nb, int c,
                                                   float* dgamma, float* dbeta) {
-  __shared__ double red[TB];
-  const int cl = threadIdx.x & 3, l = threadIdx.x >> 2;
-  const int64_t j = (int64_t)blockIdx.x * 4 + cl, n = 2 * (int64_t)c;
+  __shared__ double red[CB];
+  const int cl = threadIdx.x % CC, l = threadIdx.x / CC;
+  const int64_t j = (int64_t)blockIdx.x * CC + cl, n = 2 * (int64_t)c;
   double a = 0.0;
   if (j < n) {
 #pragma unroll 8
-    for (int64_t b = l; b < nb; b += 64) a += (double)part[b * n + j];
+    for (int64_t b = l; b < nb; b += CB / CC) a += (double)part[b * n + j];
   }
   red[threadIdx.x] = a;
   __syncthreads();
-  for (int h = TB / 2; h >= 4; h >>= 1) {
+  for (int h = CB / 2; h >= CC; h >>= 1) {
     if ((int)threadIdx.x < h) red[threadIdx.x] += red[threadIdx.x + h];
     __syncthreads();
   }
@@ -286,7 +288,7 @@ void bwd(NormBwd a, float* dgamma, float* dbeta, void* ws, hipStream_t s) {
                  part);
   }
   if (cols)
-    oc::launch(k_ln_colsum, dim3((unsigned)cdiv(2 * (int64_t)a.c, 4)), dim3(TB), 0, s,
+    oc::launch(k_ln_colsum, dim3((unsigned)cdiv(2 * (int64_t)a.c, CC)), dim3(CB), 0, s,
                (const float*)part, a.rows > 0 ? w.blocks : 0, a.c, dgamma, dbeta);
 }
 

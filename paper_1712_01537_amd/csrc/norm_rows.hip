@@ -27,27 +27,62 @@ template <>
 struct Raw<false> {
   d_v4f a, b;
 };
-__device__ __forceinline__ void raw_load(Raw<true>& r, const void* p, int64_t i, int64_t n) {
-  if (i + 8 <= n) {
-    r.u = *(const d_v4u_any*)((const uint16_t*)p + i);
+// A lane's number of values, behind the compiler's back: it would form the eight
+// comparisons with it in front of the loop over the rows and keep them there in 16 scalar
+// registers, which it then has to save and fetch.
+__device__ __forceinline__ int hidden(int cnt) {
+  asm("" : "+v"(cnt));
+  return cnt;
+}
+// Zeros behind the row's end, in the lanes that have it.
+__device__ __forceinline__ void cut(float (&v)[8], int cnt) {
+  if (cnt < 8) {
+    const int q = hidden(cnt);
+#pragma unroll
+    for (int k = 0; k < 8; ++k) v[k] = k < q ? v[k] : 0.f;
+  }
+}
+
+// A row's place in an array: where a wave has one row (all but the shortest), the row's
+// start is the same for its lanes and a lane's own part 32 bits.
+struct Place {
+  int64_t at;  // the row's first element
+  int col, cnt;
+  int64_t left;  // elements from there to the array's end
+};
+__device__ __forceinline__ void raw_load(Raw<true>& r, const void* p, const Place& w) {
+  const uint16_t* q = (const uint16_t*)p + w.at;
+  if (w.cnt >= 8 || w.col + 8 <= w.left) {
+    r.u = *(const d_v4u_any*)(q + (uint32_t)w.col);
   } else {
+    const int c = hidden(w.cnt);
     uint32_t h[8];
 #pragma unroll
-    for (int k = 0; k < 8; ++k) h[k] = i + k < n ? ((const uint16_t*)p)[i + k] : 0;
+    for (int k = 0; k < 8; ++k) h[k] = k < c ? q[w.col + k] : 0;
     r.u = d_v4u{h[0] | h[1] << 16, h[2] | h[3] << 16, h[4] | h[5] << 16, h[6] | h[7] << 16};
   }
 }
-__device__ __forceinline__ void raw_load(Raw<false>& r, const void* p, int64_t i, int64_t n) {
-  if (i + 8 <= n) {
-    r.a = *(const d_v4f_any*)((const float*)p + i);
-    r.b = *(const d_v4f_any*)((const float*)p + i + 4);
+__device__ __forceinline__ void raw_load(Raw<false>& r, const void* p, const Place& w) {
+  const float* q = (const float*)p + w.at;
+  if (w.cnt >= 8 || w.col + 8 <= w.left) {
+    r.a = *(const d_v4f_any*)(q + (uint32_t)w.col);
+    r.b = *(const d_v4f_any*)(q + (uint32_t)w.col + 4);
   } else {
+    const int c = hidden(w.cnt);
     float v[8];
 #pragma unroll
-    for (int k = 0; k < 8; ++k) v[k] = i + k < n ? ((const float*)p)[i + k] : 0.f;
+    for (int k = 0; k < 8; ++k) v[k] = k < c ? q[w.col + k] : 0.f;
     r.a = d_v4f{v[0], v[1], v[2], v[3]};
     r.b = d_v4f{v[4], v[5], v[6], v[7]};
   }
+}
+template <bool BF>
+__device__ __forceinline__ void row_store(void* p, const Place& w, const float (&v)[8]) {
+  void* q = BF ? (void*)((uint16_t*)p + w.at) : (void*)((float*)p + w.at);
+  if (w.cnt >= 8)
+    oc::store8(q, BF, (uint32_t)w.col, v);
+  else
+    oc::store8n(q, BF, (uint32_t)w.col, hidden(w.cnt), v);
 }
 __device__ __forceinline__ void unpack(const Raw<true>& r, float (&v)[8]) {
 #pragma unroll
@@ -92,14 +127,15 @@ __device__ __forceinline__ float lanes_sum(float v) {
   return v;
 }
 
-// (one row a workgroup where its waves share sums: they pass the barriers together)
-constexpr int block_of(int tpr) { return tpr <= 64 ? 256 : tpr; }
+// Threads of a workgroup.
+constexpr int block_fwd(int tpr) { return tpr <= 64 ? 256 : tpr; }
+constexpr int block_bwd(int tpr) { return tpr <= 512 ? 512 : tpr; }
 
-// The row's h from what lies in memory; values behind the row's end are 0.
+// The row's h from what lies in memory.
 template <bool BF, bool STEP>
 __device__ __forceinline__ void form_h(const Raw<BF>& x, const Raw<BF>& res, bool has_res,
                                        const oc::Drop& drop, const oc::DropKey& key,
-                                       uint64_t index, int cnt, float (&v)[8], bool (&keep)[8]) {
+                                       uint64_t index, float (&v)[8], bool (&keep)[8]) {
   unpack(x, v);
   if (STEP) {
     if (drop.on) {
@@ -113,23 +149,25 @@ __device__ __forceinline__ void form_h(const Raw<BF>& x, const Raw<BF>& res, boo
       for (int k = 0; k < 8; ++k) v[k] += r[k];
     }
   }
-  if (cnt < 8) {
-#pragma unroll
-    for (int k = 0; k < 8; ++k) v[k] = k < cnt ? v[k] : 0.f;
-  }
 }
 
-// The sums over the waves of a row (at most 16), wave by wave.  Rows in turn use the two
-// halves of `red`: a wave that has passed a row's barrier has read the row's before.
+// The lanes that share a row's index, as one number where a wave has one row.
+template <int TPR>
+__device__ __forceinline__ int group_of(int thread) {
+  return TPR >= 64 ? __builtin_amdgcn_readfirstlane(thread / TPR) : thread / TPR;
+}
+
+// Rows of more than one wave add their waves' sums through `red`, wave by wave.  Rows in
+// turn use its two halves: a wave that has passed a row's barrier has read the row before.
 //
 // Forward.  The lanes of a wave find their mean m by one sum, then delta = mean of v - m
 // and the squares of v - m by two more; waves are joined by Chan et al.'s formula for
 // counts, means and sums of squared deviations, relative to the first wave's mean.
 template <bool BF, int TPR, int NV, bool STEP>
-__global__ __launch_bounds__(block_of(TPR)) void k_ln_rows(Norm a) {
-  constexpr int BLK = block_of(TPR), G = BLK / TPR, L = TPR < 64 ? TPR : 64, W = TPR / L;
-  __shared__ float red[2][BLK / 64][3];
-  const int t = threadIdx.x % TPR, g = threadIdx.x / TPR;
+__global__ __launch_bounds__(block_fwd(TPR)) void k_ln_rows(Norm a) {
+  constexpr int BLK = block_fwd(TPR), G = BLK / TPR, L = TPR < 64 ? TPR : 64, W = TPR / L;
+  __shared__ float red[2][W > 1 ? W : 1][3];
+  const int t = threadIdx.x % TPR, g = group_of<TPR>(threadIdx.x);
   const int nv = (a.c + 7) / 8;
   const int64_t n = a.rows * a.c, stride = (int64_t)gridDim.x * G;
   const oc::DropKey key = STEP && a.drop.on ? oc::drop_key(a.drop) : oc::DropKey{};
@@ -145,7 +183,10 @@ __global__ __launch_bounds__(block_of(TPR)) void k_ln_rows(Norm a) {
     if (a.gamma && cnt[j] > 0) oc::load8n(a.gamma, false, col, cnt[j], a.c, gam[j]);
     if (a.beta && cnt[j] > 0) oc::load8n(a.beta, false, col, cnt[j], a.c, bet[j]);
   }
-  // channels of this wave's part of a row
+  const auto place = [&](int64_t row, int j) {
+    return Place{row * a.c, (j * TPR + t) * 8, cnt[j], n - row * a.c};
+  };
+  // channels of a wave's part of a row
   const auto channels = [&](int w) {
     int have = 0;
 #pragma unroll
@@ -162,9 +203,8 @@ __global__ __launch_bounds__(block_of(TPR)) void k_ln_rows(Norm a) {
 #pragma unroll
     for (int j = 0; j < NV; ++j)
       if (cnt[j] > 0) {
-        const int64_t at = row * a.c + (j * TPR + t) * 8;
-        raw_load(x[j], a.x, at, n);
-        if (has_res) raw_load(res[j], a.res, at, n);
+        raw_load(x[j], a.x, place(row, j));
+        if (has_res) raw_load(res[j], a.res, place(row, j));
       }
   };
   int64_t row = (int64_t)blockIdx.x * G + g;
@@ -174,18 +214,15 @@ __global__ __launch_bounds__(block_of(TPR)) void k_ln_rows(Norm a) {
     bool keep[8];
 #pragma unroll
     for (int j = 0; j < NV; ++j) {
-      if (cnt[j] > 0)
-        form_h<BF, STEP>(x[j], res[j], has_res, a.drop, key,
-                         (uint64_t)row * nv + (j * TPR + t), cnt[j], v[j], keep);
-      else
-#pragma unroll
-        for (int k = 0; k < 8; ++k) v[j][k] = 0.f;
+      form_h<BF, STEP>(x[j], res[j], has_res, a.drop, key, (uint64_t)row * nv + (j * TPR + t),
+                       v[j], keep);
+      cut(v[j], cnt[j]);
     }
     if (row + stride < a.rows) load(row + stride);
     if (STEP) {
 #pragma unroll
       for (int j = 0; j < NV; ++j)
-        if (cnt[j] > 0) oc::store8n(a.h, BF, row * a.c + (j * TPR + t) * 8, cnt[j], v[j]);
+        if (cnt[j] > 0) row_store<BF>(a.h, place(row, j), v[j]);
     }
     float m = 0.f;
 #pragma unroll
@@ -196,12 +233,16 @@ __global__ __launch_bounds__(block_of(TPR)) void k_ln_rows(Norm a) {
     float s1 = 0.f, s2 = 0.f;
 #pragma unroll
     for (int j = 0; j < NV; ++j)
+    {
+#pragma unroll
+      for (int k = 0; k < 8; ++k) v[j][k] -= m;
+      cut(v[j], cnt[j]);
 #pragma unroll
       for (int k = 0; k < 8; ++k) {
-        v[j][k] = k < cnt[j] ? v[j][k] - m : 0.f;
         s1 += v[j][k];
         s2 = fmaf(v[j][k], v[j][k], s2);
       }
+    }
     s1 = lanes_sum<L>(s1);
     s2 = lanes_sum<L>(s2);
     float delta = s1 * r_own, m2 = fmaf(-delta, s1, s2), mean = m + delta;
@@ -235,7 +276,7 @@ __global__ __launch_bounds__(block_of(TPR)) void k_ln_rows(Norm a) {
 #pragma unroll
       for (int k = 0; k < 8; ++k)
         v[j][k] = fmaf((v[j][k] - delta) * invstd, gam[j][k], bet[j][k]);
-      oc::store8n(a.y, BF, row * a.c + (j * TPR + t) * 8, cnt[j], v[j]);
+      row_store<BF>(a.y, place(row, j), v[j]);
     }
     if (t == 0) {
       if (a.mean) a.mean[row] = mean;
@@ -248,11 +289,11 @@ __global__ __launch_bounds__(block_of(TPR)) void k_ln_rows(Norm a) {
 // registers over the group's rows, at most MOST_ADDED; the workgroup's groups are then
 // added in double through LDS, and its sums written for the sum over the workgroups.
 template <bool BF, int TPR, int NV, bool STEP>
-__global__ __launch_bounds__(block_of(TPR)) void k_ln_rows_bwd(NormBwd a, float* part) {
-  constexpr int BLK = block_of(TPR), G = BLK / TPR, L = TPR < 64 ? TPR : 64, W = TPR / L;
-  __shared__ float red[2][BLK / 64][3];
+__global__ __launch_bounds__(block_bwd(TPR), 4) void k_ln_rows_bwd(NormBwd a, float* part) {
+  constexpr int BLK = block_bwd(TPR), G = BLK / TPR, L = TPR < 64 ? TPR : 64, W = TPR / L;
+  __shared__ float red[2][W > 1 ? BLK / 64 : 1][3];
   __shared__ float cols[G > 1 ? 2 : 1][G > 1 ? 8 : 1][G > 1 ? BLK : 1];
-  const int t = threadIdx.x % TPR, g = threadIdx.x / TPR;
+  const int t = threadIdx.x % TPR, g = group_of<TPR>(threadIdx.x);
   const int nv = (a.c + 7) / 8;
   const int64_t n = a.rows * a.c, nb = gridDim.x, b = blockIdx.x;
   const int64_t r0 = a.rows * b / nb, r1 = a.rows * (b + 1) / nb;
@@ -269,6 +310,9 @@ __global__ __launch_bounds__(block_of(TPR)) void k_ln_rows_bwd(NormBwd a, float*
     for (int k = 0; k < 8; ++k) gam[j][k] = 1.f, sg[j][k] = sb[j][k] = 0.f;
     if (a.gamma && cnt[j] > 0) oc::load8n(a.gamma, false, col, cnt[j], a.c, gam[j]);
   }
+  const auto place = [&](int64_t row, int j) {
+    return Place{row * a.c, (j * TPR + t) * 8, cnt[j], n - row * a.c};
+  };
   Raw<BF> x[NV], res[NV], dy[NV], dh[NV];
   float mean = 0.f, invstd = 0.f;
   const auto load = [&](int64_t row) {
@@ -277,71 +321,76 @@ __global__ __launch_bounds__(block_of(TPR)) void k_ln_rows_bwd(NormBwd a, float*
 #pragma unroll
     for (int j = 0; j < NV; ++j)
       if (cnt[j] > 0) {
-        const int64_t at = row * a.c + (j * TPR + t) * 8;
-        raw_load(x[j], a.x, at, n);
-        raw_load(dy[j], a.dy, at, n);
-        if (has_res) raw_load(res[j], a.res, at, n);
-        if (has_dh) raw_load(dh[j], a.dh, at, n);
+        raw_load(x[j], a.x, place(row, j));
+        raw_load(dy[j], a.dy, place(row, j));
+        if (has_res) raw_load(res[j], a.res, place(row, j));
       }
   };
-  int64_t row = r0 + g;
-  if (row < r1) load(row);
-  for (int par = 0; row < r1; row += G, par ^= 1) {
-    float d[NV][8], e[NV][8], u[NV][8];
+  // (groups that share a workgroup's barriers make the same number of steps)
+  if (r0 + g < r1) load(r0 + g);
+  for (int64_t first = r0, par = 0; first < r1; first += G, par ^= 1) {
+    const int64_t row = first + g;
+    const bool here = W == 1 || G == 1 || row < r1;
+    if (W == 1 && row >= r1) break;
+    float d[NV][8], e[NV][8];
     bool keep[NV][8];
     const float m = mean, r = invstd;
     float s[3] = {0.f, 0.f, 0.f};
 #pragma unroll
     for (int j = 0; j < NV; ++j) {
-      if (cnt[j] > 0) {
-        form_h<BF, STEP>(x[j], res[j], has_res, a.drop, key,
-                         (uint64_t)row * nv + (j * TPR + t), cnt[j], d[j], keep[j]);
-        unpack(dy[j], e[j]);
-        if (has_dh) unpack(dh[j], u[j]);
-      }
+      form_h<BF, STEP>(x[j], res[j], has_res, a.drop, key, (uint64_t)row * nv + (j * TPR + t),
+                       d[j], keep[j]);
+      unpack(dy[j], e[j]);
+#pragma unroll
+      for (int k = 0; k < 8; ++k) d[j][k] -= m;
+      cut(d[j], here ? cnt[j] : 0);
+      cut(e[j], here ? cnt[j] : 0);
 #pragma unroll
       for (int k = 0; k < 8; ++k) {
-        d[j][k] = k < cnt[j] ? d[j][k] - m : 0.f;
-        e[j][k] = k < cnt[j] ? e[j][k] : 0.f;
         const float q = e[j][k] * gam[j][k];
         s[0] += q;
         s[1] = fmaf(q, d[j][k], s[1]);
         s[2] += d[j][k];
       }
     }
+    // needed behind the sums only: loaded while they are formed
+#pragma unroll
+    for (int j = 0; j < NV; ++j)
+      if (has_dh && here && cnt[j] > 0) raw_load(dh[j], a.dh, place(row, j));
     if (row + G < r1) load(row + G);
 #pragma unroll
     for (int k = 0; k < 3; ++k) s[k] = lanes_sum<L>(s[k]);
     if (W > 1) {
       if ((t & 63) == 0) {
 #pragma unroll
-        for (int k = 0; k < 3; ++k) red[par][t / 64][k] = s[k];
+        for (int k = 0; k < 3; ++k) red[par][threadIdx.x / 64][k] = s[k];
       }
       __syncthreads();
 #pragma unroll
       for (int k = 0; k < 3; ++k) {
-        s[k] = red[par][0][k];
+        s[k] = red[par][g * W][k];
 #pragma unroll
-        for (int w = 1; w < W; ++w) s[k] += red[par][w][k];
+        for (int w = 1; w < W; ++w) s[k] += red[par][g * W + w][k];
       }
     }
     const float delta = s[2] * rc, gm = s[0] * rc, zm = fmaf(-delta, s[0], s[1]) * rc * r;
 #pragma unroll
     for (int j = 0; j < NV; ++j) {
+      float u[8] = {};
+      if (has_dh && here && cnt[j] > 0) unpack(dh[j], u);
 #pragma unroll
       for (int k = 0; k < 8; ++k) {
         const float z = (d[j][k] - delta) * r;
         sg[j][k] = fmaf(e[j][k], z, sg[j][k]);
         sb[j][k] += e[j][k];
         e[j][k] = r * fmaf(-z, zm, fmaf(e[j][k], gam[j][k], -gm));
-        if (has_dh) e[j][k] += u[j][k];
+        if (has_dh) e[j][k] += u[k];
       }
-      if (cnt[j] <= 0) continue;
-      const int64_t at = row * a.c + (j * TPR + t) * 8;
-      if (a.dres) oc::store8n(a.dres, BF, at, cnt[j], e[j]);
+      if (!here || cnt[j] <= 0) continue;
+      if (a.dres) row_store<BF>(a.dres, place(row, j), e[j]);
       if (STEP && a.dx) {
         if (a.drop.on) oc::drop8(a.drop, keep[j], e[j]);
-        oc::store8n(a.dx, BF, at, cnt[j], e[j]);
+        row_store<BF>(a.dx, place(row, j), e[j]);
       }
     }
   }
@@ -351,8 +400,8 @@ __global__ __launch_bounds__(block_of(TPR)) void k_ln_rows_bwd(NormBwd a, float*
     for (int j = 0; j < NV; ++j) {
       if (cnt[j] <= 0) continue;
       const int col = (j * TPR + t) * 8;
-      oc::store8n(part, false, b * 2 * a.c + col, cnt[j], sg[j]);
-      oc::store8n(part, false, (b * 2 + 1) * a.c + col, cnt[j], sb[j]);
+      oc::store8n(part + b * 2 * a.c, false, col, cnt[j], sg[j]);
+      oc::store8n(part + (b * 2 + 1) * a.c, false, col, cnt[j], sb[j]);
     }
     return;
   }
@@ -433,7 +482,7 @@ namespace oc {
 
 void norm_rows_fwd(const Norm& a, hipStream_t s) {
   with_fwd(a.c, [&](auto t, auto v) {
-    constexpr int TPR = decltype(t)::value, NV = decltype(v)::value, BLK = block_of(TPR);
+    constexpr int TPR = decltype(t)::value, NV = decltype(v)::value, BLK = block_fwd(TPR);
     const int64_t blocks = std::min<int64_t>(cdiv(a.rows, BLK / TPR), 2048 * 256 / BLK);
     const auto go = [&](auto kernel) {
       launch_main(kernel, dim3((unsigned)blocks), dim3(BLK), s, a);
@@ -446,9 +495,8 @@ void norm_rows_fwd(const Norm& a, hipStream_t s) {
 }
 
 int64_t norm_rows_blocks(int64_t rows, int32_t c) {
-  const int tpr = threads_bwd(c), g = block_of(tpr) / tpr;
-  const int64_t most = 2048 * 256 / block_of(tpr);
-  return std::max(std::min<int64_t>(cdiv(rows, 4 * g), most), cdiv(rows, MOST_ADDED * g));
+  const int tpr = threads_bwd(c), g = block_bwd(tpr) / tpr;
+  return std::max(std::min<int64_t>(cdiv(rows, 2 * g), 512), cdiv(rows, MOST_ADDED * g));
 }
 
 void norm_rows_bwd(const NormBwd& a, float* part, hipStream_t s) {
@@ -456,7 +504,7 @@ void norm_rows_bwd(const NormBwd& a, float* part, hipStream_t s) {
   with_bwd(a.c, [&](auto t, auto v) {
     constexpr int TPR = decltype(t)::value, NV = decltype(v)::value;
     const auto go = [&](auto kernel) {
-      launch_main(kernel, dim3((unsigned)blocks), dim3(block_of(TPR)), s, a, part);
+      launch_main(kernel, dim3((unsigned)blocks), dim3(block_bwd(TPR)), s, a, part);
     };
     if (a.drop.on || a.res || a.dx || a.dh)
       a.bf16 ? go(k_ln_rows_bwd<true, TPR, NV, true>) : go(k_ln_rows_bwd<false, TPR, NV, true>);

@@ -10,6 +10,10 @@ namespace oc {
 
 // --- the dropout mask ---------------------------------------------------------
 
+// a ^ b ^ c, one instruction.
+__device__ __forceinline__ uint32_t xor3(uint32_t a, uint32_t b, uint32_t c) {
+  return __builtin_amdgcn_bitop3_b32(a, b, c, 0x96);
+}
 // Philox4x32-10 (Salmon, Moraes, Dror and Shaw, "Parallel random numbers: as easy as 1,
 // 2, 3", SC 2011): ten rounds of two 32 x 32 -> 64 bit products on a counter of four
 // words under a key of two.
@@ -17,8 +21,8 @@ __device__ __forceinline__ void philox(uint32_t (&c)[4], uint32_t k0, uint32_t k
 #pragma unroll
   for (int r = 0; r < 10; ++r) {
     const uint64_t a = (uint64_t)c[0] * 0xD2511F53u, b = (uint64_t)c[2] * 0xCD9E8D57u;
-    c[0] = (uint32_t)(b >> 32) ^ c[1] ^ k0;
-    c[2] = (uint32_t)(a >> 32) ^ c[3] ^ k1;
+    c[0] = xor3((uint32_t)(b >> 32), c[1], k0);
+    c[2] = xor3((uint32_t)(a >> 32), c[3], k1);
     c[1] = (uint32_t)b;
     c[3] = (uint32_t)a;
     k0 += 0x9E3779B9u;
