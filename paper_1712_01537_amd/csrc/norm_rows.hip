@@ -289,7 +289,7 @@ __global__ __launch_bounds__(block_fwd(TPR)) void k_ln_rows(Norm a) {
 // registers over the group's rows, at most MOST_ADDED; the workgroup's groups are then
 // added in double through LDS, and its sums written for the sum over the workgroups.
 template <bool BF, int TPR, int NV, bool STEP>
-__global__ __launch_bounds__(block_bwd(TPR), 4) void k_ln_rows_bwd(NormBwd a, float* part) {
+__global__ __launch_bounds__(block_bwd(TPR), NV == 1 ? 4 : 2) void k_ln_rows_bwd(NormBwd a, float* part) {
   constexpr int BLK = block_bwd(TPR), G = BLK / TPR, L = TPR < 64 ? TPR : 64, W = TPR / L;
   __shared__ float red[2][W > 1 ? BLK / 64 : 1][3];
   __shared__ float cols[G > 1 ? 2 : 1][G > 1 ? 8 : 1][G > 1 ? BLK : 1];
@@ -301,63 +301,91 @@ __global__ __launch_bounds__(block_bwd(TPR), 4) void k_ln_rows_bwd(NormBwd a, fl
   const bool has_res = STEP && a.res, has_dh = STEP && a.dh;
   const float rc = 1.f / (float)a.c;
   int cnt[NV];
-  float gam[NV][8], sg[NV][8], sb[NV][8];
+  // Two vectors a thread leave no registers for the next row's loads and gamma.
+  constexpr bool AHEAD = NV <= 2;
+  float gam[NV <= 2 ? NV : 1][8], sg[NV][8], sb[NV][8];
 #pragma unroll
   for (int j = 0; j < NV; ++j) {
-    const int col = (j * TPR + t) * 8;
-    cnt[j] = a.c - col;
+    cnt[j] = a.c - (j * TPR + t) * 8;
 #pragma unroll
-    for (int k = 0; k < 8; ++k) gam[j][k] = 1.f, sg[j][k] = sb[j][k] = 0.f;
-    if (a.gamma && cnt[j] > 0) oc::load8n(a.gamma, false, col, cnt[j], a.c, gam[j]);
+    for (int k = 0; k < 8; ++k) sg[j][k] = sb[j][k] = 0.f;
   }
+  const auto load_gamma = [&](int j, float(&v)[8]) {
+#pragma unroll
+    for (int k = 0; k < 8; ++k) v[k] = 1.f;
+    if (a.gamma && cnt[j] > 0)
+      oc::load8n(a.gamma, false, (j * TPR + t) * 8, hidden(cnt[j]), a.c, v);
+  };
+  if (AHEAD)
+#pragma unroll
+    for (int j = 0; j < NV; ++j) load_gamma(j, gam[j]);
   const auto place = [&](int64_t row, int j) {
     return Place{row * a.c, (j * TPR + t) * 8, cnt[j], n - row * a.c};
   };
-  Raw<BF> x[NV], res[NV], dy[NV], dh[NV];
+  // (of four fp32 vectors one is loaded at a time)
+  constexpr int RAWS = AHEAD || BF ? NV : 1;
+  Raw<BF> x[RAWS], res[RAWS], dy[RAWS], dh[AHEAD ? NV : 1];
   float mean = 0.f, invstd = 0.f;
+  const auto load_at = [&](int64_t row, int j, Raw<BF>& rx, Raw<BF>& rdy, Raw<BF>& rres) {
+    if (cnt[j] <= 0) return;
+    raw_load(rx, a.x, place(row, j));
+    raw_load(rdy, a.dy, place(row, j));
+    if (has_res) raw_load(rres, a.res, place(row, j));
+  };
   const auto load = [&](int64_t row) {
     mean = a.mean[row];
     invstd = a.invstd[row];
+    if (RAWS == NV)
 #pragma unroll
-    for (int j = 0; j < NV; ++j)
-      if (cnt[j] > 0) {
-        raw_load(x[j], a.x, place(row, j));
-        raw_load(dy[j], a.dy, place(row, j));
-        if (has_res) raw_load(res[j], a.res, place(row, j));
-      }
+      for (int j = 0; j < NV; ++j) load_at(row, j, x[j % RAWS], dy[j % RAWS], res[j % RAWS]);
   };
   // (groups that share a workgroup's barriers make the same number of steps)
-  if (r0 + g < r1) load(r0 + g);
+  if (AHEAD && r0 + g < r1) load(r0 + g);
   for (int64_t first = r0, par = 0; first < r1; first += G, par ^= 1) {
     const int64_t row = first + g;
     const bool here = W == 1 || G == 1 || row < r1;
     if (W == 1 && row >= r1) break;
+    if (!AHEAD && here) load(row);
     float d[NV][8], e[NV][8];
-    bool keep[NV][8];
+    bool keep[AHEAD ? NV : 1][8];
+    uint32_t kept = 0;  // (bits for bools, of which each takes two scalar registers)
     const float m = mean, r = invstd;
     float s[3] = {0.f, 0.f, 0.f};
 #pragma unroll
     for (int j = 0; j < NV; ++j) {
-      form_h<BF, STEP>(x[j], res[j], has_res, a.drop, key, (uint64_t)row * nv + (j * TPR + t),
-                       d[j], keep[j]);
-      unpack(dy[j], e[j]);
+      const int i = AHEAD ? j : 0;
+      const int l = j % RAWS;
+      if (RAWS < NV && here) load_at(row, j, x[l], dy[l], res[l]);
+      form_h<BF, STEP>(x[l], res[l], has_res, a.drop, key, (uint64_t)row * nv + (j * TPR + t),
+                       d[j], keep[i]);
+      unpack(dy[l], e[j]);
 #pragma unroll
       for (int k = 0; k < 8; ++k) d[j][k] -= m;
       cut(d[j], here ? cnt[j] : 0);
       cut(e[j], here ? cnt[j] : 0);
+      if (!AHEAD) {
+        load_gamma(j, gam[i]);
+        if (STEP && a.drop.on)
+#pragma unroll
+          for (int k = 0; k < 8; ++k) kept |= (keep[i][k] ? 1u : 0u) << (j * 8 + k);
+      }
 #pragma unroll
       for (int k = 0; k < 8; ++k) {
-        const float q = e[j][k] * gam[j][k];
+        const float q = e[j][k] * gam[i][k];
         s[0] += q;
         s[1] = fmaf(q, d[j][k], s[1]);
         s[2] += d[j][k];
       }
+      // (the next vector's loads stay behind this one's use: their registers are the same)
+      if (RAWS < NV) asm volatile("" ::: "memory");
     }
     // needed behind the sums only: loaded while they are formed
+    if (AHEAD) {
 #pragma unroll
-    for (int j = 0; j < NV; ++j)
-      if (has_dh && here && cnt[j] > 0) raw_load(dh[j], a.dh, place(row, j));
-    if (row + G < r1) load(row + G);
+      for (int j = 0; j < NV; ++j)
+        if (has_dh && here && cnt[j] > 0) raw_load(dh[AHEAD ? j : 0], a.dh, place(row, j));
+      if (row + G < r1) load(row + G);
+    }
 #pragma unroll
     for (int k = 0; k < 3; ++k) s[k] = lanes_sum<L>(s[k]);
     if (W > 1) {
@@ -376,22 +404,33 @@ __global__ __launch_bounds__(block_bwd(TPR), 4) void k_ln_rows_bwd(NormBwd a, fl
     const float delta = s[2] * rc, gm = s[0] * rc, zm = fmaf(-delta, s[0], s[1]) * rc * r;
 #pragma unroll
     for (int j = 0; j < NV; ++j) {
+      const int i = AHEAD ? j : 0;
       float u[8] = {};
-      if (has_dh && here && cnt[j] > 0) unpack(dh[j], u);
+      if (!AHEAD) {
+        if (has_dh && here && cnt[j] > 0) raw_load(dh[i], a.dh, place(row, j));
+        load_gamma(j, gam[i]);
+      }
+      if (has_dh && here && cnt[j] > 0) unpack(dh[i], u);
 #pragma unroll
       for (int k = 0; k < 8; ++k) {
         const float z = (d[j][k] - delta) * r;
         sg[j][k] = fmaf(e[j][k], z, sg[j][k]);
         sb[j][k] += e[j][k];
-        e[j][k] = r * fmaf(-z, zm, fmaf(e[j][k], gam[j][k], -gm));
+        e[j][k] = r * fmaf(-z, zm, fmaf(e[j][k], gam[i][k], -gm));
         if (has_dh) e[j][k] += u[k];
       }
       if (!here || cnt[j] <= 0) continue;
       if (a.dres) row_store<BF>(a.dres, place(row, j), e[j]);
       if (STEP && a.dx) {
-        if (a.drop.on) oc::drop8(a.drop, keep[j], e[j]);
+        if (a.drop.on) {
+          if (!AHEAD)
+#pragma unroll
+            for (int k = 0; k < 8; ++k) keep[i][k] = kept >> (j * 8 + k) & 1;
+          oc::drop8(a.drop, keep[i], e[j]);
+        }
         row_store<BF>(a.dx, place(row, j), e[j]);
       }
+      if (RAWS < NV) asm volatile("" ::: "memory");
     }
   }
   if (!part) return;
@@ -434,7 +473,7 @@ int threads_of(int c, int v) {
   while (v * t < nv) t *= 2;
   return t;
 }
-int threads_bwd(int c) { return threads_of(c, c <= 8192 ? 1 : 2); }
+int threads_bwd(int c) { return threads_of(c, c <= 4096 ? 1 : c <= 8192 ? 2 : 4); }
 
 // f(threads of a row, vectors of a thread), both as constants.
 template <int V>
@@ -467,12 +506,12 @@ template <typename F>
 void with_bwd(int c, F&& f) {
   const int t = threads_bwd(c);
   if (c <= 512) return with_small(t, f);
-  if (c > 8192) return f(Int<1024>{}, Int<2>{});
+  if (c > 8192) return f(Int<512>{}, Int<4>{});
+  if (c > 4096) return f(Int<512>{}, Int<2>{});
   switch (t) {
     case 128: return f(Int<128>{}, Int<1>{});
     case 256: return f(Int<256>{}, Int<1>{});
-    case 512: return f(Int<512>{}, Int<1>{});
-    default: return f(Int<1024>{}, Int<1>{});
+    default: return f(Int<512>{}, Int<1>{});
   }
 }
 
