@@ -8,10 +8,12 @@
 // goes on over a border leaves a partial sum a chunk, added by k_embed_join.  However
 // many rows share an id, no thread's chain of additions is longer than a chunk.
 //
-// The sort takes the ids' bits in digits, lowest first, with one counter a digit value
-// and tile of rows: count, scan over the tiles, and scatter.  A tile is one wave's: it
-// takes 64 rows at a time, in order, so that the place of a row among those of its digit
-// is a count of the lanes before it with the same digit.
+// The sort takes the ids' bits in digits of up to eight, lowest first.  A tile of rows is
+// one workgroup's: count writes each tile's number of rows of every digit value, and
+// scatter adds those numbers up itself (all values below its own, and its own in the tiles
+// before), so that a digit takes two launches.  A wave takes its rows 64 at a time, in
+// order: the place of a row among those of its digit is a count of the lanes before it
+// with the same digit.  Up to SMALL rows are sorted by one workgroup in LDS.
 #include <algorithm>
 
 #include "rows.h"
@@ -58,11 +60,13 @@ struct Digit {
   uint32_t mask;
   const Pair* in;
   Pair* out;
-  uint32_t *hist, *total, *count;  // [tiles][1 << bits], [1 << bits]
+  uint32_t *hist, *count;  // hist[tiles][1 << bits]
   int64_t rows, num;
   int tiles, shift, bits;
 };
-constexpr int MOST_BITS = 12;
+constexpr int MOST_BITS = 8, MOST_D = 1 << MOST_BITS;
+constexpr int SB = 1024, SW = SB / 64;  // threads and waves of a sorting workgroup
+constexpr int SMALL = 4096;
 
 __device__ __forceinline__ bool pair_at(const Digit& a, int64_t i, int64_t n, Pair& p) {
   if (i >= n) return false;
@@ -73,88 +77,189 @@ __device__ __forceinline__ bool pair_at(const Digit& a, int64_t i, int64_t n, Pa
   p = Pair{id_of(a.ids, i, a.mask), (uint32_t)i};
   return p.id < a.num;
 }
-// The rows of tile t: multiples of 64 but for the last.
-__device__ __forceinline__ void tile_range(int64_t n, int tiles, int t, int64_t& i0, int64_t& i1) {
-  const int64_t steps = (n + 63) / 64;
-  i0 = steps * t / tiles * 64;
-  i1 = steps * (t + 1) / tiles * 64;
-  if (i1 > n) i1 = n;
+// Part t of the rows in `parts`: multiples of 64 but for the last.
+__device__ __forceinline__ void part_of(int64_t from, int64_t to, int parts, int t, int64_t& i0,
+                                        int64_t& i1) {
+  const int64_t steps = (to - from + 63) / 64;
+  i0 = from + steps * t / parts * 64;
+  i1 = from + steps * (t + 1) / parts * 64;
+  if (i1 > to) i1 = to;
+}
+// The lanes with this lane's digit, of those that have one.
+__device__ __forceinline__ uint64_t same_digit(uint32_t d, int bits, bool in) {
+  uint64_t same = __ballot(in);
+  for (int b = 0; b < bits; ++b) {
+    const bool one = d >> b & 1;
+    const uint64_t ones = __ballot(one);
+    same &= one ? ones : ~ones;
+  }
+  return same;
+}
+__device__ __forceinline__ int lanes_before(uint64_t m) {
+  return __popcll(m & (((uint64_t)1 << (threadIdx.x & 63)) - 1));
+}
+// What this wave wrote to LDS is there for its next reads.
+__device__ __forceinline__ void wave_sync() {
+  __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
+  __builtin_amdgcn_wave_barrier();
+  __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
+}
+// v[d] of D <= 256 values becomes the sum of those before it, by one wave (four a lane).
+// Returns the sum of all, in each lane.
+__device__ __forceinline__ uint32_t scan_digits(uint32_t* v, int D) {
+  const int lane = threadIdx.x & 63;
+  uint32_t x[4], sum = 0;
+#pragma unroll
+  for (int k = 0; k < 4; ++k) {
+    const uint32_t y = lane * 4 + k < D ? v[lane * 4 + k] : 0;
+    x[k] = sum;
+    sum += y;
+  }
+  uint32_t upto = sum;
+  for (int k = 1; k < 64; k <<= 1) {
+    const uint32_t u = __shfl_up(upto, k);
+    if (lane >= k) upto += u;
+  }
+#pragma unroll
+  for (int k = 0; k < 4; ++k)
+    if (lane * 4 + k < D) v[lane * 4 + k] = upto - sum + x[k];
+  return __shfl(upto, 63);
 }
 
-__global__ __launch_bounds__(64) void k_embed_count(Digit a) {
-  __shared__ uint32_t cnt[1 << MOST_BITS];
+__global__ __launch_bounds__(SB) void k_embed_count(Digit a) {
+  __shared__ uint32_t cnt[MOST_D];
   const int D = 1 << a.bits, t = blockIdx.x;
-  for (int d = threadIdx.x; d < D; d += 64) cnt[d] = 0;
+  if ((int)threadIdx.x < D) cnt[threadIdx.x] = 0;
   __syncthreads();
   const int64_t n = a.in ? (int64_t)*a.count : a.rows;
   int64_t i0, i1;
-  tile_range(n, a.tiles, t, i0, i1);
+  part_of(0, n, a.tiles, t, i0, i1);
 #pragma unroll 4
-  for (int64_t i = i0 + threadIdx.x; i < i1; i += 64) {
+  for (int64_t i = i0 + threadIdx.x; i < i1; i += SB) {
     Pair p;
     if (pair_at(a, i, n, p)) atomicAdd(&cnt[p.id >> a.shift & (D - 1)], 1u);
   }
   __syncthreads();
-  for (int d = threadIdx.x; d < D; d += 64) a.hist[(int64_t)t * D + d] = cnt[d];
+  if ((int)threadIdx.x < D) a.hist[(int64_t)t * D + threadIdx.x] = cnt[threadIdx.x];
 }
 
-// hist[t][d] becomes the number of pairs of digit d in the tiles before t; total[d] theirs
-// in all.
-__global__ __launch_bounds__(TB) void k_embed_scan(Digit a) {
-  const int D = 1 << a.bits, d = blockIdx.x * TB + threadIdx.x;
-  if (d >= D) return;
-  uint32_t sum = 0;
-  for (int t0 = 0; t0 < a.tiles; t0 += 16) {
-    uint32_t v[16];
-#pragma unroll
-    for (int j = 0; j < 16; ++j) v[j] = t0 + j < a.tiles ? a.hist[(int64_t)(t0 + j) * D + d] : 0;
-#pragma unroll
-    for (int j = 0; j < 16; ++j) {
-      if (t0 + j < a.tiles) a.hist[(int64_t)(t0 + j) * D + d] = sum;
-      sum += v[j];
-    }
-  }
-  a.total[d] = sum;
-}
-
-__global__ __launch_bounds__(64) void k_embed_scatter(Digit a) {
-  __shared__ uint32_t at[1 << MOST_BITS];
-  const int D = 1 << a.bits, t = blockIdx.x, lane = threadIdx.x;
+__global__ __launch_bounds__(SB) void k_embed_scatter(Digit a) {
+  __shared__ uint32_t total[MOST_D], before[MOST_D], at[SW][MOST_D];
+  const int D = 1 << a.bits, t = blockIdx.x, w = threadIdx.x / 64;
   const int64_t n = a.in ? (int64_t)*a.count : a.rows;
-  uint32_t before = 0;
-  for (int d0 = 0; d0 < D; d0 += 64) {
-    const int d = d0 + lane;
-    const uint32_t v = d < D ? a.total[d] : 0;
-    uint32_t s = v;
-    for (int k = 1; k < 64; k <<= 1) {
-      const uint32_t u = __shfl_up(s, k);
-      if (lane >= k) s += u;
-    }
-    if (d < D) at[d] = before + s - v + a.hist[(int64_t)t * D + d];
-    before += __shfl(s, 63);
-  }
-  if (!a.in && t == 0 && lane == 0) *a.count = before;
+  for (int i = threadIdx.x; i < SW * MOST_D; i += SB) (&at[0][0])[i] = 0;
+  if (threadIdx.x < MOST_D) total[threadIdx.x] = before[threadIdx.x] = 0;
   __syncthreads();
-  int64_t i0, i1;
-  tile_range(n, a.tiles, t, i0, i1);
-  for (int64_t i = i0; i < i1; i += 64) {
-    Pair p{0, 0};
-    const bool in = pair_at(a, i + lane, i1, p);
-    const uint32_t d = p.id >> a.shift & (D - 1);
-    uint64_t same = __ballot(in);
-    for (int b = 0; b < a.bits; ++b) {
-      const bool one = d >> b & 1;
-      const uint64_t ones = __ballot(one);
-      same &= one ? ones : ~ones;
+  int64_t i0, i1, j0, j1;
+  part_of(0, n, a.tiles, t, i0, i1);
+  part_of(i0, i1, SW, w, j0, j1);
+  // the wave's rows of each digit value
+  for (int64_t i = j0 + (threadIdx.x & 63); i < j1; i += 64) {
+    Pair p;
+    if (pair_at(a, i, n, p)) atomicAdd(&at[w][p.id >> a.shift & (D - 1)], 1u);
+  }
+  {  // every tile's, by threads of digit value d and every SB / D-th tile
+    const int d = threadIdx.x & (D - 1);
+    uint32_t all = 0, early = 0;
+#pragma unroll 8
+    for (int u = threadIdx.x >> a.bits; u < a.tiles; u += SB >> a.bits) {
+      const uint32_t v = a.hist[(int64_t)u * D + d];
+      all += v;
+      early += u < t ? v : 0;
     }
-    const int rank = __popcll(same & (((uint64_t)1 << lane) - 1));
+    atomicAdd(&total[d], all);
+    atomicAdd(&before[d], early);
+  }
+  __syncthreads();
+  if (w == 0) {
+    const uint32_t sum = scan_digits(total, D);
+    if (!a.in && t == 0 && threadIdx.x == 0) *a.count = sum;
+  }
+  __syncthreads();
+  if ((int)threadIdx.x < D) {
+    uint32_t sum = total[threadIdx.x] + before[threadIdx.x];
+    for (int u = 0; u < SW; ++u) {
+      const uint32_t v = at[u][threadIdx.x];
+      at[u][threadIdx.x] = sum;
+      sum += v;
+    }
+  }
+  __syncthreads();
+  for (int64_t i = j0; i < j1; i += 64) {
+    Pair p{0, 0};
+    const bool in = pair_at(a, i + (threadIdx.x & 63), j1, p);
+    const uint32_t d = p.id >> a.shift & (D - 1);
+    const uint64_t same = same_digit(d, a.bits, in);
+    const int rank = lanes_before(same);
     uint32_t pos = 0;
-    if (in) pos = at[d] + rank;
-    __syncthreads();
-    if (in && rank == 0) at[d] = pos + __popcll(same);
-    __syncthreads();
+    if (in) pos = at[w][d] + rank;
+    wave_sync();
+    if (in && rank == 0) at[w][d] = pos + __popcll(same);
+    wave_sync();
     if (in) a.out[pos] = p;
   }
+}
+
+// Up to SMALL rows, every digit: a thread's pairs are rows 256 w + 64 j + lane of the list.
+__global__ __launch_bounds__(SB) void k_embed_sort_small(Digit a, int passes) {
+  __shared__ Pair list[SMALL];
+  __shared__ uint32_t at[SW][MOST_D], total[MOST_D], valid;
+  constexpr int J = SMALL / SB;
+  const int D = 1 << a.bits, w = threadIdx.x / 64, lane = threadIdx.x & 63;
+  const int rows = (int)a.rows, i0 = w * 64 * J + lane;
+  if (threadIdx.x == 0) valid = 0;
+  __syncthreads();
+  Pair p[J];
+#pragma unroll
+  for (int j = 0; j < J; ++j) {
+    const int i = i0 + j * 64;
+    // ids outside the table go behind the others, where *count leaves them out
+    p[j] = Pair{i < rows ? id_of(a.ids, i, a.mask) : ~0u, (uint32_t)i};
+    const bool in = i < rows && p[j].id < a.num;
+    if (!in) p[j].id = (uint32_t)a.num;
+    const uint64_t m = __ballot(in);
+    if (lane == 0 && m) atomicAdd(&valid, (uint32_t)__popcll(m));
+  }
+  for (int s = 0; s < passes; ++s) {
+    for (int i = threadIdx.x; i < SW * MOST_D; i += SB) (&at[0][0])[i] = 0;
+    __syncthreads();
+    uint32_t rank[J];
+#pragma unroll
+    for (int j = 0; j < J; ++j) {
+      const uint32_t d = p[j].id >> s * a.bits & (D - 1);
+      const uint64_t same = same_digit(d, a.bits, true);
+      const int r = lanes_before(same);
+      rank[j] = at[w][d] + r;
+      wave_sync();
+      if (r == 0) at[w][d] = rank[j] + __popcll(same);
+      wave_sync();
+    }
+    __syncthreads();
+    if ((int)threadIdx.x < D) {
+      uint32_t sum = 0;
+      for (int u = 0; u < SW; ++u) {
+        const uint32_t v = at[u][threadIdx.x];
+        at[u][threadIdx.x] = sum;
+        sum += v;
+      }
+      total[threadIdx.x] = sum;
+    }
+    __syncthreads();
+    if (w == 0) scan_digits(total, D);
+    __syncthreads();
+#pragma unroll
+    for (int j = 0; j < J; ++j) {
+      const uint32_t d = p[j].id >> s * a.bits & (D - 1);
+      list[total[d] + at[w][d] + rank[j]] = p[j];
+    }
+    __syncthreads();
+#pragma unroll
+    for (int j = 0; j < J; ++j) p[j] = list[i0 + j * 64];
+  }
+#pragma unroll
+  for (int j = 0; j < J; ++j)
+    if (i0 + j * 64 < rows) a.out[i0 + j * 64] = p[j];
+  if (threadIdx.x == 0) *a.count = valid;
 }
 
 // --- the sums -------------------------------------------------------------------------
@@ -169,28 +274,38 @@ struct Sums {
   int c, len;  // len: pairs of a chunk
   bool bf16, out_bf16;
   float scale;
-  int64_t chunk_blocks;
+  int64_t zero_blocks;
 };
 
-// A thread's sums of eight columns: at most MOST_ADDED values in fp32, the rest in double.
+// A thread's sums of eight columns: at most MOST_ADDED values in fp32, the rest in double
+// (LONG: there may be more).
 constexpr int MOST_ADDED = 64;
+template <bool LONG>
 struct Acc {
   float f[8];
-  double d[8];
+  double d[LONG ? 8 : 1];
   int n;
   __device__ __forceinline__ void clear() {
 #pragma unroll
-    for (int k = 0; k < 8; ++k) f[k] = 0.f, d[k] = 0.0;
+    for (int k = 0; k < 8; ++k) {
+      f[k] = 0.f;
+      if (LONG) d[LONG ? k : 0] = 0.0;
+    }
     n = 0;
   }
   __device__ __forceinline__ void add(const float (&v)[8]) {
 #pragma unroll
     for (int k = 0; k < 8; ++k) f[k] += v[k];
-    if (++n == MOST_ADDED) {
+    if (LONG && ++n == MOST_ADDED) {
 #pragma unroll
-      for (int k = 0; k < 8; ++k) d[k] += (double)f[k], f[k] = 0.f;
+      for (int k = 0; k < 8; ++k) d[LONG ? k : 0] += (double)f[k], f[k] = 0.f;
       n = 0;
     }
+  }
+  __device__ __forceinline__ void times(float scale, float (&v)[8]) const {
+#pragma unroll
+    for (int k = 0; k < 8; ++k)
+      v[k] = LONG ? (float)(((double)f[k] + d[LONG ? k : 0]) * scale) : f[k] * scale;
   }
 };
 
@@ -215,56 +330,62 @@ __device__ __forceinline__ void zero_rows(const Sums& a, int64_t n, int64_t wave
 }
 
 // Groups of tpr lanes, each with 8 tpr columns of a chunk (slabs of them where rows are
-// longer).  The blocks behind the chunks' zero the table's other rows.
+// longer).  The first workgroups zero the table's other rows.
+template <bool BF, bool LONG>
 __global__ __launch_bounds__(TB) void k_embed_sums(Sums a, int tpr, int slabs) {
   const int64_t n = *a.count;
-  if (blockIdx.x >= a.chunk_blocks) {
-    zero_rows(a, n, (int64_t)(blockIdx.x - a.chunk_blocks) * (TB / 64) + threadIdx.x / 64);
+  if (blockIdx.x < a.zero_blocks) {
+    zero_rows(a, n, (int64_t)blockIdx.x * (TB / 64) + threadIdx.x / 64);
     return;
   }
-  const int64_t unit = (int64_t)blockIdx.x * (TB / tpr) + threadIdx.x / tpr;
+  const int64_t unit = (blockIdx.x - a.zero_blocks) * (TB / tpr) + threadIdx.x / tpr;
   const int64_t chunk = unit / slabs;
   const int col = ((int)(unit - chunk * slabs) * tpr + threadIdx.x % tpr) * 8;
   const int64_t i0 = chunk * a.len, i1 = i0 + a.len < n ? i0 + a.len : n;
   if (i0 >= i1 || col >= a.c) return;
   const int cnt = a.c - col;
-  const int64_t all = a.rows * a.c;
-  uint32_t id = a.sorted[i0].id;
+  constexpr int U = BF ? 16 : 8;  // rows in flight
+  Pair p[U];
+  const auto pairs = [&](int64_t i) {
+#pragma unroll
+    for (int j = 0; j < U; ++j) p[j] = a.sorted[i + j < i1 ? i + j : i1 - 1];
+  };
+  pairs(i0);
+  uint32_t id = p[0].id;
   bool first = i0 > 0 && a.sorted[i0 - 1].id == id;  // the run began in a chunk before
   const bool goes_on = i1 < n && a.sorted[i1].id == a.sorted[i1 - 1].id;
-  Acc acc;
+  Acc<LONG> acc;
   acc.clear();
   const auto flush = [&](bool open) {
     float v[8];
-    if (first || open) {
-#pragma unroll
-      for (int k = 0; k < 8; ++k) v[k] = (float)((double)acc.f[k] + acc.d[k]);
+    acc.times(first || open ? 1.f : a.scale, v);
+    if (first || open)
       oc::store8n(a.part, false, (chunk * 2 + (first ? 0 : 1)) * a.c + col, cnt, v);
-    } else {
-#pragma unroll
-      for (int k = 0; k < 8; ++k) v[k] = (float)(((double)acc.f[k] + acc.d[k]) * a.scale);
+    else
       oc::store8n(a.out, a.out_bf16, (int64_t)id * a.c + col, cnt, v);
-    }
   };
-  constexpr int U = 8;  // rows in flight
   for (int64_t i = i0; i < i1; i += U) {
-    Pair p[U];
-    float v[U][8];
+    oc::Raw<BF> raw[U];
+    uint32_t ids[U];
 #pragma unroll
-    for (int j = 0; j < U; ++j) p[j] = a.sorted[i + j < i1 ? i + j : i1 - 1];
-#pragma unroll
-    for (int j = 0; j < U; ++j)
-      oc::load8n(a.dy, a.bf16, (int64_t)p[j].row * a.c + col, cnt, all, v[j]);
+    for (int j = 0; j < U; ++j) {
+      const int64_t at = (int64_t)p[j].row * a.c;
+      oc::raw_load(raw[j], a.dy, oc::Place{at, col, cnt, a.rows * a.c - at});
+      ids[j] = p[j].id;
+    }
+    if (i + U < i1) pairs(i + U);
 #pragma unroll
     for (int j = 0; j < U; ++j) {
       if (i + j >= i1) break;
-      if (p[j].id != id) {
+      if (ids[j] != id) {
         flush(false);
         acc.clear();
-        id = p[j].id;
+        id = ids[j];
         first = false;
       }
-      acc.add(v[j]);
+      float v[8];
+      oc::unpack(raw[j], v);
+      acc.add(v);
     }
   }
   flush(goes_on);
@@ -272,25 +393,28 @@ __global__ __launch_bounds__(TB) void k_embed_sums(Sums a, int tpr, int slabs) {
 
 // The runs that go on over a chunk's end: the workgroup of the chunk where one begins adds
 // its partial sums, rl lanes a column, in double and in a fixed order.
-__global__ __launch_bounds__(TB) void k_embed_join(Sums a, int tpr) {
-  __shared__ double red[TB][9];
+constexpr int JB = 512;
+__global__ __launch_bounds__(JB) void k_embed_join(Sums a, int tpr) {
+  __shared__ double red[JB][9];
   const int64_t n = *a.count, chunk = blockIdx.x;
   const int64_t i0 = chunk * a.len, i1 = i0 + a.len;
   if (i1 >= n) return;
-  const uint32_t id = a.sorted[i1 - 1].id;
-  if (a.sorted[i1].id != id) return;
-  if (a.sorted[i0].id == id && i0 > 0 && a.sorted[i0 - 1].id == id) return;
+  const uint32_t id = a.sorted[i1 - 1].id, next = a.sorted[i1].id, from = a.sorted[i0].id;
+  const uint32_t last = i0 > 0 ? a.sorted[i0 - 1].id : ~0u;  // (no id: they are below num)
+  if (next != id || (from == id && last == id)) return;
   int64_t more = 0;  // chunks that the run goes on in
   for (;;) {
     const int64_t at = (chunk + 1 + more + threadIdx.x) * a.len;
     const int k = __syncthreads_count(at < n && a.sorted[at].id == id);
     more += k;
-    if (k < TB) break;
+    if (k < JB) break;
   }
-  const int tc = threadIdx.x % tpr, tr = threadIdx.x / tpr, rl = TB / tpr;
-  for (int col = (blockIdx.y * tpr + tc) * 8; col - tc * 8 < a.c; col += gridDim.y * tpr * 8) {
+  const int tc = threadIdx.x % tpr, tr = threadIdx.x / tpr, rl = JB / tpr;
+  for (int c0 = 0; c0 < a.c; c0 += tpr * 8) {
+    const int col = c0 + tc * 8;
     double s[8] = {};
-    if (col < a.c)
+    if (col < a.c) {
+#pragma unroll 4
       for (int64_t j = tr; j <= more; j += rl) {
         float v[8];
         oc::load8n(a.part, false, ((chunk + j) * 2 + (j ? 0 : 1)) * a.c + col, a.c - col,
@@ -298,12 +422,14 @@ __global__ __launch_bounds__(TB) void k_embed_join(Sums a, int tpr) {
 #pragma unroll
         for (int k = 0; k < 8; ++k) s[k] += (double)v[k];
       }
+    }
 #pragma unroll
     for (int k = 0; k < 8; ++k) red[threadIdx.x][k] = s[k];
     __syncthreads();
     if (tr == 0 && col < a.c) {
       float v[8];
-      for (int r = 1; r < rl; ++r)
+      const int most = more < rl - 1 ? (int)more : rl - 1;
+      for (int r = 1; r <= most; ++r)
 #pragma unroll
         for (int k = 0; k < 8; ++k) s[k] += red[r * tpr + tc][k];
 #pragma unroll
@@ -343,19 +469,20 @@ __global__ __launch_bounds__(TB) void k_embed_few(const int32_t* ids, uint32_t m
 struct Plan {
   int passes, bits, tiles, len, tpr, slabs;
   int64_t chunks;
-  size_t hist, total, count, a, b, part, bytes;
+  size_t hist, count, a, b, part, bytes;
 };
 constexpr int FEW = 64;
 Plan plan_of(int64_t rows, int64_t num, int c) {
   Plan p{};
+  const bool small = rows <= SMALL;
   int bits = 1;
-  while (((int64_t)1 << bits) < num) ++bits;
+  while (((int64_t)1 << bits) < num + (small ? 1 : 0)) ++bits;  // (small: num is a key too)
   p.passes = (int)cdiv(bits, MOST_BITS);
   p.bits = (int)cdiv(bits, p.passes);
-  // (a tile's steps follow one another, the scan over the tiles too)
-  p.tiles = (int)std::max<int64_t>(
-      1, rows <= (1 << 20) ? std::min<int64_t>(cdiv(rows, 512), 128)
-                           : std::min<int64_t>(cdiv(rows, 8192), 1024));
+  // a tile is one step of a workgroup's waves where there are few rows; every scatter
+  // reads all tiles' counts, so there are at most 128 of them up to 2^20 rows
+  p.tiles = (int)(rows <= (1 << 20) ? std::min<int64_t>(cdiv(rows, SB), 128)
+                                    : std::min<int64_t>(cdiv(rows, 8192), 1024));
   p.len = (int)std::max<int64_t>(32, cdiv(rows, 2048));
   p.chunks = cdiv(rows, p.len);
   const int nv = (int)cdiv(c, 8);
@@ -369,10 +496,9 @@ Plan plan_of(int64_t rows, int64_t num, int c) {
     return was;
   };
   p.count = take(4);
-  p.total = take((size_t)4 << p.bits);
-  p.hist = take(((size_t)4 << p.bits) * p.tiles);
+  p.hist = take(small ? 0 : ((size_t)4 << p.bits) * p.tiles);
   p.a = take((size_t)rows * sizeof(Pair));
-  p.b = p.passes > 1 ? take((size_t)rows * sizeof(Pair)) : p.a;
+  p.b = !small && p.passes > 1 ? take((size_t)rows * sizeof(Pair)) : p.a;
   p.part = take((size_t)p.chunks * 2 * c * sizeof(float) + 32);
   p.bytes = at;
   return p;
@@ -454,27 +580,35 @@ oc_status oc_embed_bwd(oc_dtype dt, int32_t flags, int64_t rows, int64_t num, in
   }
   const Plan p = plan_of(rows, num, c);
   char* w = (char*)ws;
-  Digit d{ids, id_mask(flags), nullptr, nullptr, (uint32_t*)(w + p.hist),
-          (uint32_t*)(w + p.total), (uint32_t*)(w + p.count), rows, num, p.tiles, 0, p.bits};
-  for (int i = 0; i < p.passes; ++i) {
-    d.out = (Pair*)(w + (i & 1 ? p.b : p.a));
-    d.shift = i * p.bits;
-    oc::launch(k_embed_count, dim3((unsigned)p.tiles), dim3(64), 0, s, d);
-    oc::launch(k_embed_scan, dim3((unsigned)cdiv(1 << p.bits, TB)), dim3(TB), 0, s, d);
-    oc::launch(k_embed_scatter, dim3((unsigned)p.tiles), dim3(64), 0, s, d);
+  Digit d{ids,  id_mask(flags), nullptr, (Pair*)(w + p.a), (uint32_t*)(w + p.hist),
+          (uint32_t*)(w + p.count), rows, num, p.tiles, 0, p.bits};
+  if (rows <= SMALL) {
+    oc::launch(k_embed_sort_small, dim3(1), dim3(SB), 0, s, d, p.passes);
     d.in = d.out;
+  } else {
+    for (int i = 0; i < p.passes; ++i) {
+      d.out = (Pair*)(w + (i & 1 ? p.b : p.a));
+      d.shift = i * p.bits;
+      oc::launch(k_embed_count, dim3((unsigned)p.tiles), dim3(SB), 0, s, d);
+      oc::launch(k_embed_scatter, dim3((unsigned)p.tiles), dim3(SB), 0, s, d);
+      d.in = d.out;
+    }
   }
   a.sorted = d.in;
   a.count = d.count;
   a.part = (float*)(w + p.part);
   a.len = p.len;
-  a.chunk_blocks = cdiv(p.chunks * p.slabs, TB / p.tpr);
-  const int64_t zero_blocks = cdiv(num, TB);
-  oc::launch_main(k_embed_sums, dim3((unsigned)(a.chunk_blocks + zero_blocks)), dim3(TB), s, a,
-                  p.tpr, p.slabs);
+  a.zero_blocks = cdiv(num, TB);
+  const int64_t blocks = a.zero_blocks + cdiv(p.chunks * p.slabs, TB / p.tpr);
+  const auto sums = [&](auto kernel) {
+    oc::launch_main(kernel, dim3((unsigned)blocks), dim3(TB), s, a, p.tpr, p.slabs);
+  };
+  if (p.len > MOST_ADDED)
+    a.bf16 ? sums(k_embed_sums<true, true>) : sums(k_embed_sums<false, true>);
+  else
+    a.bf16 ? sums(k_embed_sums<true, false>) : sums(k_embed_sums<false, false>);
   if (p.chunks > 1)
-    oc::launch(k_embed_join, dim3((unsigned)p.chunks, (unsigned)std::min(p.slabs, 16)), dim3(TB),
-               0, s, a, p.tpr);
+    oc::launch(k_embed_join, dim3((unsigned)p.chunks), dim3(JB), 0, s, a, p.tpr);
   OC_LAUNCH_CHECK();
   return OC_OK;
 }

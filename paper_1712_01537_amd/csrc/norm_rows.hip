@@ -7,94 +7,15 @@
 namespace {
 
 using oc::cdiv;
-using oc::d_v4f;
-using oc::d_v4f_any;
-using oc::d_v4u;
-using oc::d_v4u_any;
+using oc::cut;
+using oc::hidden;
 using oc::MOST_ADDED;
 using oc::Norm;
 using oc::NormBwd;
-
-// Eight values as they lie in memory, so that a load can be in flight while the row
-// before is worked on.
-template <bool BF>
-struct Raw;
-template <>
-struct Raw<true> {
-  d_v4u u;
-};
-template <>
-struct Raw<false> {
-  d_v4f a, b;
-};
-// A lane's number of values, behind the compiler's back: it would form the eight
-// comparisons with it in front of the loop over the rows and keep them there in 16 scalar
-// registers, which it then has to save and fetch.
-__device__ __forceinline__ int hidden(int cnt) {
-  asm("" : "+v"(cnt));
-  return cnt;
-}
-// Zeros behind the row's end, in the lanes that have it.
-__device__ __forceinline__ void cut(float (&v)[8], int cnt) {
-  if (cnt < 8) {
-    const int q = hidden(cnt);
-#pragma unroll
-    for (int k = 0; k < 8; ++k) v[k] = k < q ? v[k] : 0.f;
-  }
-}
-
-// A row's place in an array: where a wave has one row (all but the shortest), the row's
-// start is the same for its lanes and a lane's own part 32 bits.
-struct Place {
-  int64_t at;  // the row's first element
-  int col, cnt;
-  int64_t left;  // elements from there to the array's end
-};
-__device__ __forceinline__ void raw_load(Raw<true>& r, const void* p, const Place& w) {
-  const uint16_t* q = (const uint16_t*)p + w.at;
-  if (w.cnt >= 8 || w.col + 8 <= w.left) {
-    r.u = *(const d_v4u_any*)(q + (uint32_t)w.col);
-  } else {
-    const int c = hidden(w.cnt);
-    uint32_t h[8];
-#pragma unroll
-    for (int k = 0; k < 8; ++k) h[k] = k < c ? q[w.col + k] : 0;
-    r.u = d_v4u{h[0] | h[1] << 16, h[2] | h[3] << 16, h[4] | h[5] << 16, h[6] | h[7] << 16};
-  }
-}
-__device__ __forceinline__ void raw_load(Raw<false>& r, const void* p, const Place& w) {
-  const float* q = (const float*)p + w.at;
-  if (w.cnt >= 8 || w.col + 8 <= w.left) {
-    r.a = *(const d_v4f_any*)(q + (uint32_t)w.col);
-    r.b = *(const d_v4f_any*)(q + (uint32_t)w.col + 4);
-  } else {
-    const int c = hidden(w.cnt);
-    float v[8];
-#pragma unroll
-    for (int k = 0; k < 8; ++k) v[k] = k < c ? q[w.col + k] : 0.f;
-    r.a = d_v4f{v[0], v[1], v[2], v[3]};
-    r.b = d_v4f{v[4], v[5], v[6], v[7]};
-  }
-}
-template <bool BF>
-__device__ __forceinline__ void row_store(void* p, const Place& w, const float (&v)[8]) {
-  void* q = BF ? (void*)((uint16_t*)p + w.at) : (void*)((float*)p + w.at);
-  if (w.cnt >= 8)
-    oc::store8(q, BF, (uint32_t)w.col, v);
-  else
-    oc::store8n(q, BF, (uint32_t)w.col, hidden(w.cnt), v);
-}
-__device__ __forceinline__ void unpack(const Raw<true>& r, float (&v)[8]) {
-#pragma unroll
-  for (int k = 0; k < 4; ++k) {
-    v[2 * k] = oc::bf_up(r.u[k] & 0xffffu);
-    v[2 * k + 1] = __builtin_bit_cast(float, r.u[k] & 0xffff0000u);
-  }
-}
-__device__ __forceinline__ void unpack(const Raw<false>& r, float (&v)[8]) {
-#pragma unroll
-  for (int k = 0; k < 4; ++k) v[k] = r.a[k], v[4 + k] = r.b[k];
-}
+using oc::Place;
+using oc::Raw;
+using oc::row_store;
+using oc::unpack;
 
 // (A vector's element goes by value: __builtin_bit_cast of v[1] itself takes v[0].)
 __device__ __forceinline__ float float_of(uint32_t u) { return __builtin_bit_cast(float, u); }
