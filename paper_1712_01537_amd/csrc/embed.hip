@@ -1,17 +1,20 @@
 // Table rows by id (oc_embed_fwd), y[r] = scale table[id[r]], and the table's gradient
 // (oc_embed_bwd), dtable[v] = scale times the sum of dy[r] over the rows r with id v.
 //
-// The gradient without atomics, so that its bits do not depend on the order of the
-// workgroups: the rows are sorted by id (stable, so that those of one id stay in order),
-// the sorted list is cut into chunks of equal length, and each chunk's runs of one id
-// are summed in order.  A run inside one chunk is written to the table's row; one that
-// goes on over a border leaves a partial sum a chunk, added by k_embed_join.  However
-// many rows share an id, no thread's chain of additions is longer than a chunk.
+// The gradient without floating-point atomics, so that its bits do not depend on the order
+// of the workgroups: the rows are sorted by id (stable, so that those of one id stay in
+// order) and the sorted list is cut into pieces of equal length, one for a group of
+// lanes, whose runs of one id are summed in order.  A run inside one piece is written to
+// the table's row; one that goes on over a border leaves a partial sum a piece, added
+// through LDS where the run stays in the workgroup's chunk, else by k_embed_join.
+// However many rows share an id, no chain of additions is longer than a piece.
 //
 // The sort takes the ids' bits in digits of up to eight, lowest first.  A tile of rows is
 // one workgroup's: count writes each tile's number of rows of every digit value, and
 // scatter adds those numbers up itself (all values below its own, and its own in the tiles
-// before), so that a digit takes two launches.  A wave takes its rows 64 at a time, in
+// before), so that a digit takes two launches.  (Counting the next digit by atomics where
+// the scatter puts the rows saves a launch of 3 to 5 us and costs 6 us for 65536 rows and
+// 14 for 260000.)  A wave takes its rows 64 at a time, in
 // order: the place of a row among those of its digit is a count of the lanes before it
 // with the same digit.  Up to SMALL rows are sorted by one workgroup in LDS.
 #include <algorithm>
@@ -62,7 +65,7 @@ struct Digit {
   Pair* out;
   uint32_t *hist, *count;  // hist[tiles][1 << bits]
   int64_t rows, num;
-  int tiles, shift, bits;
+  int tiles, shift, bits, passes;
 };
 constexpr int MOST_BITS = 8, MOST_D = 1 << MOST_BITS;
 constexpr int SB = 1024, SW = SB / 64;  // threads and waves of a sorting workgroup
@@ -201,7 +204,7 @@ __global__ __launch_bounds__(SB) void k_embed_scatter(Digit a) {
 }
 
 // Up to SMALL rows, every digit: a thread's pairs are rows 256 w + 64 j + lane of the list.
-__global__ __launch_bounds__(SB) void k_embed_sort_small(Digit a, int passes) {
+__global__ __launch_bounds__(SB) void k_embed_sort_small(Digit a) {
   __shared__ Pair list[SMALL];
   __shared__ uint32_t at[SW][MOST_D], total[MOST_D], valid;
   constexpr int J = SMALL / SB;
@@ -220,7 +223,7 @@ __global__ __launch_bounds__(SB) void k_embed_sort_small(Digit a, int passes) {
     const uint64_t m = __ballot(in);
     if (lane == 0 && m) atomicAdd(&valid, (uint32_t)__popcll(m));
   }
-  for (int s = 0; s < passes; ++s) {
+  for (int s = 0; s < a.passes; ++s) {
     for (int i = threadIdx.x; i < SW * MOST_D; i += SB) (&at[0][0])[i] = 0;
     __syncthreads();
     uint32_t rank[J];
@@ -269,9 +272,9 @@ struct Sums {
   const uint32_t* count;
   const void* dy;
   void* out;
-  float* part;  // [chunks][2][c]: of the run open at the chunk's start, and at its end
+  float* part;  // [chunks][2][c]: sums of the run open at the chunk's start, and its end
   int64_t num, rows;
-  int c, len;  // len: pairs of a chunk
+  int c, len, chunk;  // len, chunk: pairs of a piece and of a chunk
   bool bf16, out_bf16;
   float scale;
   int64_t zero_blocks;
@@ -309,134 +312,249 @@ struct Acc {
   }
 };
 
-// Zeros in the table's rows that no id names.  A wave has 64 rows, each lane looks for one
-// of them among the sorted ids.
-__device__ __forceinline__ void zero_rows(const Sums& a, int64_t n, int64_t wave) {
+// The first place in the sorted list whose id is at least v, by a wave: 64 probes a step.
+__device__ __forceinline__ int64_t place_of(const Sums& a, int64_t n, int64_t v) {
   const int lane = threadIdx.x & 63;
-  const int64_t v = wave * 64 + lane;
-  int64_t lo = 0, hi = n;
-  while (lo < hi) {
-    const int64_t mid = (lo + hi) >> 1;
-    if ((int64_t)a.sorted[mid].id < v) lo = mid + 1;
-    else hi = mid;
+  int64_t lo = 0, len = n;  // it is lo .. lo + len
+  while (len > 0) {
+    const int64_t step = (len + 63) / 64, at = lo + step * (lane + 1) - 1;
+    const bool below = at < lo + len && (int64_t)a.sorted[at].id < v;
+    const int k = __popcll(__ballot(below));
+    const int64_t skip = k * step;
+    lo += skip;
+    len = len - skip < step - 1 ? len - skip : step - 1;
+    if (len < 0) len = 0;
   }
-  const bool none = v < a.num && !(lo < n && (int64_t)a.sorted[lo].id == v);
+  return lo;
+}
+
+// Zeros in the table's rows that no id names, 64 rows a wave: the part of the sorted list
+// with their ids is read where it is short, else each lane looks for its own row's there.
+__device__ __forceinline__ void zero_rows(const Sums& a, int64_t n, int64_t wave) {
+  __shared__ unsigned long long named[TB / 64];
+  const int lane = threadIdx.x & 63, w = threadIdx.x / 64;
+  const int64_t v0 = wave * 64, v = v0 + lane;
+  if (v0 >= a.num) return;
+  const int64_t from = place_of(a, n, v0), to = place_of(a, n, v0 + 64);
+  uint64_t none;
+  if (to - from <= 256) {
+    if (lane == 0) named[w] = 0;
+    wave_sync();
+    for (int64_t i = from + lane; i < to; i += 64)
+      atomicOr(&named[w], 1ull << (a.sorted[i].id - (uint32_t)v0));
+    wave_sync();
+    none = ~named[w] & __ballot(v < a.num);
+  } else {
+    int64_t lo = from, hi = to;
+    while (lo < hi) {
+      const int64_t mid = (lo + hi) >> 1;
+      if ((int64_t)a.sorted[mid].id < v) lo = mid + 1;
+      else hi = mid;
+    }
+    none = __ballot(v < a.num && !(lo < to && (int64_t)a.sorted[lo].id == v));
+  }
   const float zero[8] = {};
-  for (uint64_t m = __ballot(none); m; m &= m - 1) {
-    const int64_t row = wave * 64 + __builtin_ctzll(m);
+  for (uint64_t m = none; m; m &= m - 1) {
+    const int64_t row = v0 + __builtin_ctzll(m);
     for (int col = lane * 8; col < a.c; col += 512)
       oc::store8n(a.out, a.out_bf16, row * a.c + col, a.c - col, zero);
   }
 }
 
-// Groups of tpr lanes, each with 8 tpr columns of a chunk (slabs of them where rows are
-// longer).  The first workgroups zero the table's other rows.
+// A workgroup has a chunk of the sorted list and 8 tpr columns (a slab of them where rows
+// are longer), each of its groups of tpr lanes a piece of the chunk.  The first
+// workgroups zero the table's other rows.
 template <bool BF, bool LONG>
 __global__ __launch_bounds__(TB) void k_embed_sums(Sums a, int tpr, int slabs) {
+  __shared__ float open[2][8][TB];  // sums of the run open at the piece's start, and its end
+  __shared__ bool through[TB];      // the first is the second: all of the piece
   const int64_t n = *a.count;
   if (blockIdx.x < a.zero_blocks) {
     zero_rows(a, n, (int64_t)blockIdx.x * (TB / 64) + threadIdx.x / 64);
     return;
   }
-  const int64_t unit = (blockIdx.x - a.zero_blocks) * (TB / tpr) + threadIdx.x / tpr;
-  const int64_t chunk = unit / slabs;
-  const int col = ((int)(unit - chunk * slabs) * tpr + threadIdx.x % tpr) * 8;
-  const int64_t i0 = chunk * a.len, i1 = i0 + a.len < n ? i0 + a.len : n;
-  if (i0 >= i1 || col >= a.c) return;
-  const int cnt = a.c - col;
-  constexpr int U = BF ? 16 : 8;  // rows in flight
-  Pair p[U];
-  const auto pairs = [&](int64_t i) {
-#pragma unroll
-    for (int j = 0; j < U; ++j) p[j] = a.sorted[i + j < i1 ? i + j : i1 - 1];
+  const int64_t unit = blockIdx.x - a.zero_blocks, chunk = unit / slabs;
+  const int g = threadIdx.x / tpr, tc = threadIdx.x % tpr, G = TB / tpr;
+  const int col = ((int)(unit - chunk * slabs) * tpr + tc) * 8, cnt = a.c - col;
+  const int64_t b0 = chunk * G * a.len, i0 = b0 + (int64_t)g * a.len;
+  const int64_t i1 = i0 + a.len < n ? i0 + a.len : n;
+  if (b0 >= n) return;
+  uint32_t id = 0;
+  bool first = false, goes_on = false, begun = false;  // begun: the last run began here
+  const auto store = [&](uint32_t row, const float(&v)[8]) {
+    oc::store8n(a.out, a.out_bf16, (int64_t)row * a.c + col, cnt, v);
   };
-  pairs(i0);
-  uint32_t id = p[0].id;
-  bool first = i0 > 0 && a.sorted[i0 - 1].id == id;  // the run began in a chunk before
-  const bool goes_on = i1 < n && a.sorted[i1].id == a.sorted[i1 - 1].id;
-  Acc<LONG> acc;
-  acc.clear();
-  const auto flush = [&](bool open) {
-    float v[8];
-    acc.times(first || open ? 1.f : a.scale, v);
-    if (first || open)
-      oc::store8n(a.part, false, (chunk * 2 + (first ? 0 : 1)) * a.c + col, cnt, v);
-    else
-      oc::store8n(a.out, a.out_bf16, (int64_t)id * a.c + col, cnt, v);
-  };
-  for (int64_t i = i0; i < i1; i += U) {
-    oc::Raw<BF> raw[U];
-    uint32_t ids[U];
+  if (i0 < i1) {
+    constexpr int U = BF ? 16 : 8;  // rows in flight
+    Pair p[U];
+    const auto pairs = [&](int64_t i) {
 #pragma unroll
-    for (int j = 0; j < U; ++j) {
-      const int64_t at = (int64_t)p[j].row * a.c;
-      oc::raw_load(raw[j], a.dy, oc::Place{at, col, cnt, a.rows * a.c - at});
-      ids[j] = p[j].id;
-    }
-    if (i + U < i1) pairs(i + U);
-#pragma unroll
-    for (int j = 0; j < U; ++j) {
-      if (i + j >= i1) break;
-      if (ids[j] != id) {
-        flush(false);
-        acc.clear();
-        id = ids[j];
-        first = false;
-      }
+      for (int j = 0; j < U; ++j) p[j] = a.sorted[i + j < i1 ? i + j : i1 - 1];
+    };
+    pairs(i0);
+    id = p[0].id;
+    first = i0 > 0 && a.sorted[i0 - 1].id == id;  // the run began in a piece before
+    goes_on = i1 < n && a.sorted[i1].id == a.sorted[i1 - 1].id;
+    begun = !first;
+    Acc<LONG> acc;
+    acc.clear();
+    const auto flush = [&](bool left_open) {
       float v[8];
-      oc::unpack(raw[j], v);
-      acc.add(v);
+      if (cnt <= 0) return;
+      if (begun && !left_open) {
+        acc.times(a.scale, v);
+        store(id, v);
+      } else {
+        acc.times(1.f, v);
+#pragma unroll
+        for (int k = 0; k < 8; ++k) open[begun ? 1 : 0][k][threadIdx.x] = v[k];
+      }
+    };
+    for (int64_t i = i0; i < i1; i += U) {
+      oc::Raw<BF> raw[U];
+      uint32_t ids[U];
+#pragma unroll
+      for (int j = 0; j < U; ++j) {
+        const int64_t at = (int64_t)p[j].row * a.c;
+        if (cnt > 0) oc::raw_load(raw[j], a.dy, oc::Place{at, col, cnt, a.rows * a.c - at});
+        ids[j] = p[j].id;
+      }
+      if (i + U < i1) pairs(i + U);
+#pragma unroll
+      for (int j = 0; j < U; ++j) {
+        if (i + j >= i1) break;
+        if (ids[j] != id) {
+          flush(false);
+          acc.clear();
+          id = ids[j];
+          begun = true;
+        }
+        float v[8];
+        oc::unpack(raw[j], v);
+        acc.add(v);
+      }
+    }
+    flush(goes_on);
+  }
+  if (tc == 0) through[g] = first && !begun && goes_on;
+  __syncthreads();
+  if (cnt <= 0) return;
+  double sum[8];
+  // pieces from g + 1 on, to the run's end: whether that is in this chunk
+  const auto add_on = [&]() {
+    for (int h = g + 1; h < G; ++h) {
+#pragma unroll
+      for (int k = 0; k < 8; ++k) sum[k] += (double)open[0][k][h * tpr + tc];
+      if (!through[h]) return true;
+    }
+    return false;
+  };
+  const auto store_part = [&](int which) {
+    float v[8];
+#pragma unroll
+    for (int k = 0; k < 8; ++k) v[k] = (float)sum[k];
+    oc::store8n(a.part, false, (chunk * 2 + which) * a.c + col, cnt, v);
+  };
+  if (goes_on && begun) {
+#pragma unroll
+    for (int k = 0; k < 8; ++k) sum[k] = (double)open[1][k][threadIdx.x];
+    if (add_on()) {
+      float v[8];
+#pragma unroll
+      for (int k = 0; k < 8; ++k) v[k] = (float)(sum[k] * a.scale);
+      store(id, v);
+    } else {
+      store_part(1);
     }
   }
-  flush(goes_on);
+  if (g == 0 && first) {
+#pragma unroll
+    for (int k = 0; k < 8; ++k) sum[k] = (double)open[0][k][threadIdx.x];
+    if (through[0]) add_on();
+    store_part(0);
+  }
 }
 
-// The runs that go on over a chunk's end: the workgroup of the chunk where one begins adds
-// its partial sums, rl lanes a column, in double and in a fixed order.
-constexpr int JB = 512;
-__global__ __launch_bounds__(JB) void k_embed_join(Sums a, int tpr) {
-  __shared__ double red[JB][9];
-  const int64_t n = *a.count, chunk = blockIdx.x;
-  const int64_t i0 = chunk * a.len, i1 = i0 + a.len;
-  if (i1 >= n) return;
-  const uint32_t id = a.sorted[i1 - 1].id, next = a.sorted[i1].id, from = a.sorted[i0].id;
-  const uint32_t last = i0 > 0 ? a.sorted[i0 - 1].id : ~0u;  // (no id: they are below num)
-  if (next != id || (from == id && last == id)) return;
-  int64_t more = 0;  // chunks that the run goes on in
-  for (;;) {
-    const int64_t at = (chunk + 1 + more + threadIdx.x) * a.len;
-    const int k = __syncthreads_count(at < n && a.sorted[at].id == id);
-    more += k;
-    if (k < JB) break;
-  }
-  const int tc = threadIdx.x % tpr, tr = threadIdx.x / tpr, rl = JB / tpr;
-  for (int c0 = 0; c0 < a.c; c0 += tpr * 8) {
-    const int col = c0 + tc * 8;
-    double s[8] = {};
-    if (col < a.c) {
-#pragma unroll 4
-      for (int64_t j = tr; j <= more; j += rl) {
-        float v[8];
-        oc::load8n(a.part, false, ((chunk + j) * 2 + (j ? 0 : 1)) * a.c + col, a.c - col,
-                   INT64_MAX, v);
+// The runs that go on over a chunk's end.  Each wave looks at the end of one chunk.  Where
+// a run begins in it and ends in the next, as most do, the wave adds the two partial sums;
+// the others it leaves to the workgroup, which adds them in double and in a fixed order,
+// rl lanes a column.
+constexpr int JB = 512, JW = JB / 64;
+__global__ __launch_bounds__(JB, 4) void k_embed_join(Sums a, int tpr) {
+  __shared__ double red[8][JB];
+  __shared__ bool longer[JW];
+  const int64_t n = *a.count;
+  const int w = threadIdx.x / 64, lane = threadIdx.x & 63;
+  const auto load = [&](int64_t chunk, int which, int col, float(&v)[8]) {
+    oc::load8n(a.part, false, (chunk * 2 + which) * a.c + col, a.c - col, INT64_MAX, v);
+  };
+  const auto finish = [&](uint32_t id, int col, const double(&s)[8]) {
+    float v[8];
 #pragma unroll
-        for (int k = 0; k < 8; ++k) s[k] += (double)v[k];
+    for (int k = 0; k < 8; ++k) v[k] = (float)(s[k] * a.scale);
+    oc::store8n(a.out, a.out_bf16, (int64_t)id * a.c + col, a.c - col, v);
+  };
+  {
+    const int64_t chunk = (int64_t)blockIdx.x * JW + w, i0 = chunk * a.chunk, i1 = i0 + a.chunk;
+    bool more = false;
+    if (i1 < n) {
+      const uint32_t id = a.sorted[i1].id, was = a.sorted[i1 - 1].id, from = a.sorted[i0].id;
+      const uint32_t before = i0 > 0 ? a.sorted[i0 - 1].id : ~0u;  // (no id)
+      const int64_t i2 = i1 + a.chunk;
+      const uint32_t then = i2 < n ? a.sorted[i2].id : ~0u;
+      if (was == id && !(from == id && before == id)) {
+        more = then == id;
+        for (int col = (blockIdx.y * tpr + lane) * 8; !more && lane < tpr && col < a.c;
+             col += gridDim.y * tpr * 8) {
+          float v[8], u[8];
+          double s[8];
+          load(chunk, 1, col, v);
+          load(chunk + 1, 0, col, u);
+#pragma unroll
+          for (int k = 0; k < 8; ++k) s[k] = (double)v[k] + (double)u[k];
+          finish(id, col, s);
+        }
       }
     }
-#pragma unroll
-    for (int k = 0; k < 8; ++k) red[threadIdx.x][k] = s[k];
-    __syncthreads();
-    if (tr == 0 && col < a.c) {
-      float v[8];
-      const int most = more < rl - 1 ? (int)more : rl - 1;
-      for (int r = 1; r <= most; ++r)
-#pragma unroll
-        for (int k = 0; k < 8; ++k) s[k] += red[r * tpr + tc][k];
-#pragma unroll
-      for (int k = 0; k < 8; ++k) v[k] = (float)(s[k] * a.scale);
-      oc::store8n(a.out, a.out_bf16, (int64_t)id * a.c + col, a.c - col, v);
+    if (lane == 0) longer[w] = more;
+  }
+  __syncthreads();
+  const int tc = threadIdx.x % tpr, tr = threadIdx.x / tpr, rl = JB / tpr;
+  for (int q = 0; q < JW; ++q) {
+    if (!longer[q]) continue;
+    const int64_t chunk = (int64_t)blockIdx.x * JW + q;
+    const uint32_t id = a.sorted[(chunk + 1) * a.chunk].id;
+    int64_t more = 0;  // chunks that the run goes on in
+    for (;;) {
+      const int64_t at = (chunk + 1 + more + threadIdx.x) * a.chunk;
+      const int k = __syncthreads_count(at < n && a.sorted[at].id == id);
+      more += k;
+      if (k < JB) break;
     }
-    __syncthreads();
+    for (int c0 = blockIdx.y * tpr * 8; c0 < a.c; c0 += gridDim.y * tpr * 8) {
+      const int col = c0 + tc * 8;
+      double s[8] = {};
+      if (col < a.c) {
+#pragma unroll 4
+        for (int64_t j = tr; j <= more; j += rl) {
+          float v[8];
+          load(chunk + j, j ? 0 : 1, col, v);
+#pragma unroll
+          for (int k = 0; k < 8; ++k) s[k] += (double)v[k];
+        }
+      }
+#pragma unroll
+      for (int k = 0; k < 8; ++k) red[k][threadIdx.x] = s[k];
+      __syncthreads();
+      if (tr == 0 && col < a.c) {
+        const int most = more < rl - 1 ? (int)more : rl - 1;
+        for (int r = 1; r <= most; ++r)
+#pragma unroll
+          for (int k = 0; k < 8; ++k) s[k] += red[k][r * tpr + tc];
+        finish(id, col, s);
+      }
+      __syncthreads();
+    }
   }
 }
 
@@ -482,13 +600,13 @@ Plan plan_of(int64_t rows, int64_t num, int c) {
   // a tile is one step of a workgroup's waves where there are few rows; every scatter
   // reads all tiles' counts, so there are at most 128 of them up to 2^20 rows
   p.tiles = (int)(rows <= (1 << 20) ? std::min<int64_t>(cdiv(rows, SB), 128)
-                                    : std::min<int64_t>(cdiv(rows, 8192), 1024));
-  p.len = (int)std::max<int64_t>(32, cdiv(rows, 2048));
-  p.chunks = cdiv(rows, p.len);
+                                    : std::min<int64_t>(cdiv(rows, 8192), 512));
   const int nv = (int)cdiv(c, 8);
   p.tpr = 1;
   while (p.tpr < nv && p.tpr < 64) p.tpr *= 2;
   p.slabs = (int)cdiv(nv, p.tpr);
+  p.len = (int)std::max<int64_t>(16, cdiv(rows, 2048 * (TB / p.tpr)));
+  p.chunks = cdiv(rows, (int64_t)p.len * (TB / p.tpr));
   size_t at = 0;
   const auto take = [&](size_t n) {
     const size_t was = at;
@@ -580,10 +698,10 @@ oc_status oc_embed_bwd(oc_dtype dt, int32_t flags, int64_t rows, int64_t num, in
   }
   const Plan p = plan_of(rows, num, c);
   char* w = (char*)ws;
-  Digit d{ids,  id_mask(flags), nullptr, (Pair*)(w + p.a), (uint32_t*)(w + p.hist),
-          (uint32_t*)(w + p.count), rows, num, p.tiles, 0, p.bits};
+  Digit d{ids, id_mask(flags), nullptr, (Pair*)(w + p.a), (uint32_t*)(w + p.hist),
+          (uint32_t*)(w + p.count), rows, num, p.tiles, 0, p.bits, p.passes};
   if (rows <= SMALL) {
-    oc::launch(k_embed_sort_small, dim3(1), dim3(SB), 0, s, d, p.passes);
+    oc::launch(k_embed_sort_small, dim3(1), dim3(SB), 0, s, d);
     d.in = d.out;
   } else {
     for (int i = 0; i < p.passes; ++i) {
@@ -598,8 +716,9 @@ oc_status oc_embed_bwd(oc_dtype dt, int32_t flags, int64_t rows, int64_t num, in
   a.count = d.count;
   a.part = (float*)(w + p.part);
   a.len = p.len;
+  a.chunk = p.len * (TB / p.tpr);
   a.zero_blocks = cdiv(num, TB);
-  const int64_t blocks = a.zero_blocks + cdiv(p.chunks * p.slabs, TB / p.tpr);
+  const int64_t blocks = a.zero_blocks + p.chunks * p.slabs;
   const auto sums = [&](auto kernel) {
     oc::launch_main(kernel, dim3((unsigned)blocks), dim3(TB), s, a, p.tpr, p.slabs);
   };
@@ -607,8 +726,15 @@ oc_status oc_embed_bwd(oc_dtype dt, int32_t flags, int64_t rows, int64_t num, in
     a.bf16 ? sums(k_embed_sums<true, true>) : sums(k_embed_sums<false, true>);
   else
     a.bf16 ? sums(k_embed_sums<true, false>) : sums(k_embed_sums<false, false>);
-  if (p.chunks > 1)
-    oc::launch(k_embed_join, dim3((unsigned)p.chunks), dim3(JB), 0, s, a, p.tpr);
+  if (p.chunks > 1) {
+    // few columns a workgroup, so that a long run's partial sums have many lanes, and no
+    // more workgroups than the card holds at once
+    const int jt = std::min(p.tpr, 32);
+    const int64_t blocks = cdiv(p.chunks, JW), most = std::max<int64_t>(1, 512 / blocks);
+    oc::launch(k_embed_join,
+               dim3((unsigned)blocks, (unsigned)std::min(cdiv(cdiv(c, 8), jt), most)), dim3(JB), 0,
+               s, a, jt);
+  }
   OC_LAUNCH_CHECK();
   return OC_OK;
 }
