@@ -9,7 +9,7 @@
 // through LDS where the run stays in the workgroup's chunk, else by k_embed_join.
 // However many rows share an id, no chain of additions is longer than a piece.
 //
-// The sort takes the ids' bits in digits of up to eight, lowest first.  A tile of rows is
+// The sort takes the ids' bits in digits of up to nine, lowest first.  A tile of rows is
 // one workgroup's: count writes each tile's number of rows of every digit value, and
 // scatter adds those numbers up itself (all values below its own, and its own in the tiles
 // before), so that a digit takes two launches.  (Counting the next digit by atomics where
@@ -67,7 +67,7 @@ struct Digit {
   int64_t rows, num;
   int tiles, shift, bits, passes;
 };
-constexpr int MOST_BITS = 8, MOST_D = 1 << MOST_BITS;
+constexpr int MOST_BITS = 9, MOST_D = 1 << MOST_BITS;
 constexpr int SB = 1024, SW = SB / 64;  // threads and waves of a sorting workgroup
 constexpr int SMALL = 4096;
 
@@ -107,14 +107,15 @@ __device__ __forceinline__ void wave_sync() {
   __builtin_amdgcn_wave_barrier();
   __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
 }
-// v[d] of D <= 256 values becomes the sum of those before it, by one wave (four a lane).
+// v[d] of D values becomes the sum of those before it, by one wave (PER a lane).
 // Returns the sum of all, in each lane.
 __device__ __forceinline__ uint32_t scan_digits(uint32_t* v, int D) {
+  constexpr int PER = MOST_D / 64;
   const int lane = threadIdx.x & 63;
-  uint32_t x[4], sum = 0;
+  uint32_t x[PER], sum = 0;
 #pragma unroll
-  for (int k = 0; k < 4; ++k) {
-    const uint32_t y = lane * 4 + k < D ? v[lane * 4 + k] : 0;
+  for (int k = 0; k < PER; ++k) {
+    const uint32_t y = lane * PER + k < D ? v[lane * PER + k] : 0;
     x[k] = sum;
     sum += y;
   }
@@ -124,8 +125,8 @@ __device__ __forceinline__ uint32_t scan_digits(uint32_t* v, int D) {
     if (lane >= k) upto += u;
   }
 #pragma unroll
-  for (int k = 0; k < 4; ++k)
-    if (lane * 4 + k < D) v[lane * 4 + k] = upto - sum + x[k];
+  for (int k = 0; k < PER; ++k)
+    if (lane * PER + k < D) v[lane * PER + k] = upto - sum + x[k];
   return __shfl(upto, 63);
 }
 
@@ -385,7 +386,7 @@ __global__ __launch_bounds__(TB) void k_embed_sums(Sums a, int tpr, int slabs) {
     oc::store8n(a.out, a.out_bf16, (int64_t)row * a.c + col, cnt, v);
   };
   if (i0 < i1) {
-    constexpr int U = BF ? 16 : 8;  // rows in flight
+    constexpr int U = BF ? 8 : 4;  // rows in flight
     Pair p[U];
     const auto pairs = [&](int64_t i) {
 #pragma unroll
