@@ -1171,11 +1171,12 @@ def _ln_ws(rows, c):
 
 
 def _stats(x, rows, need):
-    """mean and invstd of the rows (one allocation), or None twice."""
+    """mean and invstd of the rows with their addresses, or None."""
     if not need:
         return None, None, None, None
-    st = torch.empty((2, rows), dtype=torch.float32, device=x.device)
-    return st[0], st[1], st.data_ptr(), st.data_ptr() + 4 * rows
+    mean = torch.empty(rows, dtype=torch.float32, device=x.device)
+    invstd = torch.empty_like(mean)
+    return mean, invstd, mean.data_ptr(), invstd.data_ptr()
 
 
 def _norm_sums(x, dev, rows, c, dgamma, dbeta, need_dgamma, need_dbeta):
@@ -1196,7 +1197,7 @@ def oc_ln_fwd(x, gamma=None, beta=None, eps=1e-5, need_stats=False):
     (y, mean, invstd), the last two None unless need_stats (the backward's).  gamma, beta:
     float32 [c] or None."""
     dev, dt, rows, c = _rows_of(x, "x")
-    y = x.new_empty((rows, c))
+    y = torch.empty_like(x)
     mean, invstd, mp, ip = _stats(x, rows, need_stats)
     _check(load().oc_ln_fwd(dt, rows, c, _given(x, "x", dev, x.dtype, (rows, c)),
                             _given(gamma, "gamma", dev, torch.float32, (c,)),
@@ -1210,7 +1211,7 @@ def oc_ln_bwd(x, dy, gamma, mean, invstd, need_dx=True, need_dgamma=True, need_d
     """(dx, dgamma, dbeta) of oc_ln_fwd (None where not needed); dgamma, dbeta: optional
     caller tensors to write into."""
     dev, dt, rows, c = _rows_of(x, "x")
-    dx = x.new_empty((rows, c)) if need_dx else None
+    dx = torch.empty_like(x) if need_dx else None
     dgamma, dbeta, gp, bp, ws, wsp, need = _norm_sums(x, dev, rows, c, dgamma, dbeta, need_dgamma,
                                                       need_dbeta)
     _check(load().oc_ln_bwd(dt, rows, c, _given(x, "x", dev, x.dtype, (rows, c)),
@@ -1231,7 +1232,7 @@ def oc_dropout_rng(x, p, rng, site=0, y=None):
     xp = _given(x, "x", dev, x.dtype, (rows, c))
     rp = _rng_state(rng, dev, p)
     if y is None:
-        y = x.new_empty((rows, c))
+        y = torch.empty_like(x)
     _check(load().oc_dropout_rng(dt, rows, c, xp, p, rp, site,
                                  _given(y, "y", dev, x.dtype, (rows, c)), _stream()))
     return y
@@ -1247,8 +1248,8 @@ def oc_drop_ln_fwd(x, res, p, rng, gamma=None, beta=None, site=0, eps=1e-5, need
     xp = _given(x, "x", dev, x.dtype, (rows, c))
     rp = _rng_state(rng, dev, p)
     if h is None:
-        h = x.new_empty((rows, c))
-    y = x.new_empty((rows, c))
+        h = torch.empty_like(x)
+    y = torch.empty_like(x)
     mean, invstd, mp, ip = _stats(x, rows, need_stats)
     _check(load().oc_drop_ln_fwd(dt, rows, c, xp, _given(res, "res", dev, x.dtype, (rows, c)), p,
                                  rp, site, _given(gamma, "gamma", dev, torch.float32, (c,)),
@@ -1265,8 +1266,8 @@ def oc_drop_ln_bwd(x, res, dy, p, rng, gamma, mean, invstd, dh=None, site=0, nee
     above, or None; rng holds what the forward read."""
     dev, dt, rows, c = _rows_of(x, "x")
     t = x.dtype
-    dx = x.new_empty((rows, c)) if need_dx else None
-    dres = x.new_empty((rows, c)) if need_dres else None
+    dx = torch.empty_like(x) if need_dx else None
+    dres = torch.empty_like(x) if need_dres else None
     dgamma, dbeta, gp, bp, ws, wsp, need = _norm_sums(x, dev, rows, c, dgamma, dbeta, need_dgamma,
                                                       need_dbeta)
     _check(load().oc_drop_ln_bwd(dt, rows, c, _given(x, "x", dev, t, (rows, c)),

@@ -13,24 +13,39 @@ using oc::Drop;
 constexpr int TB = 256;
 constexpr int64_t MOST_BLOCKS = (int64_t)1 << 22;
 
-// A thread has eight columns of a row.  d.on 0: a copy.
-__global__ __launch_bounds__(TB) void k_drop_rng(Drop d, const void* x, bool bf16, int64_t rows,
-                                                 int c, void* y) {
+// A thread has eight columns of a row.  d.on 0: a copy.  WHOLE: c is a multiple of eight,
+// so that group i is elements 8 i on and no row has to be known.
+template <bool BF, bool WHOLE>
+__global__ __launch_bounds__(TB) void k_drop_rng(Drop d, const void* x, int64_t rows, int c,
+                                                 void* y) {
   const int nv = (c + 7) / 8;
   const int64_t groups = rows * nv, n = rows * c;
   const oc::DropKey key = d.on ? oc::drop_key(d) : oc::DropKey{};
   for (int64_t i = (int64_t)blockIdx.x * TB + threadIdx.x; i < groups;
        i += (int64_t)gridDim.x * TB) {
-    const int64_t row = i / nv;
-    const int col = (int)(i - row * nv) * 8;
+    int64_t at = i * 8;
+    int cnt = 8;
+    if (!WHOLE) {
+      const int64_t row =
+          groups <= 0xffffffffll ? (int64_t)((uint32_t)i / (uint32_t)nv) : i / nv;
+      const int col = (int)(i - row * nv) * 8;
+      at = row * c + col;
+      cnt = c - col;
+    }
     float v[8];
-    oc::load8n(x, bf16, row * c + col, c - col, n, v);
+    if (WHOLE)
+      oc::load8(x, BF, at, v);
+    else
+      oc::load8n(x, BF, at, cnt, n, v);
     if (d.on) {
       bool k[8];
       oc::keep8(d, key, (uint64_t)i, k);
       oc::drop8(d, k, v);
     }
-    oc::store8n(y, bf16, row * c + col, c - col, v);
+    if (WHOLE)
+      oc::store8(y, BF, at, v);
+    else
+      oc::store8n(y, BF, at, cnt, v);
   }
 }
 
@@ -51,8 +66,14 @@ extern "C" oc_status oc_dropout_rng(oc_dtype dt, int64_t rows, int32_t c, const 
   OC_TRY(oc::check_spans(who, sp));
   if (!drop.on && x == y) return OC_OK;
   const int64_t groups = rows * cdiv(c, 8);
-  oc::launch_main(k_drop_rng, dim3((unsigned)std::min(cdiv(groups, TB), MOST_BLOCKS)), dim3(TB), s,
-                  drop, x, dt == OC_BF16, rows, (int)c, y);
+  const auto go = [&](auto kernel) {
+    oc::launch_main(kernel, dim3((unsigned)std::min(cdiv(groups, TB), MOST_BLOCKS)), dim3(TB), s,
+                    drop, x, rows, (int)c, y);
+  };
+  if (c % 8 == 0)
+    dt == OC_BF16 ? go(k_drop_rng<true, true>) : go(k_drop_rng<false, true>);
+  else
+    dt == OC_BF16 ? go(k_drop_rng<true, false>) : go(k_drop_rng<false, false>);
   OC_LAUNCH_CHECK();
   return OC_OK;
 }

@@ -33,21 +33,40 @@ __device__ __forceinline__ uint32_t id_of(const int32_t* ids, int64_t r, uint32_
   return (uint32_t)ids[r] & mask;
 }
 
+// A group of tpr lanes has ROWS rows, whose ids and then whose vectors are in flight
+// together; lanes step over the columns.
+template <bool BF, int ROWS>
 __global__ __launch_bounds__(TB) void k_embed(const int32_t* ids, uint32_t mask, int64_t rows,
-                                              int64_t num, int c, const void* table, bool bf16,
+                                              int64_t num, int c, const void* table, int tpr,
                                               float scale, void* y) {
-  const int nv = (c + 7) / 8;
-  const int64_t groups = rows * nv;
-  for (int64_t i = (int64_t)blockIdx.x * TB + threadIdx.x; i < groups;
-       i += (int64_t)gridDim.x * TB) {
-    const int64_t row = i / nv;
-    const int col = (int)(i - row * nv) * 8;
-    const uint32_t id = id_of(ids, row, mask);
-    float v[8] = {};
-    if (id < num) oc::load8n(table, bf16, (int64_t)id * c + col, c - col, num * c, v);
+  const int per = TB / tpr, tc = threadIdx.x % tpr;
+  const int64_t all = num * c, step = (int64_t)gridDim.x * per * ROWS;
+  for (int64_t r0 = (int64_t)blockIdx.x * per * ROWS + threadIdx.x / tpr; r0 < rows; r0 += step) {
+    uint32_t id[ROWS];
 #pragma unroll
-    for (int k = 0; k < 8; ++k) v[k] = id < num ? v[k] * scale : 0.f;
-    oc::store8n(y, bf16, row * c + col, c - col, v);
+    for (int j = 0; j < ROWS; ++j) {
+      const int64_t r = r0 + j * per;
+      id[j] = r < rows ? id_of(ids, r, mask) : ~0u;
+    }
+    for (int col = tc * 8; col < c; col += tpr * 8) {
+      const int cnt = c - col;
+      oc::Raw<BF> raw[ROWS];
+#pragma unroll
+      for (int j = 0; j < ROWS; ++j) {
+        const int64_t at = (int64_t)id[j] * c;
+        if (id[j] < num) oc::raw_load(raw[j], table, oc::Place{at, col, cnt, all - at});
+      }
+#pragma unroll
+      for (int j = 0; j < ROWS; ++j) {
+        const int64_t r = r0 + j * per;
+        if (r >= rows) break;
+        float v[8];
+        oc::unpack(raw[j], v);
+#pragma unroll
+        for (int k = 0; k < 8; ++k) v[k] = id[j] < num ? v[k] * scale : 0.f;
+        oc::row_store<BF>(y, oc::Place{r * c, col, cnt, 0}, v);
+      }
+    }
   }
 }
 
@@ -652,9 +671,18 @@ oc_status oc_embed_fwd(oc_dtype dt, int32_t flags, int64_t rows, int64_t num, in
                          {"ids", ids, (size_t)rows * 4, false, nullptr},
                          {"table", table, (size_t)num * c * e, false, nullptr}};
   OC_TRY(oc::check_spans(who, sp));
-  const int64_t groups = rows * cdiv(c, 8);
-  oc::launch_main(k_embed, dim3((unsigned)std::min(cdiv(groups, TB), MOST_BLOCKS)), dim3(TB), s,
-                  ids, id_mask(flags), rows, num, (int)c, table, dt == OC_BF16, scale, y);
+  int tpr = 1;
+  while (tpr < TB && tpr * 8 < c) tpr *= 2;
+  const auto go = [&](auto kernel, int each) {
+    oc::launch_main(kernel, dim3((unsigned)std::min(cdiv(rows, each * (TB / tpr)), MOST_BLOCKS)),
+                    dim3(TB), s, ids, id_mask(flags), rows, num, (int)c, table, tpr, scale, y);
+  };
+  // (several where there are workgroups enough)
+  const bool many = cdiv(rows, 4 * (TB / tpr)) >= 2048;
+  if (dt == OC_BF16)
+    many ? go(k_embed<true, 4>, 4) : go(k_embed<true, 1>, 1);
+  else
+    many ? go(k_embed<false, 2>, 2) : go(k_embed<false, 1>, 1);
   OC_LAUNCH_CHECK();
   return OC_OK;
 }
