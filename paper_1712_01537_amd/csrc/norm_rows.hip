@@ -51,6 +51,12 @@ __device__ __forceinline__ float lanes_sum(float v) {
 // Threads of a workgroup.
 constexpr int block_fwd(int tpr) { return tpr <= 64 ? 256 : tpr; }
 constexpr int block_bwd(int tpr) { return tpr <= 512 ? 512 : tpr; }
+// Waves that a SIMD holds of a forward kernel, by the registers it needs: the forward has
+// as many workgroups as the card holds at once (one more would be a round of its own:
+// bf16 rows of 64 to 256 channels 4.6 TB/s instead of 5.4).
+constexpr int waves_fwd(int tpr, int nv, bool step) {
+  return nv == 1 ? (step ? 6 : 8) : step || tpr >= 512 ? 4 : 5;
+}
 
 // The row's h from what lies in memory.
 template <bool BF, bool STEP>
@@ -85,7 +91,8 @@ __device__ __forceinline__ int group_of(int thread) {
 // and the squares of v - m by two more; waves are joined by Chan et al.'s formula for
 // counts, means and sums of squared deviations, relative to the first wave's mean.
 template <bool BF, int TPR, int NV, bool STEP>
-__global__ __launch_bounds__(block_fwd(TPR)) void k_ln_rows(Norm a) {
+__global__ __launch_bounds__(block_fwd(TPR), waves_fwd(TPR, NV, STEP)) void
+    k_ln_rows(Norm a) {
   constexpr int BLK = block_fwd(TPR), G = BLK / TPR, L = TPR < 64 ? TPR : 64, W = TPR / L;
   __shared__ float red[2][W > 1 ? W : 1][3];
   const int t = threadIdx.x % TPR, g = group_of<TPR>(threadIdx.x);
@@ -104,9 +111,7 @@ __global__ __launch_bounds__(block_fwd(TPR)) void k_ln_rows(Norm a) {
     if (a.gamma && cnt[j] > 0) oc::load8n(a.gamma, false, col, cnt[j], a.c, gam[j]);
     if (a.beta && cnt[j] > 0) oc::load8n(a.beta, false, col, cnt[j], a.c, bet[j]);
   }
-  const auto place = [&](int64_t row, int j) {
-    return Place{row * a.c, (j * TPR + t) * 8, cnt[j], n - row * a.c};
-  };
+  const auto place = [&](int64_t at, int j) { return Place{at, (j * TPR + t) * 8, cnt[j], n - at}; };
   // channels of a wave's part of a row
   const auto channels = [&](int w) {
     int have = 0;
@@ -120,17 +125,19 @@ __global__ __launch_bounds__(block_fwd(TPR)) void k_ln_rows(Norm a) {
   const int w0 = t / L;
   const float own = channels(w0), r_own = own > 0.f ? 1.f / own : 0.f, rc = 1.f / (float)a.c;
   Raw<BF> x[NV], res[NV];
-  const auto load = [&](int64_t row) {
+  const auto load = [&](int64_t at) {
 #pragma unroll
     for (int j = 0; j < NV; ++j)
       if (cnt[j] > 0) {
-        raw_load(x[j], a.x, place(row, j));
-        if (has_res) raw_load(res[j], a.res, place(row, j));
+        raw_load(x[j], a.x, place(at, j));
+        if (has_res) raw_load(res[j], a.res, place(at, j));
       }
   };
   int64_t row = (int64_t)blockIdx.x * G + g;
-  if (row < a.rows) load(row);
-  for (int par = 0; row < a.rows; row += stride, par ^= 1) {
+  int64_t at = row * a.c;
+  const int64_t on = stride * a.c;
+  if (row < a.rows) load(at);
+  for (int par = 0; row < a.rows; row += stride, at += on, par ^= 1) {
     float v[NV][8];
     bool keep[8];
 #pragma unroll
@@ -139,11 +146,11 @@ __global__ __launch_bounds__(block_fwd(TPR)) void k_ln_rows(Norm a) {
                        v[j], keep);
       cut(v[j], cnt[j]);
     }
-    if (row + stride < a.rows) load(row + stride);
+    if (row + stride < a.rows) load(at + on);
     if (STEP) {
 #pragma unroll
       for (int j = 0; j < NV; ++j)
-        if (cnt[j] > 0) row_store<BF>(a.h, place(row, j), v[j]);
+        if (cnt[j] > 0) row_store<BF>(a.h, place(at, j), v[j]);
     }
     float m = 0.f;
 #pragma unroll
@@ -197,7 +204,7 @@ __global__ __launch_bounds__(block_fwd(TPR)) void k_ln_rows(Norm a) {
 #pragma unroll
       for (int k = 0; k < 8; ++k)
         v[j][k] = fmaf((v[j][k] - delta) * invstd, gam[j][k], bet[j][k]);
-      row_store<BF>(a.y, place(row, j), v[j]);
+      row_store<BF>(a.y, place(at, j), v[j]);
     }
     if (t == 0) {
       if (a.mean) a.mean[row] = mean;
@@ -240,33 +247,33 @@ __global__ __launch_bounds__(block_bwd(TPR), NV == 1 ? 4 : 2) void k_ln_rows_bwd
   if (AHEAD)
 #pragma unroll
     for (int j = 0; j < NV; ++j) load_gamma(j, gam[j]);
-  const auto place = [&](int64_t row, int j) {
-    return Place{row * a.c, (j * TPR + t) * 8, cnt[j], n - row * a.c};
-  };
+  const auto place = [&](int64_t at, int j) { return Place{at, (j * TPR + t) * 8, cnt[j], n - at}; };
   // (of four fp32 vectors one is loaded at a time)
   constexpr int RAWS = AHEAD || BF ? NV : 1;
   Raw<BF> x[RAWS], res[RAWS], dy[RAWS], dh[AHEAD ? NV : 1];
   float mean = 0.f, invstd = 0.f;
-  const auto load_at = [&](int64_t row, int j, Raw<BF>& rx, Raw<BF>& rdy, Raw<BF>& rres) {
+  const auto load_at = [&](int64_t at, int j, Raw<BF>& rx, Raw<BF>& rdy, Raw<BF>& rres) {
     if (cnt[j] <= 0) return;
-    raw_load(rx, a.x, place(row, j));
-    raw_load(rdy, a.dy, place(row, j));
-    if (has_res) raw_load(rres, a.res, place(row, j));
+    raw_load(rx, a.x, place(at, j));
+    raw_load(rdy, a.dy, place(at, j));
+    if (has_res) raw_load(rres, a.res, place(at, j));
   };
-  const auto load = [&](int64_t row) {
+  const auto load = [&](int64_t row, int64_t at) {
     mean = a.mean[row];
     invstd = a.invstd[row];
     if (RAWS == NV)
 #pragma unroll
-      for (int j = 0; j < NV; ++j) load_at(row, j, x[j % RAWS], dy[j % RAWS], res[j % RAWS]);
+      for (int j = 0; j < NV; ++j) load_at(at, j, x[j % RAWS], dy[j % RAWS], res[j % RAWS]);
   };
   // (groups that share a workgroup's barriers make the same number of steps)
-  if (AHEAD && r0 + g < r1) load(r0 + g);
-  for (int64_t first = r0, par = 0; first < r1; first += G, par ^= 1) {
+  int64_t at = (r0 + g) * a.c;
+  const int64_t on = (int64_t)G * a.c;
+  if (AHEAD && r0 + g < r1) load(r0 + g, at);
+  for (int64_t first = r0, par = 0; first < r1; first += G, at += on, par ^= 1) {
     const int64_t row = first + g;
     const bool here = W == 1 || G == 1 || row < r1;
     if (W == 1 && row >= r1) break;
-    if (!AHEAD && here) load(row);
+    if (!AHEAD && here) load(row, at);
     float d[NV][8], e[NV][8];
     bool keep[AHEAD ? NV : 1][8];
     uint32_t kept = 0;  // (bits for bools, of which each takes two scalar registers)
@@ -276,7 +283,7 @@ __global__ __launch_bounds__(block_bwd(TPR), NV == 1 ? 4 : 2) void k_ln_rows_bwd
     for (int j = 0; j < NV; ++j) {
       const int i = AHEAD ? j : 0;
       const int l = j % RAWS;
-      if (RAWS < NV && here) load_at(row, j, x[l], dy[l], res[l]);
+      if (RAWS < NV && here) load_at(at, j, x[l], dy[l], res[l]);
       form_h<BF, STEP>(x[l], res[l], has_res, a.drop, key, (uint64_t)row * nv + (j * TPR + t),
                        d[j], keep[i]);
       unpack(dy[l], e[j]);
@@ -304,8 +311,8 @@ __global__ __launch_bounds__(block_bwd(TPR), NV == 1 ? 4 : 2) void k_ln_rows_bwd
     if (AHEAD) {
 #pragma unroll
       for (int j = 0; j < NV; ++j)
-        if (has_dh && here && cnt[j] > 0) raw_load(dh[AHEAD ? j : 0], a.dh, place(row, j));
-      if (row + G < r1) load(row + G);
+        if (has_dh && here && cnt[j] > 0) raw_load(dh[AHEAD ? j : 0], a.dh, place(at, j));
+      if (row + G < r1) load(row + G, at + on);
     }
 #pragma unroll
     for (int k = 0; k < 3; ++k) s[k] = lanes_sum<L>(s[k]);
@@ -328,7 +335,7 @@ __global__ __launch_bounds__(block_bwd(TPR), NV == 1 ? 4 : 2) void k_ln_rows_bwd
       const int i = AHEAD ? j : 0;
       float u[8] = {};
       if (!AHEAD) {
-        if (has_dh && here && cnt[j] > 0) raw_load(dh[i], a.dh, place(row, j));
+        if (has_dh && here && cnt[j] > 0) raw_load(dh[i], a.dh, place(at, j));
         load_gamma(j, gam[i]);
       }
       if (has_dh && here && cnt[j] > 0) unpack(dh[i], u);
@@ -341,7 +348,7 @@ __global__ __launch_bounds__(block_bwd(TPR), NV == 1 ? 4 : 2) void k_ln_rows_bwd
         if (has_dh) e[j][k] += u[k];
       }
       if (!here || cnt[j] <= 0) continue;
-      if (a.dres) row_store<BF>(a.dres, place(row, j), e[j]);
+      if (a.dres) row_store<BF>(a.dres, place(at, j), e[j]);
       if (STEP && a.dx) {
         if (a.drop.on) {
           if (!AHEAD)
@@ -349,7 +356,7 @@ __global__ __launch_bounds__(block_bwd(TPR), NV == 1 ? 4 : 2) void k_ln_rows_bwd
             for (int k = 0; k < 8; ++k) keep[i][k] = kept >> (j * 8 + k) & 1;
           oc::drop8(a.drop, keep[i], e[j]);
         }
-        row_store<BF>(a.dx, place(row, j), e[j]);
+        row_store<BF>(a.dx, place(at, j), e[j]);
       }
       if (RAWS < NV) asm volatile("" ::: "memory");
     }
@@ -443,14 +450,17 @@ namespace oc {
 void norm_rows_fwd(const Norm& a, hipStream_t s) {
   with_fwd(a.c, [&](auto t, auto v) {
     constexpr int TPR = decltype(t)::value, NV = decltype(v)::value, BLK = block_fwd(TPR);
-    const int64_t blocks = std::min<int64_t>(cdiv(a.rows, BLK / TPR), 2048 * 256 / BLK);
-    const auto go = [&](auto kernel) {
-      launch_main(kernel, dim3((unsigned)blocks), dim3(BLK), s, a);
+    const auto go = [&](auto kernel, int waves) {
+      const int64_t most = waves * 256 / BLK * (int64_t)cu_count();
+      launch_main(kernel, dim3((unsigned)std::min(cdiv(a.rows, BLK / TPR), most)), dim3(BLK), s,
+                  a);
     };
+    constexpr int PLAIN = waves_fwd(TPR, NV, false), STEP = waves_fwd(TPR, NV, true);
     if (a.h)
-      a.bf16 ? go(k_ln_rows<true, TPR, NV, true>) : go(k_ln_rows<false, TPR, NV, true>);
+      a.bf16 ? go(k_ln_rows<true, TPR, NV, true>, STEP) : go(k_ln_rows<false, TPR, NV, true>, STEP);
     else
-      a.bf16 ? go(k_ln_rows<true, TPR, NV, false>) : go(k_ln_rows<false, TPR, NV, false>);
+      a.bf16 ? go(k_ln_rows<true, TPR, NV, false>, PLAIN)
+             : go(k_ln_rows<false, TPR, NV, false>, PLAIN);
   });
 }
 
