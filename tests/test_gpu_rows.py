@@ -476,6 +476,92 @@ def test_states_and_sizes_that_do_not_fit_are_refused():
             call()
 
 
+@DT
+@pytest.mark.parametrize("rows,num,c,kind", [
+    (4096, 300, 24, "skewed"), (4097, 300, 24, "skewed"), (131_073, 513, 16, "even"),
+    (1_048_577, 70_000, 3, "outside"), (1_048_576, 2, 9, "even"), (300_000, 1 << 20, 5, "even"),
+    (600_000, 5, 520, "skewed"), (35_000_000, 3, 1, "even"), (65_536, 1 << 18, 2, "skewed")])
+def test_embed_sizes_of_every_plan(rows, num, c, kind, dt):
+    """Around the sort's limits and in pieces longer than fp32 sums go; against torch's
+    float64 sums on the GPU."""
+    d = torch.as_tensor(ids_of(rows, num, kind, 3)).cuda()
+    dy = make((rows, c), dt, 4)
+    got = oc.oc_embed_bwd(d, dy, num)
+    there = (d >= 0) & (d < num)
+    at, g = d[there].long(), dy[there].double()
+
+    def sums(t):
+        if num <= 8:
+            return torch.stack([t[at == v].sum(0) for v in range(num)])
+        return torch.zeros((num, c), dtype=torch.float64, device="cuda").index_add_(0, at, t)
+
+    want, mags = sums(g), sums(g.abs())
+    err = (got.double() - want).abs() - 68 * U * mags
+    assert float(err.max()) <= 0, float(err.max())
+    assert torch.equal(oc.oc_embed_bwd(d, dy, num), got)
+
+
+@DT
+def test_no_rows(dt):
+    for c in (1, 64, 1000, 5000, 9000, 20000):
+        x = torch.empty((0, c), device="cuda", dtype=dt)
+        y, mean, invstd = oc.oc_ln_fwd(x, need_stats=True)
+        assert y.shape == (0, c) and mean.shape == (0,)
+        dx, dg, db = oc.oc_ln_bwd(x, x, None, mean, invstd)
+        assert dx.shape == (0, c) and not dg.any() and not db.any()
+        rng = rng_of(1, 2)
+        h, y, mean, invstd = oc.oc_drop_ln_fwd(x, x.clone(), 0.5, rng, need_stats=True)
+        got = oc.oc_drop_ln_bwd(x, x.clone(), x, 0.5, rng, None, mean, invstd)
+        assert not got[2].any() and not got[3].any()
+        assert oc.oc_dropout_rng(x, 0.5, rng).shape == (0, c)
+        assert oc.oc_embed_fwd(torch.empty(0, dtype=torch.int32, device="cuda"),
+                               torch.ones((4, c), device="cuda", dtype=dt)).shape == (0, c)
+
+
+@DT
+@pytest.mark.parametrize("rows,c", [(33, 8), (70, 127), (40, 1024), (9, 5001), (3, 17000)])
+def test_in_place(rows, c, dt):
+    """Where the header lets an output be an input, the bits are the separate call's."""
+    L, code, st = oc.load(), 1 if dt == BF16 else 0, torch.cuda.current_stream().cuda_stream
+    x, res, rng = make((rows, c), dt, 1), make((rows, c), dt, 2), rng_of(3, 4)
+    P = lambda t: t.data_ptr()  # noqa: E731
+    y, _, _ = oc.oc_ln_fwd(x)
+    a = x.clone()
+    assert L.oc_ln_fwd(code, rows, c, P(a), None, None, 1e-5, P(a), None, None, st) == 0
+    assert torch.equal(a, y)
+    h, y, _, _ = oc.oc_drop_ln_fwd(x, res, 0.4, rng)
+    a, b = x.clone(), res.clone()
+    assert L.oc_drop_ln_fwd(code, rows, c, P(a), P(b), 0.4, P(rng), 0, None, None, 1e-5, P(b),
+                            P(a), None, None, st) == 0
+    assert torch.equal(b, h) and torch.equal(a, y)
+
+
+def test_two_streams_at_once():
+    """Calls in flight together share nothing: each has the bits of the call alone."""
+    torch.manual_seed(0)
+    xs = [make((20_000, 512), BF16, i) for i in range(2)]
+    ids = [torch.as_tensor(ids_of(20_000, 700, "skewed", i)).cuda() for i in range(2)]
+    rngs = [rng_of(i, i) for i in range(2)]
+
+    def run(i):
+        h, y, m, r = oc.oc_drop_ln_fwd(xs[i], None, 0.3, rngs[i], need_stats=True)
+        return [h, y, *oc.oc_drop_ln_bwd(xs[i], None, y, 0.3, rngs[i], None, m, r),
+                oc.oc_embed_bwd(ids[i], xs[i], 700), oc.oc_dropout_rng(y, 0.3, rngs[i], site=1)]
+
+    want = [run(i) for i in range(2)]
+    torch.cuda.synchronize()
+    streams = [torch.cuda.Stream() for _ in range(2)]
+    got = [[], []]
+    for _ in range(5):
+        for i in range(2):
+            with torch.cuda.stream(streams[i]):
+                got[i].append(run(i))
+    torch.cuda.synchronize()
+    for i in range(2):
+        for g in got[i]:
+            assert all(torch.equal(a, b) for a, b in zip(g, want[i]))
+
+
 class Block:
     """What a user builds of them: places from a table, a residual step, a gated layer, a
     residual step and a head, with the loss, clipping and the update."""
