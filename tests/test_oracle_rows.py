@@ -209,7 +209,9 @@ def test_workspaces_grow_with_their_sizes():
     assert L.oc_ln_bwd_workspace(-1, 8) == 0 and L.oc_ln_bwd_workspace(8, 0) == 0
     assert L.oc_embed_bwd_workspace(64, 8, 8) == 0  # few rows need none
     assert L.oc_embed_bwd_workspace(65, 8, 8) > 0
-    assert L.oc_embed_bwd_workspace(1000, 1 << 20, 64) > L.oc_embed_bwd_workspace(1000, 4, 64)
+    # several digits need a second list; up to 4096 rows none is kept outside LDS
+    assert L.oc_embed_bwd_workspace(10000, 1 << 20, 64) > L.oc_embed_bwd_workspace(10000, 4, 64)
+    assert L.oc_embed_bwd_workspace(1000, 1 << 20, 64) == L.oc_embed_bwd_workspace(1000, 4, 64)
 
 
 def test_binding_refuses_what_is_no_device_tensor():
