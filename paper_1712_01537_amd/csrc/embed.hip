@@ -495,11 +495,11 @@ __global__ __launch_bounds__(TB) void k_embed_sums(Sums a, int tpr, int slabs) {
   }
 }
 
-// The runs that go on over a chunk's end.  Each wave looks at the end of one chunk.  Where
-// a run begins in it and ends in the next, as most do, the wave adds the two partial sums;
-// the others it leaves to the workgroup, which adds them in double and in a fixed order,
-// rl lanes a column.
-constexpr int JB = 512, JW = JB / 64;
+// The runs that go on over a chunk's end, whose partial sums are added in double and in a
+// fixed order.  Each wave looks at the end of one chunk.  Where a run begins in it and goes
+// on in at most WAVE_MORE chunks, as nearly all do, the wave adds it; the others it leaves
+// to the workgroup, which has rl lanes a column.
+constexpr int JB = 512, JW = JB / 64, WAVE_MORE = 8;
 __global__ __launch_bounds__(JB, 4) void k_embed_join(Sums a, int tpr) {
   __shared__ double red[8][JB];
   __shared__ bool longer[JW];
@@ -516,27 +516,33 @@ __global__ __launch_bounds__(JB, 4) void k_embed_join(Sums a, int tpr) {
   };
   {
     const int64_t chunk = (int64_t)blockIdx.x * JW + w, i0 = chunk * a.chunk, i1 = i0 + a.chunk;
-    bool more = false;
+    bool left = false;
     if (i1 < n) {
       const uint32_t id = a.sorted[i1].id, was = a.sorted[i1 - 1].id, from = a.sorted[i0].id;
       const uint32_t before = i0 > 0 ? a.sorted[i0 - 1].id : ~0u;  // (no id)
-      const int64_t i2 = i1 + a.chunk;
-      const uint32_t then = i2 < n ? a.sorted[i2].id : ~0u;
+      const int64_t at = i1 + (int64_t)lane * a.chunk;
+      const uint64_t on = __ballot(at < n && a.sorted[at].id == id);
       if (was == id && !(from == id && before == id)) {
-        more = then == id;
-        for (int col = (blockIdx.y * tpr + lane) * 8; !more && lane < tpr && col < a.c;
+        const int more = on == ~0ull ? 64 : __builtin_ctzll(~on);  // chunks it goes on in
+        left = more > WAVE_MORE;
+        for (int col = (blockIdx.y * tpr + lane) * 8; !left && lane < tpr && col < a.c;
              col += gridDim.y * tpr * 8) {
-          float v[8], u[8];
+          float v[8];
           double s[8];
           load(chunk, 1, col, v);
-          load(chunk + 1, 0, col, u);
 #pragma unroll
-          for (int k = 0; k < 8; ++k) s[k] = (double)v[k] + (double)u[k];
+          for (int k = 0; k < 8; ++k) s[k] = (double)v[k];
+#pragma unroll 4
+          for (int j = 1; j <= more; ++j) {
+            load(chunk + j, 0, col, v);
+#pragma unroll
+            for (int k = 0; k < 8; ++k) s[k] += (double)v[k];
+          }
           finish(id, col, s);
         }
       }
     }
-    if (lane == 0) longer[w] = more;
+    if (lane == 0) longer[w] = left;
   }
   __syncthreads();
   const int tc = threadIdx.x % tpr, tr = threadIdx.x / tpr, rl = JB / tpr;
