@@ -14,9 +14,14 @@
 // scatter adds those numbers up itself (all values below its own, and its own in the tiles
 // before), so that a digit takes two launches.  (Counting the next digit by atomics where
 // the scatter puts the rows saves a launch of 3 to 5 us and costs 6 us for 65536 rows and
-// 14 for 260000.)  A wave takes its rows 64 at a time, in
-// order: the place of a row among those of its digit is a count of the lanes before it
-// with the same digit.  Up to SMALL rows are sorted by one workgroup in LDS.
+// 14 for 260000.)  A wave takes its rows 64 at a time, in order: the place of a row among
+// those of its digit is a count of the lanes before it with the same digit.  Up to SMALL
+// rows are sorted by one workgroup in LDS (4000 rows, two digits: 9.3 us; the four
+// launches take 17).
+//
+// The lookup and the sums are bound by memory, the sort by its chain of launches.  65536
+// rows of 1024 bf16 channels, a table of 32768 rows, skewed ids: lookup 39 us (4.5 TB/s of
+// what is read and written), sort 22, sums with the zeros 55 (3.7 TB/s), joins 7.
 #include <algorithm>
 
 #include "rows.h"

@@ -47,7 +47,8 @@ __device__ __forceinline__ void block_sums(float (&v)[K], float (*red)[K]) {
 }
 
 // --- rows of any length ----------------------------------------------------------
-// One workgroup a row, which it reads once a pass.
+// One workgroup a row, which it reads once a pass (from the caches but for the first): for
+// rows that fit no workgroup's registers.
 
 // The values 8 i .. 8 i + 7 of a row's h; keep: which of them dropout has kept.
 template <typename Args>
@@ -74,47 +75,47 @@ __global__ __launch_bounds__(TB) void k_ln_fwd_any(Norm a) {
   const oc::DropKey key = a.drop.on ? oc::drop_key(a.drop) : oc::DropKey{};
   const float rc = 1.f / (float)a.c;
   for (int64_t row = blockIdx.x; row < a.rows; row += gridDim.x) {
-  float v[8];
-  bool keep[8];
-  float m[1] = {0.f};
-  for (int i = threadIdx.x; i < nv; i += TB) {
-    load_h(a, key, row, i, v, keep);
+    float v[8];
+    bool keep[8];
+    float m[1] = {0.f};
+    for (int i = threadIdx.x; i < nv; i += TB) {
+      load_h(a, key, row, i, v, keep);
 #pragma unroll
-    for (int k = 0; k < 8; ++k) m[0] = fmaf(v[k], rc, m[0]);
-  }
-  block_sums(m, red0);
-  float s[2] = {0.f, 0.f};
-  for (int i = threadIdx.x; i < nv; i += TB) {
-    load_h(a, key, row, i, v, keep);
-#pragma unroll
-    for (int k = 0; k < 8; ++k) {
-      const float d = i * 8 + k < a.c ? v[k] - m[0] : 0.f;
-      s[0] += d;
-      s[1] = fmaf(d, d, s[1]);
+      for (int k = 0; k < 8; ++k) m[0] = fmaf(v[k], rc, m[0]);
     }
-  }
-  block_sums(s, red1);
-  const float delta = s[0] * rc;
-  float var = fmaf(-delta, delta, s[1] * rc);
-  if (var < 0.f) var = 0.f;  // (NaN stays NaN)
-  const float invstd = 1.f / sqrtf(var + a.eps);
-  for (int i = threadIdx.x; i < nv; i += TB) {
-    load_h(a, key, row, i, v, keep);
-    const int c = i * 8, cnt = a.c - c;
-    const int64_t at = row * a.c + c;
-    if (a.h) oc::store8n(a.h, a.bf16, at, cnt, v);
+    block_sums(m, red0);
+    float s[2] = {0.f, 0.f};
+    for (int i = threadIdx.x; i < nv; i += TB) {
+      load_h(a, key, row, i, v, keep);
 #pragma unroll
-    for (int k = 0; k < 8; ++k) {
-      const float z = ((v[k] - m[0]) - delta) * invstd;
-      const bool in = c + k < a.c;
-      v[k] = fmaf(z, a.gamma && in ? a.gamma[c + k] : 1.f, a.beta && in ? a.beta[c + k] : 0.f);
+      for (int k = 0; k < 8; ++k) {
+        const float d = i * 8 + k < a.c ? v[k] - m[0] : 0.f;
+        s[0] += d;
+        s[1] = fmaf(d, d, s[1]);
+      }
     }
-    oc::store8n(a.y, a.bf16, at, cnt, v);
-  }
-  if (threadIdx.x == 0) {
-    if (a.mean) a.mean[row] = m[0] + delta;
-    if (a.invstd) a.invstd[row] = invstd;
-  }
+    block_sums(s, red1);
+    const float delta = s[0] * rc;
+    float var = fmaf(-delta, delta, s[1] * rc);
+    if (var < 0.f) var = 0.f;  // (NaN stays NaN)
+    const float invstd = 1.f / sqrtf(var + a.eps);
+    for (int i = threadIdx.x; i < nv; i += TB) {
+      load_h(a, key, row, i, v, keep);
+      const int c = i * 8, cnt = a.c - c;
+      const int64_t at = row * a.c + c;
+      if (a.h) oc::store8n(a.h, a.bf16, at, cnt, v);
+#pragma unroll
+      for (int k = 0; k < 8; ++k) {
+        const float z = ((v[k] - m[0]) - delta) * invstd;
+        const bool in = c + k < a.c;
+        v[k] = fmaf(z, a.gamma && in ? a.gamma[c + k] : 1.f, a.beta && in ? a.beta[c + k] : 0.f);
+      }
+      oc::store8n(a.y, a.bf16, at, cnt, v);
+    }
+    if (threadIdx.x == 0) {
+      if (a.mean) a.mean[row] = m[0] + delta;
+      if (a.invstd) a.invstd[row] = invstd;
+    }
   }
 }
 
@@ -124,51 +125,51 @@ __global__ __launch_bounds__(TB) void k_ln_bwd_any(NormBwd a) {
   const int nv = (a.c + 7) / 8;
   const oc::DropKey key = a.drop.on ? oc::drop_key(a.drop) : oc::DropKey{};
   for (int64_t row = blockIdx.x; row < a.rows; row += gridDim.x) {
-  __syncthreads();  // the sums of the row before have been read
-  const float m = a.mean[row], r = a.invstd[row], rc = 1.f / (float)a.c;
-  float d[8], g[8];
-  bool keep[8];
-  const auto load = [&](int i) {
-    const int c = i * 8, cnt = a.c - c;
-    load_h(a, key, row, i, d, keep);
-    oc::load8n(a.dy, a.bf16, row * a.c + c, cnt, n, g);
+    __syncthreads();  // the sums of the row before have been read
+    const float m = a.mean[row], r = a.invstd[row], rc = 1.f / (float)a.c;
+    float d[8], g[8];
+    bool keep[8];
+    const auto load = [&](int i) {
+      const int c = i * 8, cnt = a.c - c;
+      load_h(a, key, row, i, d, keep);
+      oc::load8n(a.dy, a.bf16, row * a.c + c, cnt, n, g);
 #pragma unroll
-    for (int k = 0; k < 8; ++k) {
-      d[k] = k < cnt ? d[k] - m : 0.f;
-      if (a.gamma && k < cnt) g[k] *= a.gamma[c + k];
-    }
-  };
-  float s[3] = {0.f, 0.f, 0.f};
-  for (int i = threadIdx.x; i < nv; i += TB) {
-    load(i);
+      for (int k = 0; k < 8; ++k) {
+        d[k] = k < cnt ? d[k] - m : 0.f;
+        if (a.gamma && k < cnt) g[k] *= a.gamma[c + k];
+      }
+    };
+    float s[3] = {0.f, 0.f, 0.f};
+    for (int i = threadIdx.x; i < nv; i += TB) {
+      load(i);
 #pragma unroll
-    for (int k = 0; k < 8; ++k) {
-      s[0] += g[k];
-      s[1] = fmaf(g[k], d[k], s[1]);
-      s[2] += d[k];
+      for (int k = 0; k < 8; ++k) {
+        s[0] += g[k];
+        s[1] = fmaf(g[k], d[k], s[1]);
+        s[2] += d[k];
+      }
     }
-  }
-  block_sums(s, red);
-  const float delta = s[2] * rc, gm = s[0] * rc, zm = (s[1] - delta * s[0]) * rc * r;
-  if (threadIdx.x == 0 && a.delta) a.delta[row] = delta;
-  if (!a.dx && !a.dres) continue;
-  for (int i = threadIdx.x; i < nv; i += TB) {
-    load(i);
-    const int c = i * 8, cnt = a.c - c;
-    const int64_t at = row * a.c + c;
+    block_sums(s, red);
+    const float delta = s[2] * rc, gm = s[0] * rc, zm = (s[1] - delta * s[0]) * rc * r;
+    if (threadIdx.x == 0 && a.delta) a.delta[row] = delta;
+    if (!a.dx && !a.dres) continue;
+    for (int i = threadIdx.x; i < nv; i += TB) {
+      load(i);
+      const int c = i * 8, cnt = a.c - c;
+      const int64_t at = row * a.c + c;
 #pragma unroll
-    for (int k = 0; k < 8; ++k) g[k] = r * (g[k] - gm - (d[k] - delta) * r * zm);
-    if (a.dh) {
-      oc::load8n(a.dh, a.bf16, at, cnt, n, d);
+      for (int k = 0; k < 8; ++k) g[k] = r * (g[k] - gm - (d[k] - delta) * r * zm);
+      if (a.dh) {
+        oc::load8n(a.dh, a.bf16, at, cnt, n, d);
 #pragma unroll
-      for (int k = 0; k < 8; ++k) g[k] += d[k];
+        for (int k = 0; k < 8; ++k) g[k] += d[k];
+      }
+      if (a.dres) oc::store8n(a.dres, a.bf16, at, cnt, g);
+      if (a.dx) {
+        if (a.drop.on) oc::drop8(a.drop, keep, g);
+        oc::store8n(a.dx, a.bf16, at, cnt, g);
+      }
     }
-    if (a.dres) oc::store8n(a.dres, a.bf16, at, cnt, g);
-    if (a.dx) {
-      if (a.drop.on) oc::drop8(a.drop, keep, g);
-      oc::store8n(a.dx, a.bf16, at, cnt, g);
-    }
-  }
   }
 }
 
@@ -369,8 +370,8 @@ oc_status oc_ln_bwd(oc_dtype dt, int64_t rows, int32_t c, const void* x, const v
                          {"invstd", invstd, nr, false, nullptr}};
   OC_TRY(oc::check_spans(who, sp));
   if ((rows == 0 || !dx) && !dgamma && !dbeta) return OC_OK;
-  bwd(NormBwd{x, nullptr, dy, nullptr, nullptr, dx, gamma, mean, invstd, nullptr, rows, c, dt == OC_BF16,
-              Drop{}},
+  bwd(NormBwd{x, nullptr, dy, nullptr, nullptr, dx, gamma, mean, invstd, nullptr, rows, c,
+              dt == OC_BF16, Drop{}},
       dgamma, dbeta, ws, s);
   OC_LAUNCH_CHECK();
   return OC_OK;

@@ -1,5 +1,13 @@
 // Layer norm and the residual step on rows that fit in registers: TPR threads hold a row,
-// NV vectors of eight channels each, so that each row is read once.
+// NV vectors of eight channels each, so that each row is read once.  The next row's loads
+// are started before the present one's sums.
+//
+// Bound by memory: each value is read and written once (WRITE_SIZE of the forward of
+// 65536 x 4096 bf16 is 517 MB, of its backward 544 with the column sums).  That forward
+// takes 203 us (5.3 TB/s), its backward 326 (4.9); the residual step of 16384 x 8192 fp32
+// 410 and 642 (5.2 and 5.0); a large copy reaches 4.7.  Rows of 513 to 768 bf16 channels
+// leave a quarter of the backward's lanes without work and reach 3.8; rows of 8193 to 16384
+// keep no next row and reach 2.6 to 4.4.
 #include <algorithm>
 
 #include "norm.h"
@@ -111,7 +119,9 @@ __global__ __launch_bounds__(block_fwd(TPR), waves_fwd(TPR, NV, STEP)) void
     if (a.gamma && cnt[j] > 0) oc::load8n(a.gamma, false, col, cnt[j], a.c, gam[j]);
     if (a.beta && cnt[j] > 0) oc::load8n(a.beta, false, col, cnt[j], a.c, bet[j]);
   }
-  const auto place = [&](int64_t at, int j) { return Place{at, (j * TPR + t) * 8, cnt[j], n - at}; };
+  const auto place = [&](int64_t at, int j) {
+    return Place{at, (j * TPR + t) * 8, cnt[j], n - at};
+  };
   // channels of a wave's part of a row
   const auto channels = [&](int w) {
     int have = 0;
@@ -160,8 +170,7 @@ __global__ __launch_bounds__(block_fwd(TPR), waves_fwd(TPR, NV, STEP)) void
     m = lanes_sum<L>(m);
     float s1 = 0.f, s2 = 0.f;
 #pragma unroll
-    for (int j = 0; j < NV; ++j)
-    {
+    for (int j = 0; j < NV; ++j) {
 #pragma unroll
       for (int k = 0; k < 8; ++k) v[j][k] -= m;
       cut(v[j], cnt[j]);
@@ -213,11 +222,15 @@ __global__ __launch_bounds__(block_fwd(TPR), waves_fwd(TPR, NV, STEP)) void
   }
 }
 
-// Backward: one reduction of three sums a row.  dgamma's and dbeta's sums stay in
+// Backward: one reduction of three sums a row, of a thread's one vector up to 4096
+// channels (two vectors: 16 waves of 128 registers spill), two up to 8192 (512 threads of
+// up to 256 registers: fp32 residual step 631 us for 16384 x 8192, with 1024 threads of
+// one vector 850), four above.  dgamma's and dbeta's sums stay in
 // registers over the group's rows, at most MOST_ADDED; the workgroup's groups are then
 // added in double through LDS, and its sums written for the sum over the workgroups.
 template <bool BF, int TPR, int NV, bool STEP>
-__global__ __launch_bounds__(block_bwd(TPR), NV == 1 ? 4 : 2) void k_ln_rows_bwd(NormBwd a, float* part) {
+__global__ __launch_bounds__(block_bwd(TPR), NV == 1 ? 4 : 2) void
+    k_ln_rows_bwd(NormBwd a, float* part) {
   constexpr int BLK = block_bwd(TPR), G = BLK / TPR, L = TPR < 64 ? TPR : 64, W = TPR / L;
   __shared__ float red[2][W > 1 ? BLK / 64 : 1][3];
   __shared__ float cols[G > 1 ? 2 : 1][G > 1 ? 8 : 1][G > 1 ? BLK : 1];
@@ -229,7 +242,7 @@ __global__ __launch_bounds__(block_bwd(TPR), NV == 1 ? 4 : 2) void k_ln_rows_bwd
   const bool has_res = STEP && a.res, has_dh = STEP && a.dh;
   const float rc = 1.f / (float)a.c;
   int cnt[NV];
-  // Two vectors a thread leave no registers for the next row's loads and gamma.
+  // Four vectors a thread leave no registers for the next row's loads and gamma.
   constexpr bool AHEAD = NV <= 2;
   float gam[NV <= 2 ? NV : 1][8], sg[NV][8], sb[NV][8];
 #pragma unroll
@@ -247,7 +260,9 @@ __global__ __launch_bounds__(block_bwd(TPR), NV == 1 ? 4 : 2) void k_ln_rows_bwd
   if (AHEAD)
 #pragma unroll
     for (int j = 0; j < NV; ++j) load_gamma(j, gam[j]);
-  const auto place = [&](int64_t at, int j) { return Place{at, (j * TPR + t) * 8, cnt[j], n - at}; };
+  const auto place = [&](int64_t at, int j) {
+    return Place{at, (j * TPR + t) * 8, cnt[j], n - at};
+  };
   // (of four fp32 vectors one is loaded at a time)
   constexpr int RAWS = AHEAD || BF ? NV : 1;
   Raw<BF> x[RAWS], res[RAWS], dy[RAWS], dh[AHEAD ? NV : 1];

@@ -46,9 +46,9 @@ __device__ __forceinline__ DropKey drop_key(const Drop& d) {
 }
 // Which of the eight values of group `index` are kept.  One call of the generator gives
 // the high halves of eight numbers, which decide all but one value in 65536; the low
-// halves, from a second call, are formed only where a high half equals T's.  (With a
-// number of 32 bits from the first call for each value the generator alone would take
-// longer than bf16 values take to read and write.)
+// halves, from a second call, are formed only where a high half equals T's (16384 x 4096
+// bf16 values in the last-level cache 39.0 us, with both calls always 42.2; from memory
+// 208 either way).
 __device__ __forceinline__ void keep8(const Drop& d, const DropKey& key, uint64_t index,
                                       bool (&k)[8]) {
   const uint32_t c1 = (uint32_t)(index >> 32) | d.site << 16;

@@ -368,6 +368,11 @@ def test_embed_of_an_octrees_places(dt):
     table, dy = make((4096, 48), dt, 1), make((len(place), 48), dt, 2)
     want = R.embed_fwd(place, _np(table))
     near(oc.oc_embed_fwd(keys, table, keys=True), want, v_of(dt) * np.abs(want), "y")
+    # shapes from 128 on make the key's sign bit
+    far = (keys.long() + (200 << 24)).to(torch.int32)
+    assert int(far.min()) < 0
+    assert torch.equal(oc.oc_embed_fwd(far, table, keys=True),
+                       oc.oc_embed_fwd(keys, table, keys=True))
     w, m = R.embed_bwd(place, _np(dy), 4096), R.embed_bwd(place, np.abs(_np(dy)), 4096)
     near(oc.oc_embed_bwd(keys, dy, 4096, keys=True), w, 68 * U * m, "dtable")
 
