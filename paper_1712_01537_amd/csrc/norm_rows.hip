@@ -2,12 +2,11 @@
 // NV vectors of eight channels each, so that each row is read once.  The next row's loads
 // are started before the present one's sums.
 //
-// Bound by memory: each value is read and written once (WRITE_SIZE of the forward of
-// 65536 x 4096 bf16 is 517 MB, of its backward 544 with the column sums).  That forward
-// takes 203 us (5.3 TB/s), its backward 326 (4.9); the residual step of 16384 x 8192 fp32
-// 410 and 642 (5.2 and 5.0); a large copy reaches 4.7.  Rows of 513 to 768 bf16 channels
-// leave a quarter of the backward's lanes without work and reach 3.8; rows of 8193 to 16384
-// keep no next row and reach 2.6 to 4.4.
+// Bound by memory: each value is read and written once (the forward of 65536 x 4096 bf16
+// writes 517 MiB, its backward 544 with the column sums).  That forward takes 203 us (5.3
+// TB/s), its backward 326 (4.9); the residual step of 16384 x 8192 fp32 410 and 642 (5.2 and
+// 5.0); a large copy reaches 4.7.  Rows of 8193 to 16384 keep no next row in the backward
+// and reach 2.6 to 4.4.
 #include <algorithm>
 
 #include "norm.h"
@@ -225,7 +224,9 @@ __global__ __launch_bounds__(block_fwd(TPR), waves_fwd(TPR, NV, STEP)) void
 // Backward: one reduction of three sums a row, of a thread's one vector up to 4096
 // channels (two vectors: 16 waves of 128 registers spill), two up to 8192 (512 threads of
 // up to 256 registers: fp32 residual step 631 us for 16384 x 8192, with 1024 threads of
-// one vector 850), four above.  dgamma's and dbeta's sums stay in
+// one vector 850), four above; bf16 rows that leave a
+// quarter of the lanes of one vector without work have three (2^27 values in rows of 768:
+// 174 us instead of 215, of 1536 177 instead of 202).  dgamma's and dbeta's sums stay in
 // registers over the group's rows, at most MOST_ADDED; the workgroup's groups are then
 // added in double through LDS, and its sums written for the sum over the workgroups.
 template <bool BF, int TPR, int NV, bool STEP>
@@ -243,8 +244,8 @@ __global__ __launch_bounds__(block_bwd(TPR), NV == 1 ? 4 : 2) void
   const float rc = 1.f / (float)a.c;
   int cnt[NV];
   // Four vectors a thread leave no registers for the next row's loads and gamma.
-  constexpr bool AHEAD = NV <= 2;
-  float gam[NV <= 2 ? NV : 1][8], sg[NV][8], sb[NV][8];
+  constexpr bool AHEAD = NV <= 3;
+  float gam[AHEAD ? NV : 1][8], sg[NV][8], sb[NV][8];
 #pragma unroll
   for (int j = 0; j < NV; ++j) {
     cnt[j] = a.c - (j * TPR + t) * 8;
@@ -446,8 +447,11 @@ void with_fwd(int c, F&& f) {
   }
 }
 template <typename F>
-void with_bwd(int c, F&& f) {
+void with_bwd(int c, bool three, F&& f) {
   const int t = threads_bwd(c);
+  if (three)
+    return t == 128 ? f(Int<32>{}, Int<3>{})
+           : t == 256 ? f(Int<64>{}, Int<3>{}) : f(Int<128>{}, Int<3>{});
   if (c <= 512) return with_small(t, f);
   if (c > 8192) return f(Int<512>{}, Int<4>{});
   if (c > 4096) return f(Int<512>{}, Int<2>{});
@@ -486,16 +490,20 @@ int64_t norm_rows_blocks(int64_t rows, int32_t c) {
 
 void norm_rows_bwd(const NormBwd& a, float* part, hipStream_t s) {
   const int64_t blocks = norm_rows_blocks(a.rows, a.c);
-  with_bwd(a.c, [&](auto t, auto v) {
+  // three vectors a thread: a quarter of the threads, whose groups have the fewer rows
+  const int one = threads_bwd(a.c);
+  const bool three = a.bf16 && one >= 128 && a.c <= 4096 && cdiv(a.c, 8) * 4 <= 3 * one;
+  with_bwd(a.c, three, [&](auto t, auto v) {
     constexpr int TPR = decltype(t)::value, NV = decltype(v)::value;
     const auto go = [&](auto kernel) {
       launch_main(kernel, dim3((unsigned)blocks), dim3(block_bwd(TPR)), s, a, part);
     };
     if (a.drop.on || a.res || a.dx || a.dh)
-      a.bf16 ? go(k_ln_rows_bwd<true, TPR, NV, true>) : go(k_ln_rows_bwd<false, TPR, NV, true>);
+      a.bf16 ? go(k_ln_rows_bwd<true, TPR, NV, true>)
+             : go(k_ln_rows_bwd<NV == 3, TPR, NV, true>);  // (three: bf16 only)
     else
       a.bf16 ? go(k_ln_rows_bwd<true, TPR, NV, false>)
-             : go(k_ln_rows_bwd<false, TPR, NV, false>);
+             : go(k_ln_rows_bwd<NV == 3, TPR, NV, false>);
   });
 }
 
