@@ -485,14 +485,19 @@ void norm_rows_fwd(const Norm& a, hipStream_t s) {
 
 int64_t norm_rows_blocks(int64_t rows, int32_t c) {
   const int tpr = threads_bwd(c), g = block_bwd(tpr) / tpr;
-  return std::max(std::min<int64_t>(cdiv(rows, 2 * g), 512), cdiv(rows, MOST_ADDED * g));
+  // (twice as many workgroups as CUs where every group then has two rows or more and a
+  // workgroup four: 1000 x 4096 fp32 takes 21 us with two rows a workgroup, 16 with four)
+  return std::max(std::min<int64_t>(cdiv(rows, std::max(2 * g, 4)), 512),
+                  cdiv(rows, MOST_ADDED * g));
 }
 
 void norm_rows_bwd(const NormBwd& a, float* part, hipStream_t s) {
   const int64_t blocks = norm_rows_blocks(a.rows, a.c);
-  // three vectors a thread: a quarter of the threads, whose groups have the fewer rows
+  // three vectors a thread: a quarter of the threads, and each group needs some rows (4096
+  // x 768: 17.5 us, with one vector 13)
   const int one = threads_bwd(a.c);
-  const bool three = a.bf16 && one >= 128 && a.c <= 4096 && cdiv(a.c, 8) * 4 <= 3 * one;
+  const bool three = a.bf16 && one >= 128 && a.c <= 4096 && cdiv(a.c, 8) * 4 <= 3 * one &&
+                     a.rows >= blocks * 4 * (4 * 512 / one);
   with_bwd(a.c, three, [&](auto t, auto v) {
     constexpr int TPR = decltype(t)::value, NV = decltype(v)::value;
     const auto go = [&](auto kernel) {

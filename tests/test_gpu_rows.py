@@ -274,6 +274,25 @@ def test_drop_ln(i, dt):
         assert again[0] is res and torch.equal(res, h) and torch.equal(again[1], y)
 
 
+@pytest.mark.parametrize("rows,c", [(33_000, 520), (32_800, 768), (17_000, 1100), (8300, 2304)])
+def test_many_bf16_rows(rows, c):
+    """Widths whose backward has three vectors a thread from so many rows on."""
+    dt, p, seed, step, site = BF16, 0.25, 5, 6, 7
+    x, res = make((rows, c), dt, 1, 2.0, 1), make((rows, c), dt, 2)
+    dy, dh = make((rows, c), dt, 3, 1.0, 3), make((rows, c), dt, 4)
+    gamma, rng = make((c,), F32, 5), rng_of(seed, step)
+    y, mean, invstd = oc.oc_ln_fwd(x, gamma, need_stats=True)
+    got = oc.oc_ln_bwd(x, dy, gamma, mean, invstd)
+    check_bwd(_np(x), _np(dy), None, _np(gamma), _np(invstd), dt, (None, *got), "ln")
+    keep, q = R.mask(rows, c, p, seed, step, site)
+    xd = np.where(keep, _np(x) / q, 0.0)
+    hw = xd + _np(res)
+    herr = U * (3 * np.abs(xd) + np.abs(hw))
+    h, y, mean, invstd = oc.oc_drop_ln_fwd(x, res, p, rng, gamma, site=site, need_stats=True)
+    got = oc.oc_drop_ln_bwd(x, res, dy, p, rng, gamma, mean, invstd, dh=dh, site=site)
+    check_bwd(hw, _np(dy), _np(dh), _np(gamma), _np(invstd), dt, got, "drop_ln", keep, q, herr)
+
+
 def test_drop_ln_is_dropout_then_layer_norm():
     """fp32: the fused step's mask, sums and norm are the separate calls'."""
     x, res = make((500, 384), F32, 1), make((500, 384), F32, 2)
@@ -341,6 +360,20 @@ def test_embed(i, kind, dt):
             others[rows_at] = False
             assert not got[others].any()
         assert torch.equal(oc.oc_embed_bwd(d, dy, num, scale=scale, dtype=out), got)
+
+
+@DT
+@pytest.mark.parametrize("rows,c", [(70_000, 520), (40_001, 1000), (2_100_000, 5)])
+def test_embed_forward_of_many_rows(rows, c, dt):
+    """Several rows in flight a group of lanes, ids outside the table among them."""
+    num = 3000
+    d = torch.as_tensor(ids_of(rows, num, "outside", 9)).cuda()
+    table = make((num, c), dt, 8, 1.0, 1)
+    y = oc.oc_embed_fwd(d, table, scale=3.0)
+    there = ((d >= 0) & (d < num)).unsqueeze(1)
+    want = torch.where(there, table.float()[d.clamp(0, num - 1).long()] * 3.0,
+                       torch.zeros((), device="cuda"))
+    assert torch.equal(y, want.to(dt))  # (one product, rounded once)
 
 
 def test_embed_order_of_equal_ids_is_the_rows():
