@@ -673,8 +673,8 @@ oc_status oc_grad_clip(int32_t n, const void* const* grads, const oc_dtype* dts,
  * shapes), contiguous, c channels each.  rows 0 .. 2^28 - 1 (0: nothing is done but
  * that sums over the rows are 0), c 1 .. 65536, fewer than 2^40 values.  dt OC_F32 or
  * OC_BF16 is the type of the feature maps; gamma, beta, their gradients, mean and invstd
- * are fp32.  Sums are fp32 over at most 64 rows and double from there; each OC_BF16
- * result is rounded once.  Buffers need the alignment of their elements only, but for
+ * are fp32.  Sums over a row's channels are fp32, sums over rows fp32 over at most 64 of
+ * them and double from there; each OC_BF16 result is rounded once.  Buffers need the alignment of their elements only, but for
  * workspaces (16 bytes) and generator states (8).  An output that overlaps another
  * buffer is refused, but for those named below, which may be the same buffer as a whole.
  * Deterministic: no floating-point atomics.
@@ -707,7 +707,8 @@ oc_status oc_ln_bwd(oc_dtype dt, int64_t rows, int32_t c, const void* x, const v
  * T / 2^32, T = (1 - p) 2^32 rounded (p keeping nothing by that rounding is refused;
  * one keeping everything copies).  The mask is a function of the generator's state, the
  * site, the row and the column (and of c) alone, whatever dt is; it is never stored, and
- * the backward is the same call on dy.  oc_dropout takes a mask that the caller draws.
+ * the backward is the same call on dy, with the state as the forward read it.
+ * oc_dropout takes a mask that the caller draws.
  *   rng     dev u64 [2], {seed, step}, read when the kernel runs: a captured call draws
  *           another mask once the caller has changed the step.  Not read (may be NULL)
  *           where p keeps everything.

@@ -1227,7 +1227,8 @@ def oc_dropout_rng(x, p, rng, site=0, y=None):
     """Dropout of ratio p on x [rows][c] with a mask drawn from the generator's state rng,
     an int64 device tensor {seed, step} that the kernel reads as it runs (rng[1] += 1 goes
     on to the next step, in a captured graph too); site tells the calls of a step apart.
-    The backward is the same call on dy.  y: where to write, may be x."""
+    The backward is the same call on dy, before the state goes on.  y: where to write, may
+    be x."""
     dev, dt, rows, c = _rows_of(x, "x")
     xp = _given(x, "x", dev, x.dtype, (rows, c))
     rp = _rng_state(rng, dev, p)
