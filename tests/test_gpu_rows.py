@@ -306,7 +306,8 @@ def test_drop_ln_is_dropout_then_layer_norm():
 EMBEDS = [(0, 5, 8), (1, 1, 1), (3, 7, 5), (64, 40, 128), (65, 40, 128), (64, 1000, 3),
           (500, 1, 64), (1000, 4, 33), (3000, 257, 100), (5000, 4096, 16), (5000, 4097, 8),
           (70, 100_000, 9), (20_000, 30_000, 24), (2500, 300, 1024), (700, 11, 2049),
-          (40_000, 3, 7), (100_000, 5000, 8), (9000, 1, 513), (300, 70_000_000, 1)]
+          (40_000, 3, 7), (100_000, 5000, 8), (9000, 1, 513), (300, 70_000_000, 1),
+          (70, 5, 65536)]
 
 
 def ids_of(rows, num, kind, seed):
