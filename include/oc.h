@@ -686,8 +686,8 @@ oc_status oc_grad_clip(int32_t n, const void* const* grads, const oc_dtype* dts,
  *   gamma, beta  dev f32 [c], each or NULL (1, 0).  eps > 0.
  *   mean, invstd dev f32 [rows], written for the backward, each or NULL.
  * A row that holds an infinity or a NaN becomes NaN; so do its dx and its share of the
- * sums over rows.  Deviations from 2^63 on overflow the variance: such a row of y is beta
- * or NaN. */
+ * sums over rows.  The variance is in range for deviations up to 2^63, whatever c; with
+ * larger ones it may overflow: such a row of y is beta or NaN. */
 oc_status oc_ln_fwd(oc_dtype dt, int64_t rows, int32_t c, const void* x, const float* gamma,
                     const float* beta, float eps, void* y, float* mean, float* invstd,
                     hipStream_t stream);

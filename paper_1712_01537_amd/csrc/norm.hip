@@ -10,8 +10,8 @@
 // that the sum does not overflow), then delta = mean of h - m; h - m - delta has no
 // rounding of the mean in it, whatever the size of the mean beside the deviations.
 // The stored mean is m + delta rounded; the backward forms its delta again, as one more
-// sum of the pass it makes anyway.  Squared deviations are added in fp32: a row with
-// deviations from 2^63 on has an infinite variance.
+// sum of the pass it makes anyway.  Squared deviations are divided by c before they are
+// added too, in fp32: the variance is in range for deviations up to 2^63, whatever c.
 #include <algorithm>
 
 #include "norm.h"
@@ -91,12 +91,12 @@ __global__ __launch_bounds__(TB) void k_ln_fwd_any(Norm a) {
       for (int k = 0; k < 8; ++k) {
         const float d = i * 8 + k < a.c ? v[k] - m[0] : 0.f;
         s[0] += d;
-        s[1] = fmaf(d, d, s[1]);
+        s[1] = fmaf(d * rc, d, s[1]);
       }
     }
     block_sums(s, red1);
     const float delta = s[0] * rc;
-    float var = fmaf(-delta, delta, s[1] * rc);
+    float var = fmaf(-delta, delta, s[1]);
     if (var < 0.f) var = 0.f;  // (NaN stays NaN)
     const float invstd = 1.f / sqrtf(var + a.eps);
     for (int i = threadIdx.x; i < nv; i += TB) {

@@ -95,8 +95,10 @@ __device__ __forceinline__ int group_of(int thread) {
 // turn use its two halves: a wave that has passed a row's barrier has read the row before.
 //
 // Forward.  The lanes of a wave find their mean m by one sum, then delta = mean of v - m
-// and the squares of v - m by two more; waves are joined by Chan et al.'s formula for
-// counts, means and sums of squared deviations, relative to the first wave's mean.
+// and the mean square of v - m by two more (each square is divided by the count before it
+// is added, as the values of the mean are, so that the sum stays in range); waves are
+// joined by Chan et al.'s formula for counts, means and mean squared deviations, relative
+// to the first wave's mean.
 template <bool BF, int TPR, int NV, bool STEP>
 __global__ __launch_bounds__(block_fwd(TPR), waves_fwd(TPR, NV, STEP)) void
     k_ln_rows(Norm a) {
@@ -176,17 +178,17 @@ __global__ __launch_bounds__(block_fwd(TPR), waves_fwd(TPR, NV, STEP)) void
 #pragma unroll
       for (int k = 0; k < 8; ++k) {
         s1 += v[j][k];
-        s2 = fmaf(v[j][k], v[j][k], s2);
+        s2 = fmaf(v[j][k] * r_own, v[j][k], s2);
       }
     }
     s1 = lanes_sum<L>(s1);
     s2 = lanes_sum<L>(s2);
-    float delta = s1 * r_own, m2 = fmaf(-delta, s1, s2), mean = m + delta;
+    float delta = s1 * r_own, var = fmaf(-delta, delta, s2), mean = m + delta;
     if (W > 1) {
       if ((t & 63) == 0) {
         red[par][w0][0] = m;
         red[par][w0][1] = delta;
-        red[par][w0][2] = m2;
+        red[par][w0][2] = var;
       }
       __syncthreads();
       const float m0 = red[par][0][0];
@@ -194,16 +196,15 @@ __global__ __launch_bounds__(block_fwd(TPR), waves_fwd(TPR, NV, STEP)) void
 #pragma unroll
       for (int w = 0; w < W; ++w)
         far = fmaf(channels(w) * rc, (red[par][w][0] - m0) + red[par][w][1], far);
-      m2 = 0.f;
+      var = 0.f;
 #pragma unroll
       for (int w = 0; w < W; ++w) {
-        const float d = ((red[par][w][0] - m0) + red[par][w][1]) - far, nw = channels(w);
-        m2 += nw > 0.f ? fmaf(nw * d, d, red[par][w][2]) : 0.f;
+        const float d = ((red[par][w][0] - m0) + red[par][w][1]) - far, share = channels(w) * rc;
+        var += share > 0.f ? share * fmaf(d, d, red[par][w][2]) : 0.f;
       }
       delta = far - (m - m0);  // of this wave's deviations
       mean = m0 + far;
     }
-    float var = m2 * rc;
     if (var < 0.f) var = 0.f;  // (NaN stays NaN)
     const float invstd = 1.f / sqrtf(var + a.eps);
 #pragma unroll
