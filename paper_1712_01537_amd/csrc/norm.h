@@ -21,7 +21,7 @@ struct NormBwd {
   const void *x, *res, *dy, *dh;  // h = res + dropout(x) is formed again
   void *dx, *dres;  // dx: behind the dropout; dres: in front of it (a plain norm's dx)
   const float *gamma, *mean, *invstd;
-  float* delta;  // [rows], for the column sums of rows too long for registers
+  float* delta;  // [rows], times invstd, for the column sums of rows too long for registers
   int64_t rows;
   int c;
   bool bf16;

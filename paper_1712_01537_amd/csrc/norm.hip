@@ -9,9 +9,10 @@
 // The mean is formed twice: m from the values (each divided by c before it is added, so
 // that the sum does not overflow), then delta = mean of h - m; h - m - delta has no
 // rounding of the mean in it, whatever the size of the mean beside the deviations.
-// The stored mean is m + delta rounded; the backward forms its delta again, as one more
-// sum of the pass it makes anyway.  Squared deviations are divided by c before they are
-// added too, in fp32: the variance is in range for deviations up to 2^63, whatever c.
+// The stored mean is m + delta rounded; the backward forms its delta again (times invstd,
+// as its deviations are), as one more sum of the pass it makes anyway.  Squared deviations
+// are divided by c before they are added too, in fp32: the variance is in range for
+// deviations up to 2^63, whatever c.
 #include <algorithm>
 
 #include "norm.h"
@@ -135,7 +136,7 @@ __global__ __launch_bounds__(TB) void k_ln_bwd_any(NormBwd a) {
       oc::load8n(a.dy, a.bf16, row * a.c + c, cnt, n, g);
 #pragma unroll
       for (int k = 0; k < 8; ++k) {
-        d[k] = k < cnt ? d[k] - m : 0.f;
+        d[k] = k < cnt ? (d[k] - m) * r : 0.f;
         if (a.gamma && k < cnt) g[k] *= a.gamma[c + k];
       }
     };
@@ -150,7 +151,7 @@ __global__ __launch_bounds__(TB) void k_ln_bwd_any(NormBwd a) {
       }
     }
     block_sums(s, red);
-    const float delta = s[2] * rc, gm = s[0] * rc, zm = (s[1] - delta * s[0]) * rc * r;
+    const float delta = s[2] * rc, gm = s[0] * rc, zm = fmaf(-delta, s[0], s[1]) * rc;
     if (threadIdx.x == 0 && a.delta) a.delta[row] = delta;
     if (!a.dx && !a.dres) continue;
     for (int i = threadIdx.x; i < nv; i += TB) {
@@ -158,7 +159,7 @@ __global__ __launch_bounds__(TB) void k_ln_bwd_any(NormBwd a) {
       const int c = i * 8, cnt = a.c - c;
       const int64_t at = row * a.c + c;
 #pragma unroll
-      for (int k = 0; k < 8; ++k) g[k] = r * (g[k] - gm - (d[k] - delta) * r * zm);
+      for (int k = 0; k < 8; ++k) g[k] = r * (g[k] - gm - (d[k] - delta) * zm);
       if (a.dh) {
         oc::load8n(a.dh, a.bf16, at, cnt, n, d);
 #pragma unroll
@@ -208,7 +209,7 @@ __global__ __launch_bounds__(TB) void k_ln_cols_any(NormBwd a, int ct, float* pa
       const float m = a.mean[r], is = a.invstd[r], de = a.delta[r];
 #pragma unroll
       for (int k = 0; k < 8; ++k) {
-        sg[k] = fmaf(g[k], ((x[k] - m) - de) * is, sg[k]);
+        sg[k] = fmaf(g[k], (x[k] - m) * is - de, sg[k]);
         sb[k] += g[k];
       }
     }

@@ -222,12 +222,13 @@ __global__ __launch_bounds__(block_fwd(TPR), waves_fwd(TPR, NV, STEP)) void
   }
 }
 
-// Backward: one reduction of three sums a row, of a thread's one vector up to 4096
-// channels (two vectors: 16 waves of 128 registers spill), two up to 8192 (512 threads of
-// up to 256 registers: fp32 residual step 631 us for 16384 x 8192, with 1024 threads of
-// one vector 850), four above; bf16 rows that leave a
-// quarter of the lanes of one vector without work have three (2^27 values in rows of 768:
-// 174 us instead of 215, of 1536 177 instead of 202).  dgamma's and dbeta's sums stay in
+// Backward: one reduction of three sums a row (of g, g d and d, with d = (h - mean)
+// invstd: the deviations themselves times g can be past fp32 where dx is not), of a
+// thread's one vector up to 4096 channels (two vectors: 16 waves of 128 registers spill),
+// two up to 8192 (512 threads of up to 256 registers: fp32 residual step 631 us for 16384
+// x 8192, with 1024 threads of one vector 850), four above; bf16 rows that leave a quarter
+// of the lanes of one vector without work have three (2^27 values in rows of 768: 174 us
+// instead of 215, of 1536 177 instead of 202).  dgamma's and dbeta's sums stay in
 // registers over the group's rows, at most MOST_ADDED; the workgroup's groups are then
 // added in double through LDS, and its sums written for the sum over the workgroups.
 template <bool BF, int TPR, int NV, bool STEP>
@@ -267,6 +268,9 @@ __global__ __launch_bounds__(block_bwd(TPR), NV == 1 ? 4 : 2) void
   };
   // (of four fp32 vectors one is loaded at a time)
   constexpr int RAWS = AHEAD || BF ? NV : 1;
+  // d is held times invstd, but for four fp32 vectors, where g d is formed as (g invstd) d:
+  // the step's backward of 8192 x 16384 takes 734 us, with d held times invstd 758.
+  constexpr bool SCALED = RAWS == NV;
   Raw<BF> x[RAWS], res[RAWS], dy[RAWS], dh[AHEAD ? NV : 1];
   float mean = 0.f, invstd = 0.f;
   const auto load_at = [&](int64_t at, int j, Raw<BF>& rx, Raw<BF>& rdy, Raw<BF>& rres) {
@@ -305,7 +309,7 @@ __global__ __launch_bounds__(block_bwd(TPR), NV == 1 ? 4 : 2) void
                        d[j], keep[i]);
       unpack(dy[l], e[j]);
 #pragma unroll
-      for (int k = 0; k < 8; ++k) d[j][k] -= m;
+      for (int k = 0; k < 8; ++k) d[j][k] = SCALED ? (d[j][k] - m) * r : d[j][k] - m;
       cut(d[j], here ? cnt[j] : 0);
       cut(e[j], here ? cnt[j] : 0);
       if (!AHEAD) {
@@ -318,7 +322,7 @@ __global__ __launch_bounds__(block_bwd(TPR), NV == 1 ? 4 : 2) void
       for (int k = 0; k < 8; ++k) {
         const float q = e[j][k] * gam[i][k];
         s[0] += q;
-        s[1] = fmaf(q, d[j][k], s[1]);
+        s[1] = fmaf(SCALED ? q : q * r, d[j][k], s[1]);
         s[2] += d[j][k];
       }
       // (the next vector's loads stay behind this one's use: their registers are the same)
@@ -346,7 +350,8 @@ __global__ __launch_bounds__(block_bwd(TPR), NV == 1 ? 4 : 2) void
         for (int w = 1; w < W; ++w) s[k] += red[par][g * W + w][k];
       }
     }
-    const float delta = s[2] * rc, gm = s[0] * rc, zm = fmaf(-delta, s[0], s[1]) * rc * r;
+    const float delta = s[2] * rc, gm = s[0] * rc;
+    const float zm = fmaf(SCALED ? -delta : -delta * r, s[0], s[1]) * rc;
 #pragma unroll
     for (int j = 0; j < NV; ++j) {
       const int i = AHEAD ? j : 0;
@@ -358,7 +363,7 @@ __global__ __launch_bounds__(block_bwd(TPR), NV == 1 ? 4 : 2) void
       if (has_dh && here && cnt[j] > 0) unpack(dh[i], u);
 #pragma unroll
       for (int k = 0; k < 8; ++k) {
-        const float z = (d[j][k] - delta) * r;
+        const float z = SCALED ? d[j][k] - delta : (d[j][k] - delta) * r;
         sg[j][k] = fmaf(e[j][k], z, sg[j][k]);
         sb[j][k] += e[j][k];
         e[j][k] = r * fmaf(-z, zm, fmaf(e[j][k], gam[i][k], -gm));

@@ -47,3 +47,20 @@ def test_deviations_up_to_the_stated_limit(c, dt, power):
     check_stats(mean2, invstd2, _np(x), eps, "step's stats")
     got = oc.oc_drop_ln_bwd(half, half.clone(), dy, 0.0, rng, gamma, mean, invstd)
     check_bwd(_np(x), _np(dy), None, _np(gamma), _np(invstd), dt, got, "step's bwd")
+
+
+@DT
+@pytest.mark.parametrize("c", WIDTHS)
+@pytest.mark.parametrize("power,grad", [(62, 66), (62, -60), (-40, 80), (0, 110)])
+def test_gradients_as_large_as_the_deviations(c, dt, power, grad):
+    """dx is of the size of dy invstd; no sum on the way to it is of the size of dy times
+    the deviations (2^62 2^66 is past fp32, dx itself some 2^4)."""
+    eps = 1e-5 if power >= 0 else 1e-26
+    x, dy = far_rows(c, dt, power, c), far_rows(c, dt, grad, c + 1).flip(0).contiguous()
+    gamma = make((c,), F32, 3)
+    _, mean, invstd = oc.oc_ln_fwd(x, gamma, None, eps, need_stats=True)
+    dx, dg, db = oc.oc_ln_bwd(x, dy, gamma, mean, invstd)
+    check_bwd(_np(x), _np(dy), None, _np(gamma), _np(invstd), dt, (None, dx, dg, db), "bwd")
+    half, rng = x * 0.5, rng_of(1, 2)
+    got = oc.oc_drop_ln_bwd(half, half.clone(), dy, 0.0, rng, gamma, mean, invstd)
+    check_bwd(_np(x), _np(dy), None, _np(gamma), _np(invstd), dt, got, "step's bwd")
