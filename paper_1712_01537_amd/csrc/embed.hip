@@ -7,7 +7,11 @@
 // lanes, whose runs of one id are summed in order.  A run inside one piece is written to
 // the table's row; one that goes on over a border leaves a partial sum a piece, added
 // through LDS where the run stays in the workgroup's chunk, else by k_embed_join.
-// However many rows share an id, no chain of additions is longer than a piece.
+// A run's chain of additions: a piece's rows, at most 64 of them in fp32 and the rest in
+// double; the pieces of a chunk one after another (up to 256 of 8 columns, 4 of 512 and
+// more) in double; and in double up to nine chunks one after another, or of up to 2048
+// chunks every 16th to 512th and then those 16 to 512 sums.  Each piece's and each chunk's
+// sum is rounded to fp32 on its way.
 //
 // The sort takes the ids' bits in digits of up to nine, lowest first.  A tile of rows is
 // one workgroup's: count writes each tile's number of rows of every digit value, and
