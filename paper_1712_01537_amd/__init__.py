@@ -1156,9 +1156,10 @@ def _rows_of(x, name):
     return torch._C._cuda_getDevice(), _dtype_code(x), rows, c
 
 
-def _rng_state(rng, dev, p):
-    """Address of a generator's state {seed, step}; None where no mask is drawn."""
-    if rng is None and p == 0:
+def _rng_state(rng, dev):
+    """Address of a generator's state {seed, step}, or None, which the library refuses
+    where a mask is drawn."""
+    if rng is None:
         return None
     if not isinstance(rng, torch.Tensor):
         raise OcError(1, "rng must be a tensor of two int64: seed and step")
@@ -1227,11 +1228,11 @@ def oc_dropout_rng(x, p, rng, site=0, y=None):
     """Dropout of ratio p on x [rows][c] with a mask drawn from the generator's state rng,
     an int64 device tensor {seed, step} that the kernel reads as it runs (rng[1] += 1 goes
     on to the next step, in a captured graph too); site tells the calls of a step apart.
-    The backward is the same call on dy, before the state goes on.  y: where to write, may
-    be x."""
+    The backward is the same call on dy, before the state goes on.  rng may be None where p
+    keeps everything (0, or below 2^-33).  y: where to write, may be x."""
     dev, dt, rows, c = _rows_of(x, "x")
     xp = _given(x, "x", dev, x.dtype, (rows, c))
-    rp = _rng_state(rng, dev, p)
+    rp = _rng_state(rng, dev)
     if y is None:
         y = torch.empty_like(x)
     _check(load().oc_dropout_rng(dt, rows, c, xp, p, rp, site,
@@ -1243,11 +1244,11 @@ def oc_drop_ln_fwd(x, res, p, rng, gamma=None, beta=None, site=0, eps=1e-5, need
                    h=None):
     """The residual step h = res + dropout(x), y = the layer norm of h: (h, y, mean,
     invstd), the last two None unless need_stats.  res: as x, or None (0).  p, rng, site as
-    oc_dropout_rng's (rng may be None for p = 0).  h: where to write it; may be res where no
+    oc_dropout_rng's.  h: where to write it; may be res where no
     backward follows, which reads x and res again."""
     dev, dt, rows, c = _rows_of(x, "x")
     xp = _given(x, "x", dev, x.dtype, (rows, c))
-    rp = _rng_state(rng, dev, p)
+    rp = _rng_state(rng, dev)
     if h is None:
         h = torch.empty_like(x)
     y = torch.empty_like(x)
@@ -1274,7 +1275,7 @@ def oc_drop_ln_bwd(x, res, dy, p, rng, gamma, mean, invstd, dh=None, site=0, nee
     _check(load().oc_drop_ln_bwd(dt, rows, c, _given(x, "x", dev, t, (rows, c)),
                                  _given(res, "res", dev, t, (rows, c)),
                                  _given(dy, "dy", dev, t, (rows, c)),
-                                 _given(dh, "dh", dev, t, (rows, c)), p, _rng_state(rng, dev, p),
+                                 _given(dh, "dh", dev, t, (rows, c)), p, _rng_state(rng, dev),
                                  site, _given(gamma, "gamma", dev, torch.float32, (c,)),
                                  _given(mean, "mean", dev, torch.float32, (rows,)),
                                  _given(invstd, "invstd", dev, torch.float32, (rows,)),
