@@ -1171,6 +1171,14 @@ def _ln_ws(rows, c):
     return load().oc_ln_bwd_workspace(rows, c)
 
 
+def _out(t, name, x, dev):
+    """A caller's output as x is, or a new one, with its address."""
+    if t is None:
+        t = torch.empty_like(x)
+        return t, t.data_ptr()
+    return t, _given(t, name, dev, x.dtype, x.shape)
+
+
 def _stats(x, rows, need):
     """mean and invstd of the rows with their addresses, or None."""
     if not need:
@@ -1193,17 +1201,17 @@ def _norm_sums(x, dev, rows, c, dgamma, dbeta, need_dgamma, need_dbeta):
             ws.data_ptr() if need else None, need)
 
 
-def oc_ln_fwd(x, gamma=None, beta=None, eps=1e-5, need_stats=False):
+def oc_ln_fwd(x, gamma=None, beta=None, eps=1e-5, need_stats=False, y=None):
     """Layer norm over the channels of each row of x [rows][c] (float32 or bfloat16):
     (y, mean, invstd), the last two None unless need_stats (the backward's).  gamma, beta:
-    float32 [c] or None."""
+    float32 [c] or None.  y: where to write it; may be x where no backward follows."""
     dev, dt, rows, c = _rows_of(x, "x")
-    y = torch.empty_like(x)
+    y, yp = _out(y, "y", x, dev)
     mean, invstd, mp, ip = _stats(x, rows, need_stats)
     _check(load().oc_ln_fwd(dt, rows, c, _given(x, "x", dev, x.dtype, (rows, c)),
                             _given(gamma, "gamma", dev, torch.float32, (c,)),
-                            _given(beta, "beta", dev, torch.float32, (c,)), eps, y.data_ptr(), mp,
-                            ip, _stream()))
+                            _given(beta, "beta", dev, torch.float32, (c,)), eps, yp, mp, ip,
+                            _stream()))
     return y, mean, invstd
 
 
@@ -1233,31 +1241,27 @@ def oc_dropout_rng(x, p, rng, site=0, y=None):
     dev, dt, rows, c = _rows_of(x, "x")
     xp = _given(x, "x", dev, x.dtype, (rows, c))
     rp = _rng_state(rng, dev)
-    if y is None:
-        y = torch.empty_like(x)
-    _check(load().oc_dropout_rng(dt, rows, c, xp, p, rp, site,
-                                 _given(y, "y", dev, x.dtype, (rows, c)), _stream()))
+    y, yp = _out(y, "y", x, dev)
+    _check(load().oc_dropout_rng(dt, rows, c, xp, p, rp, site, yp, _stream()))
     return y
 
 
 def oc_drop_ln_fwd(x, res, p, rng, gamma=None, beta=None, site=0, eps=1e-5, need_stats=False,
-                   h=None):
+                   h=None, y=None):
     """The residual step h = res + dropout(x), y = the layer norm of h: (h, y, mean,
     invstd), the last two None unless need_stats.  res: as x, or None (0).  p, rng, site as
-    oc_dropout_rng's.  h: where to write it; may be res where no
+    oc_dropout_rng's.  h, y: where to write them; h may be res and y may be x where no
     backward follows, which reads x and res again."""
     dev, dt, rows, c = _rows_of(x, "x")
     xp = _given(x, "x", dev, x.dtype, (rows, c))
     rp = _rng_state(rng, dev)
-    if h is None:
-        h = torch.empty_like(x)
-    y = torch.empty_like(x)
+    h, hp = _out(h, "h", x, dev)
+    y, yp = _out(y, "y", x, dev)
     mean, invstd, mp, ip = _stats(x, rows, need_stats)
     _check(load().oc_drop_ln_fwd(dt, rows, c, xp, _given(res, "res", dev, x.dtype, (rows, c)), p,
                                  rp, site, _given(gamma, "gamma", dev, torch.float32, (c,)),
                                  _given(beta, "beta", dev, torch.float32, (c,)), eps,
-                                 _given(h, "h", dev, x.dtype, (rows, c)), y.data_ptr(), mp, ip,
-                                 _stream()))
+                                 hp, yp, mp, ip, _stream()))
     return h, y, mean, invstd
 
 

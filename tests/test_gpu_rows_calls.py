@@ -26,3 +26,31 @@ def test_a_ratio_that_keeps_everything_needs_no_state(dt):
                      lambda: oc.oc_drop_ln_bwd(x, res, dy, p, None, None, want[2], want[3])):
             with pytest.raises(oc.OcError, match="generator state"):
                 call()
+
+
+@DT
+@pytest.mark.parametrize("rows,c", [(33, 8), (70, 127), (600, 1024), (9, 5001), (3, 17000)])
+def test_outputs_where_the_caller_says(rows, c, dt):
+    """y in a tensor of the caller's, and in x's place; h in res's."""
+    x, res, rng = make((rows, c), dt, 1), make((rows, c), dt, 2), rng_of(3, 4)
+    gamma = make((c,), F32, 5)
+    y, mean, invstd = oc.oc_ln_fwd(x, gamma, need_stats=True)
+    out = torch.empty_like(x)
+    got = oc.oc_ln_fwd(x, gamma, need_stats=True, y=out)
+    assert got[0] is out and torch.equal(out, y)
+    assert torch.equal(got[1], mean) and torch.equal(got[2], invstd)
+    a = x.clone()
+    assert oc.oc_ln_fwd(a, gamma, y=a)[0] is a and torch.equal(a, y)
+    h, y, _, _ = oc.oc_drop_ln_fwd(x, res, 0.4, rng, gamma)
+    got = oc.oc_drop_ln_fwd(x, res, 0.4, rng, gamma, y=out)
+    assert got[1] is out and torch.equal(out, y) and torch.equal(got[0], h)
+    a, b = x.clone(), res.clone()
+    got = oc.oc_drop_ln_fwd(a, b, 0.4, rng, gamma, h=b, y=a)
+    assert got[0] is b and got[1] is a and torch.equal(b, h) and torch.equal(a, y)
+    for call in (lambda: oc.oc_ln_fwd(x, gamma, y=out[:1, :c // 2]),
+                 lambda: oc.oc_ln_fwd(x, gamma, y=out.float() if dt != F32 else out.bfloat16()),
+                 lambda: oc.oc_ln_fwd(x, gamma, y=out.cpu()),
+                 lambda: oc.oc_drop_ln_fwd(x, res, 0.4, rng, gamma, y=res),
+                 lambda: oc.oc_drop_ln_fwd(x, res, 0.4, rng, gamma, y=out, h=out)):
+        with pytest.raises(oc.OcError):
+            call()
