@@ -1323,6 +1323,8 @@ def oc_embed_bwd(ids, dy, num, scale=1.0, keys=False, dtable=None, dtype=None):
         raise OcError(1, f"{n} ids for {rows} rows")
     dyp = _given(dy, "dy", dev, dy.dtype, (rows, c))
     if dtable is None:
+        if not 1 <= num < 1 << 28:
+            raise OcError(1, f"oc_embed_bwd: a table of {num} rows")
         dtable = torch.empty((num, c), dtype=dtype or torch.float32, device=dy.device)
     need = _embed_ws(rows, num, c)
     ws = torch.empty(need, dtype=torch.uint8, device=dy.device) if need else None

@@ -54,3 +54,12 @@ def test_outputs_where_the_caller_says(rows, c, dt):
                  lambda: oc.oc_drop_ln_fwd(x, res, 0.4, rng, gamma, y=out, h=out)):
         with pytest.raises(oc.OcError):
             call()
+
+
+def test_sizes_of_a_table_that_no_call_takes():
+    """Refused before the gradient's memory is asked for."""
+    ids, dy = torch.zeros(100, dtype=torch.int32, device="cuda"), make((100, 8), F32, 1)
+    for num in (0, -1, 1 << 28, 1 << 40):
+        for rows in (4, 100):
+            with pytest.raises(oc.OcError, match="a table of"):
+                oc.oc_embed_bwd(ids[:rows], dy[:rows], num)
