@@ -3,6 +3,7 @@
 #pragma once
 
 #include <cmath>
+#include <cstring>
 
 #include "dense.h"
 
@@ -196,7 +197,8 @@ inline oc_status check_spans(const char* who, const Span (&s)[N]) {
       if (j == i || !s[j].p || !s[j].bytes || (s[j].out && j < i)) continue;
       const uintptr_t a = (uintptr_t)s[i].p, b = (uintptr_t)s[j].p;
       if (a >= b + s[j].bytes || b >= a + s[i].bytes) continue;
-      if (a == b && s[i].bytes == s[j].bytes && s[i].same == s[j].name && s[i].same) continue;
+      if (a == b && s[i].bytes == s[j].bytes && s[i].same && !std::strcmp(s[i].same, s[j].name))
+        continue;
       return fail(OC_ERR_ARG, "%s: %s overlaps %s", who, s[i].name, s[j].name);
     }
   }
