@@ -753,7 +753,9 @@ oc_status oc_drop_ln_bwd(oc_dtype dt, int64_t rows, int32_t c, const void* x, co
  * padded row's may be).
  *   flags   0 or OC_IDS_KEYS: the ids are shuffle keys (oc_level's keys), whose shape
  *           index in bits 24..31 is dropped: the row of an octant of depth l is its place
- *           in the cube, of a table of 8^l rows.
+ *           in the cube, of a table of 8^l rows.  A table of 8^8 rows has
+ *           one for every key, -1 (its last place) among them: to leave rows out of it,
+ *           pass ids without this flag.
  *   ids     dev i32 [rows].  table dev [num][c], num 1 .. 2^28 - 1, fewer than 2^40
  *           values.  y dev [rows][c]. */
 #define OC_IDS_KEYS 1

@@ -1302,7 +1302,8 @@ def _ids_of(ids, dev):
 
 def oc_embed_fwd(ids, table, scale=1.0, keys=False):
     """y[r] = scale table[ids[r]], 0 where the id is outside the table.  ids: int32; with
-    keys they are shuffle keys (Octree.keys), whose shape index is dropped.  table [num][c]:
+    keys they are shuffle keys (Octree.keys), whose shape index is dropped (of a table of
+    8^8 rows none is outside: -1 is its last place).  table [num][c]:
     float32 or bfloat16, as y."""
     dev, dt, num, c = _rows_of(table, "table")
     rows, idp = _ids_of(ids, dev)

@@ -63,3 +63,19 @@ def test_sizes_of_a_table_that_no_call_takes():
         for rows in (4, 100):
             with pytest.raises(oc.OcError, match="a table of"):
                 oc.oc_embed_bwd(ids[:rows], dy[:rows], num)
+
+
+@DT
+def test_a_key_of_minus_one_is_the_last_place_of_depth_8(dt):
+    """A key's 24 place bits name each row of a table of 8^8 rows, so no key lies outside
+    it: -1 is the last place, in shape 255.  Smaller tables do not have that place."""
+    keys = torch.tensor([-1, 0, 5 << 24, 0xFFFFFF] * 20, dtype=torch.int32, device="cuda")
+    dy = torch.ones((80, 1), dtype=dt, device="cuda")
+    for depth in (8, 7):
+        num, last = 8 ** depth, 1.0 if depth == 8 else 0.0
+        table = torch.full((num, 1), 2.0, dtype=dt, device="cuda")
+        y = oc.oc_embed_fwd(keys, table, keys=True)
+        assert y[:4, 0].tolist() == [2.0 * last, 2.0, 2.0, 2.0 * last]
+        g = oc.oc_embed_bwd(keys, dy, num, keys=True)
+        assert float(g[0]) == 40 and float(g[-1]) == 40 * last
+        assert float(g.sum()) == 40 + 40 * last
