@@ -674,10 +674,11 @@ oc_status oc_grad_clip(int32_t n, const void* const* grads, const oc_dtype* dts,
  * that sums over the rows are 0), c 1 .. 65536, fewer than 2^40 values.  dt OC_F32 or
  * OC_BF16 is the type of the feature maps; gamma, beta, their gradients, mean and invstd
  * are fp32.  Sums over a row's channels are fp32, sums over rows fp32 over at most 64 of
- * them and double from there; each OC_BF16 result is rounded once.  Buffers need the alignment of their elements only, but for
- * workspaces (16 bytes) and generator states (8).  An output that overlaps another
- * buffer is refused, but for those named below, which may be the same buffer as a whole.
- * Deterministic: no floating-point atomics.
+ * them and double from there, with each part's sum (a piece's, a workgroup's) rounded to
+ * fp32 on its way; each OC_BF16 result is rounded once.  Buffers need the alignment of
+ * their elements only, but for workspaces (16 bytes) and generator states (8).  An output
+ * that overlaps another buffer is refused, but for those named below, which may be the
+ * same buffer as a whole.  Deterministic: no floating-point atomics.
  *
  * Layer norm over the channels of each row:
  *   y = (x - mean) invstd gamma + beta,  invstd = 1 / sqrt(var + eps)
@@ -685,9 +686,9 @@ oc_status oc_grad_clip(int32_t n, const void* const* grads, const oc_dtype* dts,
  *   x, y    dev [rows][c]; y may be x.
  *   gamma, beta  dev f32 [c], each or NULL (1, 0).  eps > 0.
  *   mean, invstd dev f32 [rows], written for the backward, each or NULL.
- * A row that holds an infinity or a NaN becomes NaN; so do its dx and its share of the
- * sums over rows.  The variance is in range for deviations up to 2^63, whatever c; with
- * larger ones it may overflow: such a row of y is beta or NaN. */
+ * A row that holds an infinity or a NaN becomes NaN; so do its dx and its share of dgamma
+ * (its share of dbeta is its dy).  The variance is in range for deviations up to 2^63,
+ * whatever c; with larger ones it may overflow: such a row of y is beta or NaN. */
 oc_status oc_ln_fwd(oc_dtype dt, int64_t rows, int32_t c, const void* x, const float* gamma,
                     const float* beta, float eps, void* y, float* mean, float* invstd,
                     hipStream_t stream);
