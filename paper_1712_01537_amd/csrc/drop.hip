@@ -1,9 +1,9 @@
 // Dropout whose mask comes from a counter-based generator (oc_dropout_rng): y = keep ?
 // x 2^32 / T : 0, the mask a function of the state {seed, step}, the site, the row and
 // the column alone (rows.h), so that the backward forms it again instead of reading it.
-// Bound by memory: 65536 x 4096 bf16 182 to 224 us (4.8 to 5.9 TB/s read and written, by
-// what the last-level cache still holds), p = 0.1 as 0.5; 134 vector instructions for the
-// 512 values of a wave.
+// Bound by memory: 65536 x 4096 bf16 182 to 187 us (5.7 to 5.9 TB/s read and written), with
+// one pair of buffers or six in turn (6 GiB, past the last-level cache), 211 in the first
+// calls of a run; p = 0.1 as 0.5; 134 vector instructions for the 512 values of a wave.
 #include <algorithm>
 
 #include "rows.h"

@@ -3,10 +3,12 @@
 // are started before the present one's sums.
 //
 // Bound by memory: each value is read and written once (the forward of 65536 x 4096 bf16
-// writes 517 MiB, its backward 544 with the column sums).  That forward takes 203 us (5.3
-// TB/s), its backward 326 (4.9); the residual step of 16384 x 8192 fp32 410 and 642 (5.2 and
-// 5.0); a large copy reaches 4.7.  Rows of 8193 to 16384 keep no next row in the backward
-// and reach 2.6 to 4.4.
+// writes 517 MiB, its backward 544 with the column sums).  That forward takes 205 us (5.2
+// TB/s), its backward 326 (4.9); the residual step of 16384 x 8192 fp32 395 and 630 (5.4 and
+// 5.1); a large copy reaches 4.7 to 5.3.  The backward of rows of 8193 to 16384 keeps no
+// next row and reaches 2.2 to 4.5: the values of four vectors a thread do not fit its
+// registers (scratch a lane: bf16 step 224 bytes, fp32 step 148, bf16 norm 28, fp32 norm
+// none).
 #include <algorithm>
 
 #include "norm.h"
@@ -58,9 +60,12 @@ __device__ __forceinline__ float lanes_sum(float v) {
 // Threads of a workgroup.
 constexpr int block_fwd(int tpr) { return tpr <= 64 ? 256 : tpr; }
 constexpr int block_bwd(int tpr) { return tpr <= 512 ? 512 : tpr; }
-// Waves that a SIMD holds of a forward kernel, by the registers it needs: the forward has
-// as many workgroups as the card holds at once (one more would be a round of its own:
-// bf16 rows of 64 to 256 channels 4.6 TB/s instead of 5.4).
+// Waves that a SIMD holds of a forward kernel, by the registers it needs, or two fewer:
+// bf16 norms and fp32 steps of 9 to 256 channels keep two registers in scratch (12 bytes a
+// lane), the fp32 step of 1024 threads five.  (With one wave fewer and no scratch 2^27
+// values of 64 channels take 98 us as with it for the bf16 norm, 426 us instead of 431 for
+// the fp32 step.)  The forward has as many workgroups as the card holds at once (one more
+// would be a round of its own: bf16 rows of 64 to 256 channels 4.6 TB/s instead of 5.4).
 constexpr int waves_fwd(int tpr, int nv, bool step) {
   return nv == 1 ? (step ? 6 : 8) : step || tpr >= 512 ? 4 : 5;
 }
@@ -225,7 +230,7 @@ __global__ __launch_bounds__(block_fwd(TPR), waves_fwd(TPR, NV, STEP)) void
 // Backward: one reduction of three sums a row (of g, g d and d, with d = (h - mean)
 // invstd: the deviations themselves times g can be past fp32 where dx is not), of a
 // thread's one vector up to 4096 channels (two vectors: 16 waves of 128 registers spill),
-// two up to 8192 (512 threads of up to 256 registers: fp32 residual step 631 us for 16384
+// two up to 8192 (512 threads of up to 256 registers: fp32 residual step 630 us for 16384
 // x 8192, with 1024 threads of one vector 850), four above; bf16 rows that leave a quarter
 // of the lanes of one vector without work have three (2^27 values in rows of 768: 174 us
 // instead of 215, of 1536 177 instead of 202).  dgamma's and dbeta's sums stay in
